@@ -339,6 +339,153 @@ int codistill_adam_step(float* master_w, float* exp_avg, float* exp_avg_sq, cons
                         int64_t n, float lr, float beta1, float beta2, float eps, float weight_decay, int64_t t,
                         void* stream);
 
+/* ---- operators of a differential-attention Transformer layer and its update ------------------------------------- */
+/*
+ * Rotary positions with several axes.  Pair p of a head's `dim` channels is turned by the angle
+ *     positions[axis[p]][token] * freq[p]        y1 = x1 cos - x2 sin,  y2 = x2 cos + x1 sin
+ * (inverse: by the opposite angle, which is the gradient's direction).  Pairs from n_pairs on are copied.  CD_ROPE_HALVES: pair p is
+ * channels p and p + dim/2; CD_ROPE_PAIRS: channels 2p and 2p + 1.  Angles are reduced to turns in a two-part fp32 product, exact to
+ * 1e-7 turns at any position; sums in fp32, rounded once.
+ *   tensors    HOST array of n_tensors descriptors, all with the same tokens (queries and keys go in one launch): x and y device,
+ *              [tokens][heads][dim] in `dtype`, channels contiguous, heads dim elements apart, tokens x_token / y_token apart.  y may be x
+ *   positions  device int32 [axes][tokens]
+ * Any 2 <= dim <= 2 * CD_ROPE_MAX_PAIRS, even; tensors that are 16-byte aligned with 16-byte multiples for strides and half heads move
+ * in whole vectors, others element by element.  tokens == 0 is allowed and does nothing.
+ * Errors (CD_ERR_INVALID_ARG, nothing launched): NULL pointers, odd or oversized dim, n_pairs > dim/2, an axis outside [0, axes), a
+ * non-finite frequency, strides below heads * dim, n_tensors outside 1..CD_ROPE_MAX_TENSORS, pointers not aligned to their elements.
+ */
+#define CD_ROPE_MAX_PAIRS 128
+#define CD_ROPE_MAX_TENSORS 4
+enum { CD_ROPE_HALVES = 0, CD_ROPE_PAIRS = 1 };
+typedef struct {
+  int32_t dtype;                     /* CD_F32 or CD_BF16 */
+  int32_t dim, n_pairs, axes, layout;
+  int32_t axis[CD_ROPE_MAX_PAIRS];   /* axis of each pair */
+  double freq[CD_ROPE_MAX_PAIRS];    /* radians a position */
+} cd_rotary;
+typedef struct {
+  const void* x;
+  void* y;
+  int64_t heads, x_token, y_token;
+} cd_rotary_tensor;
+int codistill_rotary(const cd_rotary* rope, const int32_t* positions, int64_t tokens, const cd_rotary_tensor* tensors,
+                     int64_t n_tensors, int inverse, void* stream);
+
+/*
+ * Differential attention: the difference of two softmax maps with a learned weight.  Every head has two queries and two keys of head_dim
+ * channels and one value of 2 head_dim:
+ *     P_m = softmax over the visible keys of scale q_m . k_m   (m = 1, 2; zeros in a row that sees no key)
+ *     out = (P_1 - lambda P_2) v
+ *   q [token][heads][2][head_dim], k [token][kv_heads][2][head_dim], v [token][kv_heads][2 head_dim], out [token][heads][2 head_dim]; heads
+ *   h * kv_heads / heads share a key head.  Inside a token the channels are contiguous; token and batch strides are in elements, and q, k, v may
+ *   be ranges of one tensor
+ *   lambda     device fp32: one for each head [heads] (CD_LAMBDA_HEAD) or for each query and head [q rows][heads] (CD_LAMBDA_TOKEN)
+ *   padded     q_starts == NULL: batch sequences with room for tq queries and tk keys each; q_lens / k_lens (device int32 [batch], or NULL:
+ *              full) say how many are real, values outside [0, tq] / [0, tk] are cut to it.  out is zero in the rows behind a sequence's queries,
+ *              and so are the gradients behind its queries and keys.  What q, k, v hold there is not used (NaN does no harm)
+ *   packed     q_starts and k_starts (device int32 [batch + 1]): sequence b has rows starts[b] .. starts[b + 1]; tq and tk are the longest sequence's
+ *              (longer ones are cut), q_rows and k_rows the rows of the tensors (nothing beyond them is touched).  Rows of no sequence are not
+ *              written
+ *   causal     query i of nq sees the keys j <= i + nk - nq: the last query sees all of them (a cache in front of the new tokens); with fewer
+ *              keys than queries the first rows see none
+ *   scale      > 0, or 0 for 1 / sqrt(head_dim)
+ * head_dim: multiples of 8 up to 128.  Products with CD_BF16 run on the bf16 matrix instructions with the weights P rounded to bf16 for the
+ * second product; softmax statistics, sums and accumulators are fp32.  CD_F32 runs on the fp32 matrix instruction.
+ *   o_second   NULL, or [q rows][heads][2 head_dim] contiguous in dtype: P_2 v, kept for the backward pass; lse then has to be given too
+ *   lse        NULL, or device fp32 [2][heads][q rows]: log2 of the sum of exp2 of each row's scores
+ *   workspace  at least codistill_diff_attention_workspace_bytes(desc, 0) bytes (may be 0: then NULL is fine)
+ * q rows: batch * tq when padded (row b * tq + i), q_rows when packed.
+ * Errors (nothing launched): CD_ERR_INVALID_ARG: NULL or misaligned pointers (16 bytes; q_lens, starts and lambda 4), sizes < 1 (tq or tk 0 are
+ * allowed with padded sequences), heads no multiple of kv_heads, strides that are no multiple of 16 bytes or shorter than a token, one of the start
+ * tables alone, starts together with lens, scale < 0 or not finite; CD_ERR_UNSUPPORTED: other head dims; CD_ERR_WORKSPACE_TOO_SMALL.
+ */
+enum { CD_LAMBDA_HEAD = 0, CD_LAMBDA_TOKEN = 1 };
+typedef struct {
+  int32_t dtype;
+  int32_t batch, tq, tk, heads, kv_heads, head_dim, causal, lambda_kind;
+  float scale;
+  int64_t q_token, q_batch, k_token, k_batch, v_token, v_batch, o_token, o_batch;
+  const int32_t *q_lens, *k_lens, *q_starts, *k_starts;
+  int64_t q_rows, k_rows;
+} cd_diff_attn;
+int codistill_diff_attention_workspace_bytes(const cd_diff_attn* desc, int backward, size_t* bytes);
+int codistill_diff_attention(const cd_diff_attn* desc, const void* q, const void* k, const void* v, const float* lambda, void* out,
+                             void* o_second, float* lse, void* workspace, size_t workspace_bytes, void* stream);
+/*
+ * Its gradients.  q, k, v, lambda, out, o_second and lse as the forward call had and left them; dout has out's strides, dq, dk, dv those of q, k, v.
+ * Gradients of a key head are summed over the heads that share it, in a fixed order: the same inputs give the same bits.
+ *   dlambda   lambda's shape, fp32
+ *   workspace at least codistill_diff_attention_workspace_bytes(desc, 1) bytes
+ * Errors as above; also CD_ERR_INVALID_ARG where sequences share memory (a batch stride below the rows of a sequence), in which gradients would race.
+ */
+int codistill_diff_attention_backward(const cd_diff_attn* desc, const void* q, const void* k, const void* v, const float* lambda, const void* out,
+                                      const void* o_second, const float* lse, const void* dout, void* dq, void* dk, void* dv, float* dlambda,
+                                      void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Norm of every head's channels, as it follows differential attention: y = post gain x / sqrt(mean(x^2) + eps) over the `width` channels
+ * of each of rows * heads groups; post is a constant factor (the 1 - lambda_init of that layer, or 1).
+ *   x, y   [rows][heads][width] in dtype (heads contiguous, rows x_row / y_row elements apart); y may be x
+ *   gain   device [width] in dtype, shared by all heads
+ * Backward: dx, and dgain (fp32 [width], sums over all rows and heads in a fixed order).  x is read again and its statistics are taken again:
+ * nothing is kept.  dx may be dy.  workspace: codistill_head_norm_workspace_bytes.
+ * 1 <= width <= 1024; rows == 0 is allowed (dgain is then zero).  Errors: CD_ERR_INVALID_ARG, CD_ERR_WORKSPACE_TOO_SMALL, nothing launched.
+ */
+int codistill_head_norm(int dtype, const void* x, int64_t x_row, const void* gain, void* y, int64_t y_row, int64_t rows, int64_t heads,
+                        int64_t width, float eps, float post, void* stream);
+int codistill_head_norm_workspace_bytes(int64_t rows, int64_t heads, int64_t width, size_t* bytes);
+int codistill_head_norm_backward(int dtype, const void* x, int64_t x_row, const void* gain, const void* dy, int64_t dy_row, void* dx, int64_t dx_row,
+                                 float* dgain, int64_t rows, int64_t heads, int64_t width, float eps, float post, void* workspace,
+                                 size_t workspace_bytes, void* stream);
+
+/*
+ * AdamW over many tensors in one launch (decoupled weight decay, each tensor its own):
+ *     g = grad_scale grad;  m = beta1 m + (1 - beta1) g;  v = beta2 v + (1 - beta2) g g;
+ *     w = w (1 - lr wd) - lr / (1 - beta1^t) m / (sqrt(v) / sqrt(1 - beta2^t) + eps),   lr = cfg.lr * lr_scale of the tensor
+ * The tensors are named once, in a table that the caller keeps in device memory: codistill_adamw_table fills a HOST buffer of
+ * codistill_adamw_table_bytes bytes and a small host plan; the caller copies the buffer to the device and hands both to every step.  The library
+ * retains neither.
+ *   w      device fp32, updated in place;  grad  device fp32 or bf16 (grad_dtype), read only;  lowp  device bf16 copy of the new weights, or NULL
+ *   m, v   state_bits 32: device fp32 [n].  state_bits 8: device uint8 [n] and exps: device uint8 [blocks][2], block = 256 elements of the tensor
+ *          (the last one may be shorter); all zeros to begin with
+ *   m_out, v_out  device bf16 [n], or NULL: where codistill_adamw_unpack writes the values that 8-bit moments stand for
+ * 8-bit moments are floats with three mantissa bits whose exponents count down from a block's own power of two: m has a sign and 4 exponent bits, v
+ * none and 5, so that m and sqrt(v) reach equally far below the largest of the block (2^-17).  The stored value is rounded up or down at random
+ * in proportion to the distance (an average over steps is exact, where rounding to nearest would hold v still: beta2 = 0.999 moves it by less than half a
+ * step); a positive v never becomes zero.  The random bits come from cfg.seed and the element's place among all blocks: the same seed
+ * gives the same bits, give each step its own.  A block with a gradient that is not finite is NaN from then on.  w is updated with the
+ * moments before they are rounded.
+ *   grad_scale  device fp32 [1] or NULL (1): clipping or unscaling factor, read by the kernel
+ *   t, lr, betas, eps: host values; the step is computed from them in double
+ * Errors (CD_ERR_INVALID_ARG, nothing launched): NULL or misaligned pointers (16 bytes; bf16 tensors 8, 8-bit moments 4), n < 1, n_tensors < 1,
+ * t < 1, betas outside [0, 1), eps <= 0, NaN lr, decay or lr_scale, state_bits other than 8 and 32; CD_ERR_WORKSPACE_TOO_SMALL: the buffer.
+ */
+typedef struct {
+  float* w;
+  const void* grad;
+  void* lowp;
+  void *m, *v;
+  uint8_t* exps;
+  void *m_out, *v_out;
+  int64_t n;
+  float weight_decay, lr_scale;
+} cd_adamw_tensor;
+typedef struct {
+  int64_t tensors, elements, workgroups;
+  int32_t state_bits, grad_dtype;
+  int32_t has_out, reserved;
+} cd_adamw_plan;
+typedef struct {
+  double lr, beta1, beta2, eps;
+  int64_t t;
+  uint32_t seed;
+} cd_adamw_cfg;
+int codistill_adamw_table_bytes(const cd_adamw_tensor* tensors, int64_t n_tensors, size_t* bytes);
+int codistill_adamw_table(const cd_adamw_tensor* tensors, int64_t n_tensors, int state_bits, int grad_dtype, void* table, size_t table_bytes,
+                          cd_adamw_plan* plan);
+int codistill_adamw_step(const cd_adamw_plan* plan, const void* device_table, const cd_adamw_cfg* cfg, const float* grad_scale, void* stream);
+int codistill_adamw_unpack(const cd_adamw_plan* plan, const void* device_table, void* stream);
+
 /* ---- introspection ----------------------------------------------------------------------- */
 /* The fused op list and where each tensor lives inside a save_for_backward workspace, so that
  * tools and tests can read intermediate activations and activation gradients after a forward /

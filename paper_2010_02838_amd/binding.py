@@ -25,6 +25,10 @@ CD_ARCH_RESNET_BASIC_IMAGENET = 5
 CD_ARCH_RESNEXT = 6
 CD_ARCH_WIDE_RESNET_SPLIT = 7
 CD_MAX_STAGES, CD_NAME_LEN, CD_LOSS_MAX_PEERS = 4, 48, 8
+CD_ROPE_HALVES, CD_ROPE_PAIRS = 0, 1
+CD_ROPE_MAX_PAIRS, CD_ROPE_MAX_TENSORS = 128, 4
+CD_LAMBDA_HEAD, CD_LAMBDA_TOKEN = 0, 1
+ADAMW_BLOCK = 256   # elements that share an exponent in 8-bit moments
 KERNEL_CLASSES = ["conv_fprop", "conv_dgrad", "conv_wgrad", "norm", "glue", "linear", "loss", "sgd", "conv_fprop_narrow",
                   "bn_apply", "conv_fprop_wide", "attention"]
 PARAM_KINDS = ["conv_w", "bias", "bn_gamma", "bn_beta", "linear_w", "embed_w"]
@@ -64,6 +68,38 @@ class LossCfg(ctypes.Structure):
                 ("temperature", ctypes.c_float)]
 
 
+class Rotary(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("dim", ctypes.c_int32), ("n_pairs", ctypes.c_int32), ("axes", ctypes.c_int32),
+                ("layout", ctypes.c_int32), ("axis", ctypes.c_int32 * CD_ROPE_MAX_PAIRS), ("freq", ctypes.c_double * CD_ROPE_MAX_PAIRS)]
+
+
+class RotaryTensor(ctypes.Structure):
+    _fields_ = [("x", ctypes.c_void_p), ("y", ctypes.c_void_p), ("heads", ctypes.c_int64), ("x_token", ctypes.c_int64),
+                ("y_token", ctypes.c_int64)]
+
+
+class DiffAttn(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("dtype", "batch", "tq", "tk", "heads", "kv_heads", "head_dim", "causal", "lambda_kind")] + [
+        ("scale", ctypes.c_float)] + [(n, ctypes.c_int64) for n in (
+            "q_token", "q_batch", "k_token", "k_batch", "v_token", "v_batch", "o_token", "o_batch")] + [
+        (n, ctypes.c_void_p) for n in ("q_lens", "k_lens", "q_starts", "k_starts")] + [("q_rows", ctypes.c_int64), ("k_rows", ctypes.c_int64)]
+
+
+class AdamwTensor(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("w", "grad", "lowp", "m", "v", "exps", "m_out", "v_out")] + [
+        ("n", ctypes.c_int64), ("weight_decay", ctypes.c_float), ("lr_scale", ctypes.c_float)]
+
+
+class AdamwPlan(ctypes.Structure):
+    _fields_ = [("tensors", ctypes.c_int64), ("elements", ctypes.c_int64), ("workgroups", ctypes.c_int64), ("state_bits", ctypes.c_int32),
+                ("grad_dtype", ctypes.c_int32), ("has_out", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class AdamwCfg(ctypes.Structure):
+    _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double), ("eps", ctypes.c_double),
+                ("t", ctypes.c_int64), ("seed", ctypes.c_uint32)]
+
+
 if not os.path.exists(LIB_PATH):
     raise ImportError("libcodistill.so is not built: run `python -m paper_2010_02838_amd.build` "
                       "(or __graft_entry__.build()) first; there is no fallback path")
@@ -88,6 +124,17 @@ _SIGS = {
     "codistill_backward_streams": [_vp, _vp, _vp, _i64, _vp, _sz, _vp, _vp, _i32, _vp],
     "codistill_sgd_step": [_vp, _vp, _vp, _vp, _i64, _f32, _f32, _f32, _i32, _vp],
     "codistill_adam_step": [_vp, _vp, _vp, _vp, _vp, _i64, _f32, _f32, _f32, _f32, _f32, _i64, _vp],
+    "codistill_rotary": [ctypes.POINTER(Rotary), _vp, _i64, ctypes.POINTER(RotaryTensor), _i64, _i32, _vp],
+    "codistill_diff_attention_workspace_bytes": [ctypes.POINTER(DiffAttn), _i32, ctypes.POINTER(_sz)],
+    "codistill_diff_attention": [ctypes.POINTER(DiffAttn)] + [_vp] * 8 + [_sz, _vp],
+    "codistill_diff_attention_backward": [ctypes.POINTER(DiffAttn)] + [_vp] * 13 + [_sz, _vp],
+    "codistill_head_norm": [_i32, _vp, _i64, _vp, _vp, _i64, _i64, _i64, _i64, _f32, _f32, _vp],
+    "codistill_head_norm_workspace_bytes": [_i64, _i64, _i64, ctypes.POINTER(_sz)],
+    "codistill_head_norm_backward": [_i32, _vp, _i64, _vp, _vp, _i64, _vp, _i64, _vp, _i64, _i64, _i64, _f32, _f32, _vp, _sz, _vp],
+    "codistill_adamw_table_bytes": [ctypes.POINTER(AdamwTensor), _i64, ctypes.POINTER(_sz)],
+    "codistill_adamw_table": [ctypes.POINTER(AdamwTensor), _i64, _i32, _i32, _vp, _sz, ctypes.POINTER(AdamwPlan)],
+    "codistill_adamw_step": [ctypes.POINTER(AdamwPlan), _vp, ctypes.POINTER(AdamwCfg), _vp, _vp],
+    "codistill_adamw_unpack": [ctypes.POINTER(AdamwPlan), _vp, _vp],
     "codistill_profile_enable": [_i32],
     "codistill_profile_collect": [],
     "codistill_profile_get": [_i32, ctypes.POINTER(ctypes.c_double), ctypes.POINTER(_i64),
@@ -252,6 +299,180 @@ def codistill_adam_step(master_w, exp_avg, exp_avg_sq, grad, lowp_w_out, lr, t, 
                         weight_decay=0.0):
     _check(lib.codistill_adam_step(_ptr(master_w), _ptr(exp_avg), _ptr(exp_avg_sq), _ptr(grad), _ptr(lowp_w_out),
                                    master_w.numel(), lr, beta1, beta2, eps, weight_decay, int(t), _stream()))
+
+
+def _dtype(t):
+    if t.dtype is torch.bfloat16:
+        return CD_BF16
+    if t.dtype is torch.float32:
+        return CD_F32
+    raise TypeError("bf16 or fp32 tensors only, got %s" % t.dtype)
+
+
+def _inner(t, dims, what):
+    """The last `dims` dimensions have to be contiguous; returns the strides of the others."""
+    run = 1
+    for d in range(t.dim() - 1, t.dim() - 1 - dims, -1):
+        if t.shape[d] != 1 and t.stride(d) != run:
+            raise ValueError("%s: the channels of a token have to be contiguous" % what)
+        run *= t.shape[d]
+    return t.stride()[:t.dim() - dims]
+
+
+def rotary_desc(dim, sections, theta, dtype, layout=CD_ROPE_HALVES, freq=None):
+    """Rotary positions of heads of `dim` channels.  sections: pairs of each axis, in the order of `positions`' rows; pairs behind the last
+    one are copied.  One ladder of frequencies over all pairs, theta^(-2p/dim), unless `freq` gives them (radians a position)."""
+    axis = [a for a, n in enumerate(sections) for _ in range(n)]
+    if len(axis) > min(dim // 2, CD_ROPE_MAX_PAIRS):
+        raise ValueError("rotary: %d pairs in heads of %d channels" % (len(axis), dim))
+    freq = [theta ** (-2.0 * p / dim) for p in range(len(axis))] if freq is None else list(freq)
+    if len(freq) != len(axis):
+        raise ValueError("rotary: %d frequencies for %d pairs" % (len(freq), len(axis)))
+    d = Rotary(CD_BF16 if dtype is torch.bfloat16 else CD_F32, dim, len(axis), len(sections), layout)
+    d.axis[:len(axis)] = axis
+    d.freq[:len(freq)] = freq
+    return d
+
+
+def codistill_rotary(desc, positions, tensors, inverse=False):
+    """positions: int32 [axes, tokens]; tensors: up to four pairs (x, y) of [tokens, heads, dim] (y may be x); inverse: the gradient."""
+    arr = (RotaryTensor * len(tensors))()
+    tokens = positions.shape[1]
+    if positions.dtype is not torch.int32 or not positions.is_contiguous() or positions.shape[0] < desc.axes:
+        raise ValueError("rotary: positions are contiguous int32 [axes, tokens]")
+    for a, (x, y) in zip(arr, tensors):
+        if x.shape != y.shape or x.shape[0] != tokens or x.shape[2] != desc.dim or _dtype(x) != desc.dtype or _dtype(y) != desc.dtype:
+            raise ValueError("rotary: tensors are [tokens, heads, dim] of the descriptor's type")
+        a.x, a.y, a.heads = x.data_ptr(), y.data_ptr(), x.shape[1]
+        a.x_token, a.y_token = _inner(x, 2, "rotary")[0], _inner(y, 2, "rotary")[0]
+    _check(lib.codistill_rotary(ctypes.byref(desc), _ptr(positions), tokens, arr, len(tensors), int(inverse), _stream()))
+
+
+def diff_attention_desc(q, k, v, out, lam, causal=False, scale=0.0, q_lens=None, k_lens=None, q_starts=None, k_starts=None, max_q=0, max_k=0):
+    """What differential attention of tensors laid out like these needs to know; kept by the caller and handed to every call.
+
+    Padded: q [B, Tq, H, 2, D], k [B, Tk, Hk, 2, D], v [B, Tk, Hk, 2 D], out [B, Tq, H, 2 D], q_lens / k_lens int32 [B] or None.
+    Packed (q_starts, k_starts int32 [B + 1] and the longest sequence's max_q, max_k): the same without the batch dimension.
+    lam: fp32 [H], or [B, Tq, H] / [rows, H].  Tokens and sequences may be strided, the channels of a token are contiguous."""
+    packed = q_starts is not None or k_starts is not None
+    off = 0 if packed else 1
+    if q.dim() != 4 + off or k.dim() != 4 + off or v.dim() != 3 + off or out.dim() != 3 + off or q.shape[-2] != 2 or k.shape[-2] != 2:
+        raise ValueError("diff_attention: q, k are [.., heads, 2, head_dim], v and out [.., heads, 2 head_dim]")
+    dim, heads, kv_heads = q.shape[-1], q.shape[off + 1], k.shape[off + 1]
+    if (k.shape[-1] != dim or v.shape[-1] != 2 * dim or v.shape[off + 1] != kv_heads or out.shape != q.shape[:off + 2] + (2 * dim,)
+            or k.shape[:off + 1] != v.shape[:off + 1] or (off and k.shape[0] != q.shape[0])):
+        raise ValueError("diff_attention: the shapes of q, k, v and out do not fit")
+    if any(t.dtype is not q.dtype for t in (k, v, out)) or lam.dtype is not torch.float32 or not lam.is_contiguous():
+        raise TypeError("diff_attention: q, k, v and out have one type, lambda is contiguous fp32")
+    if tuple(lam.shape) not in ((heads,), tuple(q.shape[:off + 2])):
+        raise ValueError("diff_attention: lambda is [heads] or one for each query and head")
+    batch = q_starts.numel() - 1 if packed else q.shape[0]
+    for t, n in ((q_lens, batch), (k_lens, batch), (q_starts, batch + 1), (k_starts, batch + 1)):
+        if t is not None and (t.dtype is not torch.int32 or t.numel() != n or not t.is_contiguous()):
+            raise ValueError("diff_attention: lens are int32 [batch], starts int32 [batch + 1]")
+    d = DiffAttn(dtype=_dtype(q), batch=batch, tq=max_q if packed else q.shape[1], tk=max_k if packed else k.shape[1], heads=heads, kv_heads=kv_heads,
+                 head_dim=dim, causal=int(causal), lambda_kind=CD_LAMBDA_HEAD if lam.dim() == 1 else CD_LAMBDA_TOKEN, scale=scale,
+                 q_rows=q.shape[0] if packed else 0, k_rows=k.shape[0] if packed else 0)
+    for name, t, inner in (("q", q, 3), ("k", k, 3), ("v", v, 2), ("o", out, 2)):
+        s = _inner(t, inner, "diff_attention")
+        least = t.shape[off + 1] * 2 * dim   # (the stride of a dimension of one element says nothing)
+        setattr(d, name + "_token", s[-1] if t.shape[off] > 1 else max(s[-1], least))
+        setattr(d, name + "_batch", s[0] if off and batch > 1 else 0)
+    for name, t in (("q_lens", q_lens), ("k_lens", k_lens), ("q_starts", q_starts), ("k_starts", k_starts)):
+        if t is not None:
+            setattr(d, name, t.data_ptr())
+    d.keep = (q_lens, k_lens, q_starts, k_starts)
+    d.layout = tuple((t.shape, t.stride(), t.dtype) for t in (q, k, v, out, lam))
+    d.lse_shape = (2, heads, q.shape[0] * (q.shape[1] if off else 1))
+    return d
+
+
+def _laid_out(desc, tensors):
+    """The kernels go by the descriptor: a tensor of another shape, stride or type would be read beyond its end."""
+    for t, want in zip(tensors, desc.layout):
+        if (t.shape, t.stride(), t.dtype) != want:
+            raise ValueError("diff_attention: a tensor of shape %s, strides %s, %s where the descriptor has %s, %s, %s" % (
+                tuple(t.shape), t.stride(), t.dtype, tuple(want[0]), want[1], want[2]))
+
+
+def _kept(desc, o_second, lse):
+    shape, _, dtype = desc.layout[3]
+    if o_second.shape != shape or o_second.dtype is not dtype or not o_second.is_contiguous() or lse.shape != desc.lse_shape or (
+            lse.dtype is not torch.float32 or not lse.is_contiguous()):
+        raise ValueError("diff_attention: o_second is contiguous in out's shape, lse fp32 %s" % (desc.lse_shape,))
+
+
+def diff_attention_workspace_bytes(desc, backward):
+    b = _sz()
+    _check(lib.codistill_diff_attention_workspace_bytes(ctypes.byref(desc), int(backward), ctypes.byref(b)))
+    return b.value
+
+
+def _room(t):
+    return 0 if t is None else t.numel() * t.element_size()
+
+
+def codistill_diff_attention(desc, q, k, v, lam, out, o_second=None, lse=None, workspace=None):
+    """out = (softmax(q_1 k_1) - lam softmax(q_2 k_2)) v.  o_second (contiguous, out's shape) and lse (fp32 [2, heads, rows of q]) are kept for
+    the backward pass; both or neither."""
+    _laid_out(desc, (q, k, v, out, lam))
+    if o_second is not None and lse is not None:
+        _kept(desc, o_second, lse)
+    _check(lib.codistill_diff_attention(ctypes.byref(desc), _ptr(q), _ptr(k), _ptr(v), _ptr(lam), _ptr(out), _ptr(o_second), _ptr(lse), _ptr(workspace),
+                                        _room(workspace), _stream()))
+
+
+def codistill_diff_attention_backward(desc, q, k, v, lam, out, o_second, lse, dout, dq, dk, dv, dlam, workspace):
+    """Gradients; dout is laid out like out, dq, dk, dv like q, k, v, dlam like lam."""
+    _laid_out(desc, (q, k, v, out, lam))
+    _laid_out(desc, (dq, dk, dv, dout, dlam))
+    _kept(desc, o_second, lse)
+    _check(lib.codistill_diff_attention_backward(ctypes.byref(desc), _ptr(q), _ptr(k), _ptr(v), _ptr(lam), _ptr(out), _ptr(o_second), _ptr(lse), _ptr(dout),
+                                                 _ptr(dq), _ptr(dk), _ptr(dv), _ptr(dlam), _ptr(workspace), _room(workspace), _stream()))
+
+
+def head_norm_workspace_bytes(rows, heads, width):
+    b = _sz()
+    _check(lib.codistill_head_norm_workspace_bytes(rows, heads, width, ctypes.byref(b)))
+    return b.value
+
+
+def codistill_head_norm(x, gain, y, eps=1e-5, post=1.0):
+    """y = post gain x / sqrt(mean(x^2) + eps) over the last dimension of x [rows, heads, width]."""
+    if x.shape != y.shape or gain.shape != x.shape[2:] or y.dtype is not x.dtype or gain.dtype is not x.dtype:
+        raise ValueError("head_norm: x and y are [rows, heads, width], gain [width], all of one type")
+    _check(lib.codistill_head_norm(_dtype(x), _ptr(x), _inner(x, 2, "head_norm")[0], _ptr(gain), _ptr(y), _inner(y, 2, "head_norm")[0], x.shape[0], x.shape[1],
+                                   x.shape[2], eps, post, _stream()))
+
+
+def codistill_head_norm_backward(x, gain, dy, dx, dgain, workspace, eps=1e-5, post=1.0):
+    """dx (may be dy) and dgain (fp32 [width]) of codistill_head_norm."""
+    if x.shape != dy.shape or x.shape != dx.shape or gain.shape != x.shape[2:] or dgain.shape != gain.shape:
+        raise ValueError("head_norm_backward: x, dy and dx are [rows, heads, width], gain and dgain [width]")
+    if any(t.dtype is not x.dtype for t in (gain, dy, dx)) or dgain.dtype is not torch.float32:
+        raise ValueError("head_norm_backward: one type, dgain fp32")
+    _check(lib.codistill_head_norm_backward(_dtype(x), _ptr(x), _inner(x, 2, "head_norm")[0], _ptr(gain), _ptr(dy), _inner(dy, 2, "head_norm")[0], _ptr(dx),
+                                            _inner(dx, 2, "head_norm")[0], _ptr(dgain), x.shape[0], x.shape[1], x.shape[2], eps, post, _ptr(workspace),
+                                            _room(workspace), _stream()))
+
+
+def adamw_table(tensors, state_bits, grad_dtype):
+    """(plan, host bytes) of a list of AdamwTensor: the bytes go to device memory, and both to every step."""
+    arr = (AdamwTensor * len(tensors))(*tensors)
+    n, plan = _sz(), AdamwPlan()
+    _check(lib.codistill_adamw_table_bytes(arr, len(tensors), ctypes.byref(n)))
+    host = torch.empty(n.value, dtype=torch.uint8)
+    _check(lib.codistill_adamw_table(arr, len(tensors), state_bits, grad_dtype, _ptr(host), n.value, ctypes.byref(plan)))
+    return plan, host
+
+
+def codistill_adamw_step(plan, table, lr, t, beta1=0.9, beta2=0.999, eps=1e-8, seed=0, grad_scale=None):
+    cfg = AdamwCfg(lr, beta1, beta2, eps, int(t), seed & 0xffffffff)
+    _check(lib.codistill_adamw_step(ctypes.byref(plan), _ptr(table), ctypes.byref(cfg), _ptr(grad_scale), _stream()))
+
+
+def codistill_adamw_unpack(plan, table):
+    _check(lib.codistill_adamw_unpack(ctypes.byref(plan), _ptr(table), _stream()))
 
 
 def profile_enable(on):
