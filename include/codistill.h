@@ -344,13 +344,14 @@ int codistill_adam_step(float* master_w, float* exp_avg, float* exp_avg_sq, cons
  * Rotary positions with several axes.  Pair p of a head's `dim` channels is turned by the angle
  *     positions[axis[p]][token] * freq[p]        y1 = x1 cos - x2 sin,  y2 = x2 cos + x1 sin
  * (inverse: by the opposite angle, which is the gradient's direction).  Pairs from n_pairs on are copied.  CD_ROPE_HALVES: pair p is
- * channels p and p + dim/2; CD_ROPE_PAIRS: channels 2p and 2p + 1.  Angles are reduced to turns in a two-part fp32 product, exact to
- * 1e-7 turns at any position; sums in fp32, rounded once.
+ * channels p and p + dim/2; CD_ROPE_PAIRS: channels 2p and 2p + 1.  Angles are exact to
+ * 2^-25 of a turn at any position; sums in fp32, rounded once.
  *   tensors    HOST array of n_tensors descriptors, all with the same tokens (queries and keys go in one launch): x and y device,
  *              [tokens][heads][dim] in `dtype`, channels contiguous, heads dim elements apart, tokens x_token / y_token apart.  y may be x
  *   positions  device int32 [axes][tokens]
  * Any 2 <= dim <= 2 * CD_ROPE_MAX_PAIRS, even; tensors that are 16-byte aligned with 16-byte multiples for strides and half heads move
- * in whole vectors, others element by element.  tokens == 0 is allowed and does nothing.
+ * in whole vectors, others element by element.  tokens == 0 is allowed and does nothing (x, y and positions may then be
+ * NULL).
  * Errors (CD_ERR_INVALID_ARG, nothing launched): NULL pointers, odd or oversized dim, n_pairs > dim/2, an axis outside [0, axes), a
  * non-finite frequency, strides below heads * dim, n_tensors outside 1..CD_ROPE_MAX_TENSORS, pointers not aligned to their elements.
  */
@@ -429,7 +430,7 @@ int codistill_diff_attention_backward(const cd_diff_attn* desc, const void* q, c
  *   gain   device [width] in dtype, shared by all heads
  * Backward: dx, and dgain (fp32 [width], sums over all rows and heads in a fixed order).  x is read again and its statistics are taken again:
  * nothing is kept.  dx may be dy.  workspace: codistill_head_norm_workspace_bytes.
- * 1 <= width <= 1024; rows == 0 is allowed (dgain is then zero).  Errors: CD_ERR_INVALID_ARG, CD_ERR_WORKSPACE_TOO_SMALL, nothing launched.
+ * 1 <= width <= 1024; rows == 0 is allowed (dgain is then zero; x, y, dy, dx may be NULL).  Errors: CD_ERR_INVALID_ARG, CD_ERR_WORKSPACE_TOO_SMALL, nothing launched.
  */
 int codistill_head_norm(int dtype, const void* x, int64_t x_row, const void* gain, void* y, int64_t y_row, int64_t rows, int64_t heads,
                         int64_t width, float eps, float post, void* stream);

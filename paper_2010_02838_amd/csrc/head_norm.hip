@@ -220,7 +220,7 @@ using namespace cd;
 
 extern "C" int codistill_head_norm(int dtype, const void* x, int64_t x_row, const void* gain, void* y, int64_t y_row, int64_t rows, int64_t heads,
                                    int64_t width, float eps, float post, void* stream) {
-  CD_REQUIRE(x && gain && y, "head_norm: NULL pointer argument");
+  CD_REQUIRE(gain && (rows == 0 || (x && y)), "head_norm: NULL pointer argument");
   if (const int rc = check("head_norm", dtype, rows, heads, width, eps, post)) return rc;
   const int elem = dtype == CD_BF16 ? 2 : 4;
   CD_REQUIRE(fits(x, elem) && fits(gain, elem) && fits(y, elem), "head_norm: misaligned pointer");
@@ -249,7 +249,7 @@ extern "C" int codistill_head_norm_workspace_bytes(int64_t rows, int64_t heads, 
 extern "C" int codistill_head_norm_backward(int dtype, const void* x, int64_t x_row, const void* gain, const void* dy, int64_t dy_row, void* dx,
                                             int64_t dx_row, float* dgain, int64_t rows, int64_t heads, int64_t width, float eps, float post,
                                             void* workspace, size_t workspace_bytes, void* stream) {
-  CD_REQUIRE(x && gain && dy && dx && dgain && workspace, "head_norm_backward: NULL pointer argument");
+  CD_REQUIRE(gain && dgain && workspace && (rows == 0 || (x && dy && dx)), "head_norm_backward: NULL pointer argument");
   if (const int rc = check("head_norm_backward", dtype, rows, heads, width, eps, post)) return rc;
   const int elem = dtype == CD_BF16 ? 2 : 4;
   CD_REQUIRE(fits(x, elem) && fits(gain, elem) && fits(dy, elem) && fits(dx, elem) && fits(dgain, 4) && aligned16(workspace), "head_norm_backward: misaligned pointer");

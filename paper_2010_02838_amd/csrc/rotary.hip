@@ -21,18 +21,14 @@ struct RopeArgs {
   int64_t tokens;
   const int32_t* pos;
   float sign;
-  float hi[CD_ROPE_MAX_PAIRS], lo[CD_ROPE_MAX_PAIRS];   // turns a position, in two parts
+  uint64_t freq[CD_ROPE_MAX_PAIRS];   // turns a position, as a fraction of 2^64
   uint8_t axis[CD_ROPE_MAX_PAIRS];
 };
 static_assert(sizeof(RopeArgs) <= 4096, "kernel arguments");
 
-// Turns, reduced to about [-1, 1]: position and frequency in two parts each.  A single fp32 product is half a turn off at a position of 2^24
-// and a thousandth of a radian at 30000.
-__device__ inline float turns(int32_t pos, float hi, float lo) {
-  const float ph = (float)(pos & ~0xfff), pl = (float)(pos & 0xfff);
-  // (fused: the product keeps its low bits while the whole turns leave it)
-  return fmaf(ph, hi, -rintf(ph * hi)) + fmaf(pl, hi, -rintf(pl * hi)) + (ph + pl) * lo;
-}
+// The angle in turns, in [-1/2, 1/2).  A frequency is a 64-bit fraction of a turn, so that whole turns fall out of the integer product and 2^-25
+// of a turn is all that is lost at any position.  A single fp32 product is a thousandth of a radian off at 30000 and half a turn at 2^24.
+__device__ inline float turns(int32_t pos, uint64_t freq) { return (float)(int32_t)(((uint64_t)(int64_t)pos * freq) >> 32) * 0x1p-32f; }
 
 template <typename T, int N> struct Vec { T e[N]; };
 template <typename T, int N> __device__ inline Vec<T, N> load_vec(const T* p) {
@@ -67,7 +63,7 @@ __global__ void __launch_bounds__(256) rotary_kernel(RopeArgs a) {
   const int nt = (int)min((int64_t)a.block_tokens, a.tokens - t0);
   for (int i = threadIdx.x; i < nt * a.n_pairs; i += 256) {
     const int t = i / a.n_pairs, p = i % a.n_pairs;
-    const float r = turns(a.pos[(int64_t)a.axis[p] * a.tokens + t0 + t], a.hi[p], a.lo[p]);
+    const float r = turns(a.pos[(int64_t)a.axis[p] * a.tokens + t0 + t], a.freq[p]);
     if (sizeof(T) == 2) {   // the instructions take turns; their error, 1e-6, is far below a bf16 rounding
       cs[t * CD_ROPE_MAX_PAIRS + p] = __builtin_amdgcn_cosf(r);
       sn[t * CD_ROPE_MAX_PAIRS + p] = a.sign * __builtin_amdgcn_sinf(r);
@@ -123,7 +119,7 @@ using namespace cd;
 
 extern "C" int codistill_rotary(const cd_rotary* rope, const int32_t* positions, int64_t tokens, const cd_rotary_tensor* tensors,
                                 int64_t n_tensors, int inverse, void* stream) {
-  CD_REQUIRE(rope && positions && tensors, "rotary: NULL pointer argument");
+  CD_REQUIRE(rope && tensors && (positions || tokens == 0), "rotary: NULL pointer argument");
   CD_REQUIRE(rope->dtype == CD_F32 || rope->dtype == CD_BF16, "rotary: unknown dtype %d", rope->dtype);
   CD_REQUIRE(rope->dim >= 2 && rope->dim % 2 == 0 && rope->dim <= 2 * CD_ROPE_MAX_PAIRS, "rotary: dim=%d must be even and in 2..%d", rope->dim,
              2 * CD_ROPE_MAX_PAIRS);
@@ -139,7 +135,7 @@ extern "C" int codistill_rotary(const cd_rotary* rope, const int32_t* positions,
   int64_t heads = 0, moved = 0;
   for (int64_t i = 0; i < n_tensors; i++) {
     const cd_rotary_tensor& t = tensors[i];
-    CD_REQUIRE(t.x && t.y, "rotary: NULL pointer in tensor %lld", (long long)i);
+    CD_REQUIRE((t.x && t.y) || tokens == 0, "rotary: NULL pointer in tensor %lld", (long long)i);
     CD_REQUIRE(t.heads >= 1 && t.heads <= 65536, "rotary: heads=%lld of tensor %lld out of range", (long long)t.heads, (long long)i);
     CD_REQUIRE((t.x_token >= t.heads * rope->dim && t.y_token >= t.heads * rope->dim) || tokens <= 1, "rotary: a token of tensor %lld is longer than its stride",
                (long long)i);
@@ -154,8 +150,8 @@ extern "C" int codistill_rotary(const cd_rotary* rope, const int32_t* positions,
     CD_REQUIRE(rope->axis[p] >= 0 && rope->axis[p] < rope->axes && rope->axis[p] < 256, "rotary: axis %d of pair %d outside 0..%d", rope->axis[p], p, rope->axes - 1);
     CD_REQUIRE(isfinite(rope->freq[p]) && fabs(rope->freq[p]) < 1e6, "rotary: frequency of pair %d", p);
     const double turn = rope->freq[p] / 6.283185307179586476925;
-    a.hi[p] = (float)turn;
-    a.lo[p] = (float)(turn - a.hi[p]);
+    const double part = turn - floor(turn);
+    a.freq[p] = part < 1.0 ? (uint64_t)ldexp(part, 64) : 0;
     a.axis[p] = (uint8_t)rope->axis[p];
   }
   if (tokens == 0) return CD_OK;
