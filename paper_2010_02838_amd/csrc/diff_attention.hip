@@ -121,7 +121,7 @@ template <> struct Ops<float> {
 // Sizes of an instance: DT = head_dim rounded up to 32, 64 or 128, rows of 2 DT elements in LDS (both maps, or the values), KC streamed rows at
 // a time, 16 bytes of padding a row so that 16-byte reads of many rows spread over the banks.
 template <typename T, int DT> struct Sizes {
-  static constexpr int W = 2 * DT, PITCH = W + Ops<T>::VE, KC = sizeof(T) == 4 && DT == 128 ? 32 : 64;
+  static constexpr int W = 2 * DT, PITCH = W + Ops<T>::VE, KC = 32;
   static constexpr int KS = DT / 16, VT = W / 32, DTT = DT / 32;
 };
 constexpr int EXACT_KEYS = 128;   // rows that reach no more keys than this get their deltas in a pass of their own
@@ -151,23 +151,29 @@ template <typename T> __device__ inline T* rows_of(const DiffArgs& a, T* p, int 
 }
 __device__ inline int query_of(const DiffArgs& a, int r) { return a.group == 1 ? r : (int)__umulhi((uint32_t)r, a.group_inv); }
 
-// Workgroups go to the eight L2 caches in turn: neighbours in this order share their keys and land on the same one.
-__device__ inline int work_index(int n) {
-  const int per = (n + 7) >> 3;
-  return (int)(blockIdx.x & 7) * per + (int)(blockIdx.x >> 3);
+// Workgroups go to the eight L2 caches in turn; each cache gets a run of neighbours in the order (unit, tile), which share their keys.  Under a
+// causal mask the run's units are taken in turns, so that the long tiles of all of them start before the short ones.
+__device__ inline int work_index(int n, int per_unit, bool turns) {
+  const int per = (n + 7) >> 3, at = (int)(blockIdx.x >> 3);
+  int x = at;
+  if (turns) {
+    const int units = per / per_unit;
+    if (units > 1 && units * per_unit == per) x = at % units * per_unit + at / units;
+  }
+  return (int)(blockIdx.x & 7) * per + x;
 }
 static unsigned work_blocks(int64_t n) { return (unsigned)(cdiv(n, 8) * 8); }
 
 // Up to KC rows of 2 dim elements (two ranges of dim for the maps, MAPS, or one of 2 dim) on their way into LDS; what lies beyond the rows and the
 // channels becomes zero.  `at(r)` is the address of row r < n.
-template <typename T, int DT, bool MAPS> struct Stage {
+template <typename T, int DT, bool MAPS, int THREADS = 256> struct Stage {
   typedef Sizes<T, DT> S;
-  static constexpr int VE = Ops<T>::VE, VPR = S::W / VE, IT = S::KC * VPR / 256;
+  static constexpr int VE = Ops<T>::VE, VPR = S::W / VE, IT = S::KC * VPR / THREADS;
   uint4 u[IT];
   template <typename At> __device__ inline void load(int n, int dim, At at) {
 #pragma unroll
     for (int i = 0; i < IT; i++) {
-      const int x = threadIdx.x + 256 * i, r = x / VPR, c = (x % VPR) * VE;
+      const int x = threadIdx.x + THREADS * i, r = x / VPR, c = (x % VPR) * VE;
       u[i] = make_uint4(0, 0, 0, 0);
       const int cc = MAPS ? (c >= DT ? c - DT : c) : c;
       const bool in = r < n && cc < (MAPS ? dim : 2 * dim);
@@ -177,7 +183,7 @@ template <typename T, int DT, bool MAPS> struct Stage {
   __device__ inline void store(T* dst) const {
 #pragma unroll
     for (int i = 0; i < IT; i++) {
-      const int x = threadIdx.x + 256 * i, r = x / VPR, c = (x % VPR) * VE;
+      const int x = threadIdx.x + THREADS * i, r = x / VPR, c = (x % VPR) * VE;
       *reinterpret_cast<uint4*>(dst + r * S::PITCH + c) = u[i];
     }
   }
@@ -204,162 +210,167 @@ __device__ inline float other_half(float v) { return __shfl_xor(v, 32, 64); }
 __device__ inline float finite_or_zero(float m) { return m == -INFINITY ? 0.f : m; }
 
 // ---- forward -------------------------------------------------------------------------------------------------------------------
+// A wave owns 32 rows of one of the two maps; the waves of a pair exchange their results at the end.  (Both maps in one wave share the fragments of
+// v, but need 256 accumulators for the widest heads, which spill, and 128 for heads of 64, which leave two waves a SIMD and nothing in
+// flight beside them.)
+constexpr int F_GROUPS = 2, F_ROWS = 32 * F_GROUPS, F_THREADS = 128 * F_GROUPS;
+
 template <typename T, int DT>
-__global__ void __launch_bounds__(256, sizeof(T) == 2 && DT <= 64 ? 2 : 1) diff_forward_kernel(DiffArgs a) {
+__global__ void __launch_bounds__(F_THREADS, sizeof(T) == 4 ? (DT == 128 ? 1 : 2) : DT == 128 ? 2 : 3) diff_forward_kernel(DiffArgs a) {
   typedef Ops<T> O;
   typedef Sizes<T, DT> S;
-  __shared__ __attribute__((aligned(16))) T Ks[S::KC * S::PITCH];
-  __shared__ __attribute__((aligned(16))) T Vs[S::KC * S::PITCH];
-  const int w = work_index(a.units * a.tiles * a.parts);
-  if (w >= a.units * a.tiles * a.parts) return;
+  __shared__ __attribute__((aligned(16))) T lds[4 * S::KC * S::PITCH];   // keys and values, two buffers each
+  constexpr int BUF = S::KC * S::PITCH;
+  const int total = a.units * a.tiles * a.parts;
+  const int w = work_index(total, a.tiles * a.parts, a.causal);
+  if (w >= total) return;
   const int part = w % a.parts, ut = w / a.parts, unit = ut / a.tiles;
   const int tile = a.tiles - 1 - ut % a.tiles;   // under a causal mask the last rows see the most keys: they go first
   const int b = unit / a.kv_heads, hk = unit % a.kv_heads;
   const Seq s = sequence(a, b);
-  const int R = s.nq * a.group, r0 = tile * ROWS, room = a.q_starts ? R : a.tq * a.group;
+  const int R = s.nq * a.group, r0 = tile * F_ROWS, room = a.q_starts ? R : a.tq * a.group;
   if (r0 >= room) return;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 31, hh = lane >> 5;
-  const int r = r0 + 32 * wave + c;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 31, hh = lane >> 5, m = wave & 1, rg = wave >> 1;
+  const int wr0 = r0 + 32 * rg, r = wr0 + c;
   const bool live = r < R;
   const int i = query_of(a, r), h = hk * a.group + (r - i * a.group);
   const T* kp = rows_of(a, static_cast<const T*>(a.k), b, s.k0, a.k_token, a.k_batch) + (int64_t)hk * 2 * a.dim;
   const T* vp = rows_of(a, static_cast<const T*>(a.v), b, s.k0, a.v_token, a.v_batch) + (int64_t)hk * 2 * a.dim;
-  typename O::Frag qf[2 * S::KS];
-  own_row<T, DT, true>(qf, rows_of(a, static_cast<const T*>(a.q), b, s.q0, a.q_token, a.q_batch) + i * a.q_token + (int64_t)h * 2 * a.dim, live, a.dim, hh);
+  typename O::Frag qf[S::KS];
+  {
+    const T* qp = rows_of(a, static_cast<const T*>(a.q), b, s.q0, a.q_token, a.q_batch) + i * a.q_token + (int64_t)h * 2 * a.dim + m * a.dim;
+#pragma unroll
+    for (int t = 0; t < S::KS; t++) {
+      qf[t] = O::zero();
+      if (live && 16 * t + 8 * hh < a.dim) qf[t] = O::load(qp + 16 * t + 8 * hh);
+    }
+  }
   // keys this row sees, and those that the rows of the wave and of the workgroup reach
   const int off = s.nk - s.nq;
   auto limit = [&](int row) { return a.causal ? min(s.nk, query_of(a, row) + off + 1) : s.nk; };
-  const int see = live ? limit(r) : s.nk;
-  const int wr0 = r0 + 32 * wave, least = limit(wr0), reach = wr0 < R ? limit(min(wr0 + 31, R - 1)) : 0;
   // (the keys of a part: whole tiles of 32)
   const int per = a.parts == 1 ? s.nk : (((s.nk + 31) / 32 + a.parts - 1) / a.parts) * 32;
-  const int begin = part * per, last = r0 < R ? min(limit(min(r0 + ROWS, R) - 1), begin + per) : 0;
-  v16f o[2][S::VT];
+  const int begin = part * per, last = r0 < R ? min(limit(min(r0 + F_ROWS, R) - 1), begin + per) : 0;
+  const int see = min(live ? limit(r) : s.nk, last), least = min(limit(wr0), last), reach = wr0 < R ? min(limit(min(wr0 + 31, R - 1)), last) : 0;
+  v16f o[S::VT];
 #pragma unroll
-  for (int m = 0; m < 2; m++)
+  for (int t = 0; t < S::VT; t++) clear(o[t]);
+  float mx = -INFINITY, sum = 0.f;
+  // One barrier a tile: while a tile of keys and values is worked on, the next one is written to the other buffer and the one after it is
+  // on its way into registers.
+  Stage<T, DT, true, F_THREADS> ks;
+  Stage<T, DT, false, F_THREADS> vs;
+  auto fetch = [&](int j) {
+    ks.load(min(S::KC, s.nk - j), a.dim, [&](int row) { return kp + (int64_t)(j + row) * a.k_token; });
+    vs.load(min(S::KC, s.nk - j), a.dim, [&](int row) { return vp + (int64_t)(j + row) * a.v_token; });
+  };
+  if (begin < last) {
+    fetch(begin);
+    ks.store(lds);
+    vs.store(lds + 2 * BUF);
+    if (begin + S::KC < last) fetch(begin + S::KC);
+  }
+  __syncthreads();
+  for (int j0 = begin, buf = 0; j0 < last; j0 += S::KC, buf ^= 1) {
+    const T* Ks = lds + buf * BUF;
+    const T* Vs = lds + (2 + buf) * BUF;
+    if (j0 < reach) {
+      v16f sc;
+      clear(sc);
 #pragma unroll
-    for (int t = 0; t < S::VT; t++) clear(o[m][t]);
-  float mx[2] = {-INFINITY, -INFINITY}, sum[2] = {0.f, 0.f};
-  for (int j0 = begin; j0 < last; j0 += S::KC) {
-    Stage<T, DT, true> ks;
-    Stage<T, DT, false> vs;
-    const int n = min(S::KC, s.nk - j0);
-    ks.load(n, a.dim, [&](int row) { return kp + (int64_t)(j0 + row) * a.k_token; });
-    vs.load(n, a.dim, [&](int row) { return vp + (int64_t)(j0 + row) * a.v_token; });
-    __syncthreads();
-    ks.store(Ks);
-    vs.store(Vs);
-    __syncthreads();
-#pragma unroll
-    for (int kt = 0; kt < S::KC / 32; kt++) {
-      const int jt = j0 + 32 * kt;
-      if (jt >= min(reach, last)) break;
-      v16f sc[2];
-      float top[2];
-#pragma unroll
-      for (int m = 0; m < 2; m++) {
-        clear(sc[m]);
-#pragma unroll
-        for (int t = 0; t < S::KS; t++)
-          sc[m] = O::mma(O::load(Ks + (32 * kt + c) * S::PITCH + m * DT + 16 * t + 8 * hh), qf[m * S::KS + t], sc[m]);
-      }
-      const int visible = min(see, last);
-      if (jt + 32 > min(least, last)) {   // some row of the wave does not see all of the tile
+      for (int t = 0; t < S::KS; t++) sc = O::mma(O::load(Ks + c * S::PITCH + m * DT + 16 * t + 8 * hh), qf[t], sc);
+      if (j0 + 32 > least) {   // some row of the wave does not see all of the tile
 #pragma unroll
         for (int v = 0; v < 16; v++)
-          if (jt + 8 * (v >> 2) + 4 * hh + (v & 3) >= visible) { sc[0][v] = -INFINITY; sc[1][v] = -INFINITY; }
+          if (j0 + 8 * (v >> 2) + 4 * hh + (v & 3) >= see) sc[v] = -INFINITY;
       }
+      float top = sc[0];
 #pragma unroll
-      for (int m = 0; m < 2; m++) {
-        top[m] = sc[m][0];
-#pragma unroll
-        for (int v = 1; v < 16; v++) top[m] = fmaxf(top[m], sc[m][v]);
-        top[m] *= a.c;
-      }
+      for (int v = 1; v < 16; v++) top = fmaxf(top, sc[v]);
+      top *= a.c;
       // The maximum is only raised, and what has been summed only rescaled, when a score exceeds it by 2^8: weights up to 256 round as well
       // as weights up to 1, and after the first tiles this is rare.
-      if (__any(top[0] > mx[0] + 8.f || top[1] > mx[1] + 8.f)) {
+      if (__any(top > mx + 8.f)) {
+        const float now = fmaxf(mx, fmaxf(top, other_half(top)));
+        const float f = exp2_fast(mx - finite_or_zero(now));
+        mx = now;
+        sum *= f;
 #pragma unroll
-        for (int m = 0; m < 2; m++) {
-          const float now = fmaxf(mx[m], fmaxf(top[m], other_half(top[m])));
-          const float r = exp2_fast(mx[m] - finite_or_zero(now));
-          mx[m] = now;
-          sum[m] *= r;
-#pragma unroll
-          for (int t = 0; t < S::VT; t++) o[m][t] *= r;
-        }
+        for (int t = 0; t < S::VT; t++) o[t] *= f;
       }
+      const float base = finite_or_zero(mx);   // (a row that has seen no key: exp2(-inf) = 0)
 #pragma unroll
-      for (int m = 0; m < 2; m++) {
-        const float base = finite_or_zero(mx[m]);   // (a row that has seen no key: exp2(-inf) = 0)
-#pragma unroll
-        for (int v = 0; v < 16; v++) {
-          sc[m][v] = exp2_fast(fmaf(sc[m][v], a.c, -base));
-          sum[m] += sc[m][v];
-        }
+      for (int v = 0; v < 16; v++) {
+        sc[v] = exp2_fast(fmaf(sc[v], a.c, -base));
+        sum += sc[v];
       }
 #pragma unroll
       for (int u = 0; u < 2; u++) {
-        const typename O::Frag p0 = O::operand(sc[0], u), p1 = O::operand(sc[1], u);
+        const typename O::Frag p = O::operand(sc, u);
 #pragma unroll
-        for (int t = 0; t < S::VT; t++) {
-          const typename O::Frag vf = O::template transposed<S::PITCH>(Vs, 32 * t, 32 * kt + 16 * u, lane);
-          o[0][t] = O::mma(vf, p0, o[0][t]);
-          o[1][t] = O::mma(vf, p1, o[1][t]);
-        }
+        for (int t = 0; t < S::VT; t++) o[t] = O::mma(O::template transposed<S::PITCH>(Vs, 32 * t, 16 * u, lane), p, o[t]);
       }
     }
+    if (j0 + S::KC < last) {
+      ks.store(lds + (buf ^ 1) * BUF);
+      vs.store(lds + (2 + (buf ^ 1)) * BUF);
+      if (j0 + 2 * S::KC < last) fetch(j0 + 2 * S::KC);
+    }
+    __syncthreads();
   }
-  sum[0] += other_half(sum[0]);
-  sum[1] += other_half(sum[1]);
+  sum += other_half(sum);
   if (a.parts > 1) {   // a part's sums, joined by diff_join_kernel
     if (!live) return;
-    const int64_t at = ((int64_t)part * a.units + unit) * (a.tq * a.group) + r;
+    const int64_t at = (((int64_t)part * a.units + unit) * (a.tq * a.group) + r) * 2 + m;
+    float* p = a.part + at * 2 * a.dim + 4 * hh;
 #pragma unroll
-    for (int m = 0; m < 2; m++) {
-      float* p = a.part + (at * 2 + m) * 2 * a.dim + 4 * hh;
+    for (int t = 0; t < S::VT; t++)
 #pragma unroll
-      for (int t = 0; t < S::VT; t++)
-#pragma unroll
-        for (int g = 0; g < 4; g++)
-          if (32 * t + 8 * g < 2 * a.dim)
-            *reinterpret_cast<float4*>(p + 32 * t + 8 * g) = make_float4(o[m][t][4 * g], o[m][t][4 * g + 1], o[m][t][4 * g + 2], o[m][t][4 * g + 3]);
-      if (hh == 0) *reinterpret_cast<float2*>(a.part_ml + (at * 2 + m) * 2) = make_float2(mx[m], sum[m]);
-    }
+      for (int g = 0; g < 4; g++)
+        if (32 * t + 8 * g < 2 * a.dim) *reinterpret_cast<float4*>(p + 32 * t + 8 * g) = make_float4(o[t][4 * g], o[t][4 * g + 1], o[t][4 * g + 2], o[t][4 * g + 3]);
+    if (hh == 0) *reinterpret_cast<float2*>(a.part_ml + at * 2) = make_float2(mx, sum);
     return;
   }
-  if (r >= room) return;
   const int64_t row = s.q0 + i;
+  const float norm = sum > 0.f || sum != sum ? 1.f / sum : 0.f;   // (NaN stays NaN)
+#pragma unroll
+  for (int t = 0; t < S::VT; t++) o[t] *= norm;
+  if (a.lse && live && hh == 0) a.lse[(int64_t)(m * a.heads + h) * a.q_rows + row] = sum > 0.f ? mx + __log2f(sum) : sum;
+  // P_2 v to the wave that holds P_1 v: [row group][4 channels][row], 16 bytes a lane
+  static_assert(F_GROUPS * S::VT * 4096 <= (int)sizeof(lds), "exchange");
+  float4* ex = reinterpret_cast<float4*>(lds) + (rg * S::VT * 8) * 32;
+  T* second = a.o2 ? static_cast<T*>(a.o2) + row * a.o2_token + (int64_t)h * 2 * a.dim + 4 * hh : nullptr;
+  if (m == 1) {
+#pragma unroll
+    for (int t = 0; t < S::VT; t++)
+#pragma unroll
+      for (int g = 0; g < 4; g++) {
+        ex[(t * 8 + 2 * g + hh) * 32 + c] = make_float4(o[t][4 * g], o[t][4 * g + 1], o[t][4 * g + 2], o[t][4 * g + 3]);
+        if (second && live && 32 * t + 8 * g < 2 * a.dim) O::store4(second + 32 * t + 8 * g, o[t][4 * g], o[t][4 * g + 1], o[t][4 * g + 2], o[t][4 * g + 3]);
+      }
+  }
+  __syncthreads();
+  if (m == 1 || r >= room) return;
   const float lam = live ? a.lam[a.lam_token ? row * a.heads + h : h] : 0.f;
-  const float n0 = sum[0] > 0.f || sum[0] != sum[0] ? 1.f / sum[0] : 0.f, n1 = sum[1] > 0.f || sum[1] != sum[1] ? 1.f / sum[1] : 0.f;   // (NaN stays NaN)
   T* op = rows_of(a, static_cast<T*>(a.out), b, s.q0, a.o_token, a.o_batch) + i * a.o_token + (int64_t)h * 2 * a.dim + 4 * hh;
-  T* o2 = a.o2 ? static_cast<T*>(a.o2) + row * a.o2_token + (int64_t)h * 2 * a.dim + 4 * hh : nullptr;
 #pragma unroll
   for (int t = 0; t < S::VT; t++)
 #pragma unroll
     for (int g = 0; g < 4; g++) {
       if (32 * t + 8 * g >= 2 * a.dim) continue;
-      float x[4], y[4];
-#pragma unroll
-      for (int e = 0; e < 4; e++) {
-        y[e] = live ? o[1][t][4 * g + e] * n1 : 0.f;
-        x[e] = live ? o[0][t][4 * g + e] * n0 - lam * y[e] : 0.f;
-      }
-      O::store4(op + 32 * t + 8 * g, x[0], x[1], x[2], x[3]);
-      if (o2 && live) O::store4(o2 + 32 * t + 8 * g, y[0], y[1], y[2], y[3]);
+      const float4 y = ex[(t * 8 + 2 * g + hh) * 32 + c];
+      O::store4(op + 32 * t + 8 * g, live ? o[t][4 * g] - lam * y.x : 0.f, live ? o[t][4 * g + 1] - lam * y.y : 0.f, live ? o[t][4 * g + 2] - lam * y.z : 0.f,
+                live ? o[t][4 * g + 3] - lam * y.w : 0.f);
     }
-  if (a.lse && live && hh == 0) {
-    a.lse[(int64_t)h * a.q_rows + row] = sum[0] > 0.f ? mx[0] + __log2f(sum[0]) : sum[0];
-    a.lse[(int64_t)(a.heads + h) * a.q_rows + row] = sum[1] > 0.f ? mx[1] + __log2f(sum[1]) : sum[1];
-  }
 }
 
-// Joins the parts of a row: one wave a row.
+// Joins the parts of a row: one wave a row.  Lane p holds the maximum and the sum of part p (at most 64 parts), so that the weights of all parts are
+// known before the sums are read.
 template <typename T>
 __global__ void __launch_bounds__(256) diff_join_kernel(DiffArgs a) {
   const int room = a.tq * a.group;
   const int64_t x = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  const int lane = threadIdx.x & 63, unit = (int)(x / room), r = (int)(x % room);
+  const int lane = threadIdx.x & 63, unit = (int)(x / room), r = (int)(x - (int64_t)unit * room);
   if (unit >= a.units) return;
   const int b = unit / a.kv_heads, hk = unit % a.kv_heads;
   const Seq s = sequence(a, b);
@@ -367,22 +378,38 @@ __global__ void __launch_bounds__(256) diff_join_kernel(DiffArgs a) {
   const bool live = r < s.nq * a.group;
   if (!live && a.q_starts) return;
   const int64_t row = s.q0 + i, step = (int64_t)a.units * room, at = (int64_t)unit * room + r;
-  float m[2] = {-INFINITY, -INFINITY}, sum[2] = {0.f, 0.f}, acc[2][4] = {};
+  float f[2] = {0.f, 0.f}, acc[2][4] = {};
   if (live) {
-    for (int p = 0; p < a.parts; p++)
+    float lse[2];
 #pragma unroll
-      for (int k = 0; k < 2; k++) m[k] = fmaxf(m[k], a.part_ml[((at + p * step) * 2 + k) * 2]);
-    for (int p = 0; p < a.parts; p++)
+    for (int k = 0; k < 2; k++) {
+      float2 ml = make_float2(-INFINITY, 0.f);
+      if (lane < a.parts) ml = *reinterpret_cast<const float2*>(a.part_ml + ((at + lane * step) * 2 + k) * 2);
+      const float top = wave_max(ml.x), e = exp2_fast(ml.x - finite_or_zero(top)), sum = wave_sum(e * ml.y);
+      f[k] = sum > 0.f || sum != sum ? e / sum : 0.f;   // (NaN stays NaN)
+      lse[k] = sum > 0.f ? top + __log2f(sum) : sum;
+    }
+    if (a.lse && lane < 2) a.lse[(int64_t)(lane * a.heads + h) * a.q_rows + row] = lane ? lse[1] : lse[0];
+    for (int p0 = 0; p0 < a.parts; p0 += 4) {   // (four parts' loads in flight)
+      float g[2][4], v[2][4][4];
 #pragma unroll
-      for (int k = 0; k < 2; k++) {
-        const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + ((at + p * step) * 2 + k) * 2);
-        const float f = exp2_fast(ml.x - finite_or_zero(m[k]));
-        sum[k] += f * ml.y;
-        const float* o = a.part + ((at + p * step) * 2 + k) * 2 * a.dim;
+      for (int q = 0; q < 4; q++) {
+        const int p = min(p0 + q, a.parts - 1);
+        const float* o = a.part + (at + p * step) * 4 * a.dim;
 #pragma unroll
-        for (int e = 0; e < 4; e++)
-          if (lane + 64 * e < 2 * a.dim) acc[k][e] += f * o[lane + 64 * e];
+        for (int k = 0; k < 2; k++) {
+          g[k][q] = p0 + q < a.parts ? __shfl(f[k], p, 64) : 0.f;
+#pragma unroll
+          for (int e = 0; e < 4; e++) v[k][q][e] = lane + 64 * e < 2 * a.dim && p0 + q < a.parts ? o[k * 2 * a.dim + lane + 64 * e] : 0.f;
+        }
       }
+#pragma unroll
+      for (int q = 0; q < 4; q++)
+#pragma unroll
+        for (int k = 0; k < 2; k++)
+#pragma unroll
+          for (int e = 0; e < 4; e++) acc[k][e] += g[k][q] * v[k][q][e];
+    }
   }
   const float lam = live ? a.lam[a.lam_token ? row * a.heads + h : h] : 0.f;
   T* op = rows_of(a, static_cast<T*>(a.out), b, s.q0, a.o_token, a.o_batch) + i * a.o_token + (int64_t)h * 2 * a.dim;
@@ -390,11 +417,9 @@ __global__ void __launch_bounds__(256) diff_join_kernel(DiffArgs a) {
   for (int e = 0; e < 4; e++) {
     const int d = lane + 64 * e;
     if (d >= 2 * a.dim) continue;
-    const float y = sum[1] != 0.f ? acc[1][e] / sum[1] : 0.f, z = sum[0] != 0.f ? acc[0][e] / sum[0] : 0.f;
-    op[d] = Cvt<T>::st(z - lam * y);
-    if (a.o2 && live) static_cast<T*>(a.o2)[row * a.o2_token + (int64_t)h * 2 * a.dim + d] = Cvt<T>::st(y);
+    op[d] = Cvt<T>::st(acc[0][e] - lam * acc[1][e]);
+    if (a.o2 && live) static_cast<T*>(a.o2)[row * a.o2_token + (int64_t)h * 2 * a.dim + d] = Cvt<T>::st(acc[1][e]);
   }
-  if (a.lse && live && lane < 2) a.lse[(int64_t)(lane * a.heads + h) * a.q_rows + row] = sum[lane] > 0.f ? m[lane] + __log2f(sum[lane]) : sum[lane];
 }
 
 // ---- backward: queries ------------------------------------------------------------------------------------------------------------
@@ -407,7 +432,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 && DT <= 64 ? 2 : 1) diff_
   typedef Sizes<T, DT> S;
   __shared__ __attribute__((aligned(16))) T Ks[S::KC * S::PITCH];
   __shared__ __attribute__((aligned(16))) T Vs[S::KC * S::PITCH];
-  const int w = work_index(a.units * a.tiles);
+  const int w = work_index(a.units * a.tiles, a.tiles, a.causal);
   if (w >= a.units * a.tiles) return;
   const int unit = w / a.tiles, tile = a.tiles - 1 - w % a.tiles;
   const int b = unit / a.kv_heads, hk = unit % a.kv_heads;
@@ -574,7 +599,7 @@ __global__ void __launch_bounds__(256, 1) diff_backward_kv_kernel(DiffArgs a) {
   __shared__ __attribute__((aligned(16))) T Qs[S::KC * S::PITCH];
   __shared__ __attribute__((aligned(16))) T Gs[S::KC * S::PITCH];
   __shared__ __attribute__((aligned(16))) float st[5][S::KC];   // log-sums, deltas and lambda of the rows
-  const int w = work_index(a.units * a.tiles);
+  const int w = work_index(a.units * a.tiles, a.tiles, a.causal);
   if (w >= a.units * a.tiles) return;
   const int unit = w / a.tiles, tile = w % a.tiles;   // (under a causal mask the first keys are seen by the most rows)
   const int b = unit / a.kv_heads, hk = unit % a.kv_heads;
@@ -717,7 +742,7 @@ static int check(const char* what, const cd_diff_attn* d) {
   CD_REQUIRE(d->tq >= 0 && d->tk >= 0, "%s: tq=%d tk=%d", what, d->tq, d->tk);
   const int64_t group = d->heads / d->kv_heads;
   CD_REQUIRE(group <= 1024 && d->tq * group <= (1 << 30) / group, "%s: tq=%d with %lld heads a key head is too long", what, d->tq, (long long)group);
-  CD_REQUIRE((int64_t)d->batch * d->kv_heads * (cdiv(d->tq * group, ROWS) + cdiv(d->tk, ROWS) + 1) < (1 << 30) && (int64_t)d->batch * d->tq <= INT32_MAX,
+  CD_REQUIRE((int64_t)d->batch * d->kv_heads * (cdiv(d->tq * group, F_ROWS) + cdiv(d->tk, ROWS) + 1) < (1 << 30) && (int64_t)d->batch * d->tq <= INT32_MAX,
              "%s: too many rows", what);
   for (const void* p : {(const void*)d->q_lens, (const void*)d->k_lens, (const void*)d->q_starts, (const void*)d->k_starts})
     CD_REQUIRE((reinterpret_cast<uintptr_t>(p) & 3) == 0, "%s: length and start tables must be 4-byte aligned", what);
@@ -746,8 +771,8 @@ static int check_apart(const char* what, const cd_diff_attn* d, bool out_only) {
 
 // Parts of the keys that get a workgroup of their own: few rows against many keys would leave most of the chip without work.
 static int parts_of(const cd_diff_attn* d) {
-  const int64_t groups = (int64_t)d->batch * d->kv_heads * cdiv((int64_t)d->tq * (d->heads / d->kv_heads), ROWS);
-  int64_t p = groups ? 512 / groups : 1;
+  const int64_t groups = (int64_t)d->batch * d->kv_heads * cdiv((int64_t)d->tq * (d->heads / d->kv_heads), F_ROWS);
+  int64_t p = groups ? 768 / groups : 1;
   if (p > cdiv(d->tk, 128)) p = cdiv(d->tk, 128);
   if (p > 64) p = 64;
   return p < 2 || groups > 128 ? 1 : (int)p;
@@ -769,17 +794,17 @@ static DiffArgs args_of(const cd_diff_attn* d) {
 }
 
 // f<T, DT>() of this dtype and head_dim
-#define CD_DIFF_DISPATCH(d, KERNEL, BLOCKS, s, a)                                                                                  \
+#define CD_DIFF_DISPATCH(d, KERNEL, THREADS, BLOCKS, s, a)                                                                                  \
   do {                                                                                                                             \
-    const dim3 grid_(BLOCKS);                                                                                                      \
+    const dim3 grid_(BLOCKS), block_(THREADS);                                                                                                      \
     if ((d)->dtype == CD_BF16) {                                                                                                   \
-      if ((d)->head_dim <= 32) hipLaunchKernelGGL((KERNEL<bf16_t, 32>), grid_, dim3(256), 0, s, a);                                \
-      else if ((d)->head_dim <= 64) hipLaunchKernelGGL((KERNEL<bf16_t, 64>), grid_, dim3(256), 0, s, a);                           \
-      else hipLaunchKernelGGL((KERNEL<bf16_t, 128>), grid_, dim3(256), 0, s, a);                                                   \
+      if ((d)->head_dim <= 32) hipLaunchKernelGGL((KERNEL<bf16_t, 32>), grid_, block_, 0, s, a);                                \
+      else if ((d)->head_dim <= 64) hipLaunchKernelGGL((KERNEL<bf16_t, 64>), grid_, block_, 0, s, a);                           \
+      else hipLaunchKernelGGL((KERNEL<bf16_t, 128>), grid_, block_, 0, s, a);                                                   \
     } else {                                                                                                                       \
-      if ((d)->head_dim <= 32) hipLaunchKernelGGL((KERNEL<float, 32>), grid_, dim3(256), 0, s, a);                                 \
-      else if ((d)->head_dim <= 64) hipLaunchKernelGGL((KERNEL<float, 64>), grid_, dim3(256), 0, s, a);                            \
-      else hipLaunchKernelGGL((KERNEL<float, 128>), grid_, dim3(256), 0, s, a);                                                    \
+      if ((d)->head_dim <= 32) hipLaunchKernelGGL((KERNEL<float, 32>), grid_, block_, 0, s, a);                                 \
+      else if ((d)->head_dim <= 64) hipLaunchKernelGGL((KERNEL<float, 64>), grid_, block_, 0, s, a);                            \
+      else hipLaunchKernelGGL((KERNEL<float, 128>), grid_, block_, 0, s, a);                                                    \
     }                                                                                                                              \
   } while (0)
 
@@ -818,14 +843,14 @@ extern "C" int codistill_diff_attention(const cd_diff_attn* desc, const void* q,
   if (desc->tq == 0) return CD_OK;
   DiffArgs a = args_of(desc);
   a.q = q; a.k = k; a.v = v; a.lam = lambda; a.out = out; a.o2 = o_second; a.lse = lse;
-  a.tiles = (int)cdiv((int64_t)a.tq * a.group, ROWS);
+  a.tiles = (int)cdiv((int64_t)a.tq * a.group, F_ROWS);
   a.parts = parts_of(desc);
   a.part_ml = static_cast<float*>(workspace);
   a.part = a.part_ml + (size_t)a.parts * a.units * a.tq * a.group * 4;
   hipStream_t s = static_cast<hipStream_t>(stream);
   const double e = elem_of(desc), qe = 2.0 * a.q_rows * a.heads * 2 * a.dim, ke = 2.0 * a.k_rows * a.kv_heads * 2 * a.dim;
   ProfScope prof(CD_K_ATTN, s, 12.0 * a.dim * pairs(desc), e * (qe + ke));
-  CD_DIFF_DISPATCH(desc, diff_forward_kernel, work_blocks((int64_t)a.units * a.tiles * a.parts), s, a);
+  CD_DIFF_DISPATCH(desc, diff_forward_kernel, F_THREADS, work_blocks((int64_t)a.units * a.tiles * a.parts), s, a);
   if (a.parts > 1) {
     const dim3 grid((unsigned)cdiv((int64_t)a.units * a.tq * a.group, 4));
     if (desc->dtype == CD_BF16) hipLaunchKernelGGL((diff_join_kernel<bf16_t>), grid, dim3(256), 0, s, a);
@@ -856,12 +881,12 @@ extern "C" int codistill_diff_attention_backward(const cd_diff_attn* desc, const
   ProfScope prof(CD_K_ATTN, s, 20.0 * a.dim * pairs(desc), e * (qe + ke));
   if (a.tq > 0) {
     a.tiles = (int)cdiv((int64_t)a.tq * a.group, ROWS);
-    CD_DIFF_DISPATCH(desc, diff_backward_q_kernel, work_blocks((int64_t)a.units * a.tiles), s, a);
+    CD_DIFF_DISPATCH(desc, diff_backward_q_kernel, 256, work_blocks((int64_t)a.units * a.tiles), s, a);
   }
   if (!a.lam_token) hipLaunchKernelGGL(diff_lambda_kernel, dim3((unsigned)a.heads), dim3(1024), 0, s, a);
   if (a.tk > 0) {
     a.tiles = (int)cdiv(a.tk, ROWS);
-    CD_DIFF_DISPATCH(desc, diff_backward_kv_kernel, work_blocks((int64_t)a.units * a.tiles), s, a);
+    CD_DIFF_DISPATCH(desc, diff_backward_kv_kernel, 256, work_blocks((int64_t)a.units * a.tiles), s, a);
   }
   return check_launch("diff_attention_backward");
 }
