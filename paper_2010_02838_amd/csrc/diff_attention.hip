@@ -44,9 +44,25 @@ struct DiffArgs {
   int64_t q_token, q_batch, k_token, k_batch, v_token, v_batch, o_token, o_batch, o2_token;
   const int32_t* q_lens; const int32_t* k_lens; const int32_t* q_starts; const int32_t* k_starts;
   int64_t q_rows, k_rows;                         // rows of the q and k tensors (batch * tq when padded)
-  int32_t batch, tq, tk, heads, kv_heads, group, dim, causal, lam_token, parts, tiles, units;
+  int32_t batch, tq, tk, heads, kv_heads, group, dim, causal, lam_token, parts, tiles, units, near_k, near_q;
   uint32_t group_inv;                             // floor(2^32 / group) + 1 (group > 1)
   float scale, c;                                 // c = scale log2(e)
+};
+
+// A copy in LDS: rows of W elements, the 16-byte pieces of a row exchanged among themselves so that both kinds of reads meet all banks.  Sixteen rows
+// read at the same column (row by row) differ in four bits of the row, four consecutive rows read over 64 bytes (transposed) in bits 2 and 3 of
+// the piece.  Padded rows serve one of the two: with 16 bytes a row the transposing loads met each bank four times.
+template <typename T, int W> __host__ __device__ constexpr int lds_at(int row, int col) {
+  constexpr int VE = 16 / (int)sizeof(T);
+  const int f = W * (int)sizeof(T) == 128 ? ((row >> 1 & 1) << 2) | (row >> 2 & 3) : ((row & 3) << 2) | (row >> 2 & 3);   // (rows of 128 bytes: bit 0 changes banks by itself)
+  return row * W + ((col / VE) ^ f) * VE + col % VE;
+}
+
+// Where a lane's reads begin: the pieces are exchanged by exclusive or, so a constant column is one more exclusive or.
+struct LaneAt {
+  int row, lo, hi;
+  // forgets what the compiler knows of them, so that it does not keep the address of every read of a loop in a register of its own
+  __device__ inline void fresh() { asm volatile("" : "+v"(row), "+v"(lo), "+v"(hi)); }
 };
 
 // ---- fragments ----------------------------------------------------------------------------------------------------------
@@ -70,15 +86,19 @@ template <> struct Ops<bf16_t> {
     }
     return f;
   }
-  // rows row0 .. row0 + 15 of a row-major copy as contraction, columns col0 .. col0 + 31 on the lanes.  In a group of 16 lanes, lane i of a
-  // transposing load receives element i & 3 of the four 8-byte pieces that lanes i >> 2, 4 + (i >> 2), ... address.
-  template <int PITCH> static __device__ inline Frag transposed(const bf16_t* t, int col0, int row0, int lane) {
-    const int grp = lane >> 4, li = lane & 15;
+  // rows row0 .. row0 + 15 (row0 a multiple of 16) of a copy as contraction, columns col0 .. col0 + 31 on the lanes.  In a group of 16 lanes, lane i
+  // of a transposing load receives element i & 3 of the four 8-byte pieces that lanes i >> 2, 4 + (i >> 2), ... address.
+  template <int W> static __device__ inline Frag transposed(const bf16_t* t, int col0, int row0, const LaneAt& at) {
     typedef __attribute__((address_space(3))) v4bf lds4;
-    const bf16_t* p = t + (row0 + 4 * (grp >> 1) + (li >> 2)) * PITCH + col0 + 16 * (grp & 1) + 4 * (li & 3);
-    const v4bf lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds4*)p);
-    const v4bf hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds4*)(p + 8 * PITCH));
+    const v4bf lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds4*)(t + row0 * W + (at.lo ^ col0)));
+    const v4bf hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds4*)(t + row0 * W + (at.hi ^ col0)));
     return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+  }
+  // columns col + 8 (l / 32) .. + 7 of row row0 + l % 32 (col a multiple of 16, row0 of 32)
+  template <int W> static __device__ inline Frag rowwise(const bf16_t* t, int row0, int col, const LaneAt& at) { return load(t + row0 * W + (at.row ^ col)); }
+  template <int W> static __device__ inline LaneAt lane_at(int lane) {
+    const int grp = lane >> 4, li = lane & 15, row = 4 * (grp >> 1) + (li >> 2), col = 16 * (grp & 1) + 4 * (li & 3);
+    return {lds_at<bf16_t, W>(lane & 31, 8 * (lane >> 5)), lds_at<bf16_t, W>(row, col), lds_at<bf16_t, W>(row + 8, col)};
   }
   static __device__ inline void store4(bf16_t* p, float a, float b, float c, float d) {
     const v2f lo = {a, b}, hi = {c, d};
@@ -108,24 +128,29 @@ template <> struct Ops<float> {
     for (int e = 0; e < 8; e++) f[e] = d[8 * u + e];
     return f;
   }
-  template <int PITCH> static __device__ inline Frag transposed(const float* t, int col0, int row0, int lane) {
-    const float* p = t + (row0 + 4 * (lane >> 5)) * PITCH + col0 + (lane & 31);
+  template <int W> static __device__ inline Frag transposed(const float* t, int col0, int row0, const LaneAt& at) {
     Frag f;
 #pragma unroll
-    for (int e = 0; e < 8; e++) f[e] = p[(8 * (e >> 2) + (e & 3)) * PITCH];
+    for (int e = 0; e < 8; e++) f[e] = t[(row0 + 8 * (e >> 2) + (e & 3)) * W + (at.lo ^ col0 ^ (16 * (e & 3) + 8 * (e >> 2)))];
     return f;
+  }
+  template <int W> static __device__ inline Frag rowwise(const float* t, int row0, int col, const LaneAt& at) {
+    const float4 a = *reinterpret_cast<const float4*>(t + row0 * W + (at.row ^ col)), b = *reinterpret_cast<const float4*>(t + row0 * W + (at.row ^ (col + 4)));
+    return Frag{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+  }
+  template <int W> static __device__ inline LaneAt lane_at(int lane) {
+    static_assert(W * sizeof(float) >= 256, "rows of 16 pieces");
+    return {lds_at<float, W>(lane & 31, 8 * (lane >> 5)), lds_at<float, W>(4 * (lane >> 5), lane & 31), 0};
   }
   static __device__ inline void store4(float* p, float a, float b, float c, float d) { *reinterpret_cast<float4*>(p) = make_float4(a, b, c, d); }
 };
 
-// Sizes of an instance: DT = head_dim rounded up to 32, 64 or 128, rows of 2 DT elements in LDS (both maps, or the values), KC streamed rows at
-// a time, 16 bytes of padding a row so that 16-byte reads of many rows spread over the banks.
+// Sizes of an instance: DT = head_dim rounded up to 32, 64 or 128, rows of 2 DT elements in LDS (both maps, or the values), KC streamed rows at a time.
 template <typename T, int DT> struct Sizes {
-  static constexpr int W = 2 * DT, PITCH = W + Ops<T>::VE, KC = 32;
+  static constexpr int W = 2 * DT, KC = 32;
   static constexpr int KS = DT / 16, VT = W / 32, DTT = DT / 32;
 };
 constexpr int EXACT_KEYS = 128;   // rows that reach no more keys than this get their deltas in a pass of their own
-constexpr int ROWS = 128;   // rows (or keys) of a workgroup: four waves of 32
 
 // ---- sequences and rows ---------------------------------------------------------------------------------------------------
 struct Seq { int nq, nk; int64_t q0, k0; };   // lengths; rows of the sequence's first query and key in their tensors
@@ -165,27 +190,41 @@ __device__ inline int work_index(int n, int per_unit, bool turns) {
 static unsigned work_blocks(int64_t n) { return (unsigned)(cdiv(n, 8) * 8); }
 
 // Up to KC rows of 2 dim elements (two ranges of dim for the maps, MAPS, or one of 2 dim) on their way into LDS; what lies beyond the rows and the
-// channels becomes zero.  `at(r)` is the address of row r < n.
+// channels becomes zero.  A whole tile whose rows lie within 32-bit offsets of its first is read from one address that all threads share and offsets
+// that stay the same from tile to tile: computing 64-bit addresses of each row anew was a third of the forward kernel's vector instructions.
 template <typename T, int DT, bool MAPS, int THREADS = 256> struct Stage {
   typedef Sizes<T, DT> S;
   static constexpr int VE = Ops<T>::VE, VPR = S::W / VE, IT = S::KC * VPR / THREADS;
+  static constexpr int STEP = THREADS / VPR;   // rows between a thread's loads
   uint4 u[IT];
-  template <typename At> __device__ inline void load(int n, int dim, At at) {
+  uint32_t off;        // bytes from the tile's first row to the thread's first piece
+  static __device__ inline int row(int i) { return (threadIdx.x + THREADS * i) / VPR; }
+  static __device__ inline int column(int i) { return (threadIdx.x + THREADS * i) % VPR * VE; }
+  // where a row's column lies in its range or ranges of dim channels; negative: padding
+  static __device__ inline int channel(int c, int dim) {
+    if (!MAPS) return c < 2 * dim ? c : -1;
+    const int cc = c >= DT ? c - DT : c;
+    return cc < dim ? (c >= DT ? dim + cc : cc) : -1;
+  }
+  // at(r): elements from the tile's first row to row r
+  template <typename At> __device__ inline void plan(int dim, At at) { off = (uint32_t)((at(row(0)) + max(channel(column(0), dim), 0)) * sizeof(T)); }
+  // step: elements from a row to the one STEP rows further
+  __device__ inline void load_whole(const T* first, int64_t step) {
+#pragma unroll
+    for (int i = 0; i < IT; i++) u[i] = *reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(first + i * step) + off);
+  }
+  // row(r): address of row r < n
+  template <typename Row> __device__ inline void load(int n, int dim, Row address) {
 #pragma unroll
     for (int i = 0; i < IT; i++) {
-      const int x = threadIdx.x + THREADS * i, r = x / VPR, c = (x % VPR) * VE;
       u[i] = make_uint4(0, 0, 0, 0);
-      const int cc = MAPS ? (c >= DT ? c - DT : c) : c;
-      const bool in = r < n && cc < (MAPS ? dim : 2 * dim);
-      if (in) u[i] = *reinterpret_cast<const uint4*>(at(r) + (MAPS && c >= DT ? dim + cc : cc));
+      const int c = channel(column(i), dim);
+      if (row(i) < n && c >= 0) u[i] = *reinterpret_cast<const uint4*>(address(row(i)) + c);
     }
   }
   __device__ inline void store(T* dst) const {
 #pragma unroll
-    for (int i = 0; i < IT; i++) {
-      const int x = threadIdx.x + THREADS * i, r = x / VPR, c = (x % VPR) * VE;
-      *reinterpret_cast<uint4*>(dst + r * S::PITCH + c) = u[i];
-    }
+    for (int i = 0; i < IT; i++) *reinterpret_cast<uint4*>(dst + lds_at<T, S::W>(row(i), column(i))) = u[i];
   }
 };
 
@@ -198,6 +237,36 @@ __device__ inline void own_row(RowFrags<T, DT>& f, const T* row, bool live, int 
     const int c = 16 * t + 8 * hh, cc = MAPS && c >= DT ? c - DT : c;
     f[t] = Ops<T>::zero();
     if (live && cc < (MAPS ? dim : 2 * dim)) f[t] = Ops<T>::load(row + (MAPS && c >= DT ? dim + cc : cc));
+  }
+}
+
+// Everything loaded so far has arrived: a value that is first used inside a loop would otherwise make every turn of it wait for all loads, those
+// of the tile after next among them.
+template <typename V> __device__ inline void arrived(V& v) { asm volatile("" : "+v"(v)); }
+__device__ inline void arrived(v8bf& v) {
+  typedef int v4i __attribute__((ext_vector_type(4)));
+  v4i u = __builtin_bit_cast(v4i, v);
+  asm volatile("" : "+v"(u));
+  v = __builtin_bit_cast(v8bf, u);
+}
+__device__ inline int wave_of_thread() { return __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6); }   // (the same value in all lanes, and known to be)
+
+// N fragments, used in order, G of them on their way from LDS while the G before are used.  (Left alone, the compiler reads a fragment, waits for it and
+// uses it, a fragment at a time.)
+template <typename F, int N, int G, typename Load, typename Use> __device__ inline void stream(Load load, Use use) {
+  static_assert(N % G == 0, "groups");
+  F f[2][G];
+#pragma unroll
+  for (int e = 0; e < G; e++) f[0][e] = load(e);
+#pragma unroll
+  for (int g = 0; g < N / G; g++) {
+    if (g + 1 < N / G) {
+#pragma unroll
+      for (int e = 0; e < G; e++) f[(g + 1) & 1][e] = load((g + 1) * G + e);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int e = 0; e < G; e++) use(g * G + e, f[g & 1][e]);
   }
 }
 
@@ -219,8 +288,8 @@ template <typename T, int DT>
 __global__ void __launch_bounds__(F_THREADS, sizeof(T) == 4 ? (DT == 128 ? 1 : 2) : DT == 128 ? 2 : 3) diff_forward_kernel(DiffArgs a) {
   typedef Ops<T> O;
   typedef Sizes<T, DT> S;
-  __shared__ __attribute__((aligned(16))) T lds[4 * S::KC * S::PITCH];   // keys and values, two buffers each
-  constexpr int BUF = S::KC * S::PITCH;
+  __shared__ __attribute__((aligned(16))) T lds[4 * S::KC * S::W];   // keys and values, two buffers each
+  constexpr int BUF = S::KC * S::W, G = sizeof(T) == 2 && DT > 32 ? 4 : 2;
   const int total = a.units * a.tiles * a.parts;
   const int w = work_index(total, a.tiles * a.parts, a.causal);
   if (w >= total) return;
@@ -230,7 +299,7 @@ __global__ void __launch_bounds__(F_THREADS, sizeof(T) == 4 ? (DT == 128 ? 1 : 2
   const Seq s = sequence(a, b);
   const int R = s.nq * a.group, r0 = tile * F_ROWS, room = a.q_starts ? R : a.tq * a.group;
   if (r0 >= room) return;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 31, hh = lane >> 5, m = wave & 1, rg = wave >> 1;
+  const int lane = threadIdx.x & 63, wave = wave_of_thread(), c = lane & 31, hh = lane >> 5, m = wave & 1, rg = wave >> 1;
   const int wr0 = r0 + 32 * rg, r = wr0 + c;
   const bool live = r < R;
   const int i = query_of(a, r), h = hk * a.group + (r - i * a.group);
@@ -256,16 +325,26 @@ __global__ void __launch_bounds__(F_THREADS, sizeof(T) == 4 ? (DT == 128 ? 1 : 2
 #pragma unroll
   for (int t = 0; t < S::VT; t++) clear(o[t]);
   float mx = -INFINITY, sum = 0.f;
+  LaneAt at = O::template lane_at<S::W>(lane);
   // One barrier a tile: while a tile of keys and values is worked on, the next one is written to the other buffer and the one after it is
   // on its way into registers.
   Stage<T, DT, true, F_THREADS> ks;
   Stage<T, DT, false, F_THREADS> vs;
+  ks.plan(a.dim, [&](int row) { return row * a.k_token; });
+  vs.plan(a.dim, [&](int row) { return row * a.v_token; });
   auto fetch = [&](int j) {
-    ks.load(min(S::KC, s.nk - j), a.dim, [&](int row) { return kp + (int64_t)(j + row) * a.k_token; });
-    vs.load(min(S::KC, s.nk - j), a.dim, [&](int row) { return vp + (int64_t)(j + row) * a.v_token; });
+    if (a.near_k && a.dim == DT && j + S::KC <= s.nk) {
+      ks.load_whole(kp + j * a.k_token, ks.STEP * a.k_token);
+      vs.load_whole(vp + j * a.v_token, vs.STEP * a.v_token);
+    } else {
+      ks.load(s.nk - j, a.dim, [&](int row) { return kp + (j + row) * a.k_token; });
+      vs.load(s.nk - j, a.dim, [&](int row) { return vp + (j + row) * a.v_token; });
+    }
   };
+  if (begin < last) fetch(begin);
+#pragma unroll
+  for (int t = 0; t < S::KS; t++) arrived(qf[t]);
   if (begin < last) {
-    fetch(begin);
     ks.store(lds);
     vs.store(lds + 2 * BUF);
     if (begin + S::KC < last) fetch(begin + S::KC);
@@ -275,10 +354,11 @@ __global__ void __launch_bounds__(F_THREADS, sizeof(T) == 4 ? (DT == 128 ? 1 : 2
     const T* Ks = lds + buf * BUF;
     const T* Vs = lds + (2 + buf) * BUF;
     if (j0 < reach) {
+      at.fresh();
       v16f sc;
       clear(sc);
-#pragma unroll
-      for (int t = 0; t < S::KS; t++) sc = O::mma(O::load(Ks + c * S::PITCH + m * DT + 16 * t + 8 * hh), qf[t], sc);
+      stream<typename O::Frag, S::KS, G>([&](int t) { return O::template rowwise<S::W>(Ks, 0, m * DT + 16 * t, at); },
+                                         [&](int t, const typename O::Frag& f) { sc = O::mma(f, qf[t], sc); });
       if (j0 + 32 > least) {   // some row of the wave does not see all of the tile
 #pragma unroll
         for (int v = 0; v < 16; v++)
@@ -304,12 +384,9 @@ __global__ void __launch_bounds__(F_THREADS, sizeof(T) == 4 ? (DT == 128 ? 1 : 2
         sc[v] = exp2_fast(fmaf(sc[v], a.c, -base));
         sum += sc[v];
       }
-#pragma unroll
-      for (int u = 0; u < 2; u++) {
-        const typename O::Frag p = O::operand(sc, u);
-#pragma unroll
-        for (int t = 0; t < S::VT; t++) o[t] = O::mma(O::template transposed<S::PITCH>(Vs, 32 * t, 16 * u, lane), p, o[t]);
-      }
+      const typename O::Frag p[2] = {O::operand(sc, 0), O::operand(sc, 1)};
+      stream<typename O::Frag, 2 * S::VT, G>([&](int x) { return O::template transposed<S::W>(Vs, 32 * (x % S::VT), 16 * (x / S::VT), at); },
+                                             [&](int x, const typename O::Frag& f) { o[x % S::VT] = O::mma(f, p[x / S::VT], o[x % S::VT]); });
     }
     if (j0 + S::KC < last) {
       ks.store(lds + (buf ^ 1) * BUF);
@@ -321,14 +398,14 @@ __global__ void __launch_bounds__(F_THREADS, sizeof(T) == 4 ? (DT == 128 ? 1 : 2
   sum += other_half(sum);
   if (a.parts > 1) {   // a part's sums, joined by diff_join_kernel
     if (!live) return;
-    const int64_t at = (((int64_t)part * a.units + unit) * (a.tq * a.group) + r) * 2 + m;
-    float* p = a.part + at * 2 * a.dim + 4 * hh;
+    const int64_t place = (((int64_t)part * a.units + unit) * (a.tq * a.group) + r) * 2 + m;
+    float* p = a.part + place * 2 * a.dim + 4 * hh;
 #pragma unroll
     for (int t = 0; t < S::VT; t++)
 #pragma unroll
       for (int g = 0; g < 4; g++)
         if (32 * t + 8 * g < 2 * a.dim) *reinterpret_cast<float4*>(p + 32 * t + 8 * g) = make_float4(o[t][4 * g], o[t][4 * g + 1], o[t][4 * g + 2], o[t][4 * g + 3]);
-    if (hh == 0) *reinterpret_cast<float2*>(a.part_ml + at * 2) = make_float2(mx, sum);
+    if (hh == 0) *reinterpret_cast<float2*>(a.part_ml + place * 2) = make_float2(mx, sum);
     return;
   }
   const int64_t row = s.q0 + i;
@@ -426,143 +503,179 @@ __global__ void __launch_bounds__(256) diff_join_kernel(DiffArgs a) {
 // dq, delta and dlambda.  delta first comes from the kept outputs, delta_2 = dO . (P_2 v), delta_1 = dO . out + lambda delta_2, which were rounded;
 // the pass over the keys gives what is missing, rowsum(P_m (dP - delta_m)) in fp32, so that dlambda and the deltas that the other kernel
 // reads are exact to fp32 rounding (with the kept bf16 outputs alone dlambda is off by their rounding, a thousandth).
+// Both maps of 32 rows in a wave share dP; where that needs more registers than two waves a SIMD have (the widest heads, fp32), a wave takes one
+// map and computes dP for itself.
+template <typename T, int DT> struct QSizes {
+  static constexpr bool SPLIT = DT * sizeof(T) >= 256;
+  static constexpr int MAPS = SPLIT ? 1 : 2, ROWS = SPLIT ? 64 : 128;
+};
+
 template <typename T, int DT>
-__global__ void __launch_bounds__(256, sizeof(T) == 2 && DT <= 64 ? 2 : 1) diff_backward_q_kernel(DiffArgs a) {
+__global__ void __launch_bounds__(256, DT * sizeof(T) <= 256 ? 2 : 1) diff_backward_q_kernel(DiffArgs a) {
   typedef Ops<T> O;
   typedef Sizes<T, DT> S;
-  __shared__ __attribute__((aligned(16))) T Ks[S::KC * S::PITCH];
-  __shared__ __attribute__((aligned(16))) T Vs[S::KC * S::PITCH];
+  typedef QSizes<T, DT> Z;
+  __shared__ __attribute__((aligned(16))) T lds[4 * S::KC * S::W];   // keys and values, two buffers each
+  constexpr int BUF = S::KC * S::W, G = 2, MAPS = Z::MAPS;
   const int w = work_index(a.units * a.tiles, a.tiles, a.causal);
   if (w >= a.units * a.tiles) return;
   const int unit = w / a.tiles, tile = a.tiles - 1 - w % a.tiles;
   const int b = unit / a.kv_heads, hk = unit % a.kv_heads;
   const Seq s = sequence(a, b);
-  const int R = s.nq * a.group, r0 = tile * ROWS, room = a.q_starts ? R : a.tq * a.group;
+  const int R = s.nq * a.group, r0 = tile * Z::ROWS, room = a.q_starts ? R : a.tq * a.group;
   if (r0 >= room) return;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 31, hh = lane >> 5;
-  const int r = r0 + 32 * wave + c;
+  const int lane = threadIdx.x & 63, wave = wave_of_thread(), c = lane & 31, hh = lane >> 5;
+  const int m0 = Z::SPLIT ? wave & 1 : 0, wr0 = r0 + 32 * (Z::SPLIT ? wave >> 1 : wave), r = wr0 + c;   // the wave's first map, its first row
   const bool live = r < R;
   const int i = query_of(a, r), h = hk * a.group + (r - i * a.group);
   const int64_t row = s.q0 + i;
   const T* kp = rows_of(a, static_cast<const T*>(a.k), b, s.k0, a.k_token, a.k_batch) + (int64_t)hk * 2 * a.dim;
   const T* vp = rows_of(a, static_cast<const T*>(a.v), b, s.k0, a.v_token, a.v_batch) + (int64_t)hk * 2 * a.dim;
-  typename O::Frag qf[2 * S::KS], gf[2 * S::KS];
-  own_row<T, DT, true>(qf, rows_of(a, static_cast<const T*>(a.q), b, s.q0, a.q_token, a.q_batch) + i * a.q_token + (int64_t)h * 2 * a.dim, live, a.dim, hh);
+  typename O::Frag qf[MAPS * S::KS];
+  RowFrags<T, DT> gf;
+  {
+    const T* qp = rows_of(a, static_cast<const T*>(a.q), b, s.q0, a.q_token, a.q_batch) + i * a.q_token + (int64_t)h * 2 * a.dim + m0 * a.dim;
+#pragma unroll
+    for (int t = 0; t < MAPS * S::KS; t++) {
+      const int d = 16 * (t % S::KS) + 8 * hh;
+      qf[t] = O::zero();
+      if (live && d < a.dim) qf[t] = O::load(qp + t / S::KS * a.dim + d);
+    }
+  }
   const int64_t o_at = i * a.o_token + (int64_t)h * 2 * a.dim;
   own_row<T, DT, false>(gf, rows_of(a, static_cast<const T*>(a.dout), b, s.q0, a.o_token, a.o_batch) + o_at, live, a.dim, hh);
-  float lam = 0.f, lse[2] = {0.f, 0.f}, delta[2] = {0.f, 0.f}, rest[2] = {0.f, 0.f};
-  if (live) {
-    lam = a.lam[a.lam_token ? row * a.heads + h : h];
-    lse[0] = a.lse[(int64_t)h * a.q_rows + row];
-    lse[1] = a.lse[(int64_t)(a.heads + h) * a.q_rows + row];
+  float lam = 0.f, lse[MAPS], delta[MAPS], rest[MAPS];
+  if (live) lam = a.lam[a.lam_token ? row * a.heads + h : h];
+#pragma unroll
+  for (int m = 0; m < MAPS; m++) {
+    lse[m] = live ? a.lse[(int64_t)((m0 + m) * a.heads + h) * a.q_rows + row] : 0.f;
+    rest[m] = 0.f;
   }
   {
-    typename O::Frag f[2 * S::KS];
-    own_row<T, DT, false>(f, rows_of(a, static_cast<const T*>(a.out), b, s.q0, a.o_token, a.o_batch) + o_at, live, a.dim, hh);
+    const T* kept[2] = {rows_of(a, static_cast<const T*>(a.out), b, s.q0, a.o_token, a.o_batch) + o_at,
+                        static_cast<const T*>(a.o2) + row * a.o2_token + (int64_t)h * 2 * a.dim};
+    float dot[2] = {0.f, 0.f};
 #pragma unroll
-    for (int t = 0; t < 2 * S::KS; t++)
+    for (int k = 0; k < 2; k++)
 #pragma unroll
-      for (int e = 0; e < 8; e++) delta[0] += O::get(f[t], e) * O::get(gf[t], e);
-    own_row<T, DT, false>(f, static_cast<const T*>(a.o2) + row * a.o2_token + (int64_t)h * 2 * a.dim, live, a.dim, hh);
+      for (int t = 0; t < 2 * S::KS; t++)
+        if (live && 16 * t + 8 * hh < 2 * a.dim) {
+          const typename O::Frag f = O::load(kept[k] + 16 * t + 8 * hh);
 #pragma unroll
-    for (int t = 0; t < 2 * S::KS; t++)
+          for (int e = 0; e < 8; e++) dot[k] += O::get(f, e) * O::get(gf[t], e);
+        }
+    dot[0] += other_half(dot[0]);
+    dot[1] += other_half(dot[1]);
+    dot[0] += lam * dot[1];
 #pragma unroll
-      for (int e = 0; e < 8; e++) delta[1] += O::get(f[t], e) * O::get(gf[t], e);
-    delta[0] += other_half(delta[0]);
-    delta[1] += other_half(delta[1]);
-    delta[0] += lam * delta[1];
+    for (int m = 0; m < MAPS; m++) delta[m] = m0 + m ? dot[1] : dot[0];
   }
   const int off = s.nk - s.nq;
   auto limit = [&](int x) { return a.causal ? min(s.nk, query_of(a, x) + off + 1) : s.nk; };
   const int see = live ? limit(r) : s.nk;
-  const int wr0 = r0 + 32 * wave, least = limit(wr0), reach = wr0 < R ? limit(min(wr0 + 31, R - 1)) : 0;
-  const int last = r0 < R ? limit(min(r0 + ROWS, R) - 1) : 0;
-  v16f dq[2][S::DTT];
+  const int least = limit(wr0), reach = wr0 < R ? limit(min(wr0 + 31, R - 1)) : 0;
+  const int last = r0 < R ? limit(min(r0 + Z::ROWS, R) - 1) : 0;
+  v16f dq[MAPS][S::DTT];
 #pragma unroll
-  for (int m = 0; m < 2; m++)
+  for (int m = 0; m < MAPS; m++)
 #pragma unroll
     for (int t = 0; t < S::DTT; t++) clear(dq[m][t]);
   // Rows with few keys: a rounding of the kept outputs is as large as their small dS (two keys: dq off by 5e-3 where its own rounding is 1.7e-3,
   // 128 keys 2.8e-3, 700 keys 2.5e-3 as without it), so delta is completed by a pass of its own first.
+  LaneAt at = O::template lane_at<S::W>(lane);
   const bool two = last <= EXACT_KEYS;
+  Stage<T, DT, true> ks;
+  Stage<T, DT, false> vs;
+  ks.plan(a.dim, [&](int row) { return row * a.k_token; });
+  vs.plan(a.dim, [&](int row) { return row * a.v_token; });
+  auto fetch = [&](int j) {
+    if (a.near_k && a.dim == DT && j + S::KC <= s.nk) {
+      ks.load_whole(kp + j * a.k_token, ks.STEP * a.k_token);
+      vs.load_whole(vp + j * a.v_token, vs.STEP * a.v_token);
+    } else {
+      ks.load(s.nk - j, a.dim, [&](int row) { return kp + (j + row) * a.k_token; });
+      vs.load(s.nk - j, a.dim, [&](int row) { return vp + (j + row) * a.v_token; });
+    }
+  };
   for (int pass = two ? 0 : 1; pass < 2; pass++) {
-  if (two && pass == 1) {
+    if (two && pass == 1) {
 #pragma unroll
-    for (int m = 0; m < 2; m++) {
-      delta[m] += rest[m] + other_half(rest[m]);
-      rest[m] = 0.f;
-    }
-  }
-  for (int j0 = 0; j0 < last; j0 += S::KC) {
-    if (pass == 0 || !two || last > S::KC) {   // (else the first pass has staged all keys)
-      Stage<T, DT, true> ks;
-      Stage<T, DT, false> vs;
-      const int n = min(S::KC, s.nk - j0);
-      ks.load(n, a.dim, [&](int x) { return kp + (int64_t)(j0 + x) * a.k_token; });
-      vs.load(n, a.dim, [&](int x) { return vp + (int64_t)(j0 + x) * a.v_token; });
-      __syncthreads();
-      ks.store(Ks);
-      vs.store(Vs);
-      __syncthreads();
-    }
-#pragma unroll
-    for (int kt = 0; kt < S::KC / 32; kt++) {
-      const int jt = j0 + 32 * kt;
-      if (jt >= reach) break;
-      v16f sc[2], dp;
-#pragma unroll
-      for (int m = 0; m < 2; m++) {
-        clear(sc[m]);
-#pragma unroll
-        for (int t = 0; t < S::KS; t++)
-          sc[m] = O::mma(O::load(Ks + (32 * kt + c) * S::PITCH + m * DT + 16 * t + 8 * hh), qf[m * S::KS + t], sc[m]);
+      for (int m = 0; m < MAPS; m++) {
+        delta[m] += rest[m] + other_half(rest[m]);
+        rest[m] = 0.f;
       }
-      clear(dp);
-#pragma unroll
-      for (int t = 0; t < 2 * S::KS; t++) dp = O::mma(O::load(Vs + (32 * kt + c) * S::PITCH + 16 * t + 8 * hh), gf[t], dp);
-      if (jt + 32 > least) {
-#pragma unroll
-        for (int v = 0; v < 16; v++)
-          if (jt + 8 * (v >> 2) + 4 * hh + (v & 3) >= see) { sc[0][v] = -INFINITY; sc[1][v] = -INFINITY; }
-      }
-#pragma unroll
-      for (int m = 0; m < 2; m++)
-#pragma unroll
-        for (int v = 0; v < 16; v++) {
-          sc[m][v] = exp2_fast(fmaf(sc[m][v], a.c, -lse[m])) * (dp[v] - delta[m]);
-          rest[m] += sc[m][v];
-        }
-      if (pass == 0) continue;
-#pragma unroll
-      for (int u = 0; u < 2; u++)
-#pragma unroll
-        for (int m = 0; m < 2; m++) {
-          const typename O::Frag p = O::operand(sc[m], u);
-#pragma unroll
-          for (int t = 0; t < S::DTT; t++)
-            dq[m][t] = O::mma(O::template transposed<S::PITCH>(Ks, m * DT + 32 * t, 32 * kt + 16 * u, lane), p, dq[m][t]);
-        }
     }
-  }
+    if (last > 0) fetch(0);
+#pragma unroll
+    for (int t = 0; t < 2 * S::KS; t++) arrived(gf[t]);
+#pragma unroll
+    for (int t = 0; t < MAPS * S::KS; t++) arrived(qf[t]);
+#pragma unroll
+    for (int m = 0; m < MAPS; m++) { arrived(lse[m]); arrived(delta[m]); }
+    if (last > 0) {
+      ks.store(lds);
+      vs.store(lds + 2 * BUF);
+      if (S::KC < last) fetch(S::KC);
+    }
+    __syncthreads();
+    for (int j0 = 0, buf = 0; j0 < last; j0 += S::KC, buf ^= 1) {
+      const T* Ks = lds + buf * BUF;
+      const T* Vs = lds + (2 + buf) * BUF;
+      if (j0 < reach) {
+        at.fresh();
+        v16f dp;
+        clear(dp);
+        stream<typename O::Frag, 2 * S::KS, G>([&](int x) { return O::template rowwise<S::W>(Vs, 0, 16 * x, at); },
+                                               [&](int x, const typename O::Frag& f) { dp = O::mma(f, gf[x], dp); });
+#pragma unroll
+        for (int m = 0; m < MAPS; m++) {
+          const int base = (m0 + m) * DT;   // the map's columns
+          v16f sc;
+          clear(sc);
+          stream<typename O::Frag, S::KS, G>([&](int t) { return O::template rowwise<S::W>(Ks, 0, base + 16 * t, at); },
+                                             [&](int t, const typename O::Frag& f) { sc = O::mma(f, qf[m * S::KS + t], sc); });
+          if (j0 + 32 > least) {
+#pragma unroll
+            for (int v = 0; v < 16; v++)
+              if (j0 + 8 * (v >> 2) + 4 * hh + (v & 3) >= see) sc[v] = -INFINITY;
+          }
+#pragma unroll
+          for (int v = 0; v < 16; v++) {
+            sc[v] = exp2_fast(fmaf(sc[v], a.c, -lse[m])) * (dp[v] - delta[m]);
+            rest[m] += sc[v];
+          }
+          if (pass == 1) {
+            const typename O::Frag p[2] = {O::operand(sc, 0), O::operand(sc, 1)};
+            constexpr int GT = 2 * S::DTT < G ? 2 * S::DTT : G;
+            stream<typename O::Frag, 2 * S::DTT, GT>([&](int x) { return O::template transposed<S::W>(Ks, base + 32 * (x % S::DTT), 16 * (x / S::DTT), at); },
+                                                     [&](int x, const typename O::Frag& f) { dq[m][x % S::DTT] = O::mma(f, p[x / S::DTT], dq[m][x % S::DTT]); });
+          }
+        }
+      }
+      if (j0 + S::KC < last) {
+        ks.store(lds + (buf ^ 1) * BUF);
+        vs.store(lds + (2 + (buf ^ 1)) * BUF);
+        if (j0 + 2 * S::KC < last) fetch(j0 + 2 * S::KC);
+      }
+      __syncthreads();
+    }
   }
   if (r >= room) return;
-#pragma unroll
-  for (int m = 0; m < 2; m++) delta[m] += rest[m] + other_half(rest[m]);
   T* dqp = rows_of(a, static_cast<T*>(a.dq), b, s.q0, a.q_token, a.q_batch) + i * a.q_token + (int64_t)h * 2 * a.dim + 4 * hh;
 #pragma unroll
-  for (int m = 0; m < 2; m++) {
-    const float f = live ? (m ? -lam * a.scale : a.scale) : 0.f;
+  for (int m = 0; m < MAPS; m++) {
+    delta[m] += rest[m] + other_half(rest[m]);
+    const float f = live ? (m0 + m ? -lam * a.scale : a.scale) : 0.f;
 #pragma unroll
     for (int t = 0; t < S::DTT; t++)
 #pragma unroll
       for (int g = 0; g < 4; g++)
         if (32 * t + 8 * g < a.dim)
-          O::store4(dqp + m * a.dim + 32 * t + 8 * g, f * dq[m][t][4 * g], f * dq[m][t][4 * g + 1], f * dq[m][t][4 * g + 2], f * dq[m][t][4 * g + 3]);
-  }
-  if (hh == 0) {
-    a.delta[(int64_t)h * a.q_rows + row] = live ? delta[0] : 0.f;
-    a.delta[(int64_t)(a.heads + h) * a.q_rows + row] = live ? delta[1] : 0.f;
-    if (a.lam_token) a.dlam[row * a.heads + h] = live ? -delta[1] : 0.f;
+          O::store4(dqp + (m0 + m) * a.dim + 32 * t + 8 * g, f * dq[m][t][4 * g], f * dq[m][t][4 * g + 1], f * dq[m][t][4 * g + 2], f * dq[m][t][4 * g + 3]);
+    if (hh == 0) {
+      a.delta[(int64_t)((m0 + m) * a.heads + h) * a.q_rows + row] = live ? delta[m] : 0.f;
+      if (m0 + m == 1 && a.lam_token) a.dlam[row * a.heads + h] = live ? -delta[m] : 0.f;
+    }
   }
 }
 
@@ -592,136 +705,260 @@ __global__ void __launch_bounds__(1024) diff_lambda_kernel(DiffArgs a) {
 }
 
 // ---- backward: keys ------------------------------------------------------------------------------------------------------------------
+// A pair of waves owns 32 keys: one computes P and dS of a tile of rows and leaves them in LDS as operands, the other multiplies the tile before
+// it into dk and dv.  In one wave the accumulators (128 registers for heads of 64) beside the keys' and values' fragments (64) and three tiles
+// need more than 256 registers: one wave a SIMD, and most of its time went into copies to and from accumulation registers.
+//
+// What belongs to a row (log-sums, deltas, lambda) is a register index here, not a lane.  It comes to all lanes as a product: the fp32 value in
+// three bf16 parts, which hold all of its bits, times ones; as the initial accumulator of the scores it costs no vector instruction, and an eighth of the LDS
+// traffic of reading it for every register.
+template <typename T, int DT> struct KvSizes {
+  static constexpr int PAIRS = DT * sizeof(T) <= 128 && DT > 32 ? 4 : DT * sizeof(T) <= 256 ? 2 : 1;   // pairs of waves of a workgroup
+  static constexpr int BUFFERS = DT * sizeof(T) <= 256 ? 3 : 2;   // of a tile of rows (two, and one more barrier a tile, where three exceed LDS)
+  static constexpr int KEYS = 32 * PAIRS, THREADS = 128 * PAIRS;
+};
+__device__ inline uint2 three_parts(float x) {
+  const bf16_t hi = f32_to_bf16(x), mid = f32_to_bf16(x - bf16_to_f32(hi)), lo = f32_to_bf16(x - bf16_to_f32(hi) - bf16_to_f32(mid));
+  return make_uint2((uint32_t)hi | (uint32_t)mid << 16, lo);
+}
+// adds a row's value, held by the row's lane of the lower half, to a tile's rows
+__device__ inline v16f add_rows(uint2 parts, int hh, const v16f& c) {
+  const uint4 a = hh ? make_uint4(0, 0, 0, 0) : make_uint4(parts.x, parts.y, 0, 0), one = make_uint4(0x3f803f80u, 0x3f80u, 0, 0);
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, a), __builtin_bit_cast(v8bf, one), c, 0, 0, 0);
+}
+
 template <typename T, int DT>
-__global__ void __launch_bounds__(256, 1) diff_backward_kv_kernel(DiffArgs a) {
+__global__ void __launch_bounds__((KvSizes<T, DT>::THREADS), sizeof(T) == 2 && DT <= 64 ? 2 : 1) diff_backward_kv_kernel(DiffArgs a) {
   typedef Ops<T> O;
   typedef Sizes<T, DT> S;
-  __shared__ __attribute__((aligned(16))) T Qs[S::KC * S::PITCH];
-  __shared__ __attribute__((aligned(16))) T Gs[S::KC * S::PITCH];
-  __shared__ __attribute__((aligned(16))) float st[5][S::KC];   // log-sums, deltas and lambda of the rows
-  const int w = work_index(a.units * a.tiles, a.tiles, a.causal);
-  if (w >= a.units * a.tiles) return;
-  const int unit = w / a.tiles, tile = w % a.tiles;   // (under a causal mask the first keys are seen by the most rows)
+  typedef KvSizes<T, DT> Z;
+  constexpr int BUF = S::KC * S::W, G = 2, NB = Z::BUFFERS, FRAG = sizeof(typename O::Frag);
+  __shared__ __attribute__((aligned(16))) T lds[2 * NB * BUF];                         // queries and dO
+  __shared__ __attribute__((aligned(16))) uint2 st[NB][5][S::KC];                      // the rows' values
+  __shared__ __attribute__((aligned(16))) char ex[2][Z::PAIRS][6 * 64 * FRAG];         // P_1 - lambda P_2, dS_1, dS_2 of a tile, two operands each
+  const int total = a.units * a.tiles * a.parts;
+  const int w = work_index(total, a.tiles * a.parts, a.causal);
+  if (w >= total) return;
+  const int part = w % a.parts, ut = w / a.parts, unit = ut / a.tiles, tile = ut % a.tiles;   // (under a causal mask the first keys are seen by the most rows)
   const int b = unit / a.kv_heads, hk = unit % a.kv_heads;
   const Seq s = sequence(a, b);
-  const int R = s.nq * a.group, j0 = tile * ROWS, room = a.q_starts ? s.nk : a.tk;
+  const int R = s.nq * a.group, j0 = tile * Z::KEYS, room = a.q_starts ? s.nk : a.tk;
   if (j0 >= room) return;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 31, hh = lane >> 5;
-  const int j = j0 + 32 * wave + c;
+  const int lane = threadIdx.x & 63, wave = wave_of_thread(), c = lane & 31, hh = lane >> 5;
+  const int pair = wave % Z::PAIRS;
+  const bool producer = wave < Z::PAIRS;   // (waves go to the four SIMDs in turn: one of each kind on a SIMD)
+  const int wj0 = j0 + 32 * pair, j = wj0 + c;
   const bool live = j < s.nk;
   const T* qp = rows_of(a, static_cast<const T*>(a.q), b, s.q0, a.q_token, a.q_batch) + (int64_t)hk * a.group * 2 * a.dim;
   const T* gp = rows_of(a, static_cast<const T*>(a.dout), b, s.q0, a.o_token, a.o_batch) + (int64_t)hk * a.group * 2 * a.dim;
-  typename O::Frag kf[2 * S::KS], vf[2 * S::KS];
   const int64_t k_at = (int64_t)j * a.k_token + (int64_t)hk * 2 * a.dim, v_at = (int64_t)j * a.v_token + (int64_t)hk * 2 * a.dim;
-  own_row<T, DT, true>(kf, rows_of(a, static_cast<const T*>(a.k), b, s.k0, a.k_token, a.k_batch) + k_at, live, a.dim, hh);
-  own_row<T, DT, false>(vf, rows_of(a, static_cast<const T*>(a.v), b, s.k0, a.v_token, a.v_batch) + v_at, live, a.dim, hh);
-  // the first row that sees key j, and those of the wave's first and last key
+  // the first row that sees key j, and those of the pair's first and last key
   const int off = s.nk - s.nq;
   auto from = [&](int key) { return a.causal ? max(0, key - off) * a.group : 0; };
   const int first = live ? from(j) : 0;
-  const int wfirst = j0 + 32 * wave < s.nk ? from(j0 + 32 * wave) : R, wlast = from(min(j0 + 32 * wave + 31, s.nk - 1));
-  v16f dk[2][S::DTT], dv[S::VT];
+  const int wfirst = wj0 < s.nk ? from(wj0) : R, wlast = from(min(wj0 + 31, s.nk - 1));
+  LaneAt at = O::template lane_at<S::W>(lane);
+  Stage<T, DT, true, Z::THREADS> qs;
+  Stage<T, DT, false, Z::THREADS> gs;
+  auto place = [&](int r, int64_t token) { const int x = query_of(a, r); return x * token + (int64_t)(r - x * a.group) * 2 * a.dim; };
+  qs.plan(a.dim, [&](int x) { return place(x, a.q_token); });
+  gs.plan(a.dim, [&](int x) { return place(x, a.o_token); });
+  const bool near_q = a.near_q && qs.STEP % a.group == 0;   // (the rows of a tile and of its steps lie alike)
+  const float inv_c = 1.f / a.c;
+  float sv[5];
+  auto fetch = [&](int r0) {
+    if (near_q && a.dim == DT && r0 + S::KC <= R) {
+      qs.load_whole(qp + place(r0, a.q_token), place(qs.STEP, a.q_token));
+      gs.load_whole(gp + place(r0, a.o_token), place(gs.STEP, a.o_token));
+    } else {
+      qs.load(R - r0, a.dim, [&](int x) { return qp + place(r0 + x, a.q_token); });
+      gs.load(R - r0, a.dim, [&](int x) { return gp + place(r0 + x, a.o_token); });
+    }
 #pragma unroll
-  for (int m = 0; m < 2; m++)
-#pragma unroll
-    for (int t = 0; t < S::DTT; t++) clear(dk[m][t]);
-#pragma unroll
-  for (int t = 0; t < S::VT; t++) clear(dv[t]);
-  for (int r0 = j0 < s.nk ? from(j0) / S::KC * S::KC : R; r0 < R; r0 += S::KC) {
-    Stage<T, DT, true> qs;
-    Stage<T, DT, false> gs;
-    const int n = min(S::KC, R - r0);
-    auto place = [&](int x, int64_t token) { const int r = r0 + x, i = query_of(a, r); return i * token + (int64_t)(r - i * a.group) * 2 * a.dim; };
-    qs.load(n, a.dim, [&](int x) { return qp + place(x, a.q_token); });
-    gs.load(n, a.dim, [&](int x) { return gp + place(x, a.o_token); });
-    float sv[5] = {0.f, 0.f, 0.f, 0.f, 0.f};
-    if ((int)threadIdx.x < n) {
+    for (int e = 0; e < 5; e++) sv[e] = 0.f;
+    if ((int)threadIdx.x < min(S::KC, R - r0)) {
       const int r = r0 + threadIdx.x, i = query_of(a, r), h = hk * a.group + (r - i * a.group);
-      const int64_t row = s.q0 + i, at = (int64_t)h * a.q_rows + row, two = (int64_t)a.heads * a.q_rows;
-      sv[0] = a.lse[at]; sv[1] = a.lse[at + two]; sv[2] = a.delta[at]; sv[3] = a.delta[at + two];
+      const int64_t row = s.q0 + i, first_map = (int64_t)h * a.q_rows + row, second_map = first_map + (int64_t)a.heads * a.q_rows;
+      sv[0] = a.lse[first_map]; sv[1] = a.lse[second_map]; sv[2] = a.delta[first_map]; sv[3] = a.delta[second_map];
       sv[4] = a.lam[a.lam_token ? row * a.heads + h : h];
     }
+  };
+  auto put = [&](int buf) {
+    qs.store(lds + buf * BUF);
+    gs.store(lds + (NB + buf) * BUF);
+    if ((int)threadIdx.x < S::KC) {
+      st[buf][0][threadIdx.x] = three_parts(-sv[0] * inv_c);
+      st[buf][1][threadIdx.x] = three_parts(-sv[1] * inv_c);
+      st[buf][2][threadIdx.x] = three_parts(sv[2]);
+      st[buf][3][threadIdx.x] = three_parts(sv[3]);
+      st[buf][4][threadIdx.x] = three_parts(sv[4]);
+    }
+  };
+  int begin = j0 < s.nk ? from(j0) / S::KC : (R + S::KC - 1) / S::KC, end = (R + S::KC - 1) / S::KC;   // tiles of rows
+  if (a.parts > 1) {
+    const int per = (max(end - begin, 0) + a.parts - 1) / a.parts;
+    begin += part * per;
+    end = min(end, begin + per);
+  }
+  auto seen = [&](int t) { return t * S::KC + 32 > wfirst; };   // some key of the pair is seen by the tile's rows
+  // Tile t is worked on from buffer t - begin mod NB by the first wave of a pair while the second one has the tile before it; the tile after it
+  // is written, and the one after that is on its way into registers.
+  auto next = [](int x) { return x == NB - 1 ? 0 : x + 1; };
+  if (begin < end) fetch(begin * S::KC);
+  auto stage_first = [&]() {
+    if (begin < end) {
+      put(0);
+      if (begin + 1 < end) fetch((begin + 1) * S::KC);
+    }
     __syncthreads();
-    qs.store(Qs);
-    gs.store(Gs);
-    if ((int)threadIdx.x < S::KC)
-#pragma unroll
-      for (int e = 0; e < 5; e++) st[e][threadIdx.x] = sv[e];
+  };
+  auto stage_next = [&](int t, int buf) {
+    if (NB == 2) __syncthreads();   // (the next tile goes where the one before was read)
+    if (t + 1 < end) {
+      put(next(buf));
+      if (t + 2 < end) fetch((t + 2) * S::KC);
+    }
     __syncthreads();
+  };
+  if (producer) {
+    RowFrags<T, DT> kf, vf;
+    own_row<T, DT, true>(kf, rows_of(a, static_cast<const T*>(a.k), b, s.k0, a.k_token, a.k_batch) + k_at, live, a.dim, hh);
+    own_row<T, DT, false>(vf, rows_of(a, static_cast<const T*>(a.v), b, s.k0, a.v_token, a.v_batch) + v_at, live, a.dim, hh);
 #pragma unroll
-    for (int rt = 0; rt < S::KC / 32; rt++) {
-      const int rr = r0 + 32 * rt;
-      if (rr + 32 <= wfirst || rr >= R) continue;   // no key of the wave is seen by these rows
-      v16f sc[2], dp;
-#pragma unroll
-      for (int m = 0; m < 2; m++) {
-        clear(sc[m]);
-#pragma unroll
-        for (int t = 0; t < S::KS; t++)
-          sc[m] = O::mma(O::load(Qs + (32 * rt + c) * S::PITCH + m * DT + 16 * t + 8 * hh), kf[m * S::KS + t], sc[m]);
-      }
-      clear(dp);
-#pragma unroll
-      for (int t = 0; t < 2 * S::KS; t++) dp = O::mma(O::load(Gs + (32 * rt + c) * S::PITCH + 16 * t + 8 * hh), vf[t], dp);
-      if (rr < wlast) {
-#pragma unroll
-        for (int v = 0; v < 16; v++)
-          if (rr + 8 * (v >> 2) + 4 * hh + (v & 3) < first) { sc[0][v] = -INFINITY; sc[1][v] = -INFINITY; }
-      }
-      v16f wt;
-#pragma unroll
-      for (int g = 0; g < 4; g++) {
-        const int at = 32 * rt + 8 * g + 4 * hh;
-        float x[5][4];
-#pragma unroll
-        for (int e = 0; e < 5; e++) {
-          const float4 f = *reinterpret_cast<const float4*>(&st[e][at]);
-          x[e][0] = f.x; x[e][1] = f.y; x[e][2] = f.z; x[e][3] = f.w;
-        }
-#pragma unroll
-        for (int e = 0; e < 4; e++) {
-          const int v = 4 * g + e;
-          const float p0 = exp2_fast(fmaf(sc[0][v], a.c, -x[0][e])), p1 = x[4][e] * exp2_fast(fmaf(sc[1][v], a.c, -x[1][e]));
-          wt[v] = p0 - p1;
-          sc[0][v] = p0 * (dp[v] - x[2][e]);
-          sc[1][v] = p1 * (x[3][e] - dp[v]);
-        }
-      }
-#pragma unroll
-      for (int u = 0; u < 2; u++) {
-        const typename O::Frag pw = O::operand(wt, u);
-#pragma unroll
-        for (int t = 0; t < S::VT; t++) dv[t] = O::mma(O::template transposed<S::PITCH>(Gs, 32 * t, 32 * rt + 16 * u, lane), pw, dv[t]);
+    for (int t = 0; t < 2 * S::KS; t++) { arrived(kf[t]); arrived(vf[t]); }
+    stage_first();
+    for (int t = begin, buf = 0; t <= end; t++, buf = next(buf)) {
+      if (t < end && seen(t)) {
+        const T* Qs = lds + buf * BUF;
+        const T* Gs = lds + (NB + buf) * BUF;
+        typename O::Frag* x = reinterpret_cast<typename O::Frag*>(ex[(t - begin) & 1][pair]) + lane;
+        at.fresh();
+        v16f dp, wt, sc;
+        clear(dp);
+        stream<typename O::Frag, 2 * S::KS, G>([&](int e) { return O::template rowwise<S::W>(Gs, 0, 16 * e, at); },
+                                               [&](int e, const typename O::Frag& f) { dp = O::mma(f, vf[e], dp); });
 #pragma unroll
         for (int m = 0; m < 2; m++) {
-          const typename O::Frag p = O::operand(sc[m], u);
+          clear(sc);
+          sc = add_rows(st[buf][m][c], hh, sc);
+          stream<typename O::Frag, S::KS, G>([&](int e) { return O::template rowwise<S::W>(Qs, 0, m * DT + 16 * e, at); },
+                                             [&](int e, const typename O::Frag& f) { sc = O::mma(f, kf[m * S::KS + e], sc); });
+          if (t * S::KC < wlast) {
 #pragma unroll
-          for (int t = 0; t < S::DTT; t++)
-            dk[m][t] = O::mma(O::template transposed<S::PITCH>(Qs, m * DT + 32 * t, 32 * rt + 16 * u, lane), p, dk[m][t]);
+            for (int v = 0; v < 16; v++)
+              if (t * S::KC + 8 * (v >> 2) + 4 * hh + (v & 3) < first) sc[v] = -INFINITY;
+          }
+          // (delta is subtracted from the finished dP: a softmax over one key has dP = delta to the last bit, and a gradient of zero)
+          v16f delta;
+          clear(delta);
+          delta = add_rows(st[buf][2 + m][c], hh, delta);
+          if (m == 0) {
+#pragma unroll
+            for (int v = 0; v < 16; v++) {
+              wt[v] = exp2_fast(a.c * sc[v]);
+              sc[v] = wt[v] * (dp[v] - delta[v]);
+            }
+          } else {
+            v16f lam;
+            clear(lam);
+            lam = add_rows(st[buf][4][c], hh, lam);
+#pragma unroll
+            for (int v = 0; v < 16; v++) {
+              const float p = lam[v] * exp2_fast(a.c * sc[v]);
+              wt[v] -= p;
+              sc[v] = p * (delta[v] - dp[v]);
+            }
+          }
+#pragma unroll
+          for (int u = 0; u < 2; u++) x[(2 + 2 * m + u) * 64] = O::operand(sc, u);
         }
+#pragma unroll
+        for (int u = 0; u < 2; u++) x[u * 64] = O::operand(wt, u);
       }
+      stage_next(t, buf);
     }
+    return;
+  }
+  v16f dv[S::VT], dk[2][S::DTT];
+#pragma unroll
+  for (int t = 0; t < S::VT; t++) { clear(dv[t]); clear(dk[t / S::DTT][t % S::DTT]); }
+  stage_first();
+  for (int t = begin, buf = 0, before = NB - 1; t <= end; t++, before = buf, buf = next(buf)) {
+    if (t > begin && seen(t - 1)) {
+      const T* Qs = lds + before * BUF;
+      const T* Gs = lds + (NB + before) * BUF;
+      const typename O::Frag* x = reinterpret_cast<const typename O::Frag*>(ex[(t - 1 - begin) & 1][pair]) + lane;
+      at.fresh();
+      typename O::Frag p[6];
+#pragma unroll
+      for (int e = 0; e < 6; e++) p[e] = x[e * 64];
+      // columns of dO and of the two maps' queries, 2 W in all, for either half of the rows
+      stream<typename O::Frag, 4 * S::VT, G>(
+          [&](int e) { return O::template transposed<S::W>(e % (2 * S::VT) < S::VT ? Gs : Qs, 32 * (e % S::VT), 16 * (e / (2 * S::VT)), at); },
+          [&](int e, const typename O::Frag& f) {
+            const int u = e / (2 * S::VT), z = e % (2 * S::VT), m = z / S::DTT & 1;
+            if (z < S::VT) dv[z] = O::mma(f, p[u], dv[z]);
+            else dk[m][z % S::DTT] = O::mma(f, p[2 + 2 * m + u], dk[m][z % S::DTT]);
+          });
+    }
+    stage_next(t, buf);
+  }
+  if (a.parts > 1) {   // a part's sums, joined by diff_join_kv_kernel
+    if (!live) return;
+    float* q = a.part + ((((int64_t)part * a.units + unit) * a.tk) + j) * 4 * a.dim + 4 * hh;
+#pragma unroll
+    for (int t = 0; t < S::VT; t++)
+#pragma unroll
+      for (int g = 0; g < 4; g++) {
+        if (32 * t + 8 * g < 2 * a.dim) *reinterpret_cast<float4*>(q + 32 * t + 8 * g) = make_float4(dv[t][4 * g], dv[t][4 * g + 1], dv[t][4 * g + 2], dv[t][4 * g + 3]);
+        const v16f& d = dk[t / S::DTT][t % S::DTT];
+        const int col = 32 * (t % S::DTT) + 8 * g;
+        if (col < a.dim) *reinterpret_cast<float4*>(q + (2 + t / S::DTT) * a.dim + col) = make_float4(d[4 * g], d[4 * g + 1], d[4 * g + 2], d[4 * g + 3]);
+      }
+    return;
   }
   if (j >= room) return;
   T* dkp = rows_of(a, static_cast<T*>(a.dk), b, s.k0, a.k_token, a.k_batch) + k_at + 4 * hh;
   T* dvp = rows_of(a, static_cast<T*>(a.dv), b, s.k0, a.v_token, a.v_batch) + v_at + 4 * hh;
-  const float f = live ? a.scale : 0.f;
-#pragma unroll
-  for (int m = 0; m < 2; m++)
-#pragma unroll
-    for (int t = 0; t < S::DTT; t++)
-#pragma unroll
-      for (int g = 0; g < 4; g++)
-        if (32 * t + 8 * g < a.dim)
-          O::store4(dkp + m * a.dim + 32 * t + 8 * g, live ? f * dk[m][t][4 * g] : 0.f, live ? f * dk[m][t][4 * g + 1] : 0.f,
-                    live ? f * dk[m][t][4 * g + 2] : 0.f, live ? f * dk[m][t][4 * g + 3] : 0.f);
 #pragma unroll
   for (int t = 0; t < S::VT; t++)
 #pragma unroll
-    for (int g = 0; g < 4; g++)
-      if (32 * t + 8 * g < 2 * a.dim)
-        O::store4(dvp + 32 * t + 8 * g, live ? dv[t][4 * g] : 0.f, live ? dv[t][4 * g + 1] : 0.f, live ? dv[t][4 * g + 2] : 0.f,
-                  live ? dv[t][4 * g + 3] : 0.f);
+    for (int g = 0; g < 4; g++) {
+      float y[4], z[4];
+#pragma unroll
+      for (int e = 0; e < 4; e++) {
+        y[e] = live ? dv[t][4 * g + e] : 0.f;
+        z[e] = live ? a.scale * dk[t / S::DTT][t % S::DTT][4 * g + e] : 0.f;
+      }
+      if (32 * t + 8 * g < 2 * a.dim) O::store4(dvp + 32 * t + 8 * g, y[0], y[1], y[2], y[3]);
+      const int col = 32 * (t % S::DTT) + 8 * g;
+      if (col < a.dim) O::store4(dkp + t / S::DTT * a.dim + col, z[0], z[1], z[2], z[3]);
+    }
+}
+
+// Adds the parts of a key's gradients, always in the same order: a thread takes four channels.
+template <typename T>
+__global__ void __launch_bounds__(256) diff_join_kv_kernel(DiffArgs a) {
+  const int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int col = (int)(x % a.dim) * 4, j = (int)(x / a.dim % a.tk), unit = (int)(x / ((int64_t)a.dim * a.tk));
+  if (unit >= a.units) return;
+  const int b = unit / a.kv_heads, hk = unit % a.kv_heads;
+  const Seq s = sequence(a, b);
+  const bool live = j < s.nk;
+  if (!live && a.q_starts) return;
+  float4 t = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (live)
+    for (int p = 0; p < a.parts; p++) {
+      const float4 y = *reinterpret_cast<const float4*>(a.part + (((int64_t)p * a.units + unit) * a.tk + j) * 4 * a.dim + col);
+      t.x += y.x; t.y += y.y; t.z += y.z; t.w += y.w;
+    }
+  if (col < 2 * a.dim) {
+    T* dv = rows_of(a, static_cast<T*>(a.dv), b, s.k0, a.v_token, a.v_batch) + j * a.v_token + (int64_t)hk * 2 * a.dim + col;
+    Ops<T>::store4(dv, t.x, t.y, t.z, t.w);
+  } else {
+    T* dk = rows_of(a, static_cast<T*>(a.dk), b, s.k0, a.k_token, a.k_batch) + j * a.k_token + (int64_t)hk * 2 * a.dim + col - 2 * a.dim;
+    Ops<T>::store4(dk, a.scale * t.x, a.scale * t.y, a.scale * t.z, a.scale * t.w);
+  }
 }
 
 // ---- host ----------------------------------------------------------------------------------------------------------------------------
@@ -742,7 +979,7 @@ static int check(const char* what, const cd_diff_attn* d) {
   CD_REQUIRE(d->tq >= 0 && d->tk >= 0, "%s: tq=%d tk=%d", what, d->tq, d->tk);
   const int64_t group = d->heads / d->kv_heads;
   CD_REQUIRE(group <= 1024 && d->tq * group <= (1 << 30) / group, "%s: tq=%d with %lld heads a key head is too long", what, d->tq, (long long)group);
-  CD_REQUIRE((int64_t)d->batch * d->kv_heads * (cdiv(d->tq * group, F_ROWS) + cdiv(d->tk, ROWS) + 1) < (1 << 30) && (int64_t)d->batch * d->tq <= INT32_MAX,
+  CD_REQUIRE((int64_t)d->batch * d->kv_heads * (cdiv(d->tq * group, F_ROWS) + cdiv(d->tk, 64) + 1) < (1 << 30) && (int64_t)d->batch * d->tq <= INT32_MAX,
              "%s: too many rows", what);
   for (const void* p : {(const void*)d->q_lens, (const void*)d->k_lens, (const void*)d->q_starts, (const void*)d->k_starts})
     CD_REQUIRE((reinterpret_cast<uintptr_t>(p) & 3) == 0, "%s: length and start tables must be 4-byte aligned", what);
@@ -787,6 +1024,10 @@ static DiffArgs args_of(const cd_diff_attn* d) {
   a.batch = d->batch; a.tq = d->tq; a.tk = d->tk; a.heads = d->heads; a.kv_heads = d->kv_heads; a.group = d->heads / d->kv_heads; a.dim = d->head_dim;
   a.causal = d->causal != 0; a.lam_token = d->lambda_kind == CD_LAMBDA_TOKEN; a.parts = 1;
   a.units = d->batch * d->kv_heads;
+  // tiles of 32 rows whose offsets fit 32 bits
+  const int64_t far = (1LL << 32) / (32 * elem_of(d)) - 1;
+  a.near_k = d->k_token < far && d->v_token < far;
+  a.near_q = d->q_token < far && d->o_token < far;
   a.group_inv = a.group > 1 ? (uint32_t)((1ull << 32) / a.group) + 1 : 0;
   a.scale = d->scale > 0.f ? d->scale : 1.f / sqrtf((float)d->head_dim);
   a.c = a.scale * 1.44269504088896340736f;
@@ -794,19 +1035,29 @@ static DiffArgs args_of(const cd_diff_attn* d) {
 }
 
 // f<T, DT>() of this dtype and head_dim
-#define CD_DIFF_DISPATCH(d, KERNEL, THREADS, BLOCKS, s, a)                                                                                  \
-  do {                                                                                                                             \
-    const dim3 grid_(BLOCKS), block_(THREADS);                                                                                                      \
-    if ((d)->dtype == CD_BF16) {                                                                                                   \
-      if ((d)->head_dim <= 32) hipLaunchKernelGGL((KERNEL<bf16_t, 32>), grid_, block_, 0, s, a);                                \
-      else if ((d)->head_dim <= 64) hipLaunchKernelGGL((KERNEL<bf16_t, 64>), grid_, block_, 0, s, a);                           \
-      else hipLaunchKernelGGL((KERNEL<bf16_t, 128>), grid_, block_, 0, s, a);                                                   \
-    } else {                                                                                                                       \
-      if ((d)->head_dim <= 32) hipLaunchKernelGGL((KERNEL<float, 32>), grid_, block_, 0, s, a);                                 \
-      else if ((d)->head_dim <= 64) hipLaunchKernelGGL((KERNEL<float, 64>), grid_, block_, 0, s, a);                            \
-      else hipLaunchKernelGGL((KERNEL<float, 128>), grid_, block_, 0, s, a);                                                    \
-    }                                                                                                                              \
-  } while (0)
+// f(instance) for the dtype and the head dimension of a descriptor: instance holds T and DT
+template <typename T_, int DT_> struct Instance { typedef T_ T; static constexpr int DT = DT_; };
+template <typename F> static void dispatch(const cd_diff_attn* d, F f) {
+  if (d->dtype == CD_BF16) {
+    if (d->head_dim <= 32) f(Instance<bf16_t, 32>()); else if (d->head_dim <= 64) f(Instance<bf16_t, 64>()); else f(Instance<bf16_t, 128>());
+  } else {
+    if (d->head_dim <= 32) f(Instance<float, 32>()); else if (d->head_dim <= 64) f(Instance<float, 64>()); else f(Instance<float, 128>());
+  }
+}
+static int64_t keys_of(const cd_diff_attn* d) {
+  int64_t n = 0;
+  dispatch(d, [&](auto x) { n = KvSizes<typename decltype(x)::T, decltype(x)::DT>::KEYS; });
+  return n;
+}
+// Parts of the rows that get a workgroup of their own in the pass that owns keys: few keys under many rows (shared key heads) leave compute units without
+// work.
+static int kv_parts_of(const cd_diff_attn* d) {
+  const int64_t groups = (int64_t)d->batch * d->kv_heads * cdiv(d->tk, keys_of(d)), tiles = cdiv((int64_t)d->tq * (d->heads / d->kv_heads), 32);
+  int64_t p = groups ? 512 / groups : 1;
+  if (p > tiles / 8) p = tiles / 8;
+  if (p > 16) p = 16;
+  return p < 2 ? 1 : (int)p;
+}
 
 static double pairs(const cd_diff_attn* d) { return (double)d->batch * d->heads * d->tq * d->tk * (d->causal ? 0.5 : 1.0); }
 
@@ -821,8 +1072,10 @@ extern "C" int codistill_diff_attention_workspace_bytes(const cd_diff_attn* desc
   const int parts = parts_of(desc);
   size_t n = parts > 1 ? (size_t)parts * desc->batch * desc->kv_heads * desc->tq * (desc->heads / desc->kv_heads) * 2 * (2 * desc->head_dim + 2) * 4 : 0;
   if (backward) {
-    const size_t deltas = (size_t)2 * desc->heads * rows_q(desc) * 4;
-    n = n > deltas ? n : deltas;
+    const int kv_parts = kv_parts_of(desc);
+    const size_t deltas = align_up((size_t)2 * desc->heads * rows_q(desc) * 4, 16);
+    const size_t sums = kv_parts > 1 ? (size_t)kv_parts * desc->batch * desc->kv_heads * desc->tk * 4 * desc->head_dim * 4 : 0;
+    n = n > deltas + sums ? n : deltas + sums;
   }
   *bytes = align_up(n, 16);
   return CD_OK;
@@ -850,7 +1103,9 @@ extern "C" int codistill_diff_attention(const cd_diff_attn* desc, const void* q,
   hipStream_t s = static_cast<hipStream_t>(stream);
   const double e = elem_of(desc), qe = 2.0 * a.q_rows * a.heads * 2 * a.dim, ke = 2.0 * a.k_rows * a.kv_heads * 2 * a.dim;
   ProfScope prof(CD_K_ATTN, s, 12.0 * a.dim * pairs(desc), e * (qe + ke));
-  CD_DIFF_DISPATCH(desc, diff_forward_kernel, F_THREADS, work_blocks((int64_t)a.units * a.tiles * a.parts), s, a);
+  dispatch(desc, [&](auto x) {
+    hipLaunchKernelGGL((diff_forward_kernel<typename decltype(x)::T, decltype(x)::DT>), dim3(work_blocks((int64_t)a.units * a.tiles * a.parts)), dim3(F_THREADS), 0, s, a);
+  });
   if (a.parts > 1) {
     const dim3 grid((unsigned)cdiv((int64_t)a.units * a.tq * a.group, 4));
     if (desc->dtype == CD_BF16) hipLaunchKernelGGL((diff_join_kernel<bf16_t>), grid, dim3(256), 0, s, a);
@@ -879,14 +1134,25 @@ extern "C" int codistill_diff_attention_backward(const cd_diff_attn* desc, const
   hipStream_t s = static_cast<hipStream_t>(stream);
   const double e = elem_of(desc), qe = 4.0 * a.q_rows * a.heads * 2 * a.dim, ke = 4.0 * a.k_rows * a.kv_heads * 2 * a.dim;
   ProfScope prof(CD_K_ATTN, s, 20.0 * a.dim * pairs(desc), e * (qe + ke));
-  if (a.tq > 0) {
-    a.tiles = (int)cdiv((int64_t)a.tq * a.group, ROWS);
-    CD_DIFF_DISPATCH(desc, diff_backward_q_kernel, 256, work_blocks((int64_t)a.units * a.tiles), s, a);
-  }
+  if (a.tq > 0)
+    dispatch(desc, [&](auto x) {
+      a.tiles = (int)cdiv((int64_t)a.tq * a.group, QSizes<typename decltype(x)::T, decltype(x)::DT>::ROWS);
+      hipLaunchKernelGGL((diff_backward_q_kernel<typename decltype(x)::T, decltype(x)::DT>), dim3(work_blocks((int64_t)a.units * a.tiles)), dim3(256), 0, s, a);
+    });
   if (!a.lam_token) hipLaunchKernelGGL(diff_lambda_kernel, dim3((unsigned)a.heads), dim3(1024), 0, s, a);
   if (a.tk > 0) {
-    a.tiles = (int)cdiv(a.tk, ROWS);
-    CD_DIFF_DISPATCH(desc, diff_backward_kv_kernel, 256, work_blocks((int64_t)a.units * a.tiles), s, a);
+    a.parts = kv_parts_of(desc);
+    a.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + align_up((size_t)2 * a.heads * a.q_rows * 4, 16));
+    dispatch(desc, [&](auto x) {
+      typedef KvSizes<typename decltype(x)::T, decltype(x)::DT> Z;
+      a.tiles = (int)cdiv(a.tk, Z::KEYS);
+      hipLaunchKernelGGL((diff_backward_kv_kernel<typename decltype(x)::T, decltype(x)::DT>), dim3(work_blocks((int64_t)a.units * a.tiles * a.parts)), dim3(Z::THREADS), 0, s, a);
+    });
+    if (a.parts > 1) {
+      const dim3 grid((unsigned)cdiv((int64_t)a.units * a.tk * a.dim, 256));
+      if (desc->dtype == CD_BF16) hipLaunchKernelGGL((diff_join_kv_kernel<bf16_t>), grid, dim3(256), 0, s, a);
+      else hipLaunchKernelGGL((diff_join_kv_kernel<float>), grid, dim3(256), 0, s, a);
+    }
   }
   return check_launch("diff_attention_backward");
 }
