@@ -13,6 +13,7 @@
 // full 16-byte vectors along the channels.  The MFMA "A" operand is the filter tile and "B" the
 // activation tile, so that a lane's 16 accumulators run along the output channels of one pixel.
 #include "kernels.h"
+#include "lds_load.h"
 #include "conv_rules.h"
 #include <algorithm>
 
@@ -101,47 +102,6 @@ __device__ inline float tile_diagonal(f32x16_t d, int c) {
   const float w0 = b1 ? u1 : u0, w1 = b1 ? u3 : u2, w2 = b1 ? u5 : u4, w3 = b1 ? u7 : u6;
   const float x0 = b3 ? w1 : w0, x1 = b3 ? w3 : w2;
   return b4 ? x1 : x0;
-}
-
-// 16 bytes per lane from a buffer straight into LDS: lane l of the wave writes its vector at
-// lds_addr + 16*l (lds_addr is uniform over the wave and travels in M0); an offset at or beyond the buffer's size
-// writes zeros, so that a masked-out vector costs one select instead of a branch around the load.  The compiler does
-// not see these loads: the kernel waits for them itself (wait_vmem) before a barrier publishes the tile.
-typedef int rsrc_words_t __attribute__((ext_vector_type(4)));
-// the four descriptor words of a raw buffer (stride 0): base address, size in bytes, data format
-__device__ inline rsrc_words_t make_rsrc_words(const void* p, uint32_t bytes) {
-  const uint64_t b = reinterpret_cast<uint64_t>(p);
-  rsrc_words_t w;
-  w.x = (int)(uint32_t)b;
-  w.y = (int)((uint32_t)(b >> 32) & 0xffffu);
-  w.z = (int)bytes;
-  w.w = 0x00020000;
-  return w;
-}
-__device__ inline void load_lds16(rsrc_words_t w, uint32_t lds_addr, uint32_t byte_off) {
-  asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
-               :
-               : "s"(lds_addr), "v"(byte_off), "s"(w)
-               : "memory");  // M0 cannot be named as a clobber: the compiler treats it as a reserved register (it rejects
-                             // "m0" in a clobber list as such), i.e. it never keeps a value in M0 from one statement to
-                             // the next and writes M0 itself right before each of its own uses
-}
-// wait until at most N of this wave's vector memory loads are outstanding
-template <int N>
-__device__ inline void wait_vmem() {
-  static_assert(N >= 0 && N < 64, "vmcnt is a 6-bit counter");
-  asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory");
-}
-
-// the same, and until this wave's LDS reads are done; then the workgroup's barrier.  (Builtins, so that the compiler's own
-// count of outstanding LDS reads starts from zero behind it; the empty statements keep memory accesses on their side.)
-template <int N>
-__device__ inline void wait_step() {
-  static_assert(N >= 0 && N < 64, "vmcnt is a 6-bit counter");
-  asm volatile("" : : : "memory");
-  __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | (7 << 4));   // vmcnt(N) lgkmcnt(0)
-  __builtin_amdgcn_s_barrier();
-  asm volatile("" : : : "memory");
 }
 
 // LDS tiles are [row][BKT elements], rows of 64 (BKT = 32) or 128 bytes without padding; the 16-byte column cv of a row

@@ -23,6 +23,7 @@
 // in which the first operand, the streamed tensor transposed, is read from LDS.
 #include "common.h"
 #include "kernels.h"
+#include "lds_load.h"
 #include <math.h>
 
 namespace cd {
@@ -35,16 +36,30 @@ typedef float v2f __attribute__((ext_vector_type(2)));
 typedef float v8f __attribute__((ext_vector_type(8)));
 typedef float v16f __attribute__((ext_vector_type(16)));
 
+// What the pass that owns keys needs of a row, in the form it uses it: the pass that owns queries leaves it in the workspace.
+struct RowValues {
+  uint2 lse[2];    // minus the log-sums over c, each fp32 value in three bf16 parts (all of its bits)
+  uint2 delta[2];
+  uint2 lam;
+  uint2 unused;
+};
+static_assert(sizeof(RowValues) == 48, "three pieces of 16 bytes");
+__device__ inline uint2 three_parts(float x) {
+  const bf16_t hi = f32_to_bf16(x), mid = f32_to_bf16(x - bf16_to_f32(hi)), lo = f32_to_bf16(x - bf16_to_f32(hi) - bf16_to_f32(mid));
+  return make_uint2((uint32_t)hi | (uint32_t)mid << 16, lo);
+}
+
 struct DiffArgs {
   const void* q; const void* k; const void* v; const float* lam;
   void* out; void* o2; float* lse;
   const void* dout; void* dq; void* dk; void* dv; float* dlam;
-  float* delta;                                   // backward: [2][heads][q rows]
+  RowValues* rows;                                // backward: [q rows][heads]
+  float* second;                                  // backward, a lambda for each head: delta_2 [heads][q rows]
   float* part; float* part_ml;                    // forward over parts of the keys: unnormalised sums and (maximum, sum) of a part
   int64_t q_token, q_batch, k_token, k_batch, v_token, v_batch, o_token, o_batch, o2_token;
   const int32_t* q_lens; const int32_t* k_lens; const int32_t* q_starts; const int32_t* k_starts;
   int64_t q_rows, k_rows;                         // rows of the q and k tensors (batch * tq when padded)
-  int32_t batch, tq, tk, heads, kv_heads, group, dim, causal, lam_token, parts, tiles, units, near_k, near_q;
+  int32_t batch, tq, tk, heads, kv_heads, group, dim, causal, lam_token, parts, tiles, units, work;
   uint32_t group_inv;                             // floor(2^32 / group) + 1 (group > 1)
   float scale, c;                                 // c = scale log2(e)
 };
@@ -52,10 +67,12 @@ struct DiffArgs {
 // A copy in LDS: rows of W elements, the 16-byte pieces of a row exchanged among themselves so that both kinds of reads meet all banks.  Sixteen rows
 // read at the same column (row by row) differ in four bits of the row, four consecutive rows read over 64 bytes (transposed) in bits 2 and 3 of
 // the piece.  Padded rows serve one of the two: with 16 bytes a row the transposing loads met each bank four times.
+template <typename T, int W> __host__ __device__ constexpr int lds_swap(int row) {
+  return W * (int)sizeof(T) == 128 ? ((row >> 1 & 1) << 2) | (row >> 2 & 3) : ((row & 3) << 2) | (row >> 2 & 3);   // (rows of 128 bytes: bit 0 changes banks by itself)
+}
 template <typename T, int W> __host__ __device__ constexpr int lds_at(int row, int col) {
   constexpr int VE = 16 / (int)sizeof(T);
-  const int f = W * (int)sizeof(T) == 128 ? ((row >> 1 & 1) << 2) | (row >> 2 & 3) : ((row & 3) << 2) | (row >> 2 & 3);   // (rows of 128 bytes: bit 0 changes banks by itself)
-  return row * W + ((col / VE) ^ f) * VE + col % VE;
+  return row * W + ((col / VE) ^ lds_swap<T, W>(row)) * VE + col % VE;
 }
 
 // Where a lane's reads begin: the pieces are exchanged by exclusive or, so a constant column is one more exclusive or.
@@ -189,44 +206,39 @@ __device__ inline int work_index(int n, int per_unit, bool turns) {
 }
 static unsigned work_blocks(int64_t n) { return (unsigned)(cdiv(n, 8) * 8); }
 
-// Up to KC rows of 2 dim elements (two ranges of dim for the maps, MAPS, or one of 2 dim) on their way into LDS; what lies beyond the rows and the
-// channels becomes zero.  A whole tile whose rows lie within 32-bit offsets of its first is read from one address that all threads share and offsets
-// that stay the same from tile to tile: computing 64-bit addresses of each row anew was a third of the forward kernel's vector instructions.
-template <typename T, int DT, bool MAPS, int THREADS = 256> struct Stage {
+// A buffer that is the same in all lanes, and known to be (nothing is left of this where the compiler has seen it by itself).
+__device__ inline rsrc_words_t buffer_of(const void* p, int64_t bytes) {
+  rsrc_words_t w = make_rsrc_words(p, (uint32_t)min(bytes, (int64_t)0xfffffff0));
+#pragma unroll
+  for (int i = 0; i < 4; i++) w[i] = __builtin_amdgcn_readfirstlane(w[i]);
+  return w;
+}
+
+// KC rows of 2 dim elements (two ranges of dim for the maps, MAPS, or one of 2 dim) from memory straight into LDS: no registers hold them on the way
+// and no branch asks for their end, since what lies beyond the bytes of the last row reads as zeros.  A lane's pieces are where its LDS places
+// want them from; their offsets from the tile's first row stay the same from tile to tile.  (With loads into registers the compiler turned the
+// addresses into running pointers, spilled those and waited for all loads to have them back.)
+template <typename T, int DT, bool MAPS, int THREADS> struct Loader {
   typedef Sizes<T, DT> S;
   static constexpr int VE = Ops<T>::VE, VPR = S::W / VE, IT = S::KC * VPR / THREADS;
-  static constexpr int STEP = THREADS / VPR;   // rows between a thread's loads
-  uint4 u[IT];
-  uint32_t off;        // bytes from the tile's first row to the thread's first piece
-  static __device__ inline int row(int i) { return (threadIdx.x + THREADS * i) / VPR; }
-  static __device__ inline int column(int i) { return (threadIdx.x + THREADS * i) % VPR * VE; }
-  // where a row's column lies in its range or ranges of dim channels; negative: padding
-  static __device__ inline int channel(int c, int dim) {
-    if (!MAPS) return c < 2 * dim ? c : -1;
-    const int cc = c >= DT ? c - DT : c;
-    return cc < dim ? (c >= DT ? dim + cc : cc) : -1;
-  }
+  uint32_t off[IT];   // bytes
+  static __device__ inline int row(int i) { return ((int)threadIdx.x + THREADS * i) / VPR; }
   // at(r): elements from the tile's first row to row r
-  template <typename At> __device__ inline void plan(int dim, At at) { off = (uint32_t)((at(row(0)) + max(channel(column(0), dim), 0)) * sizeof(T)); }
-  // step: elements from a row to the one STEP rows further
-  __device__ inline void load_whole(const T* first, int64_t step) {
-#pragma unroll
-    for (int i = 0; i < IT; i++) u[i] = *reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(first + i * step) + off);
-  }
-  // row(r): address of row r < n
-  template <typename Row> __device__ inline void load(int n, int dim, Row address) {
+  template <typename At> __device__ inline void plan(int dim, At at) {
 #pragma unroll
     for (int i = 0; i < IT; i++) {
-      u[i] = make_uint4(0, 0, 0, 0);
-      const int c = channel(column(i), dim);
-      if (row(i) < n && c >= 0) u[i] = *reinterpret_cast<const uint4*>(address(row(i)) + c);
+      const int r = row(i), c = (((int)threadIdx.x % VPR) ^ lds_swap<T, S::W>(r)) * VE, cc = MAPS && c >= DT ? c - DT : c;
+      off[i] = cc < (MAPS ? dim : 2 * dim) ? (uint32_t)((at(r) + (MAPS && c >= DT ? dim + cc : cc)) * sizeof(T)) : ~0u;   // (~0: beyond any buffer)
     }
   }
-  __device__ inline void store(T* dst) const {
+  // first: the tile's first row; elements: from there to the end of the last row.  The same in all lanes.
+  __device__ inline void load(const T* first, int64_t elements, uint32_t lds) const {
+    const rsrc_words_t w = buffer_of(first, elements * (int64_t)sizeof(T));
 #pragma unroll
-    for (int i = 0; i < IT; i++) *reinterpret_cast<uint4*>(dst + lds_at<T, S::W>(row(i), column(i))) = u[i];
+    for (int i = 0; i < IT; i++) load_lds16(w, (uint32_t)__builtin_amdgcn_readfirstlane((int)lds + THREADS * 16 * i), off[i]);
   }
 };
+__device__ inline uint32_t lds_address(const void* p) { return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char*)p; }
 
 // The fragments of a row of 2 dim elements that a lane owns.
 template <typename T, int DT> using RowFrags = typename Ops<T>::Frag[Sizes<T, DT>::W / 16];
@@ -252,12 +264,17 @@ __device__ inline void arrived(v8bf& v) {
 __device__ inline int wave_of_thread() { return __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6); }   // (the same value in all lanes, and known to be)
 
 // N fragments, used in order, G of them on their way from LDS while the G before are used.  (Left alone, the compiler reads a fragment, waits for it and
-// uses it, a fragment at a time.)
-template <typename F, int N, int G, typename Load, typename Use> __device__ inline void stream(Load load, Use use) {
+// uses it, a fragment at a time.)  The first G can be sent for earlier, in front of work that needs none of them.
+template <typename F, int G, typename Load> __device__ inline void stream_first(F (&f)[G], Load load) {
+#pragma unroll
+  for (int e = 0; e < G; e++) f[e] = load(e);
+  __builtin_amdgcn_sched_barrier(0);
+}
+template <typename F, int N, int G, typename Load, typename Use> __device__ inline void stream_rest(F (&first)[G], Load load, Use use) {
   static_assert(N % G == 0, "groups");
   F f[2][G];
 #pragma unroll
-  for (int e = 0; e < G; e++) f[0][e] = load(e);
+  for (int e = 0; e < G; e++) f[0][e] = first[e];
 #pragma unroll
   for (int g = 0; g < N / G; g++) {
     if (g + 1 < N / G) {
@@ -268,6 +285,12 @@ template <typename F, int N, int G, typename Load, typename Use> __device__ inli
 #pragma unroll
     for (int e = 0; e < G; e++) use(g * G + e, f[g & 1][e]);
   }
+}
+template <typename F, int N, int G, typename Load, typename Use> __device__ inline void stream(Load load, Use use) {
+  F first[G];
+#pragma unroll
+  for (int e = 0; e < G; e++) first[e] = load(e);
+  stream_rest<F, N, G>(first, load, use);
 }
 
 __device__ inline void clear(v16f& t) {
@@ -289,7 +312,8 @@ __global__ void __launch_bounds__(F_THREADS, sizeof(T) == 4 ? (DT == 128 ? 1 : 2
   typedef Ops<T> O;
   typedef Sizes<T, DT> S;
   __shared__ __attribute__((aligned(16))) T lds[4 * S::KC * S::W];   // keys and values, two buffers each
-  constexpr int BUF = S::KC * S::W, G = sizeof(T) == 2 && DT > 32 ? 4 : 2;
+  constexpr int BUF = S::KC * S::W, G = sizeof(T) == 2 ? 4 : 2, GK = G < S::KS ? G : S::KS;
+  constexpr bool EARLY = sizeof(T) == 2 && DT <= 64;
   const int total = a.units * a.tiles * a.parts;
   const int w = work_index(total, a.tiles * a.parts, a.causal);
   if (w >= total) return;
@@ -326,39 +350,34 @@ __global__ void __launch_bounds__(F_THREADS, sizeof(T) == 4 ? (DT == 128 ? 1 : 2
   for (int t = 0; t < S::VT; t++) clear(o[t]);
   float mx = -INFINITY, sum = 0.f;
   LaneAt at = O::template lane_at<S::W>(lane);
-  // One barrier a tile: while a tile of keys and values is worked on, the next one is written to the other buffer and the one after it is
-  // on its way into registers.
-  Stage<T, DT, true, F_THREADS> ks;
-  Stage<T, DT, false, F_THREADS> vs;
+  // One barrier a tile: behind it the tile has arrived, and nobody reads the other buffer any more, into which the next tile is sent for.
+  Loader<T, DT, true, F_THREADS> ks;
+  Loader<T, DT, false, F_THREADS> vs;
   ks.plan(a.dim, [&](int row) { return row * a.k_token; });
   vs.plan(a.dim, [&](int row) { return row * a.v_token; });
-  auto fetch = [&](int j) {
-    if (a.near_k && a.dim == DT && j + S::KC <= s.nk) {
-      ks.load_whole(kp + j * a.k_token, ks.STEP * a.k_token);
-      vs.load_whole(vp + j * a.v_token, vs.STEP * a.v_token);
-    } else {
-      ks.load(s.nk - j, a.dim, [&](int row) { return kp + (j + row) * a.k_token; });
-      vs.load(s.nk - j, a.dim, [&](int row) { return vp + (j + row) * a.v_token; });
-    }
+  const uint32_t to = lds_address(lds) + wave * 1024;
+  auto fetch = [&](int j, int buf) {
+    ks.load(kp + j * a.k_token, (s.nk - 1 - j) * a.k_token + 2 * a.dim, to + buf * (BUF * (int)sizeof(T)));
+    vs.load(vp + j * a.v_token, (s.nk - 1 - j) * a.v_token + 2 * a.dim, to + (2 + buf) * (BUF * (int)sizeof(T)));
   };
-  if (begin < last) fetch(begin);
 #pragma unroll
   for (int t = 0; t < S::KS; t++) arrived(qf[t]);
-  if (begin < last) {
-    ks.store(lds);
-    vs.store(lds + 2 * BUF);
-    if (begin + S::KC < last) fetch(begin + S::KC);
-  }
-  __syncthreads();
+  if (begin < last) fetch(begin, 0);
   for (int j0 = begin, buf = 0; j0 < last; j0 += S::KC, buf ^= 1) {
+    wait_step<0>();
+    if (j0 + S::KC < last) fetch(j0 + S::KC, buf ^ 1);
     const T* Ks = lds + buf * BUF;
     const T* Vs = lds + (2 + buf) * BUF;
     if (j0 < reach) {
       at.fresh();
       v16f sc;
       clear(sc);
-      stream<typename O::Frag, S::KS, G>([&](int t) { return O::template rowwise<S::W>(Ks, 0, m * DT + 16 * t, at); },
-                                         [&](int t, const typename O::Frag& f) { sc = O::mma(f, qf[t], sc); });
+      typename O::Frag kf[GK], vf[G];
+      auto key = [&](int t) { return O::template rowwise<S::W>(Ks, 0, m * DT + 16 * t, at); };
+      auto value = [&](int x) { return O::template transposed<S::W>(Vs, 32 * (x % S::VT), 16 * (x / S::VT), at); };
+      stream_first(kf, key);
+      if (EARLY) stream_first(vf, value);   // (they arrive while the scores are worked on)
+      stream_rest<typename O::Frag, S::KS, GK>(kf, key, [&](int t, const typename O::Frag& f) { sc = O::mma(f, qf[t], sc); });
       if (j0 + 32 > least) {   // some row of the wave does not see all of the tile
 #pragma unroll
         for (int v = 0; v < 16; v++)
@@ -385,16 +404,11 @@ __global__ void __launch_bounds__(F_THREADS, sizeof(T) == 4 ? (DT == 128 ? 1 : 2
         sum += sc[v];
       }
       const typename O::Frag p[2] = {O::operand(sc, 0), O::operand(sc, 1)};
-      stream<typename O::Frag, 2 * S::VT, G>([&](int x) { return O::template transposed<S::W>(Vs, 32 * (x % S::VT), 16 * (x / S::VT), at); },
-                                             [&](int x, const typename O::Frag& f) { o[x % S::VT] = O::mma(f, p[x / S::VT], o[x % S::VT]); });
+      if (!EARLY) stream_first(vf, value);
+      stream_rest<typename O::Frag, 2 * S::VT, G>(vf, value, [&](int x, const typename O::Frag& f) { o[x % S::VT] = O::mma(f, p[x / S::VT], o[x % S::VT]); });
     }
-    if (j0 + S::KC < last) {
-      ks.store(lds + (buf ^ 1) * BUF);
-      vs.store(lds + (2 + (buf ^ 1)) * BUF);
-      if (j0 + 2 * S::KC < last) fetch(j0 + 2 * S::KC);
-    }
-    __syncthreads();
   }
+  __syncthreads();   // (the exchange below writes where the last tile was read)
   sum += other_half(sum);
   if (a.parts > 1) {   // a part's sums, joined by diff_join_kernel
     if (!live) return;
@@ -516,7 +530,7 @@ __global__ void __launch_bounds__(256, DT * sizeof(T) <= 256 ? 2 : 1) diff_backw
   typedef Sizes<T, DT> S;
   typedef QSizes<T, DT> Z;
   __shared__ __attribute__((aligned(16))) T lds[4 * S::KC * S::W];   // keys and values, two buffers each
-  constexpr int BUF = S::KC * S::W, G = 2, MAPS = Z::MAPS;
+  constexpr int BUF = S::KC * S::W, G = sizeof(T) == 2 && DT == 64 ? 4 : 2, MAPS = Z::MAPS;
   const int w = work_index(a.units * a.tiles, a.tiles, a.causal);
   if (w >= a.units * a.tiles) return;
   const int unit = w / a.tiles, tile = a.tiles - 1 - w % a.tiles;
@@ -584,19 +598,21 @@ __global__ void __launch_bounds__(256, DT * sizeof(T) <= 256 ? 2 : 1) diff_backw
   // 128 keys 2.8e-3, 700 keys 2.5e-3 as without it), so delta is completed by a pass of its own first.
   LaneAt at = O::template lane_at<S::W>(lane);
   const bool two = last <= EXACT_KEYS;
-  Stage<T, DT, true> ks;
-  Stage<T, DT, false> vs;
+  Loader<T, DT, true, 256> ks;
+  Loader<T, DT, false, 256> vs;
   ks.plan(a.dim, [&](int row) { return row * a.k_token; });
   vs.plan(a.dim, [&](int row) { return row * a.v_token; });
-  auto fetch = [&](int j) {
-    if (a.near_k && a.dim == DT && j + S::KC <= s.nk) {
-      ks.load_whole(kp + j * a.k_token, ks.STEP * a.k_token);
-      vs.load_whole(vp + j * a.v_token, vs.STEP * a.v_token);
-    } else {
-      ks.load(s.nk - j, a.dim, [&](int row) { return kp + (j + row) * a.k_token; });
-      vs.load(s.nk - j, a.dim, [&](int row) { return vp + (j + row) * a.v_token; });
-    }
+  const uint32_t to = lds_address(lds) + wave * 1024;
+  auto fetch = [&](int j, int buf) {
+    ks.load(kp + j * a.k_token, (s.nk - 1 - j) * a.k_token + 2 * a.dim, to + buf * (BUF * (int)sizeof(T)));
+    vs.load(vp + j * a.v_token, (s.nk - 1 - j) * a.v_token + 2 * a.dim, to + (2 + buf) * (BUF * (int)sizeof(T)));
   };
+#pragma unroll
+  for (int t = 0; t < 2 * S::KS; t++) arrived(gf[t]);
+#pragma unroll
+  for (int t = 0; t < MAPS * S::KS; t++) arrived(qf[t]);
+#pragma unroll
+  for (int m = 0; m < MAPS; m++) { arrived(lse[m]); arrived(delta[m]); }
   for (int pass = two ? 0 : 1; pass < 2; pass++) {
     if (two && pass == 1) {
 #pragma unroll
@@ -605,59 +621,49 @@ __global__ void __launch_bounds__(256, DT * sizeof(T) <= 256 ? 2 : 1) diff_backw
         rest[m] = 0.f;
       }
     }
-    if (last > 0) fetch(0);
-#pragma unroll
-    for (int t = 0; t < 2 * S::KS; t++) arrived(gf[t]);
-#pragma unroll
-    for (int t = 0; t < MAPS * S::KS; t++) arrived(qf[t]);
-#pragma unroll
-    for (int m = 0; m < MAPS; m++) { arrived(lse[m]); arrived(delta[m]); }
-    if (last > 0) {
-      ks.store(lds);
-      vs.store(lds + 2 * BUF);
-      if (S::KC < last) fetch(S::KC);
-    }
-    __syncthreads();
+    __syncthreads();   // (the first pass may still read what is fetched anew)
+    if (last > 0) fetch(0, 0);
     for (int j0 = 0, buf = 0; j0 < last; j0 += S::KC, buf ^= 1) {
+      wait_step<0>();
+      if (j0 + S::KC < last) fetch(j0 + S::KC, buf ^ 1);
       const T* Ks = lds + buf * BUF;
       const T* Vs = lds + (2 + buf) * BUF;
       if (j0 < reach) {
         at.fresh();
-        v16f dp;
+        v16f sc[MAPS], dp;
         clear(dp);
-        stream<typename O::Frag, 2 * S::KS, G>([&](int x) { return O::template rowwise<S::W>(Vs, 0, 16 * x, at); },
-                                               [&](int x, const typename O::Frag& f) { dp = O::mma(f, gf[x], dp); });
+#pragma unroll
+        for (int m = 0; m < MAPS; m++) clear(sc[m]);
+        const int base = m0 * DT;   // the first map's columns
+        stream<typename O::Frag, (2 + MAPS) * S::KS, G>(
+            [&](int x) { return x < MAPS * S::KS ? O::template rowwise<S::W>(Ks, 0, base + 16 * x, at) : O::template rowwise<S::W>(Vs, 0, 16 * (x - MAPS * S::KS), at); },
+            [&](int x, const typename O::Frag& f) {
+              if (x < MAPS * S::KS) sc[x / S::KS] = O::mma(f, qf[x], sc[x / S::KS]);
+              else dp = O::mma(f, gf[x - MAPS * S::KS], dp);
+            });
+        if (j0 + 32 > least) {
+#pragma unroll
+          for (int v = 0; v < 16; v++)
+            if (j0 + 8 * (v >> 2) + 4 * hh + (v & 3) >= see) {
+#pragma unroll
+              for (int m = 0; m < MAPS; m++) sc[m][v] = -INFINITY;
+            }
+        }
 #pragma unroll
         for (int m = 0; m < MAPS; m++) {
-          const int base = (m0 + m) * DT;   // the map's columns
-          v16f sc;
-          clear(sc);
-          stream<typename O::Frag, S::KS, G>([&](int t) { return O::template rowwise<S::W>(Ks, 0, base + 16 * t, at); },
-                                             [&](int t, const typename O::Frag& f) { sc = O::mma(f, qf[m * S::KS + t], sc); });
-          if (j0 + 32 > least) {
-#pragma unroll
-            for (int v = 0; v < 16; v++)
-              if (j0 + 8 * (v >> 2) + 4 * hh + (v & 3) >= see) sc[v] = -INFINITY;
-          }
 #pragma unroll
           for (int v = 0; v < 16; v++) {
-            sc[v] = exp2_fast(fmaf(sc[v], a.c, -lse[m])) * (dp[v] - delta[m]);
-            rest[m] += sc[v];
+            sc[m][v] = exp2_fast(fmaf(sc[m][v], a.c, -lse[m])) * (dp[v] - delta[m]);
+            rest[m] += sc[m][v];
           }
           if (pass == 1) {
-            const typename O::Frag p[2] = {O::operand(sc, 0), O::operand(sc, 1)};
+            const typename O::Frag p[2] = {O::operand(sc[m], 0), O::operand(sc[m], 1)};
             constexpr int GT = 2 * S::DTT < G ? 2 * S::DTT : G;
-            stream<typename O::Frag, 2 * S::DTT, GT>([&](int x) { return O::template transposed<S::W>(Ks, base + 32 * (x % S::DTT), 16 * (x / S::DTT), at); },
+            stream<typename O::Frag, 2 * S::DTT, GT>([&](int x) { return O::template transposed<S::W>(Ks, base + m * DT + 32 * (x % S::DTT), 16 * (x / S::DTT), at); },
                                                      [&](int x, const typename O::Frag& f) { dq[m][x % S::DTT] = O::mma(f, p[x / S::DTT], dq[m][x % S::DTT]); });
           }
         }
       }
-      if (j0 + S::KC < last) {
-        ks.store(lds + (buf ^ 1) * BUF);
-        vs.store(lds + (2 + (buf ^ 1)) * BUF);
-        if (j0 + 2 * S::KC < last) fetch(j0 + 2 * S::KC);
-      }
-      __syncthreads();
     }
   }
   if (r >= room) return;
@@ -673,22 +679,27 @@ __global__ void __launch_bounds__(256, DT * sizeof(T) <= 256 ? 2 : 1) diff_backw
         if (32 * t + 8 * g < a.dim)
           O::store4(dqp + (m0 + m) * a.dim + 32 * t + 8 * g, f * dq[m][t][4 * g], f * dq[m][t][4 * g + 1], f * dq[m][t][4 * g + 2], f * dq[m][t][4 * g + 3]);
     if (hh == 0) {
-      a.delta[(int64_t)((m0 + m) * a.heads + h) * a.q_rows + row] = live ? delta[m] : 0.f;
-      if (m0 + m == 1 && a.lam_token) a.dlam[row * a.heads + h] = live ? -delta[m] : 0.f;
+      RowValues* v = a.rows + row * a.heads + h;
+      v->lse[m0 + m] = three_parts(live ? -lse[m] / a.c : 0.f);
+      v->delta[m0 + m] = three_parts(live ? delta[m] : 0.f);
+      if (m0 + m == 1) {
+        v->lam = three_parts(live ? lam : 0.f);
+        if (a.lam_token) a.dlam[row * a.heads + h] = live ? -delta[m] : 0.f;
+        else a.second[(int64_t)h * a.q_rows + row] = live ? delta[m] : 0.f;
+      }
     }
   }
 }
 
-// dlambda of a head: minus the sum of delta_2 over the sequences' rows, always in the same order.  One workgroup a head.
-__global__ void __launch_bounds__(1024) diff_lambda_kernel(DiffArgs a) {
-  __shared__ float red[16];
-  const int h = blockIdx.x;
-  const float* d = a.delta + (int64_t)(a.heads + h) * a.q_rows;
+// dlambda of a head: minus the sum of delta_2 over the sequences' rows, always in the same order.  One workgroup a head, beside the workgroups that own keys.
+template <int THREADS> __device__ inline void sum_lambda(const DiffArgs& a, int h) {
+  __shared__ float red[THREADS / 64];
+  const float* d = a.second + (int64_t)h * a.q_rows;
   float t = 0.f;
   if (!a.q_starts) {   // (rows behind a sequence's queries hold zeros)
-    for (int64_t x = threadIdx.x; x < a.q_rows; x += 1024) t += d[x];
+    for (int64_t x = threadIdx.x; x < a.q_rows; x += THREADS) t += d[x];
   } else {
-    for (int b = threadIdx.x >> 6; b < a.batch; b += 16) {
+    for (int b = threadIdx.x >> 6; b < a.batch; b += THREADS / 64) {
       const Seq s = sequence(a, b);
       for (int x = threadIdx.x & 63; x < s.nq; x += 64) t += d[s.q0 + x];
     }
@@ -699,7 +710,7 @@ __global__ void __launch_bounds__(1024) diff_lambda_kernel(DiffArgs a) {
   if (threadIdx.x == 0) {
     float z = 0.f;
 #pragma unroll
-    for (int k = 0; k < 16; k++) z += red[k];
+    for (int k = 0; k < THREADS / 64; k++) z += red[k];
     a.dlam[h] = -z;
   }
 }
@@ -717,10 +728,6 @@ template <typename T, int DT> struct KvSizes {
   static constexpr int BUFFERS = DT * sizeof(T) <= 256 ? 3 : 2;   // of a tile of rows (two, and one more barrier a tile, where three exceed LDS)
   static constexpr int KEYS = 32 * PAIRS, THREADS = 128 * PAIRS;
 };
-__device__ inline uint2 three_parts(float x) {
-  const bf16_t hi = f32_to_bf16(x), mid = f32_to_bf16(x - bf16_to_f32(hi)), lo = f32_to_bf16(x - bf16_to_f32(hi) - bf16_to_f32(mid));
-  return make_uint2((uint32_t)hi | (uint32_t)mid << 16, lo);
-}
 // adds a row's value, held by the row's lane of the lower half, to a tile's rows
 __device__ inline v16f add_rows(uint2 parts, int hh, const v16f& c) {
   const uint4 a = hh ? make_uint4(0, 0, 0, 0) : make_uint4(parts.x, parts.y, 0, 0), one = make_uint4(0x3f803f80u, 0x3f80u, 0, 0);
@@ -732,11 +739,15 @@ __global__ void __launch_bounds__((KvSizes<T, DT>::THREADS), sizeof(T) == 2 && D
   typedef Ops<T> O;
   typedef Sizes<T, DT> S;
   typedef KvSizes<T, DT> Z;
-  constexpr int BUF = S::KC * S::W, G = 2, NB = Z::BUFFERS, FRAG = sizeof(typename O::Frag);
+  constexpr int BUF = S::KC * S::W, G = sizeof(T) == 2 && DT <= 64 ? 4 : 2, NB = Z::BUFFERS, FRAG = sizeof(typename O::Frag);
   __shared__ __attribute__((aligned(16))) T lds[2 * NB * BUF];                         // queries and dO
-  __shared__ __attribute__((aligned(16))) uint2 st[NB][5][S::KC];                      // the rows' values
+  __shared__ __attribute__((aligned(16))) RowValues st[NB][43];                        // the rows' values: 32, and room for the 2048 bytes that two waves write
   __shared__ __attribute__((aligned(16))) char ex[2][Z::PAIRS][6 * 64 * FRAG];         // P_1 - lambda P_2, dS_1, dS_2 of a tile, two operands each
   const int total = a.units * a.tiles * a.parts;
+  if ((int)blockIdx.x >= a.work) {   // the workgroups behind those of the keys
+    sum_lambda<Z::THREADS>(a, (int)blockIdx.x - a.work);
+    return;
+  }
   const int w = work_index(total, a.tiles * a.parts, a.causal);
   if (w >= total) return;
   const int part = w % a.parts, ut = w / a.parts, unit = ut / a.tiles, tile = ut % a.tiles;   // (under a causal mask the first keys are seen by the most rows)
@@ -758,40 +769,27 @@ __global__ void __launch_bounds__((KvSizes<T, DT>::THREADS), sizeof(T) == 2 && D
   const int first = live ? from(j) : 0;
   const int wfirst = wj0 < s.nk ? from(wj0) : R, wlast = from(min(wj0 + 31, s.nk - 1));
   LaneAt at = O::template lane_at<S::W>(lane);
-  Stage<T, DT, true, Z::THREADS> qs;
-  Stage<T, DT, false, Z::THREADS> gs;
-  auto place = [&](int r, int64_t token) { const int x = query_of(a, r); return x * token + (int64_t)(r - x * a.group) * 2 * a.dim; };
-  qs.plan(a.dim, [&](int x) { return place(x, a.q_token); });
-  gs.plan(a.dim, [&](int x) { return place(x, a.o_token); });
-  const bool near_q = a.near_q && qs.STEP % a.group == 0;   // (the rows of a tile and of its steps lie alike)
-  const float inv_c = 1.f / a.c;
-  float sv[5];
-  auto fetch = [&](int r0) {
-    if (near_q && a.dim == DT && r0 + S::KC <= R) {
-      qs.load_whole(qp + place(r0, a.q_token), place(qs.STEP, a.q_token));
-      gs.load_whole(gp + place(r0, a.o_token), place(gs.STEP, a.o_token));
-    } else {
-      qs.load(R - r0, a.dim, [&](int x) { return qp + place(r0 + x, a.q_token); });
-      gs.load(R - r0, a.dim, [&](int x) { return gp + place(r0 + x, a.o_token); });
-    }
-#pragma unroll
-    for (int e = 0; e < 5; e++) sv[e] = 0.f;
-    if ((int)threadIdx.x < min(S::KC, R - r0)) {
-      const int r = r0 + threadIdx.x, i = query_of(a, r), h = hk * a.group + (r - i * a.group);
-      const int64_t row = s.q0 + i, first_map = (int64_t)h * a.q_rows + row, second_map = first_map + (int64_t)a.heads * a.q_rows;
-      sv[0] = a.lse[first_map]; sv[1] = a.lse[second_map]; sv[2] = a.delta[first_map]; sv[3] = a.delta[second_map];
-      sv[4] = a.lam[a.lam_token ? row * a.heads + h : h];
-    }
+  Loader<T, DT, true, Z::THREADS> qs;
+  Loader<T, DT, false, Z::THREADS> gs;
+  // row r0 + x of a tile, from the token of its first row
+  auto plan = [&](int r0) {
+    auto place = [&](int x, int64_t token) { const int i = query_of(a, r0 + x); return (i - query_of(a, r0)) * token + (int64_t)(r0 + x - i * a.group) * 2 * a.dim; };
+    qs.plan(a.dim, [&](int x) { return place(x, a.q_token); });
+    gs.plan(a.dim, [&](int x) { return place(x, a.o_token); });
   };
-  auto put = [&](int buf) {
-    qs.store(lds + buf * BUF);
-    gs.store(lds + (NB + buf) * BUF);
-    if ((int)threadIdx.x < S::KC) {
-      st[buf][0][threadIdx.x] = three_parts(-sv[0] * inv_c);
-      st[buf][1][threadIdx.x] = three_parts(-sv[1] * inv_c);
-      st[buf][2][threadIdx.x] = three_parts(sv[2]);
-      st[buf][3][threadIdx.x] = three_parts(sv[3]);
-      st[buf][4][threadIdx.x] = three_parts(sv[4]);
+  plan(0);
+  const bool alike = 32 % a.group == 0;   // the rows of all tiles lie alike
+  const int piece = wave * 64 + lane, value_row = piece / 3;
+  const uint32_t to = lds_address(lds) + wave * 1024;
+  auto fetch = [&](int t, int buf) {
+    const int r0 = t * S::KC, i0 = query_of(a, r0);
+    if (!alike) plan(r0);
+    qs.load(qp + i0 * a.q_token, (s.nq - 1 - i0) * a.q_token + a.group * 2 * a.dim, to + buf * (BUF * (int)sizeof(T)));
+    gs.load(gp + i0 * a.o_token, (s.nq - 1 - i0) * a.o_token + a.group * 2 * a.dim, to + (NB + buf) * (BUF * (int)sizeof(T)));
+    if (wave < 2) {   // 96 pieces of row values
+      const int r = r0 + value_row, i = query_of(a, r);
+      const rsrc_words_t w = buffer_of(a.rows + (s.q0 + i0) * a.heads + hk * a.group, 0xfffffff0);
+      load_lds16(w, (uint32_t)__builtin_amdgcn_readfirstlane((int)lds_address(st[buf]) + wave * 1024), value_row < 32 && r < R ? (uint32_t)(((i - i0) * a.heads + r - i * a.group) * 48 + piece % 3 * 16) : ~0u);
     }
   };
   int begin = j0 < s.nk ? from(j0) / S::KC : (R + S::KC - 1) / S::KC, end = (R + S::KC - 1) / S::KC;   // tiles of rows
@@ -801,24 +799,19 @@ __global__ void __launch_bounds__((KvSizes<T, DT>::THREADS), sizeof(T) == 2 && D
     end = min(end, begin + per);
   }
   auto seen = [&](int t) { return t * S::KC + 32 > wfirst; };   // some key of the pair is seen by the tile's rows
-  // Tile t is worked on from buffer t - begin mod NB by the first wave of a pair while the second one has the tile before it; the tile after it
-  // is written, and the one after that is on its way into registers.
+  // Tile t is worked on from buffer t - begin mod NB by the first wave of a pair while the second one has the tile before it and the tile after it
+  // is on its way.
   auto next = [](int x) { return x == NB - 1 ? 0 : x + 1; };
-  if (begin < end) fetch(begin * S::KC);
-  auto stage_first = [&]() {
-    if (begin < end) {
-      put(0);
-      if (begin + 1 < end) fetch((begin + 1) * S::KC);
-    }
-    __syncthreads();
+  if (begin < end) fetch(begin, 0);
+  auto stage = [&](int t, int buf) {
+    wait_step<0>();   // tile t has arrived, the pairs are done with tile t - 2, and what the first waves left of tile t - 1 is there
+    if (NB > 2 && t + 1 < end) fetch(t + 1, next(buf));
   };
-  auto stage_next = [&](int t, int buf) {
-    if (NB == 2) __syncthreads();   // (the next tile goes where the one before was read)
-    if (t + 1 < end) {
-      put(next(buf));
-      if (t + 2 < end) fetch((t + 2) * S::KC);
+  auto stage_behind = [&](int t, int buf) {
+    if (NB == 2) {   // the next tile goes where the one before was read
+      wait_step<0>();
+      if (t + 1 < end) fetch(t + 1, next(buf));
     }
-    __syncthreads();
   };
   if (producer) {
     RowFrags<T, DT> kf, vf;
@@ -826,32 +819,37 @@ __global__ void __launch_bounds__((KvSizes<T, DT>::THREADS), sizeof(T) == 2 && D
     own_row<T, DT, false>(vf, rows_of(a, static_cast<const T*>(a.v), b, s.k0, a.v_token, a.v_batch) + v_at, live, a.dim, hh);
 #pragma unroll
     for (int t = 0; t < 2 * S::KS; t++) { arrived(kf[t]); arrived(vf[t]); }
-    stage_first();
     for (int t = begin, buf = 0; t <= end; t++, buf = next(buf)) {
+      stage(t, buf);
       if (t < end && seen(t)) {
         const T* Qs = lds + buf * BUF;
         const T* Gs = lds + (NB + buf) * BUF;
         typename O::Frag* x = reinterpret_cast<typename O::Frag*>(ex[(t - begin) & 1][pair]) + lane;
         at.fresh();
-        v16f dp, wt, sc;
+        v16f dp, wt, scores[2];
         clear(dp);
-        stream<typename O::Frag, 2 * S::KS, G>([&](int e) { return O::template rowwise<S::W>(Gs, 0, 16 * e, at); },
-                                               [&](int e, const typename O::Frag& f) { dp = O::mma(f, vf[e], dp); });
 #pragma unroll
         for (int m = 0; m < 2; m++) {
-          clear(sc);
-          sc = add_rows(st[buf][m][c], hh, sc);
-          stream<typename O::Frag, S::KS, G>([&](int e) { return O::template rowwise<S::W>(Qs, 0, m * DT + 16 * e, at); },
-                                             [&](int e, const typename O::Frag& f) { sc = O::mma(f, kf[m * S::KS + e], sc); });
-          if (t * S::KC < wlast) {
+          clear(scores[m]);
+          scores[m] = add_rows(st[buf][c].lse[m], hh, scores[m]);
+        }
+        stream<typename O::Frag, 4 * S::KS, G>([&](int e) { return O::template rowwise<S::W>(e < 2 * S::KS ? Qs : Gs, 0, 16 * (e % (2 * S::KS)), at); },
+                                               [&](int e, const typename O::Frag& f) {
+                                                 if (e < 2 * S::KS) scores[e / S::KS] = O::mma(f, kf[e], scores[e / S::KS]);
+                                                 else dp = O::mma(f, vf[e - 2 * S::KS], dp);
+                                               });
+        if (t * S::KC < wlast) {
 #pragma unroll
-            for (int v = 0; v < 16; v++)
-              if (t * S::KC + 8 * (v >> 2) + 4 * hh + (v & 3) < first) sc[v] = -INFINITY;
-          }
+          for (int v = 0; v < 16; v++)
+            if (t * S::KC + 8 * (v >> 2) + 4 * hh + (v & 3) < first) { scores[0][v] = -INFINITY; scores[1][v] = -INFINITY; }
+        }
+#pragma unroll
+        for (int m = 0; m < 2; m++) {
+          v16f& sc = scores[m];
           // (delta is subtracted from the finished dP: a softmax over one key has dP = delta to the last bit, and a gradient of zero)
           v16f delta;
           clear(delta);
-          delta = add_rows(st[buf][2 + m][c], hh, delta);
+          delta = add_rows(st[buf][c].delta[m], hh, delta);
           if (m == 0) {
 #pragma unroll
             for (int v = 0; v < 16; v++) {
@@ -861,7 +859,7 @@ __global__ void __launch_bounds__((KvSizes<T, DT>::THREADS), sizeof(T) == 2 && D
           } else {
             v16f lam;
             clear(lam);
-            lam = add_rows(st[buf][4][c], hh, lam);
+            lam = add_rows(st[buf][c].lam, hh, lam);
 #pragma unroll
             for (int v = 0; v < 16; v++) {
               const float p = lam[v] * exp2_fast(a.c * sc[v]);
@@ -875,15 +873,15 @@ __global__ void __launch_bounds__((KvSizes<T, DT>::THREADS), sizeof(T) == 2 && D
 #pragma unroll
         for (int u = 0; u < 2; u++) x[u * 64] = O::operand(wt, u);
       }
-      stage_next(t, buf);
+      stage_behind(t, buf);
     }
     return;
   }
   v16f dv[S::VT], dk[2][S::DTT];
 #pragma unroll
   for (int t = 0; t < S::VT; t++) { clear(dv[t]); clear(dk[t / S::DTT][t % S::DTT]); }
-  stage_first();
   for (int t = begin, buf = 0, before = NB - 1; t <= end; t++, before = buf, buf = next(buf)) {
+    stage(t, buf);
     if (t > begin && seen(t - 1)) {
       const T* Qs = lds + before * BUF;
       const T* Gs = lds + (NB + before) * BUF;
@@ -901,7 +899,7 @@ __global__ void __launch_bounds__((KvSizes<T, DT>::THREADS), sizeof(T) == 2 && D
             else dk[m][z % S::DTT] = O::mma(f, p[2 + 2 * m + u], dk[m][z % S::DTT]);
           });
     }
-    stage_next(t, buf);
+    stage_behind(t, buf);
   }
   if (a.parts > 1) {   // a part's sums, joined by diff_join_kv_kernel
     if (!live) return;
@@ -990,6 +988,8 @@ static int check(const char* what, const cd_diff_attn* d) {
   for (int t = 0; t < 4; t++) {
     const int64_t heads = t == 1 || t == 2 ? d->kv_heads : d->heads;
     CD_REQUIRE(tokens[t] >= heads * w && tokens[t] % ve == 0, "%s: token stride %lld of %s", what, (long long)tokens[t], t == 0 ? "q" : t == 1 ? "k" : t == 2 ? "v" : "out");
+    if (tokens[t] * elem_of(d) > 1 << 27)   // (32 rows of a tile are addressed with 32 bits)
+      return set_error(CD_ERR_UNSUPPORTED, "%s: token stride %lld is above 2^27 bytes", what, (long long)tokens[t]);
     CD_REQUIRE(batches[t] >= 0 && batches[t] % ve == 0, "%s: batch stride %lld of %s", what, (long long)batches[t], t == 0 ? "q" : t == 1 ? "k" : t == 2 ? "v" : "out");
   }
   return CD_OK;
@@ -1024,10 +1024,6 @@ static DiffArgs args_of(const cd_diff_attn* d) {
   a.batch = d->batch; a.tq = d->tq; a.tk = d->tk; a.heads = d->heads; a.kv_heads = d->kv_heads; a.group = d->heads / d->kv_heads; a.dim = d->head_dim;
   a.causal = d->causal != 0; a.lam_token = d->lambda_kind == CD_LAMBDA_TOKEN; a.parts = 1;
   a.units = d->batch * d->kv_heads;
-  // tiles of 32 rows whose offsets fit 32 bits
-  const int64_t far = (1LL << 32) / (32 * elem_of(d)) - 1;
-  a.near_k = d->k_token < far && d->v_token < far;
-  a.near_q = d->q_token < far && d->o_token < far;
   a.group_inv = a.group > 1 ? (uint32_t)((1ull << 32) / a.group) + 1 : 0;
   a.scale = d->scale > 0.f ? d->scale : 1.f / sqrtf((float)d->head_dim);
   a.c = a.scale * 1.44269504088896340736f;
@@ -1059,6 +1055,17 @@ static int kv_parts_of(const cd_diff_attn* d) {
   return p < 2 ? 1 : (int)p;
 }
 
+// Workspace of the backward pass: what the pass over the queries leaves of every row, delta_2 once more where it is summed, and the parts' sums.
+struct Layout { size_t second, sums, bytes; };
+static Layout layout_of(const cd_diff_attn* d) {
+  const size_t rows = (size_t)d->heads * rows_q(d), parts = (size_t)kv_parts_of(d);
+  Layout l;
+  l.second = rows * sizeof(RowValues);
+  l.sums = l.second + (d->lambda_kind == CD_LAMBDA_HEAD ? align_up(rows * 4, 16) : 0);
+  l.bytes = l.sums + (parts > 1 ? parts * d->batch * d->kv_heads * d->tk * 4 * d->head_dim * 4 : 0);
+  return l;
+}
+
 static double pairs(const cd_diff_attn* d) { return (double)d->batch * d->heads * d->tq * d->tk * (d->causal ? 0.5 : 1.0); }
 
 }  // namespace
@@ -1072,10 +1079,8 @@ extern "C" int codistill_diff_attention_workspace_bytes(const cd_diff_attn* desc
   const int parts = parts_of(desc);
   size_t n = parts > 1 ? (size_t)parts * desc->batch * desc->kv_heads * desc->tq * (desc->heads / desc->kv_heads) * 2 * (2 * desc->head_dim + 2) * 4 : 0;
   if (backward) {
-    const int kv_parts = kv_parts_of(desc);
-    const size_t deltas = align_up((size_t)2 * desc->heads * rows_q(desc) * 4, 16);
-    const size_t sums = kv_parts > 1 ? (size_t)kv_parts * desc->batch * desc->kv_heads * desc->tk * 4 * desc->head_dim * 4 : 0;
-    n = n > deltas + sums ? n : deltas + sums;
+    const size_t back = layout_of(desc).bytes;
+    n = n > back ? n : back;
   }
   *bytes = align_up(n, 16);
   return CD_OK;
@@ -1130,7 +1135,9 @@ extern "C" int codistill_diff_attention_backward(const cd_diff_attn* desc, const
   DiffArgs a = args_of(desc);
   a.q = q; a.k = k; a.v = v; a.lam = lambda; a.out = const_cast<void*>(out); a.o2 = const_cast<void*>(o_second); a.lse = const_cast<float*>(lse);
   a.dout = dout; a.dq = dq; a.dk = dk; a.dv = dv; a.dlam = dlambda;
-  a.delta = static_cast<float*>(workspace);
+  const Layout lay = layout_of(desc);
+  a.rows = static_cast<RowValues*>(workspace);
+  a.second = reinterpret_cast<float*>(static_cast<char*>(workspace) + lay.second);
   hipStream_t s = static_cast<hipStream_t>(stream);
   const double e = elem_of(desc), qe = 4.0 * a.q_rows * a.heads * 2 * a.dim, ke = 4.0 * a.k_rows * a.kv_heads * 2 * a.dim;
   ProfScope prof(CD_K_ATTN, s, 20.0 * a.dim * pairs(desc), e * (qe + ke));
@@ -1139,15 +1146,17 @@ extern "C" int codistill_diff_attention_backward(const cd_diff_attn* desc, const
       a.tiles = (int)cdiv((int64_t)a.tq * a.group, QSizes<typename decltype(x)::T, decltype(x)::DT>::ROWS);
       hipLaunchKernelGGL((diff_backward_q_kernel<typename decltype(x)::T, decltype(x)::DT>), dim3(work_blocks((int64_t)a.units * a.tiles)), dim3(256), 0, s, a);
     });
-  if (!a.lam_token) hipLaunchKernelGGL(diff_lambda_kernel, dim3((unsigned)a.heads), dim3(1024), 0, s, a);
-  if (a.tk > 0) {
-    a.parts = kv_parts_of(desc);
-    a.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + align_up((size_t)2 * a.heads * a.q_rows * 4, 16));
+  a.parts = kv_parts_of(desc);
+  a.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + lay.sums);
+  const int heads = a.lam_token ? 0 : a.heads;   // workgroups that add up a head's dlambda
+  if (a.tk > 0 || heads)
     dispatch(desc, [&](auto x) {
       typedef KvSizes<typename decltype(x)::T, decltype(x)::DT> Z;
       a.tiles = (int)cdiv(a.tk, Z::KEYS);
-      hipLaunchKernelGGL((diff_backward_kv_kernel<typename decltype(x)::T, decltype(x)::DT>), dim3(work_blocks((int64_t)a.units * a.tiles * a.parts)), dim3(Z::THREADS), 0, s, a);
+      a.work = (int)work_blocks((int64_t)a.units * a.tiles * a.parts);
+      hipLaunchKernelGGL((diff_backward_kv_kernel<typename decltype(x)::T, decltype(x)::DT>), dim3((unsigned)(a.work + heads)), dim3(Z::THREADS), 0, s, a);
     });
+  if (a.tk > 0) {
     if (a.parts > 1) {
       const dim3 grid((unsigned)cdiv((int64_t)a.units * a.tk * a.dim, 256));
       if (desc->dtype == CD_BF16) hipLaunchKernelGGL((diff_join_kv_kernel<bf16_t>), grid, dim3(256), 0, s, a);
