@@ -38,10 +38,9 @@ typedef float v16f __attribute__((ext_vector_type(16)));
 
 // What the pass that owns keys needs of a row, in the form it uses it: the pass that owns queries leaves it in the workspace.
 struct RowValues {
-  uint2 lse[2];    // minus the log-sums over c, each fp32 value in three bf16 parts (all of its bits)
-  uint2 delta[2];
-  uint2 lam;
-  uint2 unused;
+  uint2 lse[2];    // minus the log-sums over c, each fp32 value in three bf16 parts (all of its bits); the second one with the logarithm of |lambda|
+  uint2 delta[2];  // minus the deltas
+  uint32_t lam_negative, unused[3];
 };
 static_assert(sizeof(RowValues) == 48, "three pieces of 16 bytes");
 __device__ inline uint2 three_parts(float x) {
@@ -680,10 +679,12 @@ __global__ void __launch_bounds__(256, DT * sizeof(T) <= 256 ? 2 : 1) diff_backw
           O::store4(dqp + (m0 + m) * a.dim + 32 * t + 8 * g, f * dq[m][t][4 * g], f * dq[m][t][4 * g + 1], f * dq[m][t][4 * g + 2], f * dq[m][t][4 * g + 3]);
     if (hh == 0) {
       RowValues* v = a.rows + row * a.heads + h;
-      v->lse[m0 + m] = three_parts(live ? -lse[m] / a.c : 0.f);
-      v->delta[m0 + m] = three_parts(live ? delta[m] : 0.f);
+      // (a lambda of zero: far below any score, yet finite, as its parts have to be)
+      const float weight = m0 + m == 0 ? 0.f : lam == 0.f ? -1e30f : __log2f(fabsf(lam));
+      v->lse[m0 + m] = three_parts(live ? (weight - lse[m]) / a.c : 0.f);
+      v->delta[m0 + m] = three_parts(live ? -delta[m] : 0.f);
       if (m0 + m == 1) {
-        v->lam = three_parts(live ? lam : 0.f);
+        v->lam_negative = live && lam < 0.f;
         if (a.lam_token) a.dlam[row * a.heads + h] = live ? -delta[m] : 0.f;
         else a.second[(int64_t)h * a.q_rows + row] = live ? delta[m] : 0.f;
       }
@@ -781,8 +782,8 @@ __global__ void __launch_bounds__((KvSizes<T, DT>::THREADS), sizeof(T) == 2 && D
   const bool alike = 32 % a.group == 0;   // the rows of all tiles lie alike
   const int piece = wave * 64 + lane, value_row = piece / 3;
   const uint32_t to = lds_address(lds) + wave * 1024;
-  auto fetch = [&](int t, int buf) {
-    const int r0 = t * S::KC, i0 = query_of(a, r0);
+  auto fetch = [&](int r0, int buf) {
+    const int i0 = query_of(a, r0);
     if (!alike) plan(r0);
     qs.load(qp + i0 * a.q_token, (s.nq - 1 - i0) * a.q_token + a.group * 2 * a.dim, to + buf * (BUF * (int)sizeof(T)));
     gs.load(gp + i0 * a.o_token, (s.nq - 1 - i0) * a.o_token + a.group * 2 * a.dim, to + (NB + buf) * (BUF * (int)sizeof(T)));
@@ -798,36 +799,42 @@ __global__ void __launch_bounds__((KvSizes<T, DT>::THREADS), sizeof(T) == 2 && D
     begin += part * per;
     end = min(end, begin + per);
   }
-  auto seen = [&](int t) { return t * S::KC + 32 > wfirst; };   // some key of the pair is seen by the tile's rows
-  // Tile t is worked on from buffer t - begin mod NB by the first wave of a pair while the second one has the tile before it and the tile after it
+  // The last tile first: under a causal mask all workgroups of a unit reach the last rows, few the first ones, and those that begin together find
+  // each other's tiles in the cache.
+  const int tiles = max(end - begin, 0);
+  auto row_of = [&](int t) { return (end - 1 - t) * S::KC; };
+  auto seen = [&](int t) { return row_of(t) + 32 > wfirst; };   // some key of the pair is seen by the tile's rows
+  // Tile t is worked on from buffer t mod NB by the first wave of a pair while the second one has the tile before it and the tile after it
   // is on its way.
   auto next = [](int x) { return x == NB - 1 ? 0 : x + 1; };
-  if (begin < end) fetch(begin, 0);
+  if (tiles > 0) fetch(row_of(0), 0);
   auto stage = [&](int t, int buf) {
     wait_step<0>();   // tile t has arrived, the pairs are done with tile t - 2, and what the first waves left of tile t - 1 is there
-    if (NB > 2 && t + 1 < end) fetch(t + 1, next(buf));
+    if (NB > 2 && t + 1 < tiles) fetch(row_of(t + 1), next(buf));
   };
   auto stage_behind = [&](int t, int buf) {
     if (NB == 2) {   // the next tile goes where the one before was read
       wait_step<0>();
-      if (t + 1 < end) fetch(t + 1, next(buf));
+      if (t + 1 < tiles) fetch(row_of(t + 1), next(buf));
     }
   };
   if (producer) {
+    __builtin_amdgcn_s_setprio(1);   // (the longer half of a pair)
     RowFrags<T, DT> kf, vf;
     own_row<T, DT, true>(kf, rows_of(a, static_cast<const T*>(a.k), b, s.k0, a.k_token, a.k_batch) + k_at, live, a.dim, hh);
     own_row<T, DT, false>(vf, rows_of(a, static_cast<const T*>(a.v), b, s.k0, a.v_token, a.v_batch) + v_at, live, a.dim, hh);
 #pragma unroll
     for (int t = 0; t < 2 * S::KS; t++) { arrived(kf[t]); arrived(vf[t]); }
-    for (int t = begin, buf = 0; t <= end; t++, buf = next(buf)) {
+    for (int t = 0, buf = 0; t <= tiles; t++, buf = next(buf)) {
       stage(t, buf);
-      if (t < end && seen(t)) {
+      if (t < tiles && seen(t)) {
         const T* Qs = lds + buf * BUF;
         const T* Gs = lds + (NB + buf) * BUF;
-        typename O::Frag* x = reinterpret_cast<typename O::Frag*>(ex[(t - begin) & 1][pair]) + lane;
+        typename O::Frag* x = reinterpret_cast<typename O::Frag*>(ex[t & 1][pair]) + lane;
         at.fresh();
         v16f dp, wt, scores[2];
         clear(dp);
+        const uint32_t negative = (uint32_t)__ballot(st[buf][c].lam_negative != 0);   // the rows whose lambda is below zero
 #pragma unroll
         for (int m = 0; m < 2; m++) {
           clear(scores[m]);
@@ -838,33 +845,35 @@ __global__ void __launch_bounds__((KvSizes<T, DT>::THREADS), sizeof(T) == 2 && D
                                                  if (e < 2 * S::KS) scores[e / S::KS] = O::mma(f, kf[e], scores[e / S::KS]);
                                                  else dp = O::mma(f, vf[e - 2 * S::KS], dp);
                                                });
-        if (t * S::KC < wlast) {
+        const int r0 = row_of(t);
+        if (r0 < wlast) {
 #pragma unroll
           for (int v = 0; v < 16; v++)
-            if (t * S::KC + 8 * (v >> 2) + 4 * hh + (v & 3) < first) { scores[0][v] = -INFINITY; scores[1][v] = -INFINITY; }
+            if (r0 + 8 * (v >> 2) + 4 * hh + (v & 3) < first) { scores[0][v] = -INFINITY; scores[1][v] = -INFINITY; }
         }
 #pragma unroll
         for (int m = 0; m < 2; m++) {
           v16f& sc = scores[m];
           // (delta is subtracted from the finished dP: a softmax over one key has dP = delta to the last bit, and a gradient of zero)
-          v16f delta;
-          clear(delta);
-          delta = add_rows(st[buf][c].delta[m], hh, delta);
+          const v16f ds = add_rows(st[buf][c].delta[m], hh, dp);
           if (m == 0) {
 #pragma unroll
             for (int v = 0; v < 16; v++) {
               wt[v] = exp2_fast(a.c * sc[v]);
-              sc[v] = wt[v] * (dp[v] - delta[v]);
+              sc[v] = wt[v] * ds[v];
             }
           } else {
-            v16f lam;
-            clear(lam);
-            lam = add_rows(st[buf][c].lam, hh, lam);
+#pragma unroll
+            for (int v = 0; v < 16; v++) sc[v] = exp2_fast(a.c * sc[v]);   // |lambda| P_2
+            if (negative) {
+#pragma unroll
+              for (int v = 0; v < 16; v++)
+                if (negative >> (8 * (v >> 2) + 4 * hh + (v & 3)) & 1) sc[v] = -sc[v];
+            }
 #pragma unroll
             for (int v = 0; v < 16; v++) {
-              const float p = lam[v] * exp2_fast(a.c * sc[v]);
-              wt[v] -= p;
-              sc[v] = p * (delta[v] - dp[v]);
+              wt[v] -= sc[v];
+              sc[v] = -sc[v] * ds[v];
             }
           }
 #pragma unroll
@@ -880,12 +889,12 @@ __global__ void __launch_bounds__((KvSizes<T, DT>::THREADS), sizeof(T) == 2 && D
   v16f dv[S::VT], dk[2][S::DTT];
 #pragma unroll
   for (int t = 0; t < S::VT; t++) { clear(dv[t]); clear(dk[t / S::DTT][t % S::DTT]); }
-  for (int t = begin, buf = 0, before = NB - 1; t <= end; t++, before = buf, buf = next(buf)) {
+  for (int t = 0, buf = 0, before = NB - 1; t <= tiles; t++, before = buf, buf = next(buf)) {
     stage(t, buf);
-    if (t > begin && seen(t - 1)) {
+    if (t > 0 && seen(t - 1)) {
       const T* Qs = lds + before * BUF;
       const T* Gs = lds + (NB + before) * BUF;
-      const typename O::Frag* x = reinterpret_cast<const typename O::Frag*>(ex[(t - 1 - begin) & 1][pair]) + lane;
+      const typename O::Frag* x = reinterpret_cast<const typename O::Frag*>(ex[(t - 1) & 1][pair]) + lane;
       at.fresh();
       typename O::Frag p[6];
 #pragma unroll
