@@ -340,8 +340,8 @@ __global__ void __launch_bounds__(F_THREADS, sizeof(T) == 4 ? (DT == 128 ? 1 : 2
   // keys this row sees, and those that the rows of the wave and of the workgroup reach
   const int off = s.nk - s.nq;
   auto limit = [&](int row) { return a.causal ? min(s.nk, query_of(a, row) + off + 1) : s.nk; };
-  // (the keys of a part: whole tiles of 32)
-  const int per = a.parts == 1 ? s.nk : (((s.nk + 31) / 32 + a.parts - 1) / a.parts) * 32;
+  // (the keys of a part: whole tiles of 32; the same number in long and short sequences, which then have fewer parts)
+  const int per = a.parts == 1 ? s.nk : (((a.tk + 31) / 32 + a.parts - 1) / a.parts) * 32;
   const int begin = part * per, last = r0 < R ? min(limit(min(r0 + F_ROWS, R) - 1), begin + per) : 0;
   const int see = min(live ? limit(r) : s.nk, last), least = min(limit(wr0), last), reach = wr0 < R ? min(limit(min(wr0 + 31, R - 1)), last) : 0;
   v16f o[S::VT];
@@ -1018,7 +1018,7 @@ static int check_apart(const char* what, const cd_diff_attn* d, bool out_only) {
 // Parts of the keys that get a workgroup of their own: few rows against many keys would leave most of the chip without work.
 static int parts_of(const cd_diff_attn* d) {
   const int64_t groups = (int64_t)d->batch * d->kv_heads * cdiv((int64_t)d->tq * (d->heads / d->kv_heads), F_ROWS);
-  int64_t p = groups ? 768 / groups : 1;
+  int64_t p = groups ? 768 / groups : 1;   // (three workgroups a compute unit: all parts at once)
   if (p > cdiv(d->tk, 128)) p = cdiv(d->tk, 128);
   if (p > 64) p = 64;
   return p < 2 || groups > 128 ? 1 : (int)p;

@@ -13,7 +13,7 @@ namespace cd {
 namespace {
 
 constexpr int HN_MAX_WIDTH = 1024;
-constexpr int HN_BLOCKS = 1024;   // most workgroups of the backward pass: rows of partial sums of dg
+constexpr int HN_BLOCKS = 512;   // most workgroups of the backward pass: rows of partial sums of dg
 
 struct HeadNormArgs {
   const void* x; const void* gain; const void* dy; void* y; void* dx;
@@ -154,19 +154,23 @@ __global__ void __launch_bounds__(256) head_norm_backward_kernel(HeadNormArgs a)
   }
 }
 
-// dg = post * sum of the workgroups' rows: a workgroup takes 16 channels, 16 threads each
+// dg = post * sum of the workgroups' rows: a workgroup takes 8 channels, 32 threads each, 8 loads of a thread in flight
 __global__ void __launch_bounds__(256) head_norm_gain_kernel(const float* __restrict__ partial, float* __restrict__ dgain, int rows, int width, float post) {
-  __shared__ float red[16][17];
-  const int col = blockIdx.x * 16 + (threadIdx.x & 15), part = threadIdx.x >> 4;
-  float t = 0.f;
+  __shared__ float red[32][9];
+  const int at = threadIdx.x & 7, col = blockIdx.x * 8 + at, part = threadIdx.x >> 3;
+  float t[8] = {};
   if (col < width)
-    for (int r = part; r < rows; r += 16) t += partial[(int64_t)r * width + col];
-  red[part][threadIdx.x & 15] = t;
+    for (int r = part; r < rows; r += 256) {
+#pragma unroll
+      for (int e = 0; e < 8; e++)
+        if (r + 32 * e < rows) t[e] += partial[(int64_t)(r + 32 * e) * width + col];
+    }
+  red[part][at] = ((t[0] + t[1]) + (t[2] + t[3])) + ((t[4] + t[5]) + (t[6] + t[7]));
   __syncthreads();
   if (part == 0 && col < width) {
     float s = 0.f;
 #pragma unroll
-    for (int q = 0; q < 16; q++) s += red[q][threadIdx.x];
+    for (int q = 0; q < 32; q++) s += red[q][at];
     dgain[col] = post * s;
   }
 }
@@ -269,6 +273,6 @@ extern "C" int codistill_head_norm_backward(int dtype, const void* x, int64_t x_
   const dim3 grid((unsigned)workgroups(a.groups, sh.lanes, HN_BLOCKS));
   if (dtype == CD_BF16) { if (sh.vector) Kernels<bf16_t, 8>::backward(sh.nv, grid, s, a); else Kernels<bf16_t, 1>::backward(sh.nv, grid, s, a); }
   else { if (sh.vector) Kernels<float, 4>::backward(sh.nv, grid, s, a); else Kernels<float, 1>::backward(sh.nv, grid, s, a); }
-  hipLaunchKernelGGL(head_norm_gain_kernel, dim3((unsigned)cdiv(width, 16)), dim3(256), 0, s, a.partial, dgain, (int)grid.x, (int)width, post);
+  hipLaunchKernelGGL(head_norm_gain_kernel, dim3((unsigned)cdiv(width, 8)), dim3(256), 0, s, a.partial, dgain, (int)grid.x, (int)width, post);
   return check_launch("head_norm");
 }
