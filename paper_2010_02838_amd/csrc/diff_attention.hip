@@ -512,6 +512,20 @@ __global__ void __launch_bounds__(256) diff_join_kernel(DiffArgs a) {
   }
 }
 
+// What the pass over the queries leaves of a row's map m for the pass over the keys, and dlambda.
+__device__ inline void leave_row(const DiffArgs& a, int64_t row, int h, int m, bool live, float lse, float delta, float lam) {
+  RowValues* v = a.rows + row * a.heads + h;
+  // (a lambda of zero: far below any score, yet finite, as its parts have to be)
+  const float weight = m == 0 ? 0.f : lam == 0.f ? -1e30f : __log2f(fabsf(lam));
+  v->lse[m] = three_parts(live ? (weight - lse) / a.c : 0.f);
+  v->delta[m] = three_parts(live ? -delta : 0.f);
+  if (m == 1) {
+    v->lam_negative = live && lam < 0.f;
+    if (a.lam_token) a.dlam[row * a.heads + h] = live ? -delta : 0.f;
+    else a.second[(int64_t)h * a.q_rows + row] = live ? delta : 0.f;
+  }
+}
+
 // ---- backward: queries ------------------------------------------------------------------------------------------------------------
 // dq, delta and dlambda.  delta first comes from the kept outputs, delta_2 = dO . (P_2 v), delta_1 = dO . out + lambda delta_2, which were rounded;
 // the pass over the keys gives what is missing, rowsum(P_m (dP - delta_m)) in fp32, so that dlambda and the deltas that the other kernel
@@ -530,9 +544,10 @@ __global__ void __launch_bounds__(256, DT * sizeof(T) <= 256 ? 2 : 1) diff_backw
   typedef QSizes<T, DT> Z;
   __shared__ __attribute__((aligned(16))) T lds[4 * S::KC * S::W];   // keys and values, two buffers each
   constexpr int BUF = S::KC * S::W, G = sizeof(T) == 2 && DT == 64 ? 4 : 2, MAPS = Z::MAPS;
-  const int w = work_index(a.units * a.tiles, a.tiles, a.causal);
-  if (w >= a.units * a.tiles) return;
-  const int unit = w / a.tiles, tile = a.tiles - 1 - w % a.tiles;
+  const int total = a.units * a.tiles * a.parts;
+  const int w = work_index(total, a.tiles * a.parts, a.causal);
+  if (w >= total) return;
+  const int part = w % a.parts, ut = w / a.parts, unit = ut / a.tiles, tile = a.tiles - 1 - ut % a.tiles;
   const int b = unit / a.kv_heads, hk = unit % a.kv_heads;
   const Seq s = sequence(a, b);
   const int R = s.nq * a.group, r0 = tile * Z::ROWS, room = a.q_starts ? R : a.tq * a.group;
@@ -587,7 +602,13 @@ __global__ void __launch_bounds__(256, DT * sizeof(T) <= 256 ? 2 : 1) diff_backw
   auto limit = [&](int x) { return a.causal ? min(s.nk, query_of(a, x) + off + 1) : s.nk; };
   const int see = live ? limit(r) : s.nk;
   const int least = limit(wr0), reach = wr0 < R ? limit(min(wr0 + 31, R - 1)) : 0;
-  const int last = r0 < R ? limit(min(r0 + Z::ROWS, R) - 1) : 0;
+  int begin = 0, last = r0 < R ? limit(min(r0 + Z::ROWS, R) - 1) : 0;
+  const bool two = last <= EXACT_KEYS;
+  if (a.parts > 1) {   // (few keys are one part's, so that the two passes below see all of them)
+    const int per = two ? EXACT_KEYS : (((a.tk + 31) / 32 + a.parts - 1) / a.parts) * 32;
+    begin = part * per;
+    last = min(last, begin + per);
+  }
   v16f dq[MAPS][S::DTT];
 #pragma unroll
   for (int m = 0; m < MAPS; m++)
@@ -596,7 +617,6 @@ __global__ void __launch_bounds__(256, DT * sizeof(T) <= 256 ? 2 : 1) diff_backw
   // Rows with few keys: a rounding of the kept outputs is as large as their small dS (two keys: dq off by 5e-3 where its own rounding is 1.7e-3,
   // 128 keys 2.8e-3, 700 keys 2.5e-3 as without it), so delta is completed by a pass of its own first.
   LaneAt at = O::template lane_at<S::W>(lane);
-  const bool two = last <= EXACT_KEYS;
   Loader<T, DT, true, 256> ks;
   Loader<T, DT, false, 256> vs;
   ks.plan(a.dim, [&](int row) { return row * a.k_token; });
@@ -621,8 +641,8 @@ __global__ void __launch_bounds__(256, DT * sizeof(T) <= 256 ? 2 : 1) diff_backw
       }
     }
     __syncthreads();   // (the first pass may still read what is fetched anew)
-    if (last > 0) fetch(0, 0);
-    for (int j0 = 0, buf = 0; j0 < last; j0 += S::KC, buf ^= 1) {
+    if (begin < last) fetch(begin, 0);
+    for (int j0 = begin, buf = 0; j0 < last; j0 += S::KC, buf ^= 1) {
       wait_step<0>();
       if (j0 + S::KC < last) fetch(j0 + S::KC, buf ^ 1);
       const T* Ks = lds + buf * BUF;
@@ -665,6 +685,23 @@ __global__ void __launch_bounds__(256, DT * sizeof(T) <= 256 ? 2 : 1) diff_backw
       }
     }
   }
+  if (a.parts > 1) {   // a part's sums, joined by diff_join_q_kernel
+    if (!live) return;
+    const int64_t rows = (int64_t)a.tq * a.group, place = ((int64_t)part * a.units + unit) * rows + r;
+#pragma unroll
+    for (int m = 0; m < MAPS; m++) {
+      float* p = a.part + place * 2 * a.dim + (m0 + m) * a.dim + 4 * hh;
+#pragma unroll
+      for (int t = 0; t < S::DTT; t++)
+#pragma unroll
+        for (int g = 0; g < 4; g++)
+          if (32 * t + 8 * g < a.dim)
+            *reinterpret_cast<float4*>(p + 32 * t + 8 * g) = make_float4(dq[m][t][4 * g], dq[m][t][4 * g + 1], dq[m][t][4 * g + 2], dq[m][t][4 * g + 3]);
+      rest[m] += other_half(rest[m]);
+      if (hh == 0) a.part_ml[place * 2 + m0 + m] = rest[m] + (part == 0 ? delta[m] : 0.f);   // (their sum is delta)
+    }
+    return;
+  }
   if (r >= room) return;
   T* dqp = rows_of(a, static_cast<T*>(a.dq), b, s.q0, a.q_token, a.q_batch) + i * a.q_token + (int64_t)h * 2 * a.dim + 4 * hh;
 #pragma unroll
@@ -677,19 +714,34 @@ __global__ void __launch_bounds__(256, DT * sizeof(T) <= 256 ? 2 : 1) diff_backw
       for (int g = 0; g < 4; g++)
         if (32 * t + 8 * g < a.dim)
           O::store4(dqp + (m0 + m) * a.dim + 32 * t + 8 * g, f * dq[m][t][4 * g], f * dq[m][t][4 * g + 1], f * dq[m][t][4 * g + 2], f * dq[m][t][4 * g + 3]);
-    if (hh == 0) {
-      RowValues* v = a.rows + row * a.heads + h;
-      // (a lambda of zero: far below any score, yet finite, as its parts have to be)
-      const float weight = m0 + m == 0 ? 0.f : lam == 0.f ? -1e30f : __log2f(fabsf(lam));
-      v->lse[m0 + m] = three_parts(live ? (weight - lse[m]) / a.c : 0.f);
-      v->delta[m0 + m] = three_parts(live ? -delta[m] : 0.f);
-      if (m0 + m == 1) {
-        v->lam_negative = live && lam < 0.f;
-        if (a.lam_token) a.dlam[row * a.heads + h] = live ? -delta[m] : 0.f;
-        else a.second[(int64_t)h * a.q_rows + row] = live ? delta[m] : 0.f;
-      }
-    }
+    if (hh == 0) leave_row(a, row, h, m0 + m, live, lse[m], delta[m], lam);
   }
+}
+
+// Adds the parts of a row's dq and delta, always in the same order: a thread takes four channels.
+template <typename T>
+__global__ void __launch_bounds__(256) diff_join_q_kernel(DiffArgs a) {
+  const int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x, rows = (int64_t)a.tq * a.group;
+  const int quads = a.dim / 2, col = (int)(x % quads) * 4, unit = (int)(x / quads / rows), r = (int)(x / quads - unit * rows);
+  if (unit >= a.units) return;
+  const int b = unit / a.kv_heads, hk = unit % a.kv_heads;
+  const Seq s = sequence(a, b);
+  const bool live = r < s.nq * a.group;
+  if (!live && a.q_starts) return;
+  const int i = query_of(a, r), h = hk * a.group + (r - i * a.group), m = col / a.dim;
+  const int64_t row = s.q0 + i, step = a.units * rows, at = unit * rows + r;
+  float4 t = make_float4(0.f, 0.f, 0.f, 0.f);
+  float delta = 0.f;
+  if (live)
+    for (int p = 0; p < a.parts; p++) {
+      const float4 y = *reinterpret_cast<const float4*>(a.part + (at + p * step) * 2 * a.dim + col);
+      t.x += y.x; t.y += y.y; t.z += y.z; t.w += y.w;
+      delta += a.part_ml[(at + p * step) * 2 + m];
+    }
+  const float lam = live ? a.lam[a.lam_token ? row * a.heads + h : h] : 0.f, f = m ? -lam * a.scale : a.scale;
+  T* dq = rows_of(a, static_cast<T*>(a.dq), b, s.q0, a.q_token, a.q_batch) + i * a.q_token + (int64_t)h * 2 * a.dim + col;
+  Ops<T>::store4(dq, f * t.x, f * t.y, f * t.z, f * t.w);
+  if (col == m * a.dim) leave_row(a, row, h, m, live, live ? a.lse[(int64_t)(m * a.heads + h) * a.q_rows + row] : 0.f, delta, lam);
 }
 
 // dlambda of a head: minus the sum of delta_2 over the sequences' rows, always in the same order.  One workgroup a head, beside the workgroups that own keys.
@@ -1019,9 +1071,11 @@ static int check_apart(const char* what, const cd_diff_attn* d, bool out_only) {
 static int parts_of(const cd_diff_attn* d) {
   const int64_t groups = (int64_t)d->batch * d->kv_heads * cdiv((int64_t)d->tq * (d->heads / d->kv_heads), F_ROWS);
   int64_t p = groups ? 768 / groups : 1;   // (three workgroups a compute unit: all parts at once)
-  if (p > cdiv(d->tk, 128)) p = cdiv(d->tk, 128);
+  // (a single tile of rows is split down to 128 keys; where the rows fill more, what the parts write and read again is worth it from 512 keys on)
+  const int64_t least = (int64_t)d->tq * (d->heads / d->kv_heads) > F_ROWS ? 512 : 128;
+  if (p > cdiv(d->tk, least)) p = cdiv(d->tk, least);
   if (p > 64) p = 64;
-  return p < 2 || groups > 128 ? 1 : (int)p;
+  return p < 2 ? 1 : (int)p;
 }
 
 static DiffArgs args_of(const cd_diff_attn* d) {
@@ -1058,9 +1112,20 @@ static int64_t keys_of(const cd_diff_attn* d) {
 // work.
 static int kv_parts_of(const cd_diff_attn* d) {
   const int64_t groups = (int64_t)d->batch * d->kv_heads * cdiv(d->tk, keys_of(d)), tiles = cdiv((int64_t)d->tq * (d->heads / d->kv_heads), 32);
-  int64_t p = groups ? 512 / groups : 1;
+  int64_t p = groups && groups < 256 ? 512 / groups : 1;
   if (p > tiles / 8) p = tiles / 8;
   if (p > 16) p = 16;
+  return p < 2 ? 1 : (int)p;
+}
+
+// The same of the keys in the pass that owns queries: a few queries against many keys.
+static int q_parts_of(const cd_diff_attn* d) {
+  int64_t rows = 0;
+  dispatch(d, [&](auto x) { rows = QSizes<typename decltype(x)::T, decltype(x)::DT>::ROWS; });
+  const int64_t groups = (int64_t)d->batch * d->kv_heads * cdiv((int64_t)d->tq * (d->heads / d->kv_heads), rows);
+  int64_t p = groups && groups < 256 ? 512 / groups : 1;
+  if (p > d->tk / 256) p = d->tk / 256;
+  if (p > 64) p = 64;
   return p < 2 ? 1 : (int)p;
 }
 
@@ -1071,7 +1136,9 @@ static Layout layout_of(const cd_diff_attn* d) {
   Layout l;
   l.second = rows * sizeof(RowValues);
   l.sums = l.second + (d->lambda_kind == CD_LAMBDA_HEAD ? align_up(rows * 4, 16) : 0);
-  l.bytes = l.sums + (parts > 1 ? parts * d->batch * d->kv_heads * d->tk * 4 * d->head_dim * 4 : 0);
+  const size_t keys = parts > 1 ? parts * d->batch * d->kv_heads * d->tk * 4 * d->head_dim * 4 : 0, q_parts = (size_t)q_parts_of(d);
+  const size_t queries = q_parts > 1 ? q_parts * d->batch * d->tq * d->heads * (2 * d->head_dim + 2) * 4 : 0;
+  l.bytes = l.sums + (keys > queries ? keys : queries);   // (the one pass has joined its parts before the other writes its own)
   return l;
 }
 
@@ -1150,13 +1217,21 @@ extern "C" int codistill_diff_attention_backward(const cd_diff_attn* desc, const
   hipStream_t s = static_cast<hipStream_t>(stream);
   const double e = elem_of(desc), qe = 4.0 * a.q_rows * a.heads * 2 * a.dim, ke = 4.0 * a.k_rows * a.kv_heads * 2 * a.dim;
   ProfScope prof(CD_K_ATTN, s, 20.0 * a.dim * pairs(desc), e * (qe + ke));
-  if (a.tq > 0)
+  a.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + lay.sums);
+  if (a.tq > 0) {
+    a.parts = q_parts_of(desc);
+    a.part_ml = a.part + (size_t)a.parts * a.units * a.tq * a.group * 2 * a.dim;
     dispatch(desc, [&](auto x) {
       a.tiles = (int)cdiv((int64_t)a.tq * a.group, QSizes<typename decltype(x)::T, decltype(x)::DT>::ROWS);
-      hipLaunchKernelGGL((diff_backward_q_kernel<typename decltype(x)::T, decltype(x)::DT>), dim3(work_blocks((int64_t)a.units * a.tiles)), dim3(256), 0, s, a);
+      hipLaunchKernelGGL((diff_backward_q_kernel<typename decltype(x)::T, decltype(x)::DT>), dim3(work_blocks((int64_t)a.units * a.tiles * a.parts)), dim3(256), 0, s, a);
     });
+    if (a.parts > 1) {
+      const dim3 grid((unsigned)cdiv((int64_t)a.units * a.tq * a.group * (a.dim / 2), 256));
+      if (desc->dtype == CD_BF16) hipLaunchKernelGGL((diff_join_q_kernel<bf16_t>), grid, dim3(256), 0, s, a);
+      else hipLaunchKernelGGL((diff_join_q_kernel<float>), grid, dim3(256), 0, s, a);
+    }
+  }
   a.parts = kv_parts_of(desc);
-  a.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + lay.sums);
   const int heads = a.lam_token ? 0 : a.heads;   // workgroups that add up a head's dlambda
   if (a.tk > 0 || heads)
     dispatch(desc, [&](auto x) {
