@@ -458,7 +458,7 @@ int codistill_head_norm_backward(int dtype, const void* x, int64_t x_row, const 
  * moments before they are rounded.
  *   grad_scale  device fp32 [1] or NULL (1): clipping or unscaling factor, read by the kernel
  *   t, lr, betas, eps: host values; the step is computed from them in double
- * Errors (CD_ERR_INVALID_ARG, nothing launched): NULL or misaligned pointers (16 bytes; bf16 tensors 8, 8-bit moments 4), n < 1, n_tensors < 1,
+ * Errors (CD_ERR_INVALID_ARG, nothing launched): NULL or misaligned pointers (16 bytes; bf16 grad and lowp 8, 8-bit moments 8), n < 1, n_tensors < 1,
  * t < 1, betas outside [0, 1), eps <= 0, NaN lr, decay or lr_scale, state_bits other than 8 and 32; CD_ERR_WORKSPACE_TOO_SMALL: the buffer.
  */
 typedef struct {
