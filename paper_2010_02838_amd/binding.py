@@ -301,6 +301,14 @@ def codistill_adam_step(master_w, exp_avg, exp_avg_sq, grad, lowp_w_out, lr, t, 
                                    master_w.numel(), lr, beta1, beta2, eps, weight_decay, int(t), _stream()))
 
 
+_raw_stream = getattr(getattr(torch, "_C", None), "_cuda_getCurrentRawStream", None)
+
+
+def _stream_ptr():
+    """The current stream's handle; without the stream object where torch lets one (5 of the 15 us of a small call were spent on it)."""
+    return _raw_stream(torch.cuda.current_device()) if _raw_stream else torch.cuda.current_stream().cuda_stream
+
+
 def _dtype(t):
     if t.dtype is torch.bfloat16:
         return CD_BF16
@@ -311,6 +319,8 @@ def _dtype(t):
 
 def _inner(t, dims, what):
     """The last `dims` dimensions have to be contiguous; returns the strides of the others."""
+    if t.is_contiguous():
+        return t.stride()[:t.dim() - dims]
     run = 1
     for d in range(t.dim() - 1, t.dim() - 1 - dims, -1):
         if t.shape[d] != 1 and t.stride(d) != run:
@@ -334,18 +344,25 @@ def rotary_desc(dim, sections, theta, dtype, layout=CD_ROPE_HALVES, freq=None):
     return d
 
 
+_ROTARY_ARRAYS = {n: RotaryTensor * n for n in range(1, CD_ROPE_MAX_TENSORS + 1)}
+
+
 def codistill_rotary(desc, positions, tensors, inverse=False):
     """positions: int32 [axes, tokens]; tensors: up to four pairs (x, y) of [tokens, heads, dim] (y may be x); inverse: the gradient."""
-    arr = (RotaryTensor * len(tensors))()
-    tokens = positions.shape[1]
+    n, tokens, dim = len(tensors), positions.shape[1], desc.dim
+    arr = _ROTARY_ARRAYS[n]() if n in _ROTARY_ARRAYS else (RotaryTensor * n)()
     if positions.dtype is not torch.int32 or not positions.is_contiguous() or positions.shape[0] < desc.axes:
         raise ValueError("rotary: positions are contiguous int32 [axes, tokens]")
+    dtype = torch.bfloat16 if desc.dtype == CD_BF16 else torch.float32
     for a, (x, y) in zip(arr, tensors):
-        if x.shape != y.shape or x.shape[0] != tokens or x.shape[2] != desc.dim or _dtype(x) != desc.dtype or _dtype(y) != desc.dtype:
+        shape = x.shape
+        if shape != y.shape or len(shape) != 3 or shape[0] != tokens or shape[2] != dim or x.dtype is not dtype or y.dtype is not dtype:
             raise ValueError("rotary: tensors are [tokens, heads, dim] of the descriptor's type")
-        a.x, a.y, a.heads = x.data_ptr(), y.data_ptr(), x.shape[1]
-        a.x_token, a.y_token = _inner(x, 2, "rotary")[0], _inner(y, 2, "rotary")[0]
-    _check(lib.codistill_rotary(ctypes.byref(desc), _ptr(positions), tokens, arr, len(tensors), int(inverse), _stream()))
+        xs, ys = x.stride(), y.stride()
+        if xs[1:] != (dim, 1) or ys[1:] != (dim, 1):
+            _inner(x, 2, "rotary"), _inner(y, 2, "rotary")
+        a.x, a.y, a.heads, a.x_token, a.y_token = x.data_ptr(), y.data_ptr(), shape[1], xs[0], ys[0]
+    _check(lib.codistill_rotary(desc, positions.data_ptr(), tokens, arr, n, inverse, _stream_ptr()))
 
 
 def diff_attention_desc(q, k, v, out, lam, causal=False, scale=0.0, q_lens=None, k_lens=None, q_starts=None, k_starts=None, max_q=0, max_k=0):
@@ -419,7 +436,7 @@ def codistill_diff_attention(desc, q, k, v, lam, out, o_second=None, lse=None, w
     if o_second is not None and lse is not None:
         _kept(desc, o_second, lse)
     _check(lib.codistill_diff_attention(ctypes.byref(desc), _ptr(q), _ptr(k), _ptr(v), _ptr(lam), _ptr(out), _ptr(o_second), _ptr(lse), _ptr(workspace),
-                                        _room(workspace), _stream()))
+                                        _room(workspace), _stream_ptr()))
 
 
 def codistill_diff_attention_backward(desc, q, k, v, lam, out, o_second, lse, dout, dq, dk, dv, dlam, workspace):
@@ -428,7 +445,7 @@ def codistill_diff_attention_backward(desc, q, k, v, lam, out, o_second, lse, do
     _laid_out(desc, (dq, dk, dv, dout, dlam))
     _kept(desc, o_second, lse)
     _check(lib.codistill_diff_attention_backward(ctypes.byref(desc), _ptr(q), _ptr(k), _ptr(v), _ptr(lam), _ptr(out), _ptr(o_second), _ptr(lse), _ptr(dout),
-                                                 _ptr(dq), _ptr(dk), _ptr(dv), _ptr(dlam), _ptr(workspace), _room(workspace), _stream()))
+                                                 _ptr(dq), _ptr(dk), _ptr(dv), _ptr(dlam), _ptr(workspace), _room(workspace), _stream_ptr()))
 
 
 def head_norm_workspace_bytes(rows, heads, width):
@@ -441,8 +458,8 @@ def codistill_head_norm(x, gain, y, eps=1e-5, post=1.0):
     """y = post gain x / sqrt(mean(x^2) + eps) over the last dimension of x [rows, heads, width]."""
     if x.shape != y.shape or gain.shape != x.shape[2:] or y.dtype is not x.dtype or gain.dtype is not x.dtype:
         raise ValueError("head_norm: x and y are [rows, heads, width], gain [width], all of one type")
-    _check(lib.codistill_head_norm(_dtype(x), _ptr(x), _inner(x, 2, "head_norm")[0], _ptr(gain), _ptr(y), _inner(y, 2, "head_norm")[0], x.shape[0], x.shape[1],
-                                   x.shape[2], eps, post, _stream()))
+    _check(lib.codistill_head_norm(_dtype(x), x.data_ptr(), _inner(x, 2, "head_norm")[0], gain.data_ptr(), y.data_ptr(), _inner(y, 2, "head_norm")[0], *x.shape, eps, post,
+                                   _stream_ptr()))
 
 
 def codistill_head_norm_backward(x, gain, dy, dx, dgain, workspace, eps=1e-5, post=1.0):
@@ -453,7 +470,7 @@ def codistill_head_norm_backward(x, gain, dy, dx, dgain, workspace, eps=1e-5, po
         raise ValueError("head_norm_backward: one type, dgain fp32")
     _check(lib.codistill_head_norm_backward(_dtype(x), _ptr(x), _inner(x, 2, "head_norm")[0], _ptr(gain), _ptr(dy), _inner(dy, 2, "head_norm")[0], _ptr(dx),
                                             _inner(dx, 2, "head_norm")[0], _ptr(dgain), x.shape[0], x.shape[1], x.shape[2], eps, post, _ptr(workspace),
-                                            _room(workspace), _stream()))
+                                            _room(workspace), _stream_ptr()))
 
 
 def adamw_table(tensors, state_bits, grad_dtype):
@@ -468,11 +485,11 @@ def adamw_table(tensors, state_bits, grad_dtype):
 
 def codistill_adamw_step(plan, table, lr, t, beta1=0.9, beta2=0.999, eps=1e-8, seed=0, grad_scale=None):
     cfg = AdamwCfg(lr, beta1, beta2, eps, int(t), seed & 0xffffffff)
-    _check(lib.codistill_adamw_step(ctypes.byref(plan), _ptr(table), ctypes.byref(cfg), _ptr(grad_scale), _stream()))
+    _check(lib.codistill_adamw_step(ctypes.byref(plan), _ptr(table), ctypes.byref(cfg), _ptr(grad_scale), _stream_ptr()))
 
 
 def codistill_adamw_unpack(plan, table):
-    _check(lib.codistill_adamw_unpack(ctypes.byref(plan), _ptr(table), _stream()))
+    _check(lib.codistill_adamw_unpack(ctypes.byref(plan), _ptr(table), _stream_ptr()))
 
 
 def profile_enable(on):
