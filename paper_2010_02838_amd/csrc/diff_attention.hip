@@ -54,7 +54,7 @@ struct DiffArgs {
   const void* dout; void* dq; void* dk; void* dv; float* dlam;
   RowValues* rows;                                // backward: [q rows][heads]
   float* second;                                  // backward, a lambda for each head: delta_2 [heads][q rows]
-  float* part; float* part_ml;                    // forward over parts of the keys: unnormalised sums and (maximum, sum) of a part
+  float* part; float* part_ml;                    // forward over parts of the keys: unnormalised sums and (maximum, sum, rounded sum, -) of a part
   int64_t q_token, q_batch, k_token, k_batch, v_token, v_batch, o_token, o_batch, o2_token;
   const int32_t* q_lens; const int32_t* k_lens; const int32_t* q_starts; const int32_t* k_starts;
   int64_t q_rows, k_rows;                         // rows of the q and k tensors (batch * tq when padded)
@@ -116,6 +116,13 @@ template <> struct Ops<bf16_t> {
     const int grp = lane >> 4, li = lane & 15, row = 4 * (grp >> 1) + (li >> 2), col = 16 * (grp & 1) + 4 * (li & 3);
     return {lds_at<bf16_t, W>(lane & 31, 8 * (lane >> 5)), lds_at<bf16_t, W>(row, col), lds_at<bf16_t, W>(row + 8, col)};
   }
+  // c and the sum of a fragment's elements (products with ones: two elements an instruction)
+  static __device__ inline float add_up(const Frag& f, float c) {
+    const v2bf one = {(__bf16)1.f, (__bf16)1.f};
+#pragma unroll
+    for (int e = 0; e < 4; e++) c = __builtin_amdgcn_fdot2_f32_bf16(v2bf{f[2 * e], f[2 * e + 1]}, one, c, false);
+    return c;
+  }
   static __device__ inline void store4(bf16_t* p, float a, float b, float c, float d) {
     const v2f lo = {a, b}, hi = {c, d};
     uint2 u;
@@ -157,6 +164,11 @@ template <> struct Ops<float> {
   template <int W> static __device__ inline LaneAt lane_at(int lane) {
     static_assert(W * sizeof(float) >= 256, "rows of 16 pieces");
     return {lds_at<float, W>(lane & 31, 8 * (lane >> 5)), lds_at<float, W>(4 * (lane >> 5), lane & 31), 0};
+  }
+  static __device__ inline float add_up(const Frag& f, float c) {
+#pragma unroll
+    for (int e = 0; e < 8; e++) c += f[e];
+    return c;
   }
   static __device__ inline void store4(float* p, float a, float b, float c, float d) { *reinterpret_cast<float4*>(p) = make_float4(a, b, c, d); }
 };
@@ -347,7 +359,9 @@ __global__ void __launch_bounds__(F_THREADS, sizeof(T) == 4 ? (DT == 128 ? 1 : 2
   v16f o[S::VT];
 #pragma unroll
   for (int t = 0; t < S::VT; t++) clear(o[t]);
-  float mx = -INFINITY, sum = 0.f;
+  // The log-sum comes from the weights before they are rounded, the values' divisor from the rounded ones: those then add up to one, so that what the
+  // values of all keys have in common, which the difference of the maps reduces to 1 - lambda of itself, is not touched by the rounding.
+  float mx = -INFINITY, sum = 0.f, weight = 0.f;
   LaneAt at = O::template lane_at<S::W>(lane);
   // One barrier a tile: behind it the tile has arrived, and nobody reads the other buffer any more, into which the next tile is sent for.
   Loader<T, DT, true, F_THREADS> ks;
@@ -393,6 +407,7 @@ __global__ void __launch_bounds__(F_THREADS, sizeof(T) == 4 ? (DT == 128 ? 1 : 2
         const float f = exp2_fast(mx - finite_or_zero(now));
         mx = now;
         sum *= f;
+        weight *= f;
 #pragma unroll
         for (int t = 0; t < S::VT; t++) o[t] *= f;
       }
@@ -403,12 +418,14 @@ __global__ void __launch_bounds__(F_THREADS, sizeof(T) == 4 ? (DT == 128 ? 1 : 2
         sum += sc[v];
       }
       const typename O::Frag p[2] = {O::operand(sc, 0), O::operand(sc, 1)};
+      weight = O::add_up(p[1], O::add_up(p[0], weight));
       if (!EARLY) stream_first(vf, value);
       stream_rest<typename O::Frag, 2 * S::VT, G>(vf, value, [&](int x, const typename O::Frag& f) { o[x % S::VT] = O::mma(f, p[x / S::VT], o[x % S::VT]); });
     }
   }
   __syncthreads();   // (the exchange below writes where the last tile was read)
   sum += other_half(sum);
+  weight += other_half(weight);
   if (a.parts > 1) {   // a part's sums, joined by diff_join_kernel
     if (!live) return;
     const int64_t place = (((int64_t)part * a.units + unit) * (a.tq * a.group) + r) * 2 + m;
@@ -418,11 +435,11 @@ __global__ void __launch_bounds__(F_THREADS, sizeof(T) == 4 ? (DT == 128 ? 1 : 2
 #pragma unroll
       for (int g = 0; g < 4; g++)
         if (32 * t + 8 * g < 2 * a.dim) *reinterpret_cast<float4*>(p + 32 * t + 8 * g) = make_float4(o[t][4 * g], o[t][4 * g + 1], o[t][4 * g + 2], o[t][4 * g + 3]);
-    if (hh == 0) *reinterpret_cast<float2*>(a.part_ml + place * 2) = make_float2(mx, sum);
+    if (hh == 0) *reinterpret_cast<float4*>(a.part_ml + place * 4) = make_float4(mx, sum, weight, 0.f);
     return;
   }
   const int64_t row = s.q0 + i;
-  const float norm = sum > 0.f || sum != sum ? 1.f / sum : 0.f;   // (NaN stays NaN)
+  const float norm = weight > 0.f || weight != weight ? 1.f / weight : 0.f;   // (NaN stays NaN)
 #pragma unroll
   for (int t = 0; t < S::VT; t++) o[t] *= norm;
   if (a.lse && live && hh == 0) a.lse[(int64_t)(m * a.heads + h) * a.q_rows + row] = sum > 0.f ? mx + __log2f(sum) : sum;
@@ -454,7 +471,7 @@ __global__ void __launch_bounds__(F_THREADS, sizeof(T) == 4 ? (DT == 128 ? 1 : 2
     }
 }
 
-// Joins the parts of a row: one wave a row.  Lane p holds the maximum and the sum of part p (at most 64 parts), so that the weights of all parts are
+// Joins the parts of a row: one wave a row.  Lane p holds the maximum and the sums of part p (at most 64 parts), so that the weights of all parts are
 // known before the sums are read.
 template <typename T>
 __global__ void __launch_bounds__(256) diff_join_kernel(DiffArgs a) {
@@ -473,10 +490,10 @@ __global__ void __launch_bounds__(256) diff_join_kernel(DiffArgs a) {
     float lse[2];
 #pragma unroll
     for (int k = 0; k < 2; k++) {
-      float2 ml = make_float2(-INFINITY, 0.f);
-      if (lane < a.parts) ml = *reinterpret_cast<const float2*>(a.part_ml + ((at + lane * step) * 2 + k) * 2);
-      const float top = wave_max(ml.x), e = exp2_fast(ml.x - finite_or_zero(top)), sum = wave_sum(e * ml.y);
-      f[k] = sum > 0.f || sum != sum ? e / sum : 0.f;   // (NaN stays NaN)
+      float4 ml = make_float4(-INFINITY, 0.f, 0.f, 0.f);
+      if (lane < a.parts) ml = *reinterpret_cast<const float4*>(a.part_ml + ((at + lane * step) * 2 + k) * 4);
+      const float top = wave_max(ml.x), e = exp2_fast(ml.x - finite_or_zero(top)), sum = wave_sum(e * ml.y), weight = wave_sum(e * ml.z);
+      f[k] = weight > 0.f || weight != weight ? e / weight : 0.f;   // (NaN stays NaN)
       lse[k] = sum > 0.f ? top + __log2f(sum) : sum;
     }
     if (a.lse && lane < 2) a.lse[(int64_t)(lane * a.heads + h) * a.q_rows + row] = lane ? lse[1] : lse[0];
@@ -1153,7 +1170,7 @@ extern "C" int codistill_diff_attention_workspace_bytes(const cd_diff_attn* desc
   if (const int rc = check("diff_attention_workspace_bytes", desc)) return rc;
   CD_REQUIRE(bytes != nullptr, "diff_attention_workspace_bytes: output pointer is NULL");
   const int parts = parts_of(desc);
-  size_t n = parts > 1 ? (size_t)parts * desc->batch * desc->kv_heads * desc->tq * (desc->heads / desc->kv_heads) * 2 * (2 * desc->head_dim + 2) * 4 : 0;
+  size_t n = parts > 1 ? (size_t)parts * desc->batch * desc->kv_heads * desc->tq * (desc->heads / desc->kv_heads) * 2 * (2 * desc->head_dim + 4) * 4 : 0;
   if (backward) {
     const size_t back = layout_of(desc).bytes;
     n = n > back ? n : back;
@@ -1180,7 +1197,7 @@ extern "C" int codistill_diff_attention(const cd_diff_attn* desc, const void* q,
   a.tiles = (int)cdiv((int64_t)a.tq * a.group, F_ROWS);
   a.parts = parts_of(desc);
   a.part_ml = static_cast<float*>(workspace);
-  a.part = a.part_ml + (size_t)a.parts * a.units * a.tq * a.group * 4;
+  a.part = a.part_ml + (size_t)a.parts * a.units * a.tq * a.group * 8;
   hipStream_t s = static_cast<hipStream_t>(stream);
   const double e = elem_of(desc), qe = 2.0 * a.q_rows * a.heads * 2 * a.dim, ke = 2.0 * a.k_rows * a.kv_heads * 2 * a.dim;
   ProfScope prof(CD_K_ATTN, s, 12.0 * a.dim * pairs(desc), e * (qe + ke));
