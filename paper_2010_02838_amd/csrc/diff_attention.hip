@@ -58,7 +58,7 @@ struct DiffArgs {
   int64_t q_token, q_batch, k_token, k_batch, v_token, v_batch, o_token, o_batch, o2_token;
   const int32_t* q_lens; const int32_t* k_lens; const int32_t* q_starts; const int32_t* k_starts;
   int64_t q_rows, k_rows;                         // rows of the q and k tensors (batch * tq when padded)
-  int32_t batch, tq, tk, heads, kv_heads, group, dim, causal, lam_token, parts, tiles, units, work;
+  int32_t batch, tq, tk, heads, kv_heads, group, dim, causal, lam_token, parts, tiles, units, work, run, uneven;
   uint32_t group_inv;                             // floor(2^32 / group) + 1 (group > 1)
   float scale, c;                                 // c = scale log2(e)
 };
@@ -204,18 +204,27 @@ template <typename T> __device__ inline T* rows_of(const DiffArgs& a, T* p, int 
 }
 __device__ inline int query_of(const DiffArgs& a, int r) { return a.group == 1 ? r : (int)__umulhi((uint32_t)r, a.group_inv); }
 
-// Workgroups go to the eight L2 caches in turn; each cache gets a run of neighbours in the order (unit, tile), which share their keys.  Under a
-// causal mask the run's units are taken in turns, so that the long tiles of all of them start before the short ones.
-__device__ inline int work_index(int n, int per_unit, bool turns) {
-  const int per = (n + 7) >> 3, at = (int)(blockIdx.x >> 3);
-  int x = at;
-  if (turns) {
-    const int units = per / per_unit;
-    if (units > 1 && units * per_unit == per) x = at % units * per_unit + at / units;
+// Workgroups go to the eight L2 caches in turn; each cache gets runs of neighbours in the order (unit, tile, part), which share their keys.  Under a
+// causal mask its run is one, and the run's units are taken in turns, so that the long tiles of all of them start before the short ones.
+__device__ inline int work_index(const DiffArgs& a) {
+  const int at = (int)(blockIdx.x >> 3), per_unit = a.tiles * a.parts;
+  int x = at % a.run;
+  if (a.causal) {
+    const int units = a.run / per_unit;
+    if (units > 1 && units * per_unit == a.run) x = x % units * per_unit + x / units;
   }
-  return (int)(blockIdx.x & 7) * per + x;
+  return (at / a.run * 8 + (int)(blockIdx.x & 7)) * a.run + x;
 }
-static unsigned work_blocks(int64_t n) { return (unsigned)(cdiv(n, 8) * 8); }
+// The number of workgroups.  Where sequences differ in length (and nothing else does), a cache that got whole units would have the short ones or the
+// long ones: every cache gets a part of every unit.  Five sequences of up to 777 tokens, 8 heads of 128 on 2: 53 instead of 55 us forward and 60 instead of 64
+// for the queries' gradients; the keys' gradients, whose rows are split over workgroups of their own, deal those parts out (110 -> 64 us).
+static unsigned work_blocks(DiffArgs& a, bool keys = false) {
+  const int64_t per_unit = (int64_t)a.tiles * a.parts, n = a.units * per_unit;
+  a.run = (int)cdiv(n, 8);
+  if (a.uneven && !a.causal) a.run = (int)(per_unit <= 8 ? per_unit : keys && a.parts > 1 ? a.tiles : cdiv(per_unit, 8));
+  if (a.run < 1) a.run = 1;
+  return (unsigned)(cdiv(n, 8 * (int64_t)a.run) * 8 * a.run);
+}
 
 // A buffer that is the same in all lanes, and known to be (nothing is left of this where the compiler has seen it by itself).
 __device__ inline rsrc_words_t buffer_of(const void* p, int64_t bytes) {
@@ -326,7 +335,7 @@ __global__ void __launch_bounds__(F_THREADS, sizeof(T) == 4 ? (DT == 128 ? 1 : 2
   constexpr int BUF = S::KC * S::W, G = sizeof(T) == 2 ? 4 : 2, GK = G < S::KS ? G : S::KS;
   constexpr bool EARLY = sizeof(T) == 2 && DT <= 64;
   const int total = a.units * a.tiles * a.parts;
-  const int w = work_index(total, a.tiles * a.parts, a.causal);
+  const int w = work_index(a);
   if (w >= total) return;
   const int part = w % a.parts, ut = w / a.parts, unit = ut / a.tiles;
   const int tile = a.tiles - 1 - ut % a.tiles;   // under a causal mask the last rows see the most keys: they go first
@@ -562,7 +571,7 @@ __global__ void __launch_bounds__(256, DT * sizeof(T) <= 256 ? 2 : 1) diff_backw
   __shared__ __attribute__((aligned(16))) T lds[4 * S::KC * S::W];   // keys and values, two buffers each
   constexpr int BUF = S::KC * S::W, G = sizeof(T) == 2 && DT == 64 ? 4 : 2, MAPS = Z::MAPS;
   const int total = a.units * a.tiles * a.parts;
-  const int w = work_index(total, a.tiles * a.parts, a.causal);
+  const int w = work_index(a);
   if (w >= total) return;
   const int part = w % a.parts, ut = w / a.parts, unit = ut / a.tiles, tile = a.tiles - 1 - ut % a.tiles;
   const int b = unit / a.kv_heads, hk = unit % a.kv_heads;
@@ -809,7 +818,7 @@ __global__ void __launch_bounds__((KvSizes<T, DT>::THREADS), sizeof(T) == 2 && D
   typedef Ops<T> O;
   typedef Sizes<T, DT> S;
   typedef KvSizes<T, DT> Z;
-  constexpr int BUF = S::KC * S::W, G = sizeof(T) == 2 && DT <= 64 ? 4 : 2, NB = Z::BUFFERS, FRAG = sizeof(typename O::Frag);
+  constexpr int BUF = S::KC * S::W, G = sizeof(T) == 2 ? 4 : 2, NB = Z::BUFFERS, FRAG = sizeof(typename O::Frag);
   __shared__ __attribute__((aligned(16))) T lds[2 * NB * BUF];                         // queries and dO
   __shared__ __attribute__((aligned(16))) RowValues st[NB][43];                        // the rows' values: 32, and room for the 2048 bytes that two waves write
   __shared__ __attribute__((aligned(16))) char ex[2][Z::PAIRS][6 * 64 * FRAG];         // P_1 - lambda P_2, dS_1, dS_2 of a tile, two operands each
@@ -818,9 +827,11 @@ __global__ void __launch_bounds__((KvSizes<T, DT>::THREADS), sizeof(T) == 2 && D
     sum_lambda<Z::THREADS>(a, (int)blockIdx.x - a.work);
     return;
   }
-  const int w = work_index(total, a.tiles * a.parts, a.causal);
+  const int w = work_index(a);
   if (w >= total) return;
-  const int part = w % a.parts, ut = w / a.parts, unit = ut / a.tiles, tile = ut % a.tiles;   // (under a causal mask the first keys are seen by the most rows)
+  // under a causal mask the first keys are seen by the most rows; without one, workgroups that read the same rows are neighbours
+  const int per_unit = a.tiles * a.parts, unit = w / per_unit, x = w % per_unit;
+  const int part = a.causal ? x % a.parts : x / a.tiles, tile = a.causal ? x / a.parts : x % a.tiles;
   const int b = unit / a.kv_heads, hk = unit % a.kv_heads;
   const Seq s = sequence(a, b);
   const int R = s.nq * a.group, j0 = tile * Z::KEYS, room = a.q_starts ? s.nk : a.tk;
@@ -1104,6 +1115,7 @@ static DiffArgs args_of(const cd_diff_attn* d) {
   a.batch = d->batch; a.tq = d->tq; a.tk = d->tk; a.heads = d->heads; a.kv_heads = d->kv_heads; a.group = d->heads / d->kv_heads; a.dim = d->head_dim;
   a.causal = d->causal != 0; a.lam_token = d->lambda_kind == CD_LAMBDA_TOKEN; a.parts = 1;
   a.units = d->batch * d->kv_heads;
+  a.uneven = d->q_lens || d->k_lens;
   a.group_inv = a.group > 1 ? (uint32_t)((1ull << 32) / a.group) + 1 : 0;
   a.scale = d->scale > 0.f ? d->scale : 1.f / sqrtf((float)d->head_dim);
   a.c = a.scale * 1.44269504088896340736f;
@@ -1201,8 +1213,9 @@ extern "C" int codistill_diff_attention(const cd_diff_attn* desc, const void* q,
   hipStream_t s = static_cast<hipStream_t>(stream);
   const double e = elem_of(desc), qe = 2.0 * a.q_rows * a.heads * 2 * a.dim, ke = 2.0 * a.k_rows * a.kv_heads * 2 * a.dim;
   ProfScope prof(CD_K_ATTN, s, 12.0 * a.dim * pairs(desc), e * (qe + ke));
+  const unsigned blocks = work_blocks(a);
   dispatch(desc, [&](auto x) {
-    hipLaunchKernelGGL((diff_forward_kernel<typename decltype(x)::T, decltype(x)::DT>), dim3(work_blocks((int64_t)a.units * a.tiles * a.parts)), dim3(F_THREADS), 0, s, a);
+    hipLaunchKernelGGL((diff_forward_kernel<typename decltype(x)::T, decltype(x)::DT>), dim3(blocks), dim3(F_THREADS), 0, s, a);
   });
   if (a.parts > 1) {
     const dim3 grid((unsigned)cdiv((int64_t)a.units * a.tq * a.group, 4));
@@ -1240,7 +1253,8 @@ extern "C" int codistill_diff_attention_backward(const cd_diff_attn* desc, const
     a.part_ml = a.part + (size_t)a.parts * a.units * a.tq * a.group * 2 * a.dim;
     dispatch(desc, [&](auto x) {
       a.tiles = (int)cdiv((int64_t)a.tq * a.group, QSizes<typename decltype(x)::T, decltype(x)::DT>::ROWS);
-      hipLaunchKernelGGL((diff_backward_q_kernel<typename decltype(x)::T, decltype(x)::DT>), dim3(work_blocks((int64_t)a.units * a.tiles * a.parts)), dim3(256), 0, s, a);
+      const unsigned blocks = work_blocks(a);
+      hipLaunchKernelGGL((diff_backward_q_kernel<typename decltype(x)::T, decltype(x)::DT>), dim3(blocks), dim3(256), 0, s, a);
     });
     if (a.parts > 1) {
       const dim3 grid((unsigned)cdiv((int64_t)a.units * a.tq * a.group * (a.dim / 2), 256));
@@ -1254,7 +1268,7 @@ extern "C" int codistill_diff_attention_backward(const cd_diff_attn* desc, const
     dispatch(desc, [&](auto x) {
       typedef KvSizes<typename decltype(x)::T, decltype(x)::DT> Z;
       a.tiles = (int)cdiv(a.tk, Z::KEYS);
-      a.work = (int)work_blocks((int64_t)a.units * a.tiles * a.parts);
+      a.work = (int)work_blocks(a, true);
       hipLaunchKernelGGL((diff_backward_kv_kernel<typename decltype(x)::T, decltype(x)::DT>), dim3((unsigned)(a.work + heads)), dim3(Z::THREADS), 0, s, a);
     });
   if (a.tk > 0) {
