@@ -178,7 +178,7 @@ template <typename T, int DT> struct Sizes {
   static constexpr int W = 2 * DT, KC = 32;
   static constexpr int KS = DT / 16, VT = W / 32, DTT = DT / 32;
 };
-constexpr int EXACT_KEYS = 128;   // rows that reach no more keys than this get their deltas in a pass of their own
+constexpr int EXACT_KEYS = 128;   // rows that reach no more keys than this get their deltas in a pass of their own (bf16)
 
 // ---- sequences and rows ---------------------------------------------------------------------------------------------------
 struct Seq { int nq, nk; int64_t q0, k0; };   // lengths; rows of the sequence's first query and key in their tensors
@@ -552,6 +552,9 @@ __device__ inline void leave_row(const DiffArgs& a, int64_t row, int h, int m, b
   }
 }
 
+// whether the weights of a row that sees so many keys depend on its scores
+__device__ inline bool moves(int keys) { return keys != 1; }
+
 // ---- backward: queries ------------------------------------------------------------------------------------------------------------
 // dq, delta and dlambda.  delta first comes from the kept outputs, delta_2 = dO . (P_2 v), delta_1 = dO . out + lambda delta_2, which were rounded;
 // the pass over the keys gives what is missing, rowsum(P_m (dP - delta_m)) in fp32, so that dlambda and the deltas that the other kernel
@@ -629,7 +632,7 @@ __global__ void __launch_bounds__(256, DT * sizeof(T) <= 256 ? 2 : 1) diff_backw
   const int see = live ? limit(r) : s.nk;
   const int least = limit(wr0), reach = wr0 < R ? limit(min(wr0 + 31, R - 1)) : 0;
   int begin = 0, last = r0 < R ? limit(min(r0 + Z::ROWS, R) - 1) : 0;
-  const bool two = last <= EXACT_KEYS;
+  const bool two = sizeof(T) == 2 && last <= EXACT_KEYS;
   if (a.parts > 1) {   // (few keys are one part's, so that the two passes below see all of them)
     const int per = two ? EXACT_KEYS : (((a.tk + 31) / 32 + a.parts - 1) / a.parts) * 32;
     begin = part * per;
@@ -641,7 +644,8 @@ __global__ void __launch_bounds__(256, DT * sizeof(T) <= 256 ? 2 : 1) diff_backw
 #pragma unroll
     for (int t = 0; t < S::DTT; t++) clear(dq[m][t]);
   // Rows with few keys: a rounding of the kept outputs is as large as their small dS (two keys: dq off by 5e-3 where its own rounding is 1.7e-3,
-  // 128 keys 2.8e-3, 700 keys 2.5e-3 as without it), so delta is completed by a pass of its own first.
+  // 128 keys 2.8e-3, 700 keys 2.5e-3 as without it), so delta is completed by a pass of its own first.  fp32 outputs are as exact as the products; there
+  // one pass does, and a row of one key, whose gradient is zero to the last bit, gets it by name (`moves`).
   LaneAt at = O::template lane_at<S::W>(lane);
   Loader<T, DT, true, 256> ks;
   Loader<T, DT, false, 256> vs;
@@ -733,7 +737,7 @@ __global__ void __launch_bounds__(256, DT * sizeof(T) <= 256 ? 2 : 1) diff_backw
 #pragma unroll
   for (int m = 0; m < MAPS; m++) {
     delta[m] += rest[m] + other_half(rest[m]);
-    const float f = live ? (m0 + m ? -lam * a.scale : a.scale) : 0.f;
+    const float f = live && moves(see) ? (m0 + m ? -lam * a.scale : a.scale) : 0.f;
 #pragma unroll
     for (int t = 0; t < S::DTT; t++)
 #pragma unroll
@@ -764,7 +768,7 @@ __global__ void __launch_bounds__(256) diff_join_q_kernel(DiffArgs a) {
       t.x += y.x; t.y += y.y; t.z += y.z; t.w += y.w;
       delta += a.part_ml[(at + p * step) * 2 + m];
     }
-  const float lam = live ? a.lam[a.lam_token ? row * a.heads + h : h] : 0.f, f = m ? -lam * a.scale : a.scale;
+  const float lam = live ? a.lam[a.lam_token ? row * a.heads + h : h] : 0.f, f = !moves(a.causal ? min(s.nk, i + s.nk - s.nq + 1) : s.nk) ? 0.f : m ? -lam * a.scale : a.scale;
   T* dq = rows_of(a, static_cast<T*>(a.dq), b, s.q0, a.q_token, a.q_batch) + i * a.q_token + (int64_t)h * 2 * a.dim + col;
   Ops<T>::store4(dq, f * t.x, f * t.y, f * t.z, f * t.w);
   if (col == m * a.dim) leave_row(a, row, h, m, live, live ? a.lse[(int64_t)(m * a.heads + h) * a.q_rows + row] : 0.f, delta, lam);

@@ -214,6 +214,20 @@ def test_few_rows_against_many_keys(dtype, tq, tk, heads, kv_heads, dim):
     assert torch.equal(kept, p.out)
 
 
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("dim", [32, 64, 128])
+@pytest.mark.parametrize("room", [0, 299, 4095])
+def test_one_key_has_no_gradient(dtype, dim, room):
+    """A softmax over one key is one: queries and keys get zeros, to the last bit, whatever way the keys' room makes the work be split."""
+    p = Problem(dtype, [3, 40], [1, 1], 4, 2, dim, False, True, seed=dim + room, room=(0, room))
+    p.run()
+    p.check()
+    assert not p.dq.any() and not p.dk.any()
+    p = Problem(dtype, [70], [70], 2, 2, dim, True, False, seed=dim)   # the first row under a causal mask
+    p.run()
+    assert not p.dq[0, 0].any() and p.dq[0, 1:].any()
+
+
 def test_large_scores():
     """Scores of some hundred: exponents far beyond fp32 but for the running maximum, which has to move at any time (late keys raise it)."""
     for dtype in (BF, F32):
