@@ -398,7 +398,8 @@ int codistill_rotary(const cd_rotary* rope, const int32_t* positions, int64_t to
  * q rows: batch * tq when padded (row b * tq + i), q_rows when packed.
  * Errors (nothing launched): CD_ERR_INVALID_ARG: NULL or misaligned pointers (16 bytes; q_lens, starts and lambda 4), sizes < 1 (tq or tk 0 are
  * allowed with padded sequences), heads no multiple of kv_heads, strides that are no multiple of 16 bytes or shorter than a token, one of the start
- * tables alone, starts together with lens, scale < 0 or not finite; CD_ERR_UNSUPPORTED: other head dims; CD_ERR_WORKSPACE_TOO_SMALL.
+ * tables alone, starts together with lens, scale < 0 or not finite; CD_ERR_UNSUPPORTED: other head dims, a token stride
+ * above 2^27 bytes; CD_ERR_WORKSPACE_TOO_SMALL.
  */
 enum { CD_LAMBDA_HEAD = 0, CD_LAMBDA_TOKEN = 1 };
 typedef struct {

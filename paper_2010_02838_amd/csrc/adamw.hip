@@ -4,7 +4,8 @@
 //
 // with step = lr / (1 - b1^t) and rs = 1 / sqrt(1 - b2^t) from the host, in double.  HBM-bound: 28 bytes a parameter with 32-bit moments, 16
 // with 8-bit ones, 2 more for the bf16 copy.  One launch whatever the number of tensors: a workgroup takes 1024 or 2048 elements of one tensor and
-// finds which in a table in device memory, so that 180 tensors of a Transformer are not 180 launches that each fill part of the chip.
+// finds which in a table in device memory, so that 180 tensors of a Transformer are not 180 launches that each fill part of the chip.  60.9 M parameters:
+// 300 to 325 us with 32-bit moments (1.83 GB, 5.6 to 6.1 TB/s), 195 to 220 with 8-bit ones (1.1 GB, 5.0 to 5.6), 65 to 70 to unpack those.
 //
 // 8-bit moments.  A block of 256 elements (four a lane of one wave) shares a power of two, 2^E, with E the smallest for which no value exceeds
 // 1.875 2^E; a value x is stored as the float y = |x| 2^-E with three mantissa bits and exponents from 0 down to -14 (m, beside its sign) or -30 (v), equally

@@ -21,6 +21,11 @@
 // wave owns 32 rows (or keys) on its lanes as the second operand, so that whatever belongs to a row is one value a lane, and a score
 // tile, rounded, is the second operand of the next product as it lies: its contraction order 8 (e / 4) + 4 (l / 32) + e % 4 is the order
 // in which the first operand, the streamed tensor transposed, is read from LDS.
+//
+// What bounds them.  Long sequences: neither memory nor LDS, but the matrix instructions (43 % of the forward kernel's cycles) and the vector ones (63 %,
+// exponentials and what surrounds them) of few waves taking turns; two causal sequences of 4096 tokens, 8 heads of 64: forward 135 us (764 TFLOP/s),
+// queries' gradients 185, keys' 220 (425 TFLOP/s together, which repeat scores and dP: 595 with those).  One query a sequence: the cache's bytes, 178 MB in
+// 40 us (4.5 TB/s).  Short sequences: the latency of a workgroup's few tiles, one after the other.
 #include "common.h"
 #include "kernels.h"
 #include "lds_load.h"
@@ -322,7 +327,7 @@ __device__ inline float other_half(float v) { return __shfl_xor(v, 32, 64); }
 __device__ inline float finite_or_zero(float m) { return m == -INFINITY ? 0.f : m; }
 
 // ---- forward -------------------------------------------------------------------------------------------------------------------
-// A wave owns 32 rows of one of the two maps; the waves of a pair exchange their results at the end.  (Both maps in one wave share the fragments of
+// Bound by its instructions (above).  A wave owns 32 rows of one of the two maps; the waves of a pair exchange their results at the end.  (Both maps in one wave share the fragments of
 // v, but need 256 accumulators for the widest heads, which spill, and 128 for heads of 64, which leave two waves a SIMD and nothing in
 // flight beside them.)
 constexpr int F_GROUPS = 2, F_ROWS = 32 * F_GROUPS, F_THREADS = 128 * F_GROUPS;
@@ -480,7 +485,7 @@ __global__ void __launch_bounds__(F_THREADS, sizeof(T) == 4 ? (DT == 128 ? 1 : 2
     }
 }
 
-// Joins the parts of a row: one wave a row.  Lane p holds the maximum and the sums of part p (at most 64 parts), so that the weights of all parts are
+// Joins the parts of a row: one wave a row, bound by the latency of two rounds of loads (8 us for 256 rows of 12 parts).  Lane p holds the maximum and the sums of part p (at most 64 parts), so that the weights of all parts are
 // known before the sums are read.
 template <typename T>
 __global__ void __launch_bounds__(256) diff_join_kernel(DiffArgs a) {
@@ -559,7 +564,7 @@ __device__ inline bool moves(int keys) { return keys != 1; }
 // dq, delta and dlambda.  delta first comes from the kept outputs, delta_2 = dO . (P_2 v), delta_1 = dO . out + lambda delta_2, which were rounded;
 // the pass over the keys gives what is missing, rowsum(P_m (dP - delta_m)) in fp32, so that dlambda and the deltas that the other kernel
 // reads are exact to fp32 rounding (with the kept bf16 outputs alone dlambda is off by their rounding, a thousandth).
-// Both maps of 32 rows in a wave share dP; where that needs more registers than two waves a SIMD have (the widest heads, fp32), a wave takes one
+// Bound by its instructions, as the forward kernel is.  Both maps of 32 rows in a wave share dP; where that needs more registers than two waves a SIMD have (the widest heads, fp32), a wave takes one
 // map and computes dP for itself.
 template <typename T, int DT> struct QSizes {
   static constexpr bool SPLIT = DT * sizeof(T) >= 256;
@@ -799,7 +804,7 @@ template <int THREADS> __device__ inline void sum_lambda(const DiffArgs& a, int 
 }
 
 // ---- backward: keys ------------------------------------------------------------------------------------------------------------------
-// A pair of waves owns 32 keys: one computes P and dS of a tile of rows and leaves them in LDS as operands, the other multiplies the tile before
+// Bound by the longer half of a pair.  A pair of waves owns 32 keys: one computes P and dS of a tile of rows and leaves them in LDS as operands, the other multiplies the tile before
 // it into dk and dv.  In one wave the accumulators (128 registers for heads of 64) beside the keys' and values' fragments (64) and three tiles
 // need more than 256 registers: one wave a SIMD, and most of its time went into copies to and from accumulation registers.
 //
@@ -1099,7 +1104,9 @@ static int check_apart(const char* what, const cd_diff_attn* d, bool out_only) {
   return CD_OK;
 }
 
-// Parts of the keys that get a workgroup of their own: few rows against many keys would leave most of the chip without work.
+// Parts of the keys that get a workgroup of their own: few rows against many keys would leave most of the chip without work.  Heads of 64, one part against
+// this rule: one query of 16 sequences and 4 key heads on up to 8192 keys 187 against 41 + 8 us (the join); 16 queries of 8 heads on 4096 keys 88
+// against 21; 4096 causal tokens of 4 heads 104 against 77; where there are rows enough (512 causal tokens of 8 heads) the rule leaves one part: 19.
 static int parts_of(const cd_diff_attn* d) {
   const int64_t groups = (int64_t)d->batch * d->kv_heads * cdiv((int64_t)d->tq * (d->heads / d->kv_heads), F_ROWS);
   int64_t p = groups ? 768 / groups : 1;   // (three workgroups a compute unit: all parts at once)
@@ -1142,7 +1149,8 @@ static int64_t keys_of(const cd_diff_attn* d) {
   return n;
 }
 // Parts of the rows that get a workgroup of their own in the pass that owns keys: few keys under many rows (shared key heads) leave compute units without
-// work.
+// work.  Five sequences of up to 777 tokens, 8 heads of 128 on 2: one part 144 us, this rule 63 and a join of 9; both passes of 4 x 1024 causal tokens, 8
+// heads of 64 on 2: 203 against 102.
 static int kv_parts_of(const cd_diff_attn* d) {
   const int64_t groups = (int64_t)d->batch * d->kv_heads * cdiv(d->tk, keys_of(d)), tiles = cdiv((int64_t)d->tq * (d->heads / d->kv_heads), 32);
   int64_t p = groups && groups < 256 ? 512 / groups : 1;
@@ -1151,7 +1159,8 @@ static int kv_parts_of(const cd_diff_attn* d) {
   return p < 2 ? 1 : (int)p;
 }
 
-// The same of the keys in the pass that owns queries: a few queries against many keys.
+// The same of the keys in the pass that owns queries: a few queries against many keys (both passes of 16 queries, 8 heads of 64 on 4096 keys: one part 146 us,
+// this rule 37).
 static int q_parts_of(const cd_diff_attn* d) {
   int64_t rows = 0;
   dispatch(d, [&](auto x) { rows = QSizes<typename decltype(x)::T, decltype(x)::DT>::ROWS; });

@@ -41,6 +41,16 @@ def test_attention_descriptors(kw, rc):
     assert backward(attn(**kw)) == rc
 
 
+@pytest.mark.parametrize("name", ["q_token", "k_token", "v_token", "o_token"])
+def test_attention_token_strides(name):
+    """A tile's 32 rows are addressed with 32 bits: token strides up to 2^27 bytes (refused before any pointer is looked at: nothing is launched)."""
+    wide = dict(q_batch=1 << 40, k_batch=1 << 40, v_batch=1 << 40, o_batch=1 << 40)
+    assert forward(attn(**{name: (1 << 26) + 8}, **wide)) == UNSUPPORTED
+    assert backward(attn(**{name: (1 << 26) + 8}, **wide)) == UNSUPPORTED
+    assert backward(attn(dtype=B.CD_F32, **{name: (1 << 25) + 4}, **wide)) == UNSUPPORTED
+    assert forward(attn(**{name: 1 << 26}, **wide), q=None) == BAD
+
+
 def test_attention_pointers_and_workspace():
     d = attn()
     for n in ("q", "k", "v", "lam", "out"):
