@@ -27,6 +27,7 @@
 // queries' gradients 185, keys' 220 (425 TFLOP/s together, which repeat scores and dP: 595 with those).  One query a sequence: the cache's bytes, 178 MB in
 // 40 us (4.5 TB/s).  Short sequences: the latency of a workgroup's few tiles, one after the other.
 #include "common.h"
+#include "conv_rules.h"
 #include "kernels.h"
 #include "lds_load.h"
 #include <math.h>
@@ -63,7 +64,8 @@ struct DiffArgs {
   int64_t q_token, q_batch, k_token, k_batch, v_token, v_batch, o_token, o_batch, o2_token;
   const int32_t* q_lens; const int32_t* k_lens; const int32_t* q_starts; const int32_t* k_starts;
   int64_t q_rows, k_rows;                         // rows of the q and k tensors (batch * tq when padded)
-  int32_t batch, tq, tk, heads, kv_heads, group, dim, causal, lam_token, parts, tiles, units, work, run, uneven;
+  int32_t batch, tq, tk, heads, kv_heads, group, dim, causal, lam_token, parts, tiles, units, work, run, turns, uneven;
+  FastDiv by_run, by_turns, by_unit, by_parts, by_tiles, by_heads, by_dim, by_quads;   // by run, turns, tiles * parts, parts, tiles, kv_heads, dim, dim / 2
   uint32_t group_inv;                             // floor(2^32 / group) + 1 (group > 1)
   float scale, c;                                 // c = scale log2(e)
 };
@@ -211,14 +213,30 @@ __device__ inline int query_of(const DiffArgs& a, int r) { return a.group == 1 ?
 
 // Workgroups go to the eight L2 caches in turn; each cache gets runs of neighbours in the order (unit, tile, part), which share their keys.  Under a
 // causal mask its run is one, and the run's units are taken in turns, so that the long tiles of all of them start before the short ones.
-__device__ inline int work_index(const DiffArgs& a) {
-  const int at = (int)(blockIdx.x >> 3), per_unit = a.tiles * a.parts;
-  int x = at % a.run;
-  if (a.causal) {
-    const int units = a.run / per_unit;
-    if (units > 1 && units * per_unit == a.run) x = x % units * per_unit + x / units;
+struct Work { int unit, part, tile, b, hk; };
+__device__ inline int quotient(int n, FastDiv d) { return (int)div_by((unsigned)n, d); }
+// KEYS: the workgroups that read the same rows, those of a part, are neighbours
+template <bool KEYS = false> __device__ inline bool work_of(const DiffArgs& a, Work& w) {
+  const int at = (int)(blockIdx.x >> 3), per_unit = a.tiles * a.parts, run = quotient(at, a.by_run);
+  int x = at - run * a.run;
+  if (a.turns > 1) {
+    const int turn = quotient(x, a.by_turns);
+    x = (x - turn * a.turns) * per_unit + turn;
   }
-  return (at / a.run * 8 + (int)(blockIdx.x & 7)) * a.run + x;
+  x += (run * 8 + (int)(blockIdx.x & 7)) * a.run;
+  w.unit = quotient(x, a.by_unit);
+  if (w.unit >= a.units) return false;
+  x -= w.unit * per_unit;
+  if (KEYS && !a.causal) {
+    w.part = quotient(x, a.by_tiles);
+    w.tile = x - w.part * a.tiles;
+  } else {
+    w.tile = quotient(x, a.by_parts);
+    w.part = x - w.tile * a.parts;
+  }
+  w.b = quotient(w.unit, a.by_heads);
+  w.hk = w.unit - w.b * a.kv_heads;
+  return true;
 }
 // The number of workgroups.  Where sequences differ in length (and nothing else does), a cache that got whole units would have the short ones or the
 // long ones: every cache gets a part of every unit.  Five sequences of up to 777 tokens, 8 heads of 128 on 2: 53 instead of 55 us forward and 60 instead of 64
@@ -228,6 +246,10 @@ static unsigned work_blocks(DiffArgs& a, bool keys = false) {
   a.run = (int)cdiv(n, 8);
   if (a.uneven && !a.causal) a.run = (int)(per_unit <= 8 ? per_unit : keys && a.parts > 1 ? a.tiles : cdiv(per_unit, 8));
   if (a.run < 1) a.run = 1;
+  const int64_t units = a.causal && per_unit ? a.run / per_unit : 0;
+  a.turns = units * per_unit == a.run ? (int)units : 1;
+  a.by_run = fast_div(a.run); a.by_turns = fast_div(a.turns > 1 ? a.turns : 1); a.by_unit = fast_div(per_unit > 1 ? (uint32_t)per_unit : 1);
+  a.by_parts = fast_div(a.parts); a.by_tiles = fast_div(a.tiles > 1 ? a.tiles : 1);
   return (unsigned)(cdiv(n, 8 * (int64_t)a.run) * 8 * a.run);
 }
 
@@ -339,12 +361,10 @@ __global__ void __launch_bounds__(F_THREADS, sizeof(T) == 4 ? (DT == 128 ? 1 : 2
   __shared__ __attribute__((aligned(16))) T lds[4 * S::KC * S::W];   // keys and values, two buffers each
   constexpr int BUF = S::KC * S::W, G = sizeof(T) == 2 ? 4 : 2, GK = G < S::KS ? G : S::KS;
   constexpr bool EARLY = sizeof(T) == 2 && DT <= 64;
-  const int total = a.units * a.tiles * a.parts;
-  const int w = work_index(a);
-  if (w >= total) return;
-  const int part = w % a.parts, ut = w / a.parts, unit = ut / a.tiles;
-  const int tile = a.tiles - 1 - ut % a.tiles;   // under a causal mask the last rows see the most keys: they go first
-  const int b = unit / a.kv_heads, hk = unit % a.kv_heads;
+  Work w;
+  if (!work_of(a, w)) return;
+  const int part = w.part, unit = w.unit, b = w.b, hk = w.hk;
+  const int tile = a.tiles - 1 - w.tile;   // under a causal mask the last rows see the most keys: they go first
   const Seq s = sequence(a, b);
   const int R = s.nq * a.group, r0 = tile * F_ROWS, room = a.q_starts ? R : a.tq * a.group;
   if (r0 >= room) return;
@@ -355,6 +375,7 @@ __global__ void __launch_bounds__(F_THREADS, sizeof(T) == 4 ? (DT == 128 ? 1 : 2
   const T* kp = rows_of(a, static_cast<const T*>(a.k), b, s.k0, a.k_token, a.k_batch) + (int64_t)hk * 2 * a.dim;
   const T* vp = rows_of(a, static_cast<const T*>(a.v), b, s.k0, a.v_token, a.v_batch) + (int64_t)hk * 2 * a.dim;
   typename O::Frag qf[S::KS];
+  float lam = live ? a.lam[a.lam_token ? (s.q0 + i) * a.heads + h : h] : 0.f;
   {
     const T* qp = rows_of(a, static_cast<const T*>(a.q), b, s.q0, a.q_token, a.q_batch) + i * a.q_token + (int64_t)h * 2 * a.dim + m * a.dim;
 #pragma unroll
@@ -389,6 +410,7 @@ __global__ void __launch_bounds__(F_THREADS, sizeof(T) == 4 ? (DT == 128 ? 1 : 2
   };
 #pragma unroll
   for (int t = 0; t < S::KS; t++) arrived(qf[t]);
+  arrived(lam);
   if (begin < last) fetch(begin, 0);
   for (int j0 = begin, buf = 0; j0 < last; j0 += S::KC, buf ^= 1) {
     wait_step<0>();
@@ -472,7 +494,6 @@ __global__ void __launch_bounds__(F_THREADS, sizeof(T) == 4 ? (DT == 128 ? 1 : 2
   }
   __syncthreads();
   if (m == 1 || r >= room) return;
-  const float lam = live ? a.lam[a.lam_token ? row * a.heads + h : h] : 0.f;
   T* op = rows_of(a, static_cast<T*>(a.out), b, s.q0, a.o_token, a.o_batch) + i * a.o_token + (int64_t)h * 2 * a.dim + 4 * hh;
 #pragma unroll
   for (int t = 0; t < S::VT; t++)
@@ -485,23 +506,25 @@ __global__ void __launch_bounds__(F_THREADS, sizeof(T) == 4 ? (DT == 128 ? 1 : 2
     }
 }
 
-// Joins the parts of a row: one wave a row, bound by the latency of two rounds of loads (8 us for 256 rows of 12 parts).  Lane p holds the maximum and the sums of part p (at most 64 parts), so that the weights of all parts are
-// known before the sums are read.
+// Joins the parts of a row: one wave a row, bound by the latency of its code and of two rounds of loads (6 us for 256 rows of 12 parts).  Lane p holds the maximum and the sums of part p (at
+// most 64 parts), so that the weights of all parts are known before the sums are read.  Then a lane has four channels, and with heads of up to 64 the halves
+// of a wave take a part each.
 template <typename T>
 __global__ void __launch_bounds__(256) diff_join_kernel(DiffArgs a) {
-  const int room = a.tq * a.group;
-  const int64_t x = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  const int lane = threadIdx.x & 63, unit = (int)(x / room), r = (int)(x - (int64_t)unit * room);
-  if (unit >= a.units) return;
-  const int b = unit / a.kv_heads, hk = unit % a.kv_heads;
+  const int room = a.tq * a.group, unit = blockIdx.y, r = (int)blockIdx.x * 4 + wave_of_thread(), lane = threadIdx.x & 63;
+  if (r >= room) return;
+  const int b = quotient(unit, a.by_heads), hk = unit - b * a.kv_heads;
   const Seq s = sequence(a, b);
   const int i = query_of(a, r), h = hk * a.group + (r - i * a.group);
   const bool live = r < s.nq * a.group;
   if (!live && a.q_starts) return;
   const int64_t row = s.q0 + i, step = (int64_t)a.units * room, at = (int64_t)unit * room + r;
-  float f[2] = {0.f, 0.f}, acc[2][4] = {};
+  const bool both = a.dim <= 64;
+  const int half = both ? lane >> 5 : 0, col = 4 * (both ? lane & 31 : lane), each = both ? 2 : 1;
+  const bool in = col < 2 * a.dim;
+  float4 o[2] = {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)};
   if (live) {
-    float lse[2];
+    float f[2], lse[2];
 #pragma unroll
     for (int k = 0; k < 2; k++) {
       float4 ml = make_float4(-INFINITY, 0.f, 0.f, 0.f);
@@ -511,36 +534,32 @@ __global__ void __launch_bounds__(256) diff_join_kernel(DiffArgs a) {
       lse[k] = sum > 0.f ? top + __log2f(sum) : sum;
     }
     if (a.lse && lane < 2) a.lse[(int64_t)(lane * a.heads + h) * a.q_rows + row] = lane ? lse[1] : lse[0];
-    for (int p0 = 0; p0 < a.parts; p0 += 4) {   // (four parts' loads in flight)
-      float g[2][4], v[2][4][4];
-#pragma unroll
-      for (int q = 0; q < 4; q++) {
-        const int p = min(p0 + q, a.parts - 1);
-        const float* o = a.part + (at + p * step) * 4 * a.dim;
-#pragma unroll
-        for (int k = 0; k < 2; k++) {
-          g[k][q] = p0 + q < a.parts ? __shfl(f[k], p, 64) : 0.f;
-#pragma unroll
-          for (int e = 0; e < 4; e++) v[k][q][e] = lane + 64 * e < 2 * a.dim && p0 + q < a.parts ? o[k * 2 * a.dim + lane + 64 * e] : 0.f;
-        }
-      }
+    const float* from = a.part + (at + half * step) * 4 * a.dim + col;
+    for (int p0 = 0; p0 < a.parts; p0 += 4 * each) {   // (the loads of four or eight parts in flight)
+      float4 v[2][4];
 #pragma unroll
       for (int q = 0; q < 4; q++)
 #pragma unroll
         for (int k = 0; k < 2; k++)
+          v[k][q] = in && p0 + q * each + half < a.parts ? *reinterpret_cast<const float4*>(from + (p0 + q * each) * step * 4 * a.dim + k * 2 * a.dim) : make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-          for (int e = 0; e < 4; e++) acc[k][e] += g[k][q] * v[k][q][e];
+      for (int q = 0; q < 4; q++)
+#pragma unroll
+        for (int k = 0; k < 2; k++) {
+          const int p = p0 + q * each + half;
+          const float g = __shfl(f[k], min(p, 63), 64);   // (zero in the lanes behind the parts)
+          o[k].x += g * v[k][q].x; o[k].y += g * v[k][q].y; o[k].z += g * v[k][q].z; o[k].w += g * v[k][q].w;
+        }
     }
-  }
-  const float lam = live ? a.lam[a.lam_token ? row * a.heads + h : h] : 0.f;
-  T* op = rows_of(a, static_cast<T*>(a.out), b, s.q0, a.o_token, a.o_batch) + i * a.o_token + (int64_t)h * 2 * a.dim;
+    if (both)
 #pragma unroll
-  for (int e = 0; e < 4; e++) {
-    const int d = lane + 64 * e;
-    if (d >= 2 * a.dim) continue;
-    op[d] = Cvt<T>::st(acc[0][e] - lam * acc[1][e]);
-    if (a.o2 && live) static_cast<T*>(a.o2)[row * a.o2_token + (int64_t)h * 2 * a.dim + d] = Cvt<T>::st(acc[1][e]);
+      for (int k = 0; k < 2; k++) { o[k].x += other_half(o[k].x); o[k].y += other_half(o[k].y); o[k].z += other_half(o[k].z); o[k].w += other_half(o[k].w); }
   }
+  if (!in || half) return;
+  const float lam = live ? a.lam[a.lam_token ? row * a.heads + h : h] : 0.f;
+  T* op = rows_of(a, static_cast<T*>(a.out), b, s.q0, a.o_token, a.o_batch) + i * a.o_token + (int64_t)h * 2 * a.dim + col;
+  Ops<T>::store4(op, o[0].x - lam * o[1].x, o[0].y - lam * o[1].y, o[0].z - lam * o[1].z, o[0].w - lam * o[1].w);
+  if (a.o2 && live) Ops<T>::store4(static_cast<T*>(a.o2) + row * a.o2_token + (int64_t)h * 2 * a.dim + col, o[1].x, o[1].y, o[1].z, o[1].w);
 }
 
 // What the pass over the queries leaves of a row's map m for the pass over the keys, and dlambda.
@@ -578,11 +597,9 @@ __global__ void __launch_bounds__(256, DT * sizeof(T) <= 256 ? 2 : 1) diff_backw
   typedef QSizes<T, DT> Z;
   __shared__ __attribute__((aligned(16))) T lds[4 * S::KC * S::W];   // keys and values, two buffers each
   constexpr int BUF = S::KC * S::W, G = sizeof(T) == 2 && DT == 64 ? 4 : 2, MAPS = Z::MAPS;
-  const int total = a.units * a.tiles * a.parts;
-  const int w = work_index(a);
-  if (w >= total) return;
-  const int part = w % a.parts, ut = w / a.parts, unit = ut / a.tiles, tile = a.tiles - 1 - ut % a.tiles;
-  const int b = unit / a.kv_heads, hk = unit % a.kv_heads;
+  Work w;
+  if (!work_of(a, w)) return;
+  const int part = w.part, unit = w.unit, b = w.b, hk = w.hk, tile = a.tiles - 1 - w.tile;
   const Seq s = sequence(a, b);
   const int R = s.nq * a.group, r0 = tile * Z::ROWS, room = a.q_starts ? R : a.tq * a.group;
   if (r0 >= room) return;
@@ -756,10 +773,10 @@ __global__ void __launch_bounds__(256, DT * sizeof(T) <= 256 ? 2 : 1) diff_backw
 // Adds the parts of a row's dq and delta, always in the same order: a thread takes four channels.
 template <typename T>
 __global__ void __launch_bounds__(256) diff_join_q_kernel(DiffArgs a) {
-  const int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x, rows = (int64_t)a.tq * a.group;
-  const int quads = a.dim / 2, col = (int)(x % quads) * 4, unit = (int)(x / quads / rows), r = (int)(x / quads - unit * rows);
-  if (unit >= a.units) return;
-  const int b = unit / a.kv_heads, hk = unit % a.kv_heads;
+  const int64_t rows = (int64_t)a.tq * a.group;
+  const int x = (int)blockIdx.x * 256 + threadIdx.x, unit = blockIdx.y, r = quotient(x, a.by_quads), col = (x - r * (a.dim / 2)) * 4;
+  if (r >= rows) return;
+  const int b = quotient(unit, a.by_heads), hk = unit - b * a.kv_heads;
   const Seq s = sequence(a, b);
   const bool live = r < s.nq * a.group;
   if (!live && a.q_starts) return;
@@ -831,17 +848,13 @@ __global__ void __launch_bounds__((KvSizes<T, DT>::THREADS), sizeof(T) == 2 && D
   __shared__ __attribute__((aligned(16))) T lds[2 * NB * BUF];                         // queries and dO
   __shared__ __attribute__((aligned(16))) RowValues st[NB][43];                        // the rows' values: 32, and room for the 2048 bytes that two waves write
   __shared__ __attribute__((aligned(16))) char ex[2][Z::PAIRS][6 * 64 * FRAG];         // P_1 - lambda P_2, dS_1, dS_2 of a tile, two operands each
-  const int total = a.units * a.tiles * a.parts;
   if ((int)blockIdx.x >= a.work) {   // the workgroups behind those of the keys
     sum_lambda<Z::THREADS>(a, (int)blockIdx.x - a.work);
     return;
   }
-  const int w = work_index(a);
-  if (w >= total) return;
-  // under a causal mask the first keys are seen by the most rows; without one, workgroups that read the same rows are neighbours
-  const int per_unit = a.tiles * a.parts, unit = w / per_unit, x = w % per_unit;
-  const int part = a.causal ? x % a.parts : x / a.tiles, tile = a.causal ? x / a.parts : x % a.tiles;
-  const int b = unit / a.kv_heads, hk = unit % a.kv_heads;
+  Work w;
+  if (!work_of<true>(a, w)) return;
+  const int part = w.part, unit = w.unit, b = w.b, hk = w.hk, tile = w.tile;   // under a causal mask the first keys are seen by the most rows
   const Seq s = sequence(a, b);
   const int R = s.nq * a.group, j0 = tile * Z::KEYS, room = a.q_starts ? s.nk : a.tk;
   if (j0 >= room) return;
@@ -1035,10 +1048,9 @@ __global__ void __launch_bounds__((KvSizes<T, DT>::THREADS), sizeof(T) == 2 && D
 // Adds the parts of a key's gradients, always in the same order: a thread takes four channels.
 template <typename T>
 __global__ void __launch_bounds__(256) diff_join_kv_kernel(DiffArgs a) {
-  const int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  const int col = (int)(x % a.dim) * 4, j = (int)(x / a.dim % a.tk), unit = (int)(x / ((int64_t)a.dim * a.tk));
-  if (unit >= a.units) return;
-  const int b = unit / a.kv_heads, hk = unit % a.kv_heads;
+  const int x = (int)blockIdx.x * 256 + threadIdx.x, unit = blockIdx.y, j = quotient(x, a.by_dim), col = (x - j * a.dim) * 4;
+  if (j >= a.tk) return;
+  const int b = quotient(unit, a.by_heads), hk = unit - b * a.kv_heads;
   const Seq s = sequence(a, b);
   const bool live = j < s.nk;
   if (!live && a.q_starts) return;
@@ -1105,8 +1117,8 @@ static int check_apart(const char* what, const cd_diff_attn* d, bool out_only) {
 }
 
 // Parts of the keys that get a workgroup of their own: few rows against many keys would leave most of the chip without work.  Heads of 64, one part against
-// this rule: one query of 16 sequences and 4 key heads on up to 8192 keys 187 against 41 + 8 us (the join); 16 queries of 8 heads on 4096 keys 88
-// against 21; 4096 causal tokens of 4 heads 104 against 77; where there are rows enough (512 causal tokens of 8 heads) the rule leaves one part: 19.
+// this rule: one query of 16 sequences and 4 key heads on up to 8192 keys 187 against 41 + 6 us (the join); 16 queries of 8 heads on 4096 keys 88
+// against 16; 4096 causal tokens of 4 heads 104 against 77; where there are rows enough (512 causal tokens of 8 heads) the rule leaves one part: 19.
 static int parts_of(const cd_diff_attn* d) {
   const int64_t groups = (int64_t)d->batch * d->kv_heads * cdiv((int64_t)d->tq * (d->heads / d->kv_heads), F_ROWS);
   int64_t p = groups ? 768 / groups : 1;   // (three workgroups a compute unit: all parts at once)
@@ -1127,6 +1139,7 @@ static DiffArgs args_of(const cd_diff_attn* d) {
   a.causal = d->causal != 0; a.lam_token = d->lambda_kind == CD_LAMBDA_TOKEN; a.parts = 1;
   a.units = d->batch * d->kv_heads;
   a.uneven = d->q_lens || d->k_lens;
+  a.by_heads = fast_div(a.kv_heads); a.by_dim = fast_div(a.dim); a.by_quads = fast_div(a.dim / 2);
   a.group_inv = a.group > 1 ? (uint32_t)((1ull << 32) / a.group) + 1 : 0;
   a.scale = d->scale > 0.f ? d->scale : 1.f / sqrtf((float)d->head_dim);
   a.c = a.scale * 1.44269504088896340736f;
@@ -1149,7 +1162,7 @@ static int64_t keys_of(const cd_diff_attn* d) {
   return n;
 }
 // Parts of the rows that get a workgroup of their own in the pass that owns keys: few keys under many rows (shared key heads) leave compute units without
-// work.  Five sequences of up to 777 tokens, 8 heads of 128 on 2: one part 144 us, this rule 63 and a join of 9; both passes of 4 x 1024 causal tokens, 8
+// work.  Five sequences of up to 777 tokens, 8 heads of 128 on 2: one part 144 us, this rule 63 and a join of 8; both passes of 4 x 1024 causal tokens, 8
 // heads of 64 on 2: 203 against 102.
 static int kv_parts_of(const cd_diff_attn* d) {
   const int64_t groups = (int64_t)d->batch * d->kv_heads * cdiv(d->tk, keys_of(d)), tiles = cdiv((int64_t)d->tq * (d->heads / d->kv_heads), 32);
@@ -1231,7 +1244,7 @@ extern "C" int codistill_diff_attention(const cd_diff_attn* desc, const void* q,
     hipLaunchKernelGGL((diff_forward_kernel<typename decltype(x)::T, decltype(x)::DT>), dim3(blocks), dim3(F_THREADS), 0, s, a);
   });
   if (a.parts > 1) {
-    const dim3 grid((unsigned)cdiv((int64_t)a.units * a.tq * a.group, 4));
+    const dim3 grid((unsigned)cdiv((int64_t)a.tq * a.group, 4), (unsigned)a.units);   // (units of few workgroups: parts_of)
     if (desc->dtype == CD_BF16) hipLaunchKernelGGL((diff_join_kernel<bf16_t>), grid, dim3(256), 0, s, a);
     else hipLaunchKernelGGL((diff_join_kernel<float>), grid, dim3(256), 0, s, a);
   }
@@ -1270,7 +1283,7 @@ extern "C" int codistill_diff_attention_backward(const cd_diff_attn* desc, const
       hipLaunchKernelGGL((diff_backward_q_kernel<typename decltype(x)::T, decltype(x)::DT>), dim3(blocks), dim3(256), 0, s, a);
     });
     if (a.parts > 1) {
-      const dim3 grid((unsigned)cdiv((int64_t)a.units * a.tq * a.group * (a.dim / 2), 256));
+      const dim3 grid((unsigned)cdiv((int64_t)a.tq * a.group * (a.dim / 2), 256), (unsigned)a.units);
       if (desc->dtype == CD_BF16) hipLaunchKernelGGL((diff_join_q_kernel<bf16_t>), grid, dim3(256), 0, s, a);
       else hipLaunchKernelGGL((diff_join_q_kernel<float>), grid, dim3(256), 0, s, a);
     }
@@ -1286,7 +1299,7 @@ extern "C" int codistill_diff_attention_backward(const cd_diff_attn* desc, const
     });
   if (a.tk > 0) {
     if (a.parts > 1) {
-      const dim3 grid((unsigned)cdiv((int64_t)a.units * a.tk * a.dim, 256));
+      const dim3 grid((unsigned)cdiv((int64_t)a.tk * a.dim, 256), (unsigned)a.units);
       if (desc->dtype == CD_BF16) hipLaunchKernelGGL((diff_join_kv_kernel<bf16_t>), grid, dim3(256), 0, s, a);
       else hipLaunchKernelGGL((diff_join_kv_kernel<float>), grid, dim3(256), 0, s, a);
     }
