@@ -418,7 +418,8 @@ int codistill_diff_attention(const cd_diff_attn* desc, const void* q, const void
  * Gradients of a key head are summed over the heads that share it, in a fixed order: the same inputs give the same bits.
  *   dlambda   lambda's shape, fp32
  *   workspace at least codistill_diff_attention_workspace_bytes(desc, 1) bytes
- * Errors as above; also CD_ERR_INVALID_ARG where sequences share memory (a batch stride below the rows of a sequence), in which gradients would race.
+ * Errors as above; also CD_ERR_INVALID_ARG where sequences share memory (a batch stride below the rows of a sequence), in which gradients would race, and
+ * CD_ERR_UNSUPPORTED for a scale above 0 and below 2^-100.  Any lambda is allowed, zero and numbers below the normal ones (which count as zero) among them.
  */
 int codistill_diff_attention_backward(const cd_diff_attn* desc, const void* q, const void* k, const void* v, const float* lambda, const void* out,
                                       const void* o_second, const float* lse, const void* dout, void* dq, void* dk, void* dv, float* dlambda,

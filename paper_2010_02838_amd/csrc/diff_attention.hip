@@ -562,11 +562,15 @@ __global__ void __launch_bounds__(256) diff_join_kernel(DiffArgs a) {
   if (a.o2 && live) Ops<T>::store4(static_cast<T*>(a.o2) + row * a.o2_token + (int64_t)h * 2 * a.dim + col, o[1].x, o[1].y, o[1].z, o[1].w);
 }
 
+// What the pass over the keys takes of a row is divided by the scale: below this one the gradients are refused.
+constexpr float LEAST_SCALE = 0x1p-100f;
+
 // What the pass over the queries leaves of a row's map m for the pass over the keys, and dlambda.
 __device__ inline void leave_row(const DiffArgs& a, int64_t row, int h, int m, bool live, float lse, float delta, float lam) {
   RowValues* v = a.rows + row * a.heads + h;
-  // (a lambda of zero: far below any score, yet finite, as its parts have to be)
-  const float weight = m == 0 ? 0.f : lam == 0.f ? -1e30f : __log2f(fabsf(lam));
+  // The parts have to be finite.  A weight P_2 is at most one, so 2^-1000 of it is zero: a lambda of zero, and those below the normal numbers, which the logarithm's
+  // instruction takes for zero.  Over the least scale of this pass (LEAST_SCALE) a thousand is still far below the largest number.
+  const float weight = m == 0 ? 0.f : fabsf(lam) < 0x1p-126f ? -1000.f : __log2f(fabsf(lam));
   v->lse[m] = three_parts(live ? (weight - lse) / a.c : 0.f);
   v->delta[m] = three_parts(live ? -delta : 0.f);
   if (m == 1) {
@@ -1261,6 +1265,7 @@ extern "C" int codistill_diff_attention_backward(const cd_diff_attn* desc, const
                  aligned16(dk) && aligned16(dv) && aligned16(workspace) && ((reinterpret_cast<uintptr_t>(lambda) | reinterpret_cast<uintptr_t>(dlambda)) & 3) == 0,
              "diff_attention_backward: pointers must be 16-byte aligned, lambda and dlambda 4-byte aligned");
   if (const int rc = check_apart("diff_attention_backward", desc, false)) return rc;
+  if (desc->scale > 0.f && desc->scale < LEAST_SCALE) return set_error(CD_ERR_UNSUPPORTED, "diff_attention_backward: scale %g is below 2^-100", desc->scale);
   size_t need = 0;
   codistill_diff_attention_workspace_bytes(desc, 1, &need);
   if (workspace_bytes < need) return set_error(CD_ERR_WORKSPACE_TOO_SMALL, "diff_attention_backward: workspace of %zu bytes, %zu needed", workspace_bytes, need);
