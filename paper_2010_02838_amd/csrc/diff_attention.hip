@@ -185,7 +185,7 @@ template <typename T, int DT> struct Sizes {
   static constexpr int W = 2 * DT, KC = 32;
   static constexpr int KS = DT / 16, VT = W / 32, DTT = DT / 32;
 };
-constexpr int EXACT_KEYS = 128;   // rows that reach no more keys than this get their deltas in a pass of their own (bf16)
+constexpr int EXACT_KEYS = 128;   // waves whose first row sees no more keys than this get their deltas in a pass of their own (bf16)
 
 // ---- sequences and rows ---------------------------------------------------------------------------------------------------
 struct Seq { int nq, nk; int64_t q0, k0; };   // lengths; rows of the sequence's first query and key in their tensors
@@ -658,11 +658,13 @@ __global__ void __launch_bounds__(256, DT * sizeof(T) <= 256 ? 2 : 1) diff_backw
   const int see = live ? limit(r) : s.nk;
   const int least = limit(wr0), reach = wr0 < R ? limit(min(wr0 + 31, R - 1)) : 0;
   int begin = 0, last = r0 < R ? limit(min(r0 + Z::ROWS, R) - 1) : 0;
-  const bool two = sizeof(T) == 2 && last <= EXACT_KEYS;
-  if (a.parts > 1) {   // (few keys are one part's, so that the two passes below see all of them)
-    const int per = two ? EXACT_KEYS : (((a.tk + 31) / 32 + a.parts - 1) / a.parts) * 32;
-    begin = part * per;
-    last = min(last, begin + per);
+  // The workgroup walks its keys twice where its first row sees few (the waves whose first row does work in the first pass, which ends where the
+  // last of their rows ends).
+  const bool two = sizeof(T) == 2 && min(limit(r0), last) <= EXACT_KEYS, few = least <= EXACT_KEYS;
+  if (a.parts > 1) {   // (the keys of rows with few are one part's, so that the two passes below see all of them)
+    const int per = (((a.tk + 31) / 32 + a.parts - 1) / a.parts) * 32;
+    if (two) begin = part ? last : 0;
+    else { begin = part * per; last = min(last, begin + per); }
   }
   v16f dq[MAPS][S::DTT];
 #pragma unroll
@@ -696,14 +698,15 @@ __global__ void __launch_bounds__(256, DT * sizeof(T) <= 256 ? 2 : 1) diff_backw
         rest[m] = 0.f;
       }
     }
+    const int end = pass ? last : min(last, EXACT_KEYS + 31);   // (32 rows of a wave see up to 31 keys more than its first)
     __syncthreads();   // (the first pass may still read what is fetched anew)
-    if (begin < last) fetch(begin, 0);
-    for (int j0 = begin, buf = 0; j0 < last; j0 += S::KC, buf ^= 1) {
+    if (begin < end) fetch(begin, 0);
+    for (int j0 = begin, buf = 0; j0 < end; j0 += S::KC, buf ^= 1) {
       wait_step<0>();
-      if (j0 + S::KC < last) fetch(j0 + S::KC, buf ^ 1);
+      if (j0 + S::KC < end) fetch(j0 + S::KC, buf ^ 1);
       const T* Ks = lds + buf * BUF;
       const T* Vs = lds + (2 + buf) * BUF;
-      if (j0 < reach) {
+      if (j0 < reach && (pass || few)) {
         at.fresh();
         v16f sc[MAPS], dp;
         clear(dp);
