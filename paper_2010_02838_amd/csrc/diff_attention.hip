@@ -194,10 +194,9 @@ __device__ inline Seq sequence(const DiffArgs& a, int b) {
   if (a.q_starts) {
     const int64_t qs = min(max((int64_t)a.q_starts[b], (int64_t)0), a.q_rows), ks = min(max((int64_t)a.k_starts[b], (int64_t)0), a.k_rows);
     s.q0 = qs; s.k0 = ks;
-    s.nq = (int)min(min((int64_t)a.q_starts[b + 1], a.q_rows) - qs, (int64_t)a.tq);
-    s.nk = (int)min(min((int64_t)a.k_starts[b + 1], a.k_rows) - ks, (int64_t)a.tk);
-    s.nq = max(s.nq, 0);
-    s.nk = max(s.nk, 0);
+    // (cut in 64 bits: the difference of two table entries may pass 32)
+    s.nq = (int)max(min(min((int64_t)a.q_starts[b + 1], a.q_rows) - qs, (int64_t)a.tq), (int64_t)0);
+    s.nk = (int)max(min(min((int64_t)a.k_starts[b + 1], a.k_rows) - ks, (int64_t)a.tk), (int64_t)0);
   } else {
     s.q0 = (int64_t)b * a.tq; s.k0 = (int64_t)b * a.tk;
     s.nq = a.q_lens ? min(max(a.q_lens[b], 0), a.tq) : a.tq;

@@ -40,3 +40,19 @@ def test_rows_of_few_keys_beside_rows_of_many(dim, heads, kv_heads, keys):
     for i in range(4):
         err = np.linalg.norm(got[:, i] - want[:, i]) / np.linalg.norm(want[:, i])
         assert err <= 3e-3, (i + 2, err)
+
+
+def test_start_tables_of_extreme_values():
+    """Differences of starts that pass 32 bits (a table nobody filled): no row, and nothing is touched."""
+    low = -2 ** 31
+    p = Problem(F32, [20, 30], [20, 30], 2, 2, 32, False, True, packed=True, seed=8)
+    for starts in ([1, low, low], [2 ** 31 - 1, low, 0], [50, low, 50], [low, low, low]):
+        for t in p.desc.keep[2:]:
+            t.copy_(torch.tensor(starts, dtype=torch.int32))
+        for t in (p.out, p.dq, p.dk, p.dv, p.dlam):
+            t.fill_(7.0)
+        p.run()
+        if starts[2] <= 0:
+            assert all((t == 7.0).all() for t in (p.out, p.dq, p.dk, p.dv)) and not (p.dlam != 7.0).any()
+        for t in (p.out, p.dq, p.dk, p.dv):
+            assert torch.isfinite(t).all()
