@@ -369,7 +369,7 @@ def diff_attention_desc(q, k, v, out, lam, causal=False, scale=0.0, q_lens=None,
     """What differential attention of tensors laid out like these needs to know; kept by the caller and handed to every call.
 
     Padded: q [B, Tq, H, 2, D], k [B, Tk, Hk, 2, D], v [B, Tk, Hk, 2 D], out [B, Tq, H, 2 D], q_lens / k_lens int32 [B] or None.
-    Packed (q_starts, k_starts int32 [B + 1] and the longest sequence's max_q, max_k): the same without the batch dimension.
+    Packed (q_starts, k_starts int32 [B + 1] and the longest sequence's max_q, max_k, both): the same without the batch dimension.
     lam: fp32 [H], or [B, Tq, H] / [rows, H].  Tokens and sequences may be strided, the channels of a token are contiguous."""
     packed = q_starts is not None or k_starts is not None
     off = 0 if packed else 1

@@ -1091,6 +1091,8 @@ static int check(const char* what, const cd_diff_attn* d) {
   CD_REQUIRE(!d->q_starts || (d->q_rows >= 0 && d->k_rows >= 0 && d->q_rows <= INT32_MAX && d->k_rows <= INT32_MAX), "%s: q_rows=%lld k_rows=%lld", what,
              (long long)d->q_rows, (long long)d->k_rows);
   CD_REQUIRE(d->tq >= 0 && d->tk >= 0, "%s: tq=%d tk=%d", what, d->tq, d->tk);
+  CD_REQUIRE(!d->q_starts || ((d->tq >= 1 || d->q_rows == 0) && (d->tk >= 1 || d->k_rows == 0)), "%s: packed rows and no longest sequence (tq=%d tk=%d)", what, d->tq,
+             d->tk);
   const int64_t group = d->heads / d->kv_heads;
   CD_REQUIRE(group <= 1024 && d->tq * group <= (1 << 30) / group, "%s: tq=%d with %lld heads a key head is too long", what, d->tq, (long long)group);
   CD_REQUIRE((int64_t)d->batch * d->kv_heads * (cdiv(d->tq * group, F_ROWS) + cdiv(d->tk, 64) + 1) < (1 << 30) && (int64_t)d->batch * d->tq <= INT32_MAX,
