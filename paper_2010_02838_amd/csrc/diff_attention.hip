@@ -1078,6 +1078,9 @@ __global__ void __launch_bounds__(256) diff_join_kv_kernel(DiffArgs a) {
 // ---- host ----------------------------------------------------------------------------------------------------------------------------
 static int elem_of(const cd_diff_attn* d) { return d->dtype == CD_BF16 ? 2 : 4; }
 static int64_t rows_q(const cd_diff_attn* d) { return d->q_starts ? d->q_rows : (int64_t)d->batch * d->tq; }
+static int64_t rows_k(const cd_diff_attn* d) { return d->k_starts ? d->k_rows : (int64_t)d->batch * d->tk; }
+// whether lambda (or its gradient) has an element
+static bool has_lambda(const cd_diff_attn* d) { return d->lambda_kind == CD_LAMBDA_HEAD || rows_q(d) > 0; }
 
 static int check(const char* what, const cd_diff_attn* d) {
   CD_REQUIRE(d != nullptr, "%s: NULL pointer argument", what);
@@ -1142,7 +1145,7 @@ static DiffArgs args_of(const cd_diff_attn* d) {
   a.q_token = d->q_token; a.q_batch = d->q_batch; a.k_token = d->k_token; a.k_batch = d->k_batch;
   a.v_token = d->v_token; a.v_batch = d->v_batch; a.o_token = d->o_token; a.o_batch = d->o_batch; a.o2_token = 2LL * d->heads * d->head_dim;
   a.q_lens = d->q_lens; a.k_lens = d->k_lens; a.q_starts = d->q_starts; a.k_starts = d->k_starts;
-  a.q_rows = rows_q(d); a.k_rows = d->q_starts ? d->k_rows : (int64_t)d->batch * d->tk;
+  a.q_rows = rows_q(d); a.k_rows = rows_k(d);
   a.batch = d->batch; a.tq = d->tq; a.tk = d->tk; a.heads = d->heads; a.kv_heads = d->kv_heads; a.group = d->heads / d->kv_heads; a.dim = d->head_dim;
   a.causal = d->causal != 0; a.lam_token = d->lambda_kind == CD_LAMBDA_TOKEN; a.parts = 1;
   a.units = d->batch * d->kv_heads;
@@ -1228,7 +1231,7 @@ extern "C" int codistill_diff_attention_workspace_bytes(const cd_diff_attn* desc
 extern "C" int codistill_diff_attention(const cd_diff_attn* desc, const void* q, const void* k, const void* v, const float* lambda, void* out,
                                         void* o_second, float* lse, void* workspace, size_t workspace_bytes, void* stream) {
   if (const int rc = check("diff_attention", desc)) return rc;
-  CD_REQUIRE(q && k && v && lambda && out, "diff_attention: NULL pointer argument");
+  CD_REQUIRE(((q && out) || rows_q(desc) == 0) && ((k && v) || rows_k(desc) == 0) && (lambda || !has_lambda(desc)), "diff_attention: NULL pointer argument");
   CD_REQUIRE((o_second != nullptr) == (lse != nullptr), "diff_attention: o_second and lse are kept together or not at all");
   CD_REQUIRE(aligned16(q) && aligned16(k) && aligned16(v) && aligned16(out) && aligned16(o_second) && aligned16(lse) && aligned16(workspace) &&
                  (reinterpret_cast<uintptr_t>(lambda) & 3) == 0,
@@ -1263,7 +1266,8 @@ extern "C" int codistill_diff_attention_backward(const cd_diff_attn* desc, const
                                                  const void* o_second, const float* lse, const void* dout, void* dq, void* dk, void* dv, float* dlambda,
                                                  void* workspace, size_t workspace_bytes, void* stream) {
   if (const int rc = check("diff_attention_backward", desc)) return rc;
-  CD_REQUIRE(q && k && v && lambda && out && o_second && lse && dout && dq && dk && dv && dlambda && (workspace || rows_q(desc) == 0),
+  CD_REQUIRE(((q && out && o_second && lse && dout && dq) || rows_q(desc) == 0) && ((k && v && dk && dv) || rows_k(desc) == 0) &&
+                 ((lambda && dlambda) || !has_lambda(desc)),
              "diff_attention_backward: NULL pointer argument");
   CD_REQUIRE(aligned16(q) && aligned16(k) && aligned16(v) && aligned16(out) && aligned16(o_second) && aligned16(lse) && aligned16(dout) && aligned16(dq) &&
                  aligned16(dk) && aligned16(dv) && aligned16(workspace) && ((reinterpret_cast<uintptr_t>(lambda) | reinterpret_cast<uintptr_t>(dlambda)) & 3) == 0,
@@ -1272,6 +1276,7 @@ extern "C" int codistill_diff_attention_backward(const cd_diff_attn* desc, const
   if (desc->scale > 0.f && desc->scale < LEAST_SCALE) return set_error(CD_ERR_UNSUPPORTED, "diff_attention_backward: scale %g is below 2^-100", desc->scale);
   size_t need = 0;
   codistill_diff_attention_workspace_bytes(desc, 1, &need);
+  CD_REQUIRE(workspace || need == 0, "diff_attention_backward: NULL pointer argument");
   if (workspace_bytes < need) return set_error(CD_ERR_WORKSPACE_TOO_SMALL, "diff_attention_backward: workspace of %zu bytes, %zu needed", workspace_bytes, need);
   DiffArgs a = args_of(desc);
   a.q = q; a.k = k; a.v = v; a.lam = lambda; a.out = const_cast<void*>(out); a.o2 = const_cast<void*>(o_second); a.lse = const_cast<float*>(lse);

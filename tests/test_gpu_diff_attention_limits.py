@@ -56,3 +56,32 @@ def test_start_tables_of_extreme_values():
             assert all((t == 7.0).all() for t in (p.out, p.dq, p.dk, p.dv)) and not (p.dlam != 7.0).any()
         for t in (p.out, p.dq, p.dk, p.dv):
             assert torch.isfinite(t).all()
+
+
+def empty_case(dtype, batch, tq, tk, packed=False):
+    """Outputs that begin as 7, of sequences without queries, without keys or without either."""
+    from paper_2010_02838_amd import binding as B
+    H, K, D = 4, 2, 32
+    lead = (lambda n: (n,)) if packed else (lambda n: (batch, n))
+    gen = torch.Generator(device=DEV).manual_seed(7)
+    new = lambda n, *s: torch.randn(*lead(n), *s, generator=gen, device=DEV).to(dtype)   # noqa: E731
+    q, k, v, dout = new(tq, H, 2, D), new(tk, K, 2, D), new(tk, K, 2 * D), new(tq, H, 2 * D)
+    out, dq, dk, dv = (torch.full_like(t, 7.0) for t in (dout, q, k, v))
+    lam, dlam = torch.rand(H, generator=gen, device=DEV), torch.full((H,), 7.0, device=DEV)
+    zero = torch.zeros(batch + 1, dtype=torch.int32, device=DEV)
+    starts = dict(q_starts=zero, k_starts=zero, max_q=tq, max_k=tk) if packed else {}
+    desc = B.diff_attention_desc(q, k, v, out, lam, **starts)
+    o2, lse = torch.empty(out.shape, dtype=dtype, device=DEV), torch.empty(desc.lse_shape, device=DEV)
+    ws = torch.empty(B.diff_attention_workspace_bytes(desc, True), dtype=torch.uint8, device=DEV)
+    B.codistill_diff_attention(desc, q, k, v, lam, out, o2, lse, ws)
+    B.codistill_diff_attention_backward(desc, q, k, v, lam, out, o2, lse, dout, dq, dk, dv, dlam, ws)
+    torch.cuda.synchronize()
+    return out, dq, dk, dv, dlam
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_no_keys_and_no_queries(dtype):
+    """Empty tensors have no address.  Without keys the outputs and the queries' gradients are zero, without queries the keys' are; lambda's always."""
+    for batch, tq, tk, packed in ((2, 5, 0, False), (2, 0, 5, False), (1, 0, 700, False), (2, 0, 0, False), (2, 0, 0, True)):
+        for t in empty_case(dtype, batch, tq, tk, packed):
+            assert not t.any(), (batch, tq, tk, packed)

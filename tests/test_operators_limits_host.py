@@ -23,3 +23,21 @@ def test_packed_rows_need_the_longest_sequence(kw):
     assert B.lib.codistill_diff_attention_workspace_bytes(ctypes.byref(attn(**dict(packed, **kw))), 0, ctypes.byref(ctypes.c_size_t())) == BAD
     none = dict(packed, q_rows=0 if "tq" in kw else 20, k_rows=0 if "tk" in kw else 24)
     assert B.lib.codistill_diff_attention_workspace_bytes(ctypes.byref(attn(**dict(none, **kw))), 0, ctypes.byref(ctypes.c_size_t())) == B.CD_OK
+
+
+def test_tensors_without_rows_have_no_address():
+    """NULL is refused for a tensor that has rows, and for no other (the workspace check behind it is what answers)."""
+    small = B.CD_ERR_WORKSPACE_TOO_SMALL
+    keys, queries = dict(k=None, v=None), dict(q=None, out=None, o2=None, lse=None)
+    assert backward(attn(tk=0), room=0, **keys, dk=None, dv=None) == small
+    assert backward(attn(), room=0, **keys, dk=None, dv=None) == BAD
+    # without queries nothing is kept for them, and with few keys no workspace is needed
+    assert forward(attn(tq=0), **queries) == B.CD_OK
+    assert forward(attn(), **queries) == BAD
+    token = dict(lambda_kind=B.CD_LAMBDA_TOKEN)
+    assert forward(attn(tq=0, **token), lam=None, **queries) == B.CD_OK and forward(attn(tq=0), lam=None, **queries) == BAD
+    assert backward(attn(tq=0, **token), lam=None, dlam=None, dk=None, **{k: None for k in ("q", "out", "o2", "lse", "dout", "dq", "ws")}) == BAD   # (dk has rows)
+    # a workspace that is claimed and not there
+    assert backward(attn(), ws=None) == BAD
+    d = attn(q_starts=4096, k_starts=4096, q_rows=0, k_rows=4096, batch=1, tq=4096, tk=64)
+    assert B.diff_attention_workspace_bytes(d, True) > 0 and backward(d, ws=None) == BAD
