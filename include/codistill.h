@@ -397,7 +397,7 @@ int codistill_rotary(const cd_rotary* rope, const int32_t* positions, int64_t to
  *   workspace  at least codistill_diff_attention_workspace_bytes(desc, 0) bytes (may be 0: then NULL is fine)
  * q rows: batch * tq when padded (row b * tq + i), q_rows when packed.  Tensors without rows may be NULL.
  * Errors (nothing launched): CD_ERR_INVALID_ARG: NULL or misaligned pointers (16 bytes; q_lens, starts and lambda 4), sizes < 1 (tq or tk 0 are
- * allowed with padded sequences, and with packed ones that have no rows), heads no multiple of kv_heads, strides that are no multiple of 16 bytes or shorter than a token, one of the start
+ * allowed with padded sequences, and with packed ones that have no rows), heads no multiple of kv_heads, strides that are no multiple of 16 bytes or shorter than a token, sequences of out that share memory, one of the start
  * tables alone, starts together with lens, scale < 0 or not finite; CD_ERR_UNSUPPORTED: other head dims, a token stride
  * above 2^27 bytes; CD_ERR_WORKSPACE_TOO_SMALL.
  */
@@ -418,7 +418,8 @@ int codistill_diff_attention(const cd_diff_attn* desc, const void* q, const void
  * Gradients of a key head are summed over the heads that share it, in a fixed order: the same inputs give the same bits.
  *   dlambda   lambda's shape, fp32
  *   workspace at least codistill_diff_attention_workspace_bytes(desc, 1) bytes
- * Errors as above; also CD_ERR_INVALID_ARG where sequences share memory (a batch stride below the rows of a sequence), in which gradients would race, and
+ * Errors as above; also CD_ERR_INVALID_ARG where sequences share memory, in which gradients would race (they lie one behind the other, or, time-major, all of a
+ * token's inside its stride), and
  * CD_ERR_UNSUPPORTED for a scale above 0 and below 2^-100.  Any lambda is allowed, zero and numbers below the normal ones (which count as zero) among them.
  */
 int codistill_diff_attention_backward(const cd_diff_attn* desc, const void* q, const void* k, const void* v, const float* lambda, const void* out,

@@ -1116,13 +1116,15 @@ static int check(const char* what, const cd_diff_attn* d) {
   return CD_OK;
 }
 
-// sequences that lie apart: a batch stride of at least their rows
+// Sequences that lie apart: one behind the other, or all of a token's sequences inside its stride (time-major).
 static int check_apart(const char* what, const cd_diff_attn* d, bool out_only) {
   if (d->q_starts || d->batch == 1) return CD_OK;
   const int64_t batches[4] = {d->o_batch, d->q_batch, d->k_batch, d->v_batch}, tokens[4] = {d->o_token, d->q_token, d->k_token, d->v_token};
   for (int t = 0; t < (out_only ? 1 : 4); t++) {
-    const int64_t rows = t < 2 ? d->tq : d->tk;
-    CD_REQUIRE(batches[t] >= rows * tokens[t] || rows == 0, "%s: the sequences that are written share memory (batch stride %lld)", what, (long long)batches[t]);
+    const int64_t rows = t < 2 ? d->tq : d->tk, width = 2LL * d->head_dim * (t < 2 ? d->heads : d->kv_heads);
+    const bool apart = batches[t] >= width && (batches[t] - width >= (rows - 1) * tokens[t] || (tokens[t] - width) / (d->batch - 1) >= batches[t]);
+    CD_REQUIRE(apart || rows == 0, "%s: the sequences that are written share memory (batch stride %lld, token stride %lld)", what, (long long)batches[t],
+               (long long)tokens[t]);
   }
   return CD_OK;
 }

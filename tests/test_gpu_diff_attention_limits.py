@@ -85,3 +85,27 @@ def test_no_keys_and_no_queries(dtype):
     for batch, tq, tk, packed in ((2, 5, 0, False), (2, 0, 5, False), (1, 0, 700, False), (2, 0, 0, False), (2, 0, 0, True)):
         for t in empty_case(dtype, batch, tq, tk, packed):
             assert not t.any(), (batch, tq, tk, packed)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_time_major_sequences(dtype):
+    """[time][batch][heads ...]: sequences whose rows alternate do not share memory.  The same numbers in rows of their own give the same bits."""
+    from paper_2010_02838_amd import binding as B
+    T, n, H, K, D = 70, 3, 4, 2, 32
+    gen = torch.Generator(device=DEV).manual_seed(3)
+    lens = torch.tensor([70, 1, 33], dtype=torch.int32, device=DEV)
+    lam = torch.rand(H, generator=gen, device=DEV)
+    shapes = ((H, 2, D), (K, 2, D), (K, 2 * D), (H, 2 * D))
+    src = [torch.randn(T, n, *s, generator=gen, device=DEV).to(dtype) for s in shapes]
+    runs = []
+    for lay in (lambda t: t.transpose(0, 1), lambda t: t.transpose(0, 1).contiguous()):
+        q, k, v, dout = (lay(t.clone()) for t in src)
+        out, dq, dk, dv = (torch.full_like(t, 7.0) for t in (dout, q, k, v))
+        assert out.stride() == dout.stride() and dk.stride() == k.stride()
+        o2, lse, dlam = torch.empty(n, T, H, 2 * D, dtype=dtype, device=DEV), torch.empty(2, H, n * T, device=DEV), torch.empty_like(lam)
+        desc = B.diff_attention_desc(q, k, v, out, lam, causal=True, q_lens=lens, k_lens=lens)
+        ws = torch.empty(B.diff_attention_workspace_bytes(desc, True), dtype=torch.uint8, device=DEV)
+        B.codistill_diff_attention(desc, q, k, v, lam, out, o2, lse, ws)
+        B.codistill_diff_attention_backward(desc, q, k, v, lam, out, o2, lse, dout, dq, dk, dv, dlam, ws)
+        runs.append((out, dq, dk, dv, dlam))
+    assert all(torch.equal(a, b) for a, b in zip(*runs)) and not (runs[0][0] == 7.0).all(-1).any()

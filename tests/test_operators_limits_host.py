@@ -41,3 +41,19 @@ def test_tensors_without_rows_have_no_address():
     assert backward(attn(), ws=None) == BAD
     d = attn(q_starts=4096, k_starts=4096, q_rows=0, k_rows=4096, batch=1, tq=4096, tk=64)
     assert B.diff_attention_workspace_bytes(d, True) > 0 and backward(d, ws=None) == BAD
+
+
+def test_sequences_that_share_memory_and_those_that_do_not():
+    """q, out: 10 tokens of 512 elements, two sequences; one behind the other, the last token without its gap, time-major, and what overlaps.  (The workspace
+    check behind it answers where they lie apart.)"""
+    small = B.CD_ERR_WORKSPACE_TOO_SMALL
+    for token, batch, ok in ((512, 5120, True), (1024, 9 * 1024 + 512, True), (1024, 9 * 1024 + 504, False), (1024, 512, True), (1536, 1024, True), (1024, 504, False),
+                             (1016, 512, False), (512, 0, False), (1024, 520, False), (512, 4608, False)):
+        for name in ("q", "o"):
+            d = attn(**{name + "_token": token, name + "_batch": batch})
+            assert backward(d, room=0) == (small if ok else BAD), (name, token, batch)
+            if not ok:
+                assert b"share memory" in B.lib.codistill_last_error()
+                assert forward(d, q=None) == BAD
+        three = attn(batch=3, q_token=token, q_batch=batch, o_batch=1 << 20, k_batch=1 << 20, v_batch=1 << 20)
+        assert backward(three, room=0) == (small if ok and (batch >= 512 * 9 or token >= 512 + 2 * batch) else BAD), (token, batch)
