@@ -456,8 +456,8 @@ def head_norm_workspace_bytes(rows, heads, width):
 
 def codistill_head_norm(x, gain, y, eps=1e-5, post=1.0):
     """y = post gain x / sqrt(mean(x^2) + eps) over the last dimension of x [rows, heads, width]."""
-    if x.shape != y.shape or gain.shape != x.shape[2:] or y.dtype is not x.dtype or gain.dtype is not x.dtype:
-        raise ValueError("head_norm: x and y are [rows, heads, width], gain [width], all of one type")
+    if x.shape != y.shape or gain.shape != x.shape[2:] or y.dtype is not x.dtype or gain.dtype is not x.dtype or not gain.is_contiguous():
+        raise ValueError("head_norm: x and y are [rows, heads, width], gain contiguous [width], all of one type")
     _check(lib.codistill_head_norm(_dtype(x), x.data_ptr(), _inner(x, 2, "head_norm")[0], gain.data_ptr(), y.data_ptr(), _inner(y, 2, "head_norm")[0], *x.shape, eps, post,
                                    _stream_ptr()))
 
@@ -466,8 +466,8 @@ def codistill_head_norm_backward(x, gain, dy, dx, dgain, workspace, eps=1e-5, po
     """dx (may be dy) and dgain (fp32 [width]) of codistill_head_norm."""
     if x.shape != dy.shape or x.shape != dx.shape or gain.shape != x.shape[2:] or dgain.shape != gain.shape:
         raise ValueError("head_norm_backward: x, dy and dx are [rows, heads, width], gain and dgain [width]")
-    if any(t.dtype is not x.dtype for t in (gain, dy, dx)) or dgain.dtype is not torch.float32:
-        raise ValueError("head_norm_backward: one type, dgain fp32")
+    if any(t.dtype is not x.dtype for t in (gain, dy, dx)) or dgain.dtype is not torch.float32 or not (gain.is_contiguous() and dgain.is_contiguous()):
+        raise ValueError("head_norm_backward: one type, dgain fp32, gain and dgain contiguous")
     _check(lib.codistill_head_norm_backward(_dtype(x), _ptr(x), _inner(x, 2, "head_norm")[0], _ptr(gain), _ptr(dy), _inner(dy, 2, "head_norm")[0], _ptr(dx),
                                             _inner(dx, 2, "head_norm")[0], _ptr(dgain), x.shape[0], x.shape[1], x.shape[2], eps, post, _ptr(workspace),
                                             _room(workspace), _stream_ptr()))

@@ -57,3 +57,14 @@ def test_sequences_that_share_memory_and_those_that_do_not():
                 assert forward(d, q=None) == BAD
         three = attn(batch=3, q_token=token, q_batch=batch, o_batch=1 << 20, k_batch=1 << 20, v_batch=1 << 20)
         assert backward(three, room=0) == (small if ok and (batch >= 512 * 9 or token >= 512 + 2 * batch) else BAD), (token, batch)
+
+
+def test_head_norm_gains_are_contiguous():
+    """The kernels take gain and dgain as `width` elements in a row."""
+    x, gain, dgain, ws = torch.zeros(2, 3, 8), torch.ones(8), torch.zeros(8), torch.empty(1 << 16, dtype=torch.uint8)
+    wide = torch.ones(8, 2)[:, 0]
+    with pytest.raises(ValueError):
+        B.codistill_head_norm(x, wide, x.clone())
+    for g, dg in ((wide, dgain), (gain, wide), (gain[:1].expand(8), dgain)):
+        with pytest.raises(ValueError):
+            B.codistill_head_norm_backward(x, g, x.clone(), x.clone(), dg, ws)
