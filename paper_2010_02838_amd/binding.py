@@ -484,6 +484,9 @@ def adamw_table(tensors, state_bits, grad_dtype):
 
 
 def codistill_adamw_step(plan, table, lr, t, beta1=0.9, beta2=0.999, eps=1e-8, seed=0, grad_scale=None):
+    """grad_scale: fp32 device tensor of one element, or None."""
+    if grad_scale is not None and (grad_scale.dtype is not torch.float32 or grad_scale.numel() != 1):
+        raise ValueError("adamw: grad_scale is an fp32 tensor of one element")
     cfg = AdamwCfg(lr, beta1, beta2, eps, int(t), seed & 0xffffffff)
     _check(lib.codistill_adamw_step(ctypes.byref(plan), _ptr(table), ctypes.byref(cfg), _ptr(grad_scale), _stream_ptr()))
 

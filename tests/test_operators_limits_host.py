@@ -6,6 +6,7 @@ import pytest
 import torch
 
 from paper_2010_02838_amd import binding as B
+from paper_2010_02838_amd.adamw import AdamW
 from test_operators_host import BAD, UNSUPPORTED, at, attn, backward, forward
 
 
@@ -68,3 +69,11 @@ def test_head_norm_gains_are_contiguous():
     for g, dg in ((wide, dgain), (gain, wide), (gain[:1].expand(8), dgain)):
         with pytest.raises(ValueError):
             B.codistill_head_norm_backward(x, g, x.clone(), x.clone(), dg, ws)
+
+
+def test_adamw_grad_scale_is_one_fp32_element():
+    """The kernel reads four bytes: of a bf16 or float64 factor they would be another number."""
+    opt = AdamW([torch.zeros(8)], [torch.zeros(8)])
+    for bad in (torch.ones(1, dtype=torch.bfloat16), torch.ones((), dtype=torch.float64), torch.ones(2), torch.ones(0)):
+        with pytest.raises(ValueError):
+            opt.step(1e-3, 1, grad_scale=bad)
