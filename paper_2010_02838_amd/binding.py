@@ -392,8 +392,8 @@ def diff_attention_desc(q, k, v, out, lam, causal=False, scale=0.0, q_lens=None,
                  q_rows=q.shape[0] if packed else 0, k_rows=k.shape[0] if packed else 0)
     for name, t, inner in (("q", q, 3), ("k", k, 3), ("v", v, 2), ("o", out, 2)):
         s = _inner(t, inner, "diff_attention")
-        least = t.shape[off + 1] * 2 * dim   # (the stride of a dimension of one element says nothing)
-        setattr(d, name + "_token", s[-1] if t.shape[off] > 1 else max(s[-1], least))
+        # (the stride of a dimension of one element says nothing)
+        setattr(d, name + "_token", s[-1] if t.shape[off] > 1 else t.shape[off + 1] * 2 * dim)
         setattr(d, name + "_batch", s[0] if off and batch > 1 else 0)
     for name, t in (("q_lens", q_lens), ("k_lens", k_lens), ("q_starts", q_starts), ("k_starts", k_starts)):
         if t is not None:
@@ -407,7 +407,8 @@ def diff_attention_desc(q, k, v, out, lam, causal=False, scale=0.0, q_lens=None,
 def _laid_out(desc, tensors):
     """The kernels go by the descriptor: a tensor of another shape, stride or type would be read beyond its end."""
     for t, want in zip(tensors, desc.layout):
-        if (t.shape, t.stride(), t.dtype) != want:
+        if (t.shape, t.stride(), t.dtype) != want and ((t.shape, t.dtype) != (want[0], want[2]) or any(
+                n > 1 and x != y for n, x, y in zip(t.shape, t.stride(), want[1]))):
             raise ValueError("diff_attention: a tensor of shape %s, strides %s, %s where the descriptor has %s, %s, %s" % (
                 tuple(t.shape), t.stride(), t.dtype, tuple(want[0]), want[1], want[2]))
 

@@ -77,3 +77,19 @@ def test_adamw_grad_scale_is_one_fp32_element():
     for bad in (torch.ones(1, dtype=torch.bfloat16), torch.ones((), dtype=torch.float64), torch.ones(2), torch.ones(0)):
         with pytest.raises(ValueError):
             opt.step(1e-3, 1, grad_scale=bad)
+
+
+def test_strides_of_one_token_say_nothing():
+    """Single tokens: the stride of their dimension is whatever the tensor was cut from."""
+    q, k, v, lam = torch.zeros(3, 1, 4, 2, 16), torch.zeros(3, 7, 2, 2, 16), torch.zeros(3, 7, 2, 32), torch.zeros(4)
+    plain, cut, odd = torch.zeros(3, 1, 4, 32), torch.zeros(1, 3, 4, 32).transpose(0, 1), torch.zeros(3 * 131).as_strided((3, 1, 4, 32), (128, 131, 32, 1))
+    for out in (plain, cut, odd):
+        d = B.diff_attention_desc(q, k, v, out, lam)
+        assert (d.o_token, d.o_batch) == (128, 128)
+        p = {n: at(i + 1) for i, n in enumerate(("q", "k", "v", "lam", "out", "o2", "lse", "dout", "dq", "dk", "dv", "dlam", "ws"))}
+        assert B.lib.codistill_diff_attention_backward(ctypes.byref(d), *p.values(), 0, None) == B.CD_ERR_WORKSPACE_TOO_SMALL
+        for other in (plain, cut, odd):
+            B._laid_out(d, (q, k, v, other, lam))
+        for other in (torch.zeros(3, 1, 8, 32)[:, :, :4], torch.zeros(3, 2, 4, 32)[:, :1], plain.bfloat16()):
+            with pytest.raises(ValueError):
+                B._laid_out(d, (q, k, v, other, lam))
