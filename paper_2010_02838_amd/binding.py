@@ -373,6 +373,8 @@ def diff_attention_desc(q, k, v, out, lam, causal=False, scale=0.0, q_lens=None,
     lam: fp32 [H], or [B, Tq, H] / [rows, H].  Tokens and sequences may be strided, the channels of a token are contiguous."""
     packed = q_starts is not None or k_starts is not None
     off = 0 if packed else 1
+    if (q_starts is None) != (k_starts is None):
+        raise ValueError("diff_attention: one of q_starts and k_starts without the other")
     if q.dim() != 4 + off or k.dim() != 4 + off or v.dim() != 3 + off or out.dim() != 3 + off or q.shape[-2] != 2 or k.shape[-2] != 2:
         raise ValueError("diff_attention: q, k are [.., heads, 2, head_dim], v and out [.., heads, 2 head_dim]")
     dim, heads, kv_heads = q.shape[-1], q.shape[off + 1], k.shape[off + 1]
@@ -385,8 +387,8 @@ def diff_attention_desc(q, k, v, out, lam, causal=False, scale=0.0, q_lens=None,
         raise ValueError("diff_attention: lambda is [heads] or one for each query and head")
     batch = q_starts.numel() - 1 if packed else q.shape[0]
     for t, n in ((q_lens, batch), (k_lens, batch), (q_starts, batch + 1), (k_starts, batch + 1)):
-        if t is not None and (t.dtype is not torch.int32 or t.numel() != n or not t.is_contiguous()):
-            raise ValueError("diff_attention: lens are int32 [batch], starts int32 [batch + 1]")
+        if t is not None and (t.dtype is not torch.int32 or t.numel() != n or not t.is_contiguous() or t.device != q.device):
+            raise ValueError("diff_attention: lens are int32 [batch], starts int32 [batch + 1], on the queries' device")
     d = DiffAttn(dtype=_dtype(q), batch=batch, tq=max_q if packed else q.shape[1], tk=max_k if packed else k.shape[1], heads=heads, kv_heads=kv_heads,
                  head_dim=dim, causal=int(causal), lambda_kind=CD_LAMBDA_HEAD if lam.dim() == 1 else CD_LAMBDA_TOKEN, scale=scale,
                  q_rows=q.shape[0] if packed else 0, k_rows=k.shape[0] if packed else 0)

@@ -93,3 +93,18 @@ def test_strides_of_one_token_say_nothing():
         for other in (torch.zeros(3, 1, 8, 32)[:, :, :4], torch.zeros(3, 2, 4, 32)[:, :1], plain.bfloat16()):
             with pytest.raises(ValueError):
                 B._laid_out(d, (q, k, v, other, lam))
+
+
+def test_tables_lie_where_the_queries_do():
+    """(A table in host memory would be read by the kernels.)"""
+    q, k, v, out = torch.zeros(2, 5, 4, 2, 16), torch.zeros(2, 7, 2, 2, 16), torch.zeros(2, 7, 2, 32), torch.zeros(2, 5, 4, 32)
+    lam, table = torch.zeros(4), torch.zeros(3, dtype=torch.int32)
+    for kw in (dict(q_lens=table[:2]), dict(k_lens=table[:2])):
+        B.diff_attention_desc(q, k, v, out, lam, **kw)
+        with pytest.raises(ValueError):
+            B.diff_attention_desc(q, k, v, out, lam, **{n: t.to("meta") for n, t in kw.items()})
+    packed = [t.flatten(0, 1) for t in (q, k, v, out)] + [lam]
+    B.diff_attention_desc(*packed, q_starts=table, k_starts=table, max_q=5, max_k=7)
+    for kw in (dict(q_starts=table), dict(k_starts=table), dict(q_starts=table, k_starts=table.to("meta")), dict(q_starts=table.to("meta"), k_starts=table)):
+        with pytest.raises(ValueError):
+            B.diff_attention_desc(*packed, **kw, max_q=5, max_k=7)
