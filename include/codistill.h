@@ -397,7 +397,7 @@ int codistill_rotary(const cd_rotary* rope, const int32_t* positions, int64_t to
  *   workspace  at least codistill_diff_attention_workspace_bytes(desc, 0) bytes (may be 0: then NULL is fine)
  * q rows: batch * tq when padded (row b * tq + i), q_rows when packed.  Tensors without rows may be NULL.
  * Errors (nothing launched): CD_ERR_INVALID_ARG: NULL or misaligned pointers (16 bytes; q_lens, starts and lambda 4), sizes < 1 (tq or tk 0 are
- * allowed with padded sequences, and with packed ones that have no rows), heads no multiple of kv_heads, strides that are no multiple of 16 bytes or shorter than a token, sequences of out that share memory, one of the start
+ * allowed with padded sequences, and with packed ones that have no rows), heads no multiple of kv_heads or above 65536, strides that are no multiple of 16 bytes or shorter than a token, sequences of out that share memory, one of the start
  * tables alone, starts together with lens, scale < 0 or not finite; CD_ERR_UNSUPPORTED: other head dims, a token stride
  * above 2^27 bytes; CD_ERR_WORKSPACE_TOO_SMALL.
  */

@@ -1096,6 +1096,7 @@ static int check(const char* what, const cd_diff_attn* d) {
   CD_REQUIRE(d->tq >= 0 && d->tk >= 0, "%s: tq=%d tk=%d", what, d->tq, d->tk);
   CD_REQUIRE(!d->q_starts || ((d->tq >= 1 || d->q_rows == 0) && (d->tk >= 1 || d->k_rows == 0)), "%s: packed rows and no longest sequence (tq=%d tk=%d)", what, d->tq,
              d->tk);
+  CD_REQUIRE(d->heads <= 65536, "%s: heads=%d above 65536", what, d->heads);   // (the row values of a tile, 31 rows of all heads apart, are addressed with 32 bits)
   const int64_t group = d->heads / d->kv_heads;
   CD_REQUIRE(group <= 1024 && d->tq * group <= (1 << 30) / group, "%s: tq=%d with %lld heads a key head is too long", what, d->tq, (long long)group);
   CD_REQUIRE((int64_t)d->batch * d->kv_heads * (cdiv(d->tq * group, F_ROWS) + cdiv(d->tk, 64) + 1) < (1 << 30) && (int64_t)d->batch * d->tq <= INT32_MAX,

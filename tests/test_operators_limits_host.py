@@ -108,3 +108,10 @@ def test_tables_lie_where_the_queries_do():
     for kw in (dict(q_starts=table), dict(k_starts=table), dict(q_starts=table, k_starts=table.to("meta")), dict(q_starts=table.to("meta"), k_starts=table)):
         with pytest.raises(ValueError):
             B.diff_attention_desc(*packed, **kw, max_q=5, max_k=7)
+
+
+def test_number_of_heads():
+    """What the keys' pass reads of a tile's rows lies up to 31 tokens of all heads apart, 48 bytes each: in 32 bits up to a million heads."""
+    for heads, rc in ((65536, B.CD_OK), (65544, BAD), (1500000, BAD)):
+        wide = dict(heads=heads, kv_heads=heads, head_dim=8, batch=1, **{n + "_token": 16 * heads for n in ("q", "k", "v", "o")})
+        assert B.lib.codistill_diff_attention_workspace_bytes(ctypes.byref(attn(**wide)), 1, ctypes.byref(ctypes.c_size_t())) == rc, heads
