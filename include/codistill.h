@@ -345,7 +345,7 @@ int codistill_adam_step(float* master_w, float* exp_avg, float* exp_avg_sq, cons
  *     positions[axis[p]][token] * freq[p]        y1 = x1 cos - x2 sin,  y2 = x2 cos + x1 sin
  * (inverse: by the opposite angle, which is the gradient's direction).  Pairs from n_pairs on are copied.  CD_ROPE_HALVES: pair p is
  * channels p and p + dim/2; CD_ROPE_PAIRS: channels 2p and 2p + 1.  Angles are exact to
- * 2^-25 of a turn at any position; sums in fp32, rounded once.
+ * 2^-24 of a turn at any position and frequency; sums in fp32, rounded once.
  *   tensors    HOST array of n_tensors descriptors, all with the same tokens (queries and keys go in one launch): x and y device,
  *              [tokens][heads][dim] in `dtype`, channels contiguous, heads dim elements apart, tokens x_token / y_token apart.  y may be x
  *   positions  device int32 [axes][tokens]
@@ -353,7 +353,7 @@ int codistill_adam_step(float* master_w, float* exp_avg, float* exp_avg_sq, cons
  * in whole vectors, others element by element.  tokens == 0 is allowed and does nothing (x, y and positions may then be
  * NULL).
  * Errors (CD_ERR_INVALID_ARG, nothing launched): NULL pointers, odd or oversized dim, n_pairs > dim/2, an axis outside [0, axes), a
- * non-finite frequency, strides below heads * dim, n_tensors outside 1..CD_ROPE_MAX_TENSORS, pointers not aligned to their elements.
+ * frequency that is not finite or not below 10^6 in size, strides below heads * dim, n_tensors outside 1..CD_ROPE_MAX_TENSORS, pointers not aligned to their elements.
  */
 #define CD_ROPE_MAX_PAIRS 128
 #define CD_ROPE_MAX_TENSORS 4

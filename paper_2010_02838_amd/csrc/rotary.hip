@@ -27,8 +27,9 @@ struct RopeArgs {
 };
 static_assert(sizeof(RopeArgs) <= 4096, "kernel arguments");
 
-// The angle in turns, in [-1/2, 1/2).  A frequency is a 64-bit fraction of a turn, so that whole turns fall out of the integer product and 2^-25
-// of a turn is all that is lost at any position.  A single fp32 product is a thousandth of a radian off at 30000 and half a turn at 2^24.
+// The angle in turns, in [-1/2, 1/2).  A frequency is a 64-bit fraction of a turn, so that whole turns fall out of the integer product; what is lost at any
+// position is the rounding to fp32, 2^-25 of a turn, and less than 2^-31 of cut bits.  A single fp32 product is a thousandth of a radian off at 30000 and half
+// a turn at 2^24.
 __device__ inline float turns(int32_t pos, uint64_t freq) { return (float)(int32_t)(((uint64_t)(int64_t)pos * freq) >> 32) * 0x1p-32f; }
 
 template <typename T, int N> struct Vec { T e[N]; };
@@ -113,6 +114,17 @@ __global__ void __launch_bounds__(256) rotary_kernel(RopeArgs a) {
   }
 }
 
+// freq / (2 pi) without its whole turns, in units of 2^-64, cut: the number's 53 bits times 1 / (2 pi) to 128 bits, in integers.  (A quotient of doubles is off by
+// 2^-53 of itself, at position 2^31 and a thousand radians a position by 4e-5 of a turn.)  |freq| < 2^20.
+static uint64_t fraction_of_turn(double freq) {
+  int e = 0;
+  const uint64_t m = (uint64_t)ldexp(frexp(fabs(freq), &e), 53);   // |freq| = m 2^(e - 53)
+  const unsigned __int128 low = (unsigned __int128)m * 0x7f09d5f47d4d3770ull, high = (unsigned __int128)m * 0x28be60db9391054aull + (uint64_t)(low >> 64);
+  const int shift = 53 - e;   // at least 33: `high` is m / (2 pi) in units of 2^-64
+  const uint64_t f = shift < 128 ? (uint64_t)(high >> shift) : 0;
+  return freq < 0 ? 0 - f : f;
+}
+
 }  // namespace
 }  // namespace cd
 
@@ -150,9 +162,7 @@ extern "C" int codistill_rotary(const cd_rotary* rope, const int32_t* positions,
   for (int p = 0; p < rope->n_pairs; p++) {
     CD_REQUIRE(rope->axis[p] >= 0 && rope->axis[p] < rope->axes && rope->axis[p] < 256, "rotary: axis %d of pair %d outside 0..%d", rope->axis[p], p, rope->axes - 1);
     CD_REQUIRE(isfinite(rope->freq[p]) && fabs(rope->freq[p]) < 1e6, "rotary: frequency of pair %d", p);
-    const double turn = rope->freq[p] / 6.283185307179586476925;
-    const double part = turn - floor(turn);
-    a.freq[p] = part < 1.0 ? (uint64_t)ldexp(part, 64) : 0;
+    a.freq[p] = fraction_of_turn(rope->freq[p]);
     a.axis[p] = (uint8_t)rope->axis[p];
   }
   if (tokens == 0) return CD_OK;
