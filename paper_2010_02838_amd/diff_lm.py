@@ -68,7 +68,7 @@ class DiffLM:
             y = self._norm(x, "norm%d" % i)
             q, k, v = self._split(y @ self.p["qkv%d" % i].t())
             self._turn(q, k, positions)
-            out, o2 = (torch.empty(rows, self.H, 2 * self.D, dtype=dt, device=dev) for _ in range(2))
+            out, o2 = torch.zeros(rows, self.H, 2 * self.D, dtype=dt, device=dev), torch.empty(rows, self.H, 2 * self.D, dtype=dt, device=dev)   # (zero where rows belong to no sequence)
             lse = torch.empty(2, self.H, rows, device=dev)
             lam = self.w["lam%d" % i]
             desc = B.diff_attention_desc(q, k, v, out, lam, causal=True, q_starts=starts, k_starts=starts, max_q=longest, max_k=longest)

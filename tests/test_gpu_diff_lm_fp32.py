@@ -1,0 +1,43 @@
+"""The small language model: bounds of its default type (fp32), rows that belong to no sequence, repeatable gradients."""
+import math
+
+import pytest
+import torch
+
+from test_gpu_diff_lm import DEV, reference
+
+pytestmark = pytest.mark.gpu
+
+
+def poison():
+    """NaN in the memory that the next small tensors get."""
+    kept = [torch.full((n,), math.nan, device=DEV) for n in (1 << 10, 1 << 13, 1 << 15, 1 << 17) for _ in range(40)]
+    torch.cuda.synchronize()
+    del kept
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_rows_of_no_sequence(dtype):
+    """Rows that no sequence has: their logits are finite, and the gradients are those without them."""
+    from paper_2010_02838_amd.diff_lm import DiffLM, copying_batch
+    tokens, positions, starts, _ = copying_batch(5, 20, 50, seed=1)
+    n, extra = tokens.numel(), 37
+    gen = torch.Generator(device=DEV).manual_seed(2)
+    dz = torch.randn(n, 50, generator=gen, device=DEV).bfloat16().float()
+    runs = []
+    for more in (0, extra):
+        lm = DiffLM(50, layers=2, heads=4, kv_heads=2, head_dim=32, seed=3, dtype=dtype)
+        t = torch.cat([tokens, torch.zeros(more, dtype=tokens.dtype, device=DEV)])
+        p = torch.cat([positions, torch.zeros(1, more, dtype=torch.int32, device=DEV)], 1)
+        poison()
+        z = lm.forward(t, p, starts, 40)
+        assert torch.isfinite(z).all()
+        poison()
+        lm.backward(torch.cat([dz, torch.zeros(more, 50, device=DEV)]))
+        runs.append((z[:n].double(), {k: g.double() for k, g in lm.g.items()}))
+    # the same sums over other tiles: fp32 products, whose results are rounded to bf16 in the bf16 model
+    tol = 1e-5 if dtype is torch.float32 else 2e-2
+    (z0, g0), (z1, g1) = runs
+    assert (z0 - z1).norm() <= tol * z0.norm()
+    for k in g0:
+        assert (g0[k] - g1[k]).norm() <= tol * g0[k].norm(), k
