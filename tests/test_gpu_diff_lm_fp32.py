@@ -41,3 +41,18 @@ def test_rows_of_no_sequence(dtype):
     assert (z0 - z1).norm() <= tol * z0.norm()
     for k in g0:
         assert (g0[k] - g1[k]).norm() <= tol * g0[k].norm(), k
+
+
+def test_gradients_repeat():
+    """The same batch, the same bits, with few words under many rows."""
+    from paper_2010_02838_amd.diff_lm import DiffLM, copying_batch
+    lm = DiffLM(7, layers=1, heads=4, kv_heads=2, head_dim=32, seed=3)
+    tokens, positions, starts, _ = copying_batch(300, 20, 7, seed=1)
+    first = None
+    for _ in range(8):
+        z = lm.forward(tokens, positions, starts, 40)
+        lm.backward(torch.cos(z))
+        got = {k: g.clone() for k, g in lm.g.items()}
+        first = first or got
+        for k, g in got.items():
+            assert torch.equal(g, first[k]), k
