@@ -118,7 +118,8 @@ class DiffLM:
 
 
 class Decoder:
-    """One token at a time for several sequences, against caches of rotated keys and of values."""
+    """One token at a time for several sequences, against caches of rotated keys and of values.  lens: the sequences' ages, on the device; a sequence
+    whose age is set to zero begins anew."""
 
     def __init__(self, lm, sequences, room):
         self.lm, self.S, self.room = lm, sequences, room
@@ -126,6 +127,7 @@ class Decoder:
         self.k = [zeros(sequences, room, lm.K, 2, lm.D) for _ in range(lm.L)]
         self.v = [zeros(sequences, room, lm.K, 2 * lm.D) for _ in range(lm.L)]
         self.lens = torch.zeros(sequences, dtype=torch.int32, device=lm.dev)
+        self.oldest = 0   # no sequence is older
         self.out = zeros(sequences, 1, lm.H, 2 * lm.D)
         self.q = zeros(sequences, 1, lm.H, 2, lm.D)
         self.all = torch.arange(sequences, device=lm.dev)
@@ -135,6 +137,11 @@ class Decoder:
     def step(self, tokens):
         """tokens int64 [sequences]: logits fp32 [sequences, V] of what follows."""
         lm = self.lm
+        if self.oldest >= self.room:   # (one past the caches' end; the device is asked only here, whether the old ones have begun anew)
+            self.oldest = int(self.lens.max())
+            if self.oldest >= self.room:
+                raise ValueError("decoder: a sequence has filled the room of %d tokens" % self.room)
+        self.oldest += 1
         positions, at = self.lens[None].clone(), self.lens.long()
         self.lens += 1
         x = lm.p["embed"][tokens].float()

@@ -56,3 +56,20 @@ def test_gradients_repeat():
         first = first or got
         for k, g in got.items():
             assert torch.equal(g, first[k]), k
+
+
+def test_decoder_fills_its_room():
+    """As many tokens as there is room for and no more; a sequence that begins anew goes on beside the others."""
+    from paper_2010_02838_amd.diff_lm import DiffLM
+    lm = DiffLM(20, layers=1, heads=2, kv_heads=1, head_dim=16, seed=2)
+    words = torch.randint(0, 20, (2, 6), generator=torch.Generator().manual_seed(1)).to(DEV)
+    decoder = lm.decoder(2, 6)
+    first = [decoder.step(words[:, t]) for t in range(6)]
+    for _ in range(2):
+        with pytest.raises(ValueError):
+            decoder.step(words[:, 0])
+    decoder.lens.zero_()
+    for t in range(6):
+        assert torch.equal(decoder.step(words[:, t]), first[t])
+    with pytest.raises(ValueError):
+        decoder.step(words[:, 0])

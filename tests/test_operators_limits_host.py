@@ -7,6 +7,7 @@ import torch
 
 from paper_2010_02838_amd import binding as B
 from paper_2010_02838_amd.adamw import AdamW
+from paper_2010_02838_amd.diff_lm import DiffLM
 from test_operators_host import BAD, UNSUPPORTED, at, attn, backward, forward
 
 
@@ -115,3 +116,14 @@ def test_number_of_heads():
     for heads, rc in ((65536, B.CD_OK), (65544, BAD), (1500000, BAD)):
         wide = dict(heads=heads, kv_heads=heads, head_dim=8, batch=1, **{n + "_token": 16 * heads for n in ("q", "k", "v", "o")})
         assert B.lib.codistill_diff_attention_workspace_bytes(ctypes.byref(attn(**wide)), 1, ctypes.byref(ctypes.c_size_t())) == rc, heads
+
+
+def test_decoder_without_room():
+    """A token more than the caches hold is refused on the host, in front of any launch."""
+    lm = DiffLM(8, layers=1, heads=2, kv_heads=1, head_dim=8, device="cpu")
+    decoder = lm.decoder(2, 3)
+    decoder.lens[1] = 3
+    decoder.oldest = 3
+    with pytest.raises(ValueError, match="room of 3"):
+        decoder.step(torch.zeros(2, dtype=torch.int64))
+    assert decoder.lens.tolist() == [0, 3] and not decoder.k[0].any()
