@@ -28,6 +28,7 @@ CD_MAX_STAGES, CD_NAME_LEN, CD_LOSS_MAX_PEERS = 4, 48, 8
 CD_ROPE_HALVES, CD_ROPE_PAIRS = 0, 1
 CD_ROPE_MAX_PAIRS, CD_ROPE_MAX_TENSORS = 128, 4
 CD_LAMBDA_HEAD, CD_LAMBDA_TOKEN = 0, 1
+HEAD_NORM_MAX_WIDTH = 1024
 ADAMW_BLOCK = 256   # elements that share an exponent in 8-bit moments
 KERNEL_CLASSES = ["conv_fprop", "conv_dgrad", "conv_wgrad", "norm", "glue", "linear", "loss", "sgd", "conv_fprop_narrow",
                   "bn_apply", "conv_fprop_wide", "attention"]

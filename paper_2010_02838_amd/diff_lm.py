@@ -19,17 +19,22 @@ EPS = 1e-5
 
 
 class DiffLM:
+    """width: of the residual stream; None: that of all heads' outputs."""
+
     def __init__(self, vocabulary, layers=2, heads=4, kv_heads=2, head_dim=32, theta=10000.0, lambda_init=0.8, state_bits=8, seed=0, dtype=torch.float32,
-                 device="cuda:0"):
+                 device="cuda:0", width=None):
         self.V, self.L, self.H, self.K, self.D, self.dev = vocabulary, layers, heads, kv_heads, head_dim, device
-        self.d, self.post, self.dt = heads * 2 * head_dim, 1.0 - lambda_init, dtype
+        every = heads * 2 * head_dim
+        self.d, self.post, self.dt = width or every, 1.0 - lambda_init, dtype
+        if not 1 <= self.d <= B.HEAD_NORM_MAX_WIDTH:
+            raise ValueError("diff_lm: a residual stream of %d channels, %d at most: give a width" % (self.d, B.HEAD_NORM_MAX_WIDTH))
         self.qkv = 2 * head_dim * (heads + 2 * kv_heads)
         gen = torch.Generator(device=device).manual_seed(seed)
         d = self.d
         shapes = [("embed", (vocabulary, d), d ** -0.5)]
         for i in range(layers):
             shapes += [("norm%d" % i, (d,), None), ("qkv%d" % i, (self.qkv, d), d ** -0.5), ("lam%d" % i, (heads,), None),
-                       ("head%d" % i, (2 * head_dim,), None), ("out%d" % i, (d, d), d ** -0.5 / math.sqrt(2 * layers))]
+                       ("head%d" % i, (2 * head_dim,), None), ("out%d" % i, (d, every), every ** -0.5 / math.sqrt(2 * layers))]
         shapes.append(("norm", (d,), None))
         self.w, self.g, self.p = {}, {}, {}
         for name, shape, scale in shapes:

@@ -73,3 +73,23 @@ def test_decoder_fills_its_room():
         assert torch.equal(decoder.step(words[:, t]), first[t])
     with pytest.raises(ValueError):
         decoder.step(words[:, 0])
+
+
+def test_width_that_the_heads_do_not_have():
+    """A residual stream narrower than all heads together: gradients as those of the square model (1e-4), and a decoder of its size."""
+    from paper_2010_02838_amd.diff_lm import DiffLM, copying_batch
+    lm = DiffLM(30, layers=2, heads=16, kv_heads=4, head_dim=64, lambda_init=0.5, seed=3, width=96)
+    for i in range(2):
+        lm.w["lam%d" % i].copy_(torch.linspace(-0.3, 0.9, 16))
+    tokens, positions, starts, _ = copying_batch(3, 12, 30, seed=1)
+    z = lm.forward(tokens, positions, starts, 24)
+    dz = torch.randn(z.shape, generator=torch.Generator(device=DEV).manual_seed(2), device=DEV)
+    lm.backward(dz)
+    want, grads = reference(lm, tokens, starts, positions, dz)
+    assert (z.double().cpu() - want).norm() <= 1e-4 * want.norm()
+    for n, g in grads.items():
+        assert (lm.g[n].double().cpu() - g).norm() <= 1e-4 * g.norm(), n
+    decoder, first = lm.decoder(1, 24), tokens[:int(starts[1])]
+    for t, word in enumerate(first):
+        got = decoder.step(word[None])[0]
+        assert (got - z[t]).norm() <= 1e-4 * z[t].norm(), t

@@ -127,3 +127,13 @@ def test_decoder_without_room():
     with pytest.raises(ValueError, match="room of 3"):
         decoder.step(torch.zeros(2, dtype=torch.int64))
     assert decoder.lens.tolist() == [0, 3] and not decoder.k[0].any()
+
+
+def test_width_of_the_residual_stream():
+    """It is normed in one group, of at most 1024 channels: wider models are refused where they are made, or given a width that their heads do not have."""
+    assert B.HEAD_NORM_MAX_WIDTH == 1024 and B.head_norm_workspace_bytes(1, 1, 1024) > 0
+    for kw in (dict(heads=16, head_dim=64), dict(heads=16, head_dim=64, width=1032), dict(width=-8)):
+        with pytest.raises(ValueError, match="width"):
+            DiffLM(8, layers=1, device="cpu", **kw)
+    lm = DiffLM(8, layers=1, heads=16, kv_heads=4, head_dim=64, device="cpu", width=1024)
+    assert lm.w["qkv0"].shape == (2 * 64 * (16 + 2 * 4), 1024) and lm.w["out0"].shape == (1024, 2048)
