@@ -109,3 +109,35 @@ def test_time_major_sequences(dtype):
         B.codistill_diff_attention_backward(desc, q, k, v, lam, out, o2, lse, dout, dq, dk, dv, dlam, ws)
         runs.append((out, dq, dk, dv, dlam))
     assert all(torch.equal(a, b) for a, b in zip(*runs)) and not (runs[0][0] == 7.0).all(-1).any()
+
+
+def split(p):
+    """Which passes split their work: (keys forward, keys or rows backward) have parts' sums in their workspace."""
+    rows = p.H * p.rq * (48 + (4 if p.lam.dim() == 1 else 0))
+    return p.B.diff_attention_workspace_bytes(p.desc, False) > 0, p.B.diff_attention_workspace_bytes(p.desc, True) > rows + 16
+
+
+@pytest.mark.parametrize("dtype,q_lens,k_lens,heads,kv_heads,dim,causal,packed", [
+    (BF, [1100], [1100], 2, 1, 64, True, False), (F32, [1100], [1100], 2, 1, 64, True, False), (BF, [1100, 90], [1100, 90], 2, 2, 32, True, False),
+    (BF, [1100, 90], [1100, 90], 2, 1, 128, True, True), (F32, [700, 33], [1300, 50], 2, 1, 32, True, True), (F32, [600], [1200], 1, 1, 128, True, False),
+    (BF, [600, 7], [1100, 1040], 4, 2, 40, False, False), (F32, [1100, 300], [600, 64], 4, 1, 64, False, True), (BF, [1500], [1300], 2, 1, 64, True, False)])
+def test_many_tiles_in_parts(dtype, q_lens, k_lens, heads, kv_heads, dim, causal, packed):
+    """Several tiles of rows and of keys, each pass split: under a causal mask the first tile of rows has few keys (two passes of its own) beside tiles whose keys
+    are dealt out, and parts lie in front of or behind what a tile reaches."""
+    p = Problem(dtype, q_lens, k_lens, heads, kv_heads, dim, causal, len(q_lens) > 1, packed=packed, seed=dim + heads, gap=5 if packed else 0)
+    assert split(p) == (True, True)
+    p.run()
+    p.check()
+
+
+def test_another_stream_computes():
+    """Outputs of a second stream's own run, in tensors that held something else before."""
+    p = Problem(BF, [300, 150], [300, 150], 8, 2, 64, True, False, seed=4)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for t in (p.out, p.dq, p.dk, p.dv, p.dlam):
+            t.fill_(7.0)
+        p.run()
+    torch.cuda.current_stream().wait_stream(side)
+    p.check()
