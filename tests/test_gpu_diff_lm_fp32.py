@@ -93,3 +93,59 @@ def test_width_that_the_heads_do_not_have():
     for t, word in enumerate(first):
         got = decoder.step(word[None])[0]
         assert (got - z[t]).norm() <= 1e-4 * z[t].norm(), t
+
+
+@pytest.mark.parametrize("kv_heads", [1, 4])
+def test_gradients_of_an_fp32_network(kv_heads):
+    """The default model is fp32 throughout.  A gradient passes some thirty sums of up to 256 terms, each rounded to a few times 2^-24 of its terms; the
+    difference of the two maps at a lambda near one and the sums of either sign cost one to two digits of that: 1e-4."""
+    from paper_2010_02838_amd.diff_lm import DiffLM, copying_batch
+    lm = DiffLM(50, layers=2, heads=4, kv_heads=kv_heads, head_dim=32, lambda_init=0.5, seed=3)
+    for i in range(2):
+        lm.w["lam%d" % i].copy_(torch.tensor([0.3, -0.2, 0.0, 0.9]))
+    tokens, positions, starts, _ = copying_batch(5, 20, 50, seed=1)
+    z = lm.forward(tokens, positions, starts, 40)
+    dz = torch.randn(z.shape, generator=torch.Generator(device=DEV).manual_seed(2), device=DEV)
+    lm.backward(dz)
+    want, grads = reference(lm, tokens, starts, positions, dz)
+    assert (z.double().cpu() - want).norm() <= 1e-4 * want.norm()
+    for n, g in grads.items():
+        assert (lm.g[n].double().cpu() - g).norm() <= 1e-4 * g.norm(), n
+
+
+def test_lambdas_gradient_of_a_bf16_network(monkeypatch):
+    """lambda's gradient is a sum of products of either sign, dO (P_2 v) of all rows and channels, which cancels; some six bf16 roundings in front of each of them,
+    1.7e-3 as a 2-norm, are 4e-3 of the root of the products' squares, five times that where a row's channels share one (2e-2)."""
+    from paper_2010_02838_amd import binding as B
+    from paper_2010_02838_amd.diff_lm import DiffLM, copying_batch
+    lm = DiffLM(50, layers=1, heads=4, kv_heads=2, head_dim=64, lambda_init=0.2, seed=5, dtype=torch.bfloat16)
+    tokens, positions, starts, _ = copying_batch(4, 30, 50, seed=2)
+    z = lm.forward(tokens, positions, starts, 60)
+    dz = torch.randn(z.shape, generator=torch.Generator(device=DEV).manual_seed(2), device=DEV).bfloat16().float()
+    call, products = B.codistill_diff_attention_backward, []
+
+    def keep(desc, q, k, v, lam, out, o_second, lse, dout, *rest):
+        products.append(o_second.double() * dout.double())
+        call(desc, q, k, v, lam, out, o_second, lse, dout, *rest)
+
+    monkeypatch.setattr(B, "codistill_diff_attention_backward", keep)
+    lm.backward(dz)
+    _, grads = reference(lm, tokens, starts, positions, dz)
+    size = products[0].square().sum((0, 2)).sqrt().cpu()
+    assert (lm.g["lam0"].double().cpu() - grads["lam0"]).norm() <= 2e-2 * size.norm()
+
+
+def test_decoding_in_fp32():
+    """Token by token against the cache and in one pass: the same fp32 products in other orders, rounded to a few times 2^-24 some thirty times: 1e-4."""
+    from paper_2010_02838_amd.diff_lm import DiffLM
+    lm = DiffLM(50, layers=2, heads=4, kv_heads=2, head_dim=32, seed=4)
+    gen = torch.Generator(device=DEV).manual_seed(5)
+    T = 140
+    words = torch.randint(0, 50, (3, T), generator=gen, device=DEV)
+    starts = torch.arange(4, dtype=torch.int32, device=DEV) * T
+    positions = torch.arange(T, dtype=torch.int32, device=DEV).repeat(3)[None]
+    z = lm.forward(words.flatten(), positions, starts, T).view(3, T, -1)
+    dec = lm.decoder(3, T)
+    for t in range(T):
+        got = dec.step(words[:, t])
+        assert (got - z[:, t]).norm() <= 1e-4 * z[:, t].norm(), t
