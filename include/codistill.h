@@ -391,7 +391,7 @@ int codistill_rotary(const cd_rotary* rope, const int32_t* positions, int64_t to
  *              keys than queries the first rows see none
  *   scale      > 0, or 0 for 1 / sqrt(head_dim)
  * head_dim: multiples of 8 up to 128.  Products with CD_BF16 run on the bf16 matrix instructions with the weights P rounded to bf16 for the
- * second product; softmax statistics, sums and accumulators are fp32.  CD_F32 runs on the fp32 matrix instruction.
+ * second product; softmax statistics, sums and accumulators are fp32.  CD_F32 runs on the fp32 matrix instruction and rounds nothing.
  *   o_second   NULL, or [q rows][heads][2 head_dim] contiguous in dtype: P_2 v, kept for the backward pass; lse then has to be given too
  *   lse        NULL, or device fp32 [2][heads][q rows]: log2 of the sum of exp2 of each row's scores
  *   workspace  at least codistill_diff_attention_workspace_bytes(desc, 0) bytes (may be 0: then NULL is fine)
@@ -415,7 +415,9 @@ int codistill_diff_attention(const cd_diff_attn* desc, const void* q, const void
                              void* o_second, float* lse, void* workspace, size_t workspace_bytes, void* stream);
 /*
  * Its gradients.  q, k, v, lambda, out, o_second and lse as the forward call had and left them; dout has out's strides, dq, dk, dv those of q, k, v.
- * Gradients of a key head are summed over the heads that share it, in a fixed order: the same inputs give the same bits.
+ * Gradients of a key head are summed over the heads that share it, in a fixed order: the same inputs give the same bits.  With CD_BF16 the gradients of the
+ * scores and P_1 - lambda P_2 are rounded to bf16 for their products, and the row sums of P_m dP begin from out and o_second as they were rounded: they are completed in
+ * fp32 for dk, dlambda and, where rows see at most 128 keys, dq; dq of rows with more keys is off by that rounding's small share.
  *   dlambda   lambda's shape, fp32
  *   workspace at least codistill_diff_attention_workspace_bytes(desc, 1) bytes
  * Errors as above; also CD_ERR_INVALID_ARG where sequences share memory, in which gradients would race (they lie one behind the other, or, time-major, all of a

@@ -5,7 +5,7 @@
 // with step = lr / (1 - b1^t) and rs = 1 / sqrt(1 - b2^t) from the host, in double.  HBM-bound: 28 bytes a parameter with 32-bit moments, 16
 // with 8-bit ones, 2 more for the bf16 copy.  One launch whatever the number of tensors: a workgroup takes 1024 or 2048 elements of one tensor and
 // finds which in a table in device memory, so that 180 tensors of a Transformer are not 180 launches that each fill part of the chip.  60.9 M parameters:
-// 300 to 325 us with 32-bit moments (1.83 GB, 5.6 to 6.1 TB/s), 195 to 220 with 8-bit ones (1.1 GB, 5.0 to 5.6), 65 to 70 to unpack those.
+// 315 to 330 us with 32-bit moments (1.83 GB, 5.5 to 5.8 TB/s), 195 to 205 with 8-bit ones (1.1 GB, 5.3 to 5.6), 65 to 70 to unpack those.
 //
 // 8-bit moments.  A block of 256 elements (four a lane of one wave) shares a power of two, 2^E, with E the smallest for which no value exceeds
 // 1.875 2^E; a value x is stored as the float y = |x| 2^-E with three mantissa bits and exponents from 0 down to -14 (m, beside its sign) or -30 (v), equally
@@ -70,7 +70,10 @@ __device__ inline uint32_t wave_max_u32(uint32_t v) {
   return v;
 }
 
-// 32 bits for an element, from its place among all blocks and the step's seed
+// 32 bits for an element, from its place among all blocks and the step's seed (times 2^32 over the golden ratio, so that seeds in a row begin far apart).  Shifts,
+// exclusive ors and products with odd numbers can be undone, so no two places of a step share their bits.  The two multipliers have nothing to them but what was
+// measured: over 2^20 numbers every bit of the place flips every bit of the result with a probability of 0.495 to 0.505, and neighbouring places, steps in a row
+// and the two halves that m and v are rounded with are correlated by less than 2e-3.
 __device__ inline uint32_t random_bits(uint32_t at, uint32_t seed) {
   uint32_t x = at + seed * 0x9E3779B9u;
   x = (x ^ (x >> 16)) * 0x6C8E9CF5u;

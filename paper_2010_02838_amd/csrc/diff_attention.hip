@@ -23,9 +23,13 @@
 // in which the first operand, the streamed tensor transposed, is read from LDS.
 //
 // What bounds them.  Long sequences: neither memory nor LDS, but the matrix instructions (43 % of the forward kernel's cycles) and the vector ones (63 %,
-// exponentials and what surrounds them) of few waves taking turns; two causal sequences of 4096 tokens, 8 heads of 64: forward 135 us (764 TFLOP/s),
-// queries' gradients 185, keys' 220 (425 TFLOP/s together, which repeat scores and dP: 595 with those).  One query a sequence: the cache's bytes, 178 MB in
-// 40 us (4.5 TB/s).  Short sequences: the latency of a workgroup's few tiles, one after the other.
+// exponentials and what surrounds them) of few waves taking turns; two causal sequences of 4096 tokens, 8 heads of 64: forward 128 us (806 TFLOP/s),
+// queries' gradients 164, keys' 182 (497 TFLOP/s together, which repeat scores and dP: 696 with those).  One query a sequence: the cache's bytes, 178 MB in
+// 41 us (4.4 TB/s).  Short sequences: the latency of a workgroup's few tiles, one after the other, and the second walk over few keys (EXACT_KEYS).
+//
+// Roundings to bf16 (fp32 has none of them).  P where it multiplies v, P_m (dP - delta_m) where it multiplies k or q, P_1 - lambda P_2 where it multiplies dO: the
+// matrix instructions take bf16, at sixteen times the rate of fp32.  Each is off by 1.7e-3 (2-norm), as the rounding of a result is, so that results are off by
+// 2.3e-3 to 2.6e-3 where 32-bit arithmetic rounded once has 1.7e-3.  out and P_2 v are kept as they are returned, rounded: deltas begin from them (below).
 #include "common.h"
 #include "conv_rules.h"
 #include "kernels.h"
@@ -185,7 +189,10 @@ template <typename T, int DT> struct Sizes {
   static constexpr int W = 2 * DT, KC = 32;
   static constexpr int KS = DT / 16, VT = W / 32, DTT = DT / 32;
 };
-constexpr int EXACT_KEYS = 128;   // waves whose first row sees no more keys than this get their deltas in a pass of their own (bf16)
+// Waves whose first row sees no more keys than this get their deltas in a pass over them of its own (bf16; why: at the pass over the queries).  What the pass
+// takes of forward and backward: 4.0 of 72.2 us for 113 packed sentences of up to 126 tokens with 4 heads of 64, 7 of 107 for 64 x 128 tokens with 8, 4.4 of 54.6
+// for 16 x 130 causal queries on 230 keys.
+constexpr int EXACT_KEYS = 128;
 
 // ---- sequences and rows ---------------------------------------------------------------------------------------------------
 struct Seq { int nq, nk; int64_t q0, k0; };   // lengths; rows of the sequence's first query and key in their tensors
@@ -670,8 +677,8 @@ __global__ void __launch_bounds__(256, DT * sizeof(T) <= 256 ? 2 : 1) diff_backw
   for (int m = 0; m < MAPS; m++)
 #pragma unroll
     for (int t = 0; t < S::DTT; t++) clear(dq[m][t]);
-  // Rows with few keys: a rounding of the kept outputs is as large as their small dS (two keys: dq off by 5e-3 where its own rounding is 1.7e-3,
-  // 128 keys 2.8e-3, 700 keys 2.5e-3 as without it), so delta is completed by a pass of its own first.  fp32 outputs are as exact as the products; there
+  // Rows with few keys: a rounding of the kept outputs is as large as their small dS (two keys: dq off by 5e-3 where its own rounding is 1.7e-3 and that of dS
+  // as much, 128 keys 2.8e-3, 700 keys 2.5e-3 as without it), so delta is completed by a pass of its own first.  fp32 outputs are as exact as the products; there
   // one pass does, and a row of one key, whose gradient is zero to the last bit, gets it by name (`moves`).
   LaneAt at = O::template lane_at<S::W>(lane);
   Loader<T, DT, true, 256> ks;
@@ -1133,6 +1140,9 @@ static int check_apart(const char* what, const cd_diff_attn* d, bool out_only) {
 // Parts of the keys that get a workgroup of their own: few rows against many keys would leave most of the chip without work.  Heads of 64, one part against
 // this rule: one query of 16 sequences and 4 key heads on up to 8192 keys 187 against 41 + 6 us (the join); 16 queries of 8 heads on 4096 keys 88
 // against 16; 4096 causal tokens of 4 heads 104 against 77; where there are rows enough (512 causal tokens of 8 heads) the rule leaves one part: 19.
+// All three rules at once in fp32, heads of 64, forward and backward: 1024 causal tokens of 8 heads 415 against 231, of 2 heads 412 against 167; 16 queries of 8 heads
+// on 4096 keys 987 against 111; 300 causal tokens of 8 heads on one key head 444 against 151; 3 x 77 on 130 keys, where they leave one part, 47.  Single queries of 4
+// sequences on 4096 keys 412 against 25.  A loss: 4 x 512 causal queries on 600 keys, 8 heads of 64 in bf16, 81 against 97 (two parts in every pass).
 static int parts_of(const cd_diff_attn* d) {
   const int64_t groups = (int64_t)d->batch * d->kv_heads * cdiv((int64_t)d->tq * (d->heads / d->kv_heads), F_ROWS);
   int64_t p = groups ? 768 / groups : 1;   // (three workgroups a compute unit: all parts at once)

@@ -4,7 +4,7 @@
 //
 // HBM-bound: every element is read and written once, 3 flops each.  A workgroup takes a few tokens: it first computes the cosines and sines of
 // their pairs (once for all heads of all tensors, into LDS), then streams the heads past them in 16-byte vectors.  8192 tokens of 32 heads of 64 in bf16 (67 MB
-// moved): 12.4 us, 5.4 TB/s; 16 tokens: 4.2, a launch and its latencies.
+// moved): 13.0 us, 5.2 TB/s; 16 tokens: 3.8, a launch and its latencies.
 #include "common.h"
 #include <math.h>
 
