@@ -492,6 +492,123 @@ int codistill_adamw_table(const cd_adamw_tensor* tensors, int64_t n_tensors, int
 int codistill_adamw_step(const cd_adamw_plan* plan, const void* device_table, const cd_adamw_cfg* cfg, const float* grad_scale, void* stream);
 int codistill_adamw_unpack(const cd_adamw_plan* plan, const void* device_table, void* stream);
 
+/* ---- operators of a language model between its tokens, its attention and its cache ----------------------------------- */
+/*
+ * Norm of every head's channels with a rotary position behind it, queries and keys in one launch:
+ *     n = gain x / sqrt(mean(x^2) + eps) over the `dim` channels of a head,     y = n turned as codistill_rotary does
+ * with nothing rounded in between.
+ *   tensors    HOST array of n_tensors descriptors, all with the same tokens: x and y device, [tokens][heads][dim] in rope->dtype, channels contiguous,
+ *              heads dim elements apart, tokens x_token / y_token apart; y may be x.  gain: device [dim] in rope->dtype, shared by the tensor's heads, or NULL (1)
+ *   rope, positions   as for codistill_rotary
+ * Backward: dx, and dgain (fp32 [dim], the sum over all tokens and heads in a fixed order: the same inputs give the same bits).  x is read again and its
+ * statistics are taken again: nothing is kept.  dx may be dy.  dgain is NULL exactly where gain is; y is not looked at (nor are dy, dx and
+ * dgain in the forward pass).
+ *   workspace  codistill_norm_rotary_workspace_bytes
+ * tokens == 0 is allowed (dgain is then zero; x, y, dy, dx and positions may be NULL).  Any even dim up to 2 * CD_ROPE_MAX_PAIRS; heads whose halves, pointers and
+ * strides are multiples of 16 or 8 bytes move in vectors, others element by element.
+ * Errors (nothing launched): CD_ERR_INVALID_ARG as for codistill_rotary, and eps negative or not finite; CD_ERR_WORKSPACE_TOO_SMALL.
+ */
+typedef struct {
+  const void *x, *gain;
+  void* y;
+  const void* dy;
+  void* dx;
+  float* dgain;
+  int64_t heads, x_token, y_token, dy_token, dx_token;
+} cd_norm_rotary_tensor;
+int codistill_norm_rotary(const cd_rotary* rope, const int32_t* positions, int64_t tokens, const cd_norm_rotary_tensor* tensors,
+                          int64_t n_tensors, float eps, void* stream);
+int codistill_norm_rotary_workspace_bytes(const cd_rotary* rope, int64_t tokens, int64_t n_tensors, size_t* bytes);
+int codistill_norm_rotary_backward(const cd_rotary* rope, const int32_t* positions, int64_t tokens, const cd_norm_rotary_tensor* tensors,
+                                   int64_t n_tensors, float eps, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Embedding lookup with a factor, and the gradient of its table by sorted tokens:
+ *     y[i] = scale table[tokens[i]],       dtable[w] (+)= scale * (sum of dy[i] over the rows i with tokens[i] == w)
+ *   tokens   device int32 or int64 [rows] (token_bytes 4 or 8); a token outside [0, vocabulary) is none: its row of y is zero, its row of dy is not read
+ *   table    device [vocabulary][width] in table_dtype, contiguous;  y, dy  device [rows][width] in row_dtype, row_stride elements apart
+ *   dtable   device fp32 [vocabulary][width], contiguous.  accumulate 0: written whole, zeros for words that do not occur; otherwise the sums are added to
+ *            it, and rows of words that do not occur are not touched
+ * The rows of a word are added up in fp32 in an order that depends on the tokens alone: the same inputs give the same bits.
+ *   workspace  codistill_embedding_workspace_bytes (the same for every content of tokens)
+ * rows == 0 is allowed (tokens, y, dy and workspace may then be NULL).
+ * Errors (nothing launched): CD_ERR_INVALID_ARG: NULL pointers, pointers not aligned to their elements (workspace: 16 bytes), rows outside 0 .. 2^30, vocabulary
+ * outside 1 .. 2^31 - 2, width outside 1 .. 65536, a row longer than its stride, a scale that is not finite, token_bytes other than 4 and 8;
+ * CD_ERR_UNSUPPORTED: rows * width above 2^40; CD_ERR_WORKSPACE_TOO_SMALL.
+ */
+typedef struct {
+  int32_t table_dtype, row_dtype;    /* CD_F32 or CD_BF16 */
+  int32_t token_bytes;
+  float scale;
+  int64_t rows, vocabulary, width, row_stride;
+} cd_embedding;
+int codistill_embedding(const cd_embedding* desc, const void* tokens, const void* table, void* y, void* stream);
+int codistill_embedding_workspace_bytes(const cd_embedding* desc, size_t* bytes);
+int codistill_embedding_backward(const cd_embedding* desc, const void* tokens, const void* dy, float* dtable, int accumulate, void* workspace,
+                                 size_t workspace_bytes, void* stream);
+
+/*
+ * A cache of keys and values in 8 bits, in pages, and differential attention against it.  The cache is the caller's memory
+ * (codistill_kv_cache_bytes), which nothing has to clear:
+ *   k       device int8 [pages][kv_heads][page_tokens][2][head_dim padded to a multiple of 32]; the padding is not written and not used
+ *   v       device int8 [pages][kv_heads][2 head_dim][page_tokens]
+ *   scales  device bf16 [pages][kv_heads][3][page_tokens]: of the two keys and of the value of a token
+ *   table   device int32 [sequences][seq_pages]: the pages of each sequence's tokens, or NULL: sequence b has the pages b * seq_pages .. .  Sequences may share pages
+ *           (a common beginning).  An entry outside [0, pages) is no page: nothing is written there, zeros are read, its keys are not seen
+ * Each of a token's two keys, and its value, is held as codes -127 .. 127 and a scale, the smallest bf16 number that is at least the largest magnitude over 127
+ * (and at least 2^-100); a code is the element over the scale, rounded to nearest even, and stands for code * scale.  Where an element is not finite the scale is NaN.
+ *
+ * codistill_kv_write quantises rows of new tokens into the cache; codistill_kv_read gives what it holds, rounded to dtype, in the same layout of rows:
+ *   k  [row][kv_heads][2][head_dim], v  [row][kv_heads][2 head_dim] in dtype; channels and heads of a token contiguous, token and batch strides in elements
+ *   first   device int32 [sequences], or NULL (0): the position of each sequence's first row; row i goes to (comes from) position first + i.  Positions outside
+ *           [0, seq_pages * page_tokens) are not written and read as zeros
+ *   padded  starts == NULL: max_new rows for each sequence, of which counts (device int32 [sequences], or NULL: all) are real, values outside
+ *           [0, max_new] cut to it; rows behind them are neither read nor written
+ *   packed  starts (device int32 [sequences + 1]): sequence b has rows starts[b] .. starts[b + 1]; max_new is the longest sequence's (longer ones are cut),
+ *           rows those of the tensors (a sequence that reaches beyond them is left out)
+ * Pages that several sequences share must not be written by two of them in one call.
+ * codistill_kv_diff_attention is codistill_diff_attention (padded, forward, nothing kept) with the cache's values for keys and values:
+ *   q [sequences][tq][heads][2][head_dim], out [..][heads][2 head_dim] in dtype, token and batch strides in elements; heads h * kv_heads / heads share a key head
+ *   k_lens  device int32 [sequences]: tokens of each sequence in the cache, the new ones among them (cut to [0, seq_pages * page_tokens]); q_lens  device
+ *           int32 [sequences] or NULL (tq): out is zero in the rows behind
+ *   causal  query i of nq sees the keys j <= i + nk - nq; rows that see no key are zero
+ *   lambda, lambda_kind, scale  as there
+ *   workspace  codistill_kv_diff_attention_workspace_bytes (may be 0: then NULL is fine; its contents do not matter)
+ * Products are exact in the codes; queries in fp32 and all weights go through the bf16 matrix instructions as sums of two (CD_BF16: weights) or three bf16
+ * numbers, with fp32 accumulators and softmax statistics.
+ * head_dim: multiples of 8 up to 128 (CD_ERR_UNSUPPORTED otherwise).  page_tokens: a multiple of 64, up to 2^21.
+ * Errors (nothing launched): CD_ERR_INVALID_ARG: NULL or misaligned pointers (16 bytes; tables and lambda 4), sizes out of range (sequences * kv_heads and all rows of
+ * queries up to 2^24, a sequence's room below 2^31 - 64), pages < sequences * seq_pages without a table, heads no multiple of kv_heads, strides that are no multiple of 16 bytes or
+ * shorter than a token, rows to be written (out, and those of codistill_kv_read) that share memory, starts together with counts, packed sequences without their longest one, scale < 0 or not finite;
+ * CD_ERR_WORKSPACE_TOO_SMALL.
+ */
+typedef struct {
+  int32_t dtype;                     /* of the rows: CD_F32 or CD_BF16 */
+  int32_t sequences, seq_pages, page_tokens, kv_heads, head_dim;
+  int64_t pages;
+  int8_t *k, *v;
+  uint16_t* scales;
+  const int32_t* table;
+} cd_kv_cache;
+typedef struct {
+  int32_t max_new, reserved;
+  int64_t rows, k_token, k_batch, v_token, v_batch;
+  const int32_t *first, *counts, *starts;
+} cd_kv_rows;
+typedef struct {
+  int32_t tq, heads, causal, lambda_kind;
+  float scale;
+  int32_t reserved;
+  int64_t q_token, q_batch, o_token, o_batch;
+  const int32_t *q_lens, *k_lens;
+} cd_kv_attn;
+int codistill_kv_cache_bytes(const cd_kv_cache* cache, size_t* k_bytes, size_t* v_bytes, size_t* scale_bytes);
+int codistill_kv_write(const cd_kv_cache* cache, const cd_kv_rows* rows, const void* k, const void* v, void* stream);
+int codistill_kv_read(const cd_kv_cache* cache, const cd_kv_rows* rows, void* k, void* v, void* stream);
+int codistill_kv_diff_attention_workspace_bytes(const cd_kv_cache* cache, const cd_kv_attn* desc, size_t* bytes);
+int codistill_kv_diff_attention(const cd_kv_cache* cache, const cd_kv_attn* desc, const void* q, const float* lambda, void* out, void* workspace,
+                                size_t workspace_bytes, void* stream);
+
 /* ---- introspection ----------------------------------------------------------------------- */
 /* The fused op list and where each tensor lives inside a save_for_backward workspace, so that
  * tools and tests can read intermediate activations and activation gradients after a forward /

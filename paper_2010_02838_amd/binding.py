@@ -86,6 +86,31 @@ class DiffAttn(ctypes.Structure):
         (n, ctypes.c_void_p) for n in ("q_lens", "k_lens", "q_starts", "k_starts")] + [("q_rows", ctypes.c_int64), ("k_rows", ctypes.c_int64)]
 
 
+class NormRotaryTensor(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("x", "gain", "y", "dy", "dx", "dgain")] + [
+        (n, ctypes.c_int64) for n in ("heads", "x_token", "y_token", "dy_token", "dx_token")]
+
+
+class Embedding(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("table_dtype", "row_dtype", "token_bytes")] + [("scale", ctypes.c_float)] + [
+        (n, ctypes.c_int64) for n in ("rows", "vocabulary", "width", "row_stride")]
+
+
+class KvCache(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("dtype", "sequences", "seq_pages", "page_tokens", "kv_heads", "head_dim")] + [("pages", ctypes.c_int64)] + [
+        (n, ctypes.c_void_p) for n in ("k", "v", "scales", "table")]
+
+
+class KvRows(ctypes.Structure):
+    _fields_ = [("max_new", ctypes.c_int32), ("reserved", ctypes.c_int32)] + [(n, ctypes.c_int64) for n in ("rows", "k_token", "k_batch", "v_token", "v_batch")] + [
+        (n, ctypes.c_void_p) for n in ("first", "counts", "starts")]
+
+
+class KvAttn(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("tq", "heads", "causal", "lambda_kind")] + [("scale", ctypes.c_float), ("reserved", ctypes.c_int32)] + [
+        (n, ctypes.c_int64) for n in ("q_token", "q_batch", "o_token", "o_batch")] + [("q_lens", ctypes.c_void_p), ("k_lens", ctypes.c_void_p)]
+
+
 class AdamwTensor(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in ("w", "grad", "lowp", "m", "v", "exps", "m_out", "v_out")] + [
         ("n", ctypes.c_int64), ("weight_decay", ctypes.c_float), ("lr_scale", ctypes.c_float)]
@@ -132,6 +157,17 @@ _SIGS = {
     "codistill_head_norm": [_i32, _vp, _i64, _vp, _vp, _i64, _i64, _i64, _i64, _f32, _f32, _vp],
     "codistill_head_norm_workspace_bytes": [_i64, _i64, _i64, ctypes.POINTER(_sz)],
     "codistill_head_norm_backward": [_i32, _vp, _i64, _vp, _vp, _i64, _vp, _i64, _vp, _i64, _i64, _i64, _f32, _f32, _vp, _sz, _vp],
+    "codistill_norm_rotary": [ctypes.POINTER(Rotary), _vp, _i64, ctypes.POINTER(NormRotaryTensor), _i64, _f32, _vp],
+    "codistill_norm_rotary_workspace_bytes": [ctypes.POINTER(Rotary), _i64, _i64, ctypes.POINTER(_sz)],
+    "codistill_norm_rotary_backward": [ctypes.POINTER(Rotary), _vp, _i64, ctypes.POINTER(NormRotaryTensor), _i64, _f32, _vp, _sz, _vp],
+    "codistill_embedding": [ctypes.POINTER(Embedding), _vp, _vp, _vp, _vp],
+    "codistill_embedding_workspace_bytes": [ctypes.POINTER(Embedding), ctypes.POINTER(_sz)],
+    "codistill_embedding_backward": [ctypes.POINTER(Embedding), _vp, _vp, _vp, _i32, _vp, _sz, _vp],
+    "codistill_kv_cache_bytes": [ctypes.POINTER(KvCache)] + [ctypes.POINTER(_sz)] * 3,
+    "codistill_kv_write": [ctypes.POINTER(KvCache), ctypes.POINTER(KvRows), _vp, _vp, _vp],
+    "codistill_kv_read": [ctypes.POINTER(KvCache), ctypes.POINTER(KvRows), _vp, _vp, _vp],
+    "codistill_kv_diff_attention_workspace_bytes": [ctypes.POINTER(KvCache), ctypes.POINTER(KvAttn), ctypes.POINTER(_sz)],
+    "codistill_kv_diff_attention": [ctypes.POINTER(KvCache), ctypes.POINTER(KvAttn), _vp, _vp, _vp, _vp, _sz, _vp],
     "codistill_adamw_table_bytes": [ctypes.POINTER(AdamwTensor), _i64, ctypes.POINTER(_sz)],
     "codistill_adamw_table": [ctypes.POINTER(AdamwTensor), _i64, _i32, _i32, _vp, _sz, ctypes.POINTER(AdamwPlan)],
     "codistill_adamw_step": [ctypes.POINTER(AdamwPlan), _vp, ctypes.POINTER(AdamwCfg), _vp, _vp],
@@ -475,6 +511,96 @@ def codistill_head_norm_backward(x, gain, dy, dx, dgain, workspace, eps=1e-5, po
     _check(lib.codistill_head_norm_backward(_dtype(x), _ptr(x), _inner(x, 2, "head_norm")[0], _ptr(gain), _ptr(dy), _inner(dy, 2, "head_norm")[0], _ptr(dx),
                                             _inner(dx, 2, "head_norm")[0], _ptr(dgain), x.shape[0], x.shape[1], x.shape[2], eps, post, _ptr(workspace),
                                             _room(workspace), _stream_ptr()))
+
+
+_NORM_ROTARY_ARRAYS = {n: NormRotaryTensor * n for n in range(1, CD_ROPE_MAX_TENSORS + 1)}
+
+
+def _norm_rotary_tensors(desc, positions, tensors, backward):
+    """The descriptors of (x, gain, y) or (x, gain, dy, dx, dgain), checked against the rotation's."""
+    n, tokens, dim, dt = len(tensors), positions.shape[1], desc.dim, torch.bfloat16 if desc.dtype == CD_BF16 else torch.float32
+    if positions.dtype is not torch.int32 or not positions.is_contiguous() or positions.shape[0] < desc.axes:
+        raise ValueError("norm_rotary: positions are contiguous int32 [axes, tokens]")
+    if n not in _NORM_ROTARY_ARRAYS:
+        raise ValueError("norm_rotary: %d tensors, up to %d in a call" % (n, CD_ROPE_MAX_TENSORS))
+    arr = _NORM_ROTARY_ARRAYS[n]()
+    for a, t in zip(arr, tensors):
+        x, gain, dgain = t[0], t[1], t[4] if backward else None
+        shape = x.shape
+        if len(shape) != 3 or shape[0] != tokens or shape[2] != dim:
+            raise ValueError("norm_rotary: tensors are [tokens, heads, dim] of the descriptor's type")
+        moved = (x, t[2], t[3]) if backward else (x, t[2])
+        for m in moved:
+            if m.shape != shape or m.dtype is not dt:
+                raise ValueError("norm_rotary: tensors are [tokens, heads, dim] of the descriptor's type")
+            if m.stride()[1:] != (dim, 1):
+                _inner(m, 2, "norm_rotary")
+        if gain is not None and (gain.shape != (dim,) or gain.dtype is not dt or not gain.is_contiguous()):
+            raise ValueError("norm_rotary: a gain is contiguous [dim] of the descriptor's type")
+        if dgain is not None and (dgain.shape != (dim,) or dgain.dtype is not torch.float32 or not dgain.is_contiguous()):
+            raise ValueError("norm_rotary: a gain's gradient is contiguous fp32 [dim]")
+        a.x, a.heads, a.x_token = x.data_ptr(), shape[1], x.stride(0)
+        if gain is not None:
+            a.gain = gain.data_ptr()
+        if backward:
+            a.dy, a.dx, a.dy_token, a.dx_token = t[2].data_ptr(), t[3].data_ptr(), t[2].stride(0), t[3].stride(0)
+            if dgain is not None:
+                a.dgain = dgain.data_ptr()
+        else:
+            a.y, a.y_token = t[2].data_ptr(), t[2].stride(0)
+    return arr, n, tokens
+
+
+def codistill_norm_rotary(desc, positions, tensors, eps=1e-5):
+    """Head norm with a rotary position behind it.  desc: rotary_desc(); positions: int32 [axes, tokens]; tensors: up to four (x, gain, y) of [tokens, heads, dim]
+    (y may be x), gain [dim] or None."""
+    arr, n, tokens = _norm_rotary_tensors(desc, positions, tensors, False)
+    _check(lib.codistill_norm_rotary(desc, positions.data_ptr(), tokens, arr, n, eps, _stream_ptr()))
+
+
+def norm_rotary_workspace_bytes(desc, tokens, n_tensors):
+    b = _sz()
+    _check(lib.codistill_norm_rotary_workspace_bytes(ctypes.byref(desc), tokens, n_tensors, ctypes.byref(b)))
+    return b.value
+
+
+def codistill_norm_rotary_backward(desc, positions, tensors, workspace, eps=1e-5):
+    """Gradients of codistill_norm_rotary: tensors are (x, gain, dy, dx, dgain), dx may be dy, dgain fp32 [dim] or None where there is no gain."""
+    arr, n, tokens = _norm_rotary_tensors(desc, positions, tensors, True)
+    _check(lib.codistill_norm_rotary_backward(desc, positions.data_ptr(), tokens, arr, n, eps, workspace.data_ptr(), _room(workspace), _stream_ptr()))
+
+
+def _embedding_desc(tokens, vocabulary, rows, table_dtype, scale):
+    if tokens.dtype not in (torch.int32, torch.int64) or tokens.dim() != 1 or not tokens.is_contiguous():
+        raise ValueError("embedding: tokens are contiguous int32 or int64 [rows]")
+    if rows.dim() != 2 or rows.shape[0] != tokens.shape[0] or (rows.shape[1] > 1 and rows.stride(1) != 1):
+        raise ValueError("embedding: rows are [rows, width], the channels of a row contiguous")
+    return Embedding(table_dtype, _dtype(rows), tokens.element_size(), scale, rows.shape[0], vocabulary, rows.shape[1], rows.stride(0))
+
+
+def codistill_embedding(tokens, table, y, scale=1.0):
+    """y[i] = scale table[tokens[i]], zero where a token lies outside the table.  tokens int32 or int64 [rows], table [vocabulary, width], y [rows, width]; both bf16 or fp32."""
+    if table.dim() != 2 or not table.is_contiguous() or table.shape[1] != y.shape[-1]:
+        raise ValueError("embedding: the table is contiguous [vocabulary, width]")
+    d = _embedding_desc(tokens, table.shape[0], y, _dtype(table), scale)
+    _check(lib.codistill_embedding(d, tokens.data_ptr(), table.data_ptr(), y.data_ptr(), _stream_ptr()))
+
+
+def embedding_workspace_bytes(rows, vocabulary, width):
+    """Room for the gradient of a table, whatever the rows' type."""
+    b, most = _sz(), 0
+    for dt in (CD_F32, CD_BF16):
+        _check(lib.codistill_embedding_workspace_bytes(Embedding(dt, dt, 8, 1.0, rows, vocabulary, width, width), ctypes.byref(b)))
+        most = max(most, b.value)
+    return most
+
+
+def codistill_embedding_backward(tokens, dy, dtable, workspace, scale=1.0, accumulate=False):
+    """dtable[w] = (or +=) scale times the sum of dy's rows whose token is w.  dy [rows, width] bf16 or fp32, dtable fp32 [vocabulary, width]."""
+    if dtable.dim() != 2 or not dtable.is_contiguous() or dtable.dtype is not torch.float32 or dtable.shape[1] != dy.shape[-1]:
+        raise ValueError("embedding_backward: the table's gradient is contiguous fp32 [vocabulary, width]")
+    d = _embedding_desc(tokens, dtable.shape[0], dy, CD_F32, scale)
+    _check(lib.codistill_embedding_backward(d, tokens.data_ptr(), dy.data_ptr(), dtable.data_ptr(), accumulate, _ptr(workspace), _room(workspace), _stream_ptr()))
 
 
 def adamw_table(tensors, state_bits, grad_dtype):

@@ -6,7 +6,7 @@
 // their pairs (once for all heads of all tensors, into LDS), then streams the heads past them in 16-byte vectors.  8192 tokens of 32 heads of 64 in bf16 (67 MB
 // moved): 13.0 us, 5.2 TB/s; 16 tokens: 3.8, a launch and its latencies.
 #include "common.h"
-#include <math.h>
+#include "rotary.h"
 
 namespace cd {
 namespace {
@@ -26,11 +26,6 @@ struct RopeArgs {
   uint8_t axis[CD_ROPE_MAX_PAIRS];
 };
 static_assert(sizeof(RopeArgs) <= 4096, "kernel arguments");
-
-// The angle in turns, in [-1/2, 1/2).  A frequency is a 64-bit fraction of a turn, so that whole turns fall out of the integer product; what is lost at any
-// position is the rounding to fp32, 2^-25 of a turn, and less than 2^-31 of cut bits.  A single fp32 product is a thousandth of a radian off at 30000 and half
-// a turn at 2^24.
-__device__ inline float turns(int32_t pos, uint64_t freq) { return (float)(int32_t)(((uint64_t)(int64_t)pos * freq) >> 32) * 0x1p-32f; }
 
 template <typename T, int N> struct Vec { T e[N]; };
 template <typename T, int N> __device__ inline Vec<T, N> load_vec(const T* p) {
@@ -66,13 +61,10 @@ __global__ void __launch_bounds__(256) rotary_kernel(RopeArgs a) {
   for (int i = threadIdx.x; i < nt * a.n_pairs; i += 256) {
     const int t = i / a.n_pairs, p = i % a.n_pairs;
     const float r = turns(a.pos[(int64_t)a.axis[p] * a.tokens + t0 + t], a.freq[p]);
-    if (sizeof(T) == 2) {   // the instructions take turns; their error, 1e-6, is far below a bf16 rounding
-      cs[t * CD_ROPE_MAX_PAIRS + p] = __builtin_amdgcn_cosf(r);
-      sn[t * CD_ROPE_MAX_PAIRS + p] = a.sign * __builtin_amdgcn_sinf(r);
-    } else {
-      cs[t * CD_ROPE_MAX_PAIRS + p] = cospif(2.f * r);
-      sn[t * CD_ROPE_MAX_PAIRS + p] = a.sign * sinpif(2.f * r);
-    }
+    float c, s;
+    cos_sin<T>(r, &c, &s);
+    cs[t * CD_ROPE_MAX_PAIRS + p] = c;
+    sn[t * CD_ROPE_MAX_PAIRS + p] = a.sign * s;
   }
   __syncthreads();
   const int half = a.dim >> 1, per_head = half / P, per_token = a.heads_end[a.n_tensors - 1] * per_head;
@@ -114,17 +106,6 @@ __global__ void __launch_bounds__(256) rotary_kernel(RopeArgs a) {
   }
 }
 
-// freq / (2 pi) without its whole turns, in units of 2^-64, cut: the number's 53 bits times 1 / (2 pi) to 128 bits, in integers.  (A quotient of doubles is off by
-// 2^-53 of itself, at position 2^31 and a thousand radians a position by 4e-5 of a turn.)  |freq| < 2^20.
-static uint64_t fraction_of_turn(double freq) {
-  int e = 0;
-  const uint64_t m = (uint64_t)ldexp(frexp(fabs(freq), &e), 53);   // |freq| = m 2^(e - 53)
-  const unsigned __int128 low = (unsigned __int128)m * 0x7f09d5f47d4d3770ull, high = (unsigned __int128)m * 0x28be60db9391054aull + (uint64_t)(low >> 64);
-  const int shift = 53 - e;   // at least 33: `high` is m / (2 pi) in units of 2^-64
-  const uint64_t f = shift < 128 ? (uint64_t)(high >> shift) : 0;
-  return freq < 0 ? 0 - f : f;
-}
-
 }  // namespace
 }  // namespace cd
 
@@ -133,14 +114,7 @@ using namespace cd;
 extern "C" int codistill_rotary(const cd_rotary* rope, const int32_t* positions, int64_t tokens, const cd_rotary_tensor* tensors,
                                 int64_t n_tensors, int inverse, void* stream) {
   CD_REQUIRE(rope && tensors && (positions || tokens == 0), "rotary: NULL pointer argument");
-  CD_REQUIRE(rope->dtype == CD_F32 || rope->dtype == CD_BF16, "rotary: unknown dtype %d", rope->dtype);
-  CD_REQUIRE(rope->dim >= 2 && rope->dim % 2 == 0 && rope->dim <= 2 * CD_ROPE_MAX_PAIRS, "rotary: dim=%d must be even and in 2..%d", rope->dim,
-             2 * CD_ROPE_MAX_PAIRS);
-  CD_REQUIRE(rope->n_pairs >= 0 && rope->n_pairs <= rope->dim / 2, "rotary: n_pairs=%d of %d", rope->n_pairs, rope->dim / 2);
-  CD_REQUIRE(rope->layout == CD_ROPE_HALVES || rope->layout == CD_ROPE_PAIRS, "rotary: unknown layout %d", rope->layout);
-  CD_REQUIRE(n_tensors >= 1 && n_tensors <= CD_ROPE_MAX_TENSORS, "rotary: n_tensors=%lld outside 1..%d", (long long)n_tensors, CD_ROPE_MAX_TENSORS);
-  CD_REQUIRE(tokens >= 0 && tokens <= INT32_MAX, "rotary: tokens=%lld out of range", (long long)tokens);
-  CD_REQUIRE((reinterpret_cast<uintptr_t>(positions) & 3) == 0, "rotary: positions must be 4-byte aligned");
+  if (const int rc = check_rope("rotary", rope, positions, tokens, n_tensors)) return rc;
   const int elem = rope->dtype == CD_BF16 ? 2 : 4, vec = 16 / elem;
   RopeArgs a = {};
   // whole vectors: both halves of a head (or the head) are vectors, and so is where every head begins
@@ -159,12 +133,7 @@ extern "C" int codistill_rotary(const cd_rotary* rope, const int32_t* positions,
     a.heads_end[i] = (int32_t)heads;
     moved += 2 * tokens * t.heads * rope->dim * elem;
   }
-  for (int p = 0; p < rope->n_pairs; p++) {
-    CD_REQUIRE(rope->axis[p] >= 0 && rope->axis[p] < rope->axes && rope->axis[p] < 256, "rotary: axis %d of pair %d outside 0..%d", rope->axis[p], p, rope->axes - 1);
-    CD_REQUIRE(isfinite(rope->freq[p]) && fabs(rope->freq[p]) < 1e6, "rotary: frequency of pair %d", p);
-    a.freq[p] = fraction_of_turn(rope->freq[p]);
-    a.axis[p] = (uint8_t)rope->axis[p];
-  }
+  if (const int rc = fill_pairs("rotary", rope, a.freq, a.axis)) return rc;
   if (tokens == 0) return CD_OK;
   a.n_tensors = (int32_t)n_tensors; a.dim = rope->dim; a.n_pairs = rope->n_pairs; a.tokens = tokens; a.pos = positions;
   a.sign = inverse ? -1.f : 1.f;

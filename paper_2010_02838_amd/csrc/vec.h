@@ -1,0 +1,37 @@
+// Runs of N elements as one load or store where they fill 8 or 16 bytes, element by element otherwise.
+#pragma once
+#include "common.h"
+
+namespace cd {
+
+template <typename T, int N> __device__ static inline void load_run(const T* p, T (&out)[N]) {
+  if constexpr (N * sizeof(T) == 16) {
+    const uint4 u = *reinterpret_cast<const uint4*>(p);
+    __builtin_memcpy(out, &u, 16);
+  } else if constexpr (N * sizeof(T) == 8) {
+    const uint2 u = *reinterpret_cast<const uint2*>(p);
+    __builtin_memcpy(out, &u, 8);
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; i++) out[i] = p[i];
+  }
+}
+template <typename T, int N> __device__ static inline void store_run(T* p, const float (&in)[N]) {
+  T t[N];
+#pragma unroll
+  for (int i = 0; i < N; i++) t[i] = Cvt<T>::st(in[i]);
+  if constexpr (N * sizeof(T) == 16) {
+    uint4 u;
+    __builtin_memcpy(&u, t, 16);
+    *reinterpret_cast<uint4*>(p) = u;
+  } else if constexpr (N * sizeof(T) == 8) {
+    uint2 u;
+    __builtin_memcpy(&u, t, 8);
+    *reinterpret_cast<uint2*>(p) = u;
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; i++) p[i] = t[i];
+  }
+}
+
+}  // namespace cd
