@@ -1,0 +1,150 @@
+"""Embedding lookup and the gradient of its table against the definition.
+
+The lookup is one product in fp32 and at most one rounding: equal.  The gradient of a word is a sum of n fp32 numbers in some order, a factor and, where
+it is added to what is there, one more addition: off by at most (n + 2) 2^-24 of the sum of magnitudes."""
+import math
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+DEV, BF, F32 = "cuda:0", torch.bfloat16, torch.float32
+
+
+def tokens_of(kind, rows, words, seed=0, dtype=torch.int64):
+    gen = torch.Generator().manual_seed(seed)
+    if kind == "uniform":
+        t = torch.randint(0, words, (rows,), generator=gen)
+    elif kind == "one":
+        t = torch.full((rows,), words - 1)
+    elif kind == "runs":        # long runs of few words, and the first word rare
+        t = torch.randint(0, words, (rows,), generator=gen) // max(1, words // 3) * max(1, words // 3)
+        t = t.clamp(max=words - 1)
+    elif kind == "none":
+        t = torch.full((rows,), -1)
+    else:                       # "text": most words rare, some frequent, a tenth outside the table
+        t = (torch.exp(torch.rand(rows, generator=gen).double() * math.log(words + 1)).long() - 1).clamp(0, words - 1)
+        out = torch.rand(rows, generator=gen) < 0.1
+        odd = torch.tensor([-1, words, -2 ** 31, 2 ** 31 - 1] + ([2 ** 32, 2 ** 32 + 1, -2 ** 63] if dtype is torch.int64 else []))
+        t = torch.where(out, odd[torch.randint(0, len(odd), (rows,), generator=gen)], t)
+    return t.to(dtype).to(DEV)
+
+
+def gradient(tokens, dy, dtable, scale=1.0, accumulate=False):
+    from paper_2010_02838_amd import binding as B
+    ws = torch.full((B.embedding_workspace_bytes(*dy.shape[:1], *dtable.shape),), 255, dtype=torch.uint8, device=DEV)
+    B.codistill_embedding_backward(tokens, dy, dtable, ws, scale, accumulate)
+
+
+def check(tokens, dy, words, scale=1.0, accumulate=False, seed=0):
+    width = dy.shape[1]
+    there = torch.randn(words, width, generator=torch.Generator(device=DEV).manual_seed(seed), device=DEV)
+    got = there.clone() if accumulate else torch.full((words, width), math.nan, device=DEV)
+    gradient(tokens, dy, got, scale, accumulate)
+    again = there.clone() if accumulate else torch.full((words, width), math.nan, device=DEV)
+    gradient(tokens, dy, again, scale, accumulate)
+    assert torch.equal(got.view(torch.int32), again.view(torch.int32))      # the same bits
+    t = tokens.cpu()
+    real = (t >= 0) & (t < words)
+    d = dy.cpu().double()[real] * scale
+    want, size, n = torch.zeros(words, width, dtype=torch.float64), torch.zeros(words, width, dtype=torch.float64), torch.zeros(words, 1, dtype=torch.float64)
+    want.index_add_(0, t[real].long(), d)
+    size.index_add_(0, t[real].long(), d.abs())
+    n.index_add_(0, t[real].long(), torch.ones(len(d), 1, dtype=torch.float64))
+    got = got.cpu()
+    if accumulate:
+        assert torch.equal(got[n[:, 0] == 0], there.cpu()[n[:, 0] == 0])    # not touched
+        want, size = want + there.cpu().double(), size + there.cpu().double().abs()
+    else:
+        assert (got[n[:, 0] == 0] == 0).all()
+    assert ((got.double() - want).abs() <= (n + 2) * 2.0 ** -24 * size).all()
+
+
+@pytest.mark.parametrize("kind", ["uniform", "one", "runs", "none", "text"])
+@pytest.mark.parametrize("rows,words,width,dtype", [
+    (1, 1, 1, F32), (2, 3, 8, BF), (31, 5, 64, F32), (33, 40, 333, BF), (300, 64, 256, F32), (300, 1000, 513, F32), (2000, 7, 100, BF), (5000, 3000, 512, BF), (16384, 1024, 40, BF),
+    (16385, 1023, 40, F32), (16385, 1024, 40, BF), (40000, 70000, 16, F32), (70000, 2 ** 21, 8, BF), (20000, 1, 24, F32)])
+def test_gradients(rows, words, width, dtype, kind):
+    gen = torch.Generator(device=DEV).manual_seed(rows)
+    dy = torch.randn(rows, width, generator=gen, device=DEV).to(dtype)
+    check(tokens_of(kind, rows, words), dy, words, scale=1.5)
+
+
+@pytest.mark.parametrize("rows", [500, 20000])
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("kind", ["uniform", "one", "text"])
+def test_gradients_beside_others(rows, dtype, kind):
+    gen = torch.Generator(device=DEV).manual_seed(rows)
+    dy = torch.randn(rows, 136, generator=gen, device=DEV).to(dtype)
+    check(tokens_of(kind, rows, 777, dtype=torch.int32), dy, 777, scale=0.3, accumulate=True)
+
+
+@pytest.mark.parametrize("rows", [400, 17000])
+def test_rows_that_are_not_read(rows):
+    """Rows of tokens outside the table hold NaN; rows lie apart, with NaN between them; or begin inside a vector."""
+    tokens = tokens_of("text", rows, 300)
+    wide = torch.full((rows, 96), math.nan, device=DEV)
+    for off in (0, 1, 16):
+        dy = wide[:, off:off + 64]
+        dy.copy_(torch.randn(rows, 64, generator=torch.Generator(device=DEV).manual_seed(1), device=DEV))
+        clean = dy.clone()
+        dy[(tokens < 0) | (tokens >= 300)] = math.nan
+        got, want = torch.empty(300, 64, device=DEV), torch.empty(300, 64, device=DEV)
+        gradient(tokens, dy, got)
+        gradient(tokens, clean, want)
+        assert torch.isfinite(got).all() and ((got - want).abs() <= 1e-4 * want.abs().clamp(min=1)).all()
+        wide.fill_(math.nan)
+
+
+def test_no_rows():
+    t, dy = torch.zeros(0, dtype=torch.int64, device=DEV), torch.zeros(0, 24, device=DEV)
+    g = torch.full((50, 24), 3.0, device=DEV)
+    gradient(t, dy, g, accumulate=True)
+    assert (g == 3).all()
+    gradient(t, dy, g)
+    assert (g == 0).all()
+
+
+def test_a_gradient_that_begins_inside_a_vector():
+    """The table's gradient is a range of one flat buffer, as flat parameter buffers have it."""
+    tokens, dy = tokens_of("text", 900, 50), torch.randn(900, 64, device=DEV)
+    flat, want = torch.full((50 * 64 + 8,), 7.0, device=DEV), torch.empty(50, 64, device=DEV)
+    gradient(tokens, dy, want)
+    for off in (1, 2, 4):
+        flat.fill_(7.0)
+        gradient(tokens, dy, flat[off:off + 3200].view(50, 64))
+        assert (flat[:off] == 7).all() and (flat[off + 3200:] == 7).all()
+        assert ((flat[off:off + 3200].view(50, 64) - want).abs() <= 1e-4 * want.abs().clamp(min=1)).all()
+
+
+@pytest.mark.parametrize("table_dtype", [BF, F32])
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("rows,words,width,off", [(1, 1, 1, 0), (7, 3, 8, 0), (100, 50, 333, 0), (1000, 50, 512, 0), (100, 20, 64, 1), (64, 9, 64, 4), (0, 5, 16, 0), (3000, 7, 2048, 8)])
+def test_lookups(table_dtype, dtype, rows, words, width, off):
+    from paper_2010_02838_amd import binding as B
+    table = torch.randn(words, width, device=DEV).to(table_dtype)
+    for token_type in (torch.int64, torch.int32):
+        tokens = tokens_of("text", rows, words, dtype=token_type)
+        wide = torch.full((rows, width + 16), 7.0, dtype=dtype, device=DEV)
+        B.codistill_embedding(tokens, table, wide[:, off:off + width], 1.7)
+        real = (tokens >= 0) & (tokens < words)
+        want = torch.where(real[:, None], table[torch.where(real, tokens, 0).long()].float() * 1.7, torch.zeros((), device=DEV)).to(dtype)
+        assert torch.equal(wide[:, off:off + width], want)
+        assert (wide[:, :off] == 7).all() and (wide[:, off + width:] == 7).all()
+
+
+def test_against_differences():
+    """The lookup is linear in its table: a difference of any step is the gradient, but for roundings (1e-6 of the sum's terms over the step's size)."""
+    from paper_2010_02838_amd import binding as B
+    gen = torch.Generator(device=DEV).manual_seed(3)
+    table, dy, tokens = torch.randn(40, 64, generator=gen, device=DEV), torch.randn(200, 64, generator=gen, device=DEV), tokens_of("text", 200, 40)
+    g, y = torch.empty(40, 64, device=DEV), torch.empty(200, 64, device=DEV)
+    gradient(tokens, dy, g, 2.5)
+
+    def value(t):
+        B.codistill_embedding(tokens, t, y, 2.5)
+        return float((dy.double() * y.double()).sum())
+
+    d = torch.randn(40, 64, generator=gen, device=DEV)
+    got, want = (value(table + d) - value(table - d)) / 2, float((g.double() * d.double()).sum())
+    assert abs(got - want) <= 1e-5 * float((dy.double() * y.double()).norm())

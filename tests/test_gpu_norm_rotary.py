@@ -1,0 +1,201 @@
+"""Norm with a rotary position behind it, forward and backward, against the formula in float64 and against differences.
+
+Tolerances, element by element.  With u = 2^-24: r is off by the sum of squares (at most 2 * 8 + 8 additions, halved by the root) and a root and a quotient, 15 u; xhat, the
+gain's product, two products and a sum of the turn 5 u; the angle is exact to 2^-24 of a turn (4e-7) and its cosine and sine to 4 u in fp32: under 2e-6 of the pair's two
+channels.  In bf16 the cosine and sine come from the instructions, 1e-6 more, and the result is rounded once, 2^-8 of itself at most.  dx: the same for
+dn, and the mean of h xhat (as many additions again): 4e-6 of r (|h| + |xhat| mean|h xhat|).  dgain: terms off by 3e-6 each, added up in chains of at most 100
+additions: 100 u + 3e-6 < 1e-5 of the sum of their magnitudes."""
+import math
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+DEV, BF, F32 = "cuda:0", torch.bfloat16, torch.float32
+EPS = 1e-5
+
+
+def turned(x, cos, sin, halves):
+    """x [tokens, heads, dim] in float64; cos, sin [tokens, pairs]."""
+    n, half = cos.shape[1], x.shape[2] // 2
+    at = (torch.arange(n), half + torch.arange(n)) if halves else (2 * torch.arange(n), 2 * torch.arange(n) + 1)
+    c, s, y = cos[:, None], sin[:, None], x.clone()
+    y[..., at[0]], y[..., at[1]] = x[..., at[0]] * c - x[..., at[1]] * s, x[..., at[1]] * c + x[..., at[0]] * s
+    return y
+
+
+def pair_size(x, halves, n):
+    """The size of the two channels that meet in a turn."""
+    half = x.shape[2] // 2
+    at = (torch.arange(n), half + torch.arange(n)) if halves else (2 * torch.arange(n), 2 * torch.arange(n) + 1)
+    y = x.abs().clone()
+    y[..., at[0]] = y[..., at[1]] = y[..., at[0]] + y[..., at[1]]
+    return y
+
+
+class Problem:
+    """Queries and keys (and more) as ranges of wider rows, `off` elements from a whole vector."""
+
+    def __init__(self, dtype, tokens, heads, dim, sections, halves=True, gains=None, off=0, seed=0, eps=EPS):
+        from paper_2010_02838_amd import binding as B
+        self.B, self.halves, self.dim, self.n, self.eps, self.dt = B, halves, dim, sum(sections), eps, dtype
+        gen = torch.Generator(device=DEV).manual_seed(seed)
+        every = sum(heads) * dim
+
+        def ranges(scale=1.0, fill=None):
+            wide = torch.randn(tokens, every + 16, generator=gen, device=DEV) * scale if fill is None else torch.full((tokens, every + 16), fill, device=DEV)
+            self.wides.append(wide.to(dtype))
+            return [p.unflatten(1, (-1, dim)) for p in self.wides[-1][:, off:off + every].split([h * dim for h in heads], 1)]
+
+        self.wides = []
+        self.x, self.dy = ranges(), ranges(0.3)
+        self.y, self.dx = ranges(fill=7.0), ranges(fill=7.0)
+        gains = [True] * len(heads) if gains is None else gains
+        self.g = [(1 + 0.3 * torch.randn(dim, generator=gen, device=DEV)).to(dtype) if has else None for has in gains]
+        self.dg = [torch.full((dim,), 7.0, device=DEV) if has else None for has in gains]
+        self.pos = torch.randint(-50, 30000, (len(sections), tokens), generator=gen, device=DEV, dtype=torch.int32)
+        self.desc = B.rotary_desc(dim, sections, 1e4, dtype, layout=B.CD_ROPE_HALVES if halves else B.CD_ROPE_PAIRS)
+        self.ws = torch.empty(B.norm_rotary_workspace_bytes(self.desc, tokens, len(heads)), dtype=torch.uint8, device=DEV)
+        axis = torch.tensor([a for a, m in enumerate(sections) for _ in range(m)], dtype=torch.long)
+        ang = self.pos.cpu().double()[axis].t() * torch.pow(1e4, -2.0 * torch.arange(self.n).double() / dim)
+        self.cos, self.sin = ang.cos(), ang.sin()
+
+    def run(self, back=True):
+        self.B.codistill_norm_rotary(self.desc, self.pos, list(zip(self.x, self.g, self.y)), self.eps)
+        if back:
+            self.B.codistill_norm_rotary_backward(self.desc, self.pos, list(zip(self.x, self.g, self.dy, self.dx, self.dg)), self.ws, self.eps)
+
+    def check(self):
+        step = 2.0 ** -8 if self.dt is BF else 0.0
+        for x, g, y, dy, dx, dg in zip(self.x, self.g, self.y, self.dy, self.dx, self.dg):
+            x, y, dy, dx = (t.cpu().double() for t in (x, y, dy, dx))
+            gain = torch.ones(self.dim, dtype=torch.float64) if g is None else g.cpu().double()
+            r = 1 / (x.square().mean(-1, keepdim=True) + self.eps).sqrt()
+            n = gain * x * r
+            want = turned(n, self.cos, self.sin, self.halves)
+            size = pair_size(n, self.halves, self.n)
+            assert ((y - want).abs() <= step * want.abs() + 4e-6 * size).all(), ((y - want).abs() - step * want.abs() - 4e-6 * size).max()
+            dn = turned(dy, self.cos, -self.sin, self.halves)
+            h, xhat = gain * dn, x * r
+            dot = (h * xhat).mean(-1, keepdim=True)
+            want = r * (h - xhat * dot)
+            size = r * (gain.abs() * pair_size(dy, self.halves, self.n) + xhat.abs() * (gain.abs() * pair_size(dy, self.halves, self.n) * xhat.abs()).mean(-1, keepdim=True))
+            assert ((dx - want).abs() <= step * want.abs() + 8e-6 * size).all()
+            if g is not None:
+                terms = pair_size(dy, self.halves, self.n) * xhat.abs()
+                assert ((dg.cpu().double() - (dn * xhat).sum((0, 1))).abs() <= 1e-5 * terms.sum((0, 1)) + 1e-30).all()
+
+    def around(self, off):
+        """What lies beside the tensors' ranges of y and dx."""
+        every = sum(t.shape[1] for t in self.x) * self.dim
+        for w in self.wides[2:]:
+            assert (w[:, :off] == 7.0).all() and (w[:, off + every:] == 7.0).all()
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("halves", [True, False])
+@pytest.mark.parametrize("tokens,heads,dim,sections", [
+    (1, (1,), 2, (1,)), (3, (2, 1), 8, (4,)), (1, (32, 8), 64, (32,)), (77, (6, 3), 40, (20,)), (333, (6, 3), 40, (5, 4, 3)), (130, (4, 4), 64, (8, 12, 12)),
+    (65, (5, 1, 2, 3), 128, (64,)), (40, (3, 2), 256, (100, 28)), (9, (2,), 254, (127,)), (700, (2, 1), 96, (0,)), (21, (3,), 6, (2,)), (5000, (2, 1), 32, (16,))])
+def test_against_the_formula(dtype, halves, tokens, heads, dim, sections):
+    p = Problem(dtype, tokens, heads, dim, sections, halves, off=8, seed=dim + tokens)
+    p.run()
+    p.check()
+    p.around(8)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("halves", [True, False])
+@pytest.mark.parametrize("off", [1, 2, 4])
+def test_ranges_that_begin_inside_a_vector(dtype, halves, off):
+    p = Problem(dtype, 50, (4, 2), 64, (24,), halves, off=off, seed=off)
+    p.run()
+    p.check()
+    p.around(off)
+
+
+@pytest.mark.parametrize("gains", [(False, False), (True, False), (False, True)])
+def test_without_gains(gains):
+    p = Problem(F32, 70, (4, 2), 64, (32,), gains=gains)
+    p.run()
+    p.check()
+
+
+def test_in_place_and_the_same_bits_again():
+    for dtype in (BF, F32):
+        p = Problem(dtype, 300, (8, 8), 64, (32,))
+        p.run()
+        first = [t.clone() for t in p.y + p.dx + p.dg]
+        p.run()
+        assert all(torch.equal(a, b) for a, b in zip(first, p.y + p.dx + p.dg))
+        x = [t.clone() for t in p.x]
+        p.B.codistill_norm_rotary(p.desc, p.pos, list(zip(x, p.g, x)), p.eps)
+        d = [t.clone() for t in p.dy]
+        p.B.codistill_norm_rotary_backward(p.desc, p.pos, list(zip(p.x, p.g, d, d, p.dg)), p.ws, p.eps)
+        assert all(torch.equal(a, b) for a, b in zip(first, x + d + p.dg))
+
+
+def test_nothing_and_zeros():
+    """No tokens: gains' gradients of zero.  Heads of zeros: outputs of zero, gradients of h / sqrt(eps)."""
+    p = Problem(F32, 0, (3, 2), 64, (32,))
+    p.run()
+    assert all((t == 0).all() for t in p.dg)
+    for dtype in (BF, F32):
+        p = Problem(dtype, 5, (2,), 64, (32,))
+        p.x[0].zero_()
+        p.run()
+        p.check()
+        assert (p.y[0] == 0).all() and (p.dg[0] == 0).all()
+
+
+def test_heads_that_are_not_finite_are_alone():
+    """An infinity or a NaN stays in its own head (and in the gain's gradient, which all heads share)."""
+    for dtype in (BF, F32):
+        p = Problem(dtype, 12, (4, 2), 64, (32,))
+        p.x[0][3, 1, 5] = math.inf
+        p.x[1][7, 0, 40] = math.nan
+        p.run()
+        bad = [torch.zeros(12, 4, dtype=torch.bool), torch.zeros(12, 2, dtype=torch.bool)]
+        bad[0][3, 1] = bad[1][7, 0] = True
+        q = Problem(dtype, 12, (4, 2), 64, (32,))
+        q.run()
+        for b, y, w, dx, dw in zip(bad, p.y, q.y, p.dx, q.dx):
+            assert torch.equal(y[~b], w[~b]) and torch.equal(dx[~b], dw[~b])
+            assert not torch.isfinite(y[b]).all() and not torch.isfinite(dx[b]).all()
+
+
+@pytest.mark.parametrize("halves", [True, False])
+def test_against_differences(halves):
+    """sum of c y along random directions: central differences of step h are off by h^2 / 6 of the third derivative (a few times the first at h = 0.01: 1e-4) and
+    by the roundings of y over h (1e-7 of the sum's terms, 1e-5 of the result)."""
+    p = Problem(F32, 6, (3,), 64, (20,), halves, seed=4)
+    c = p.dy[0]
+    p.run()
+    gen = torch.Generator(device=DEV).manual_seed(9)
+
+    def value(x, g):
+        y = torch.empty_like(x)
+        p.B.codistill_norm_rotary(p.desc, p.pos, [(x, g, y)], p.eps)
+        return float((c.double() * y.double()).sum())
+
+    for _ in range(3):
+        d = torch.randn(p.x[0].shape, generator=gen, device=DEV)
+        got = (value(p.x[0] + 0.01 * d, p.g[0]) - value(p.x[0] - 0.01 * d, p.g[0])) / 0.02
+        want, size = float((p.dx[0].double() * d.double()).sum()), float((p.dx[0].double() * d.double()).norm())
+        assert abs(got - want) <= 2e-3 * size
+        d = torch.randn(64, generator=gen, device=DEV)
+        got = (value(p.x[0], p.g[0] + 0.01 * d) - value(p.x[0], p.g[0] - 0.01 * d)) / 0.02
+        want, size = float((p.dg[0].double() * d.double()).sum()), float((p.dg[0].double() * d.double()).norm())
+        assert abs(got - want) <= 2e-3 * size
+
+
+def test_it_is_the_norm_and_the_rotation():
+    """The two operators that it takes the place of, one behind the other, in fp32: 4e-6 of a pair's size (what each rounds)."""
+    from paper_2010_02838_amd import binding as B
+    p = Problem(F32, 60, (4,), 64, (32,))
+    p.run(False)
+    n = torch.empty(60, 4, 64, device=DEV)
+    B.codistill_head_norm(p.x[0], p.g[0], n, EPS)
+    size = pair_size(n.cpu().double(), True, 32)
+    B.codistill_rotary(p.desc, p.pos, [(n, n)])
+    assert ((n.cpu().double() - p.y[0].cpu().double()).abs() <= 4e-6 * size).all()
