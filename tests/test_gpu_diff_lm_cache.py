@@ -1,0 +1,203 @@
+"""The small language model with normalised queries and keys, its embedding's gradient, and decoding from caches in 8 bits."""
+import math
+
+import pytest
+import torch
+
+from test_gpu_diff_lm import DEV
+
+pytestmark = pytest.mark.gpu
+
+
+def reference(lm, tokens, starts, positions, dlogits):
+    """The network with normalised queries and keys in float64, with torch's derivatives.  Returns logits and gradients."""
+    w = {n: (lm.w[n] if n.startswith("lam") else lm.p[n]).detach().double().cpu().requires_grad_(True) for n in lm.w}
+    tokens, pos, starts = tokens.cpu(), positions[0].double().cpu(), starts.tolist()
+    H, K, D = lm.H, lm.K, lm.D
+
+    def norm(x, g, post=1.0):
+        return post * g * x / (x.square().mean(-1, keepdim=True) + 1e-5).sqrt()
+
+    ang = pos[:, None] * 10000.0 ** (-torch.arange(D // 2).double() * 2 / D)
+
+    def turn(t):
+        c, s = ang.cos()[:, None, None], ang.sin()[:, None, None]
+        a, b = t[..., :D // 2], t[..., D // 2:]
+        return torch.cat([a * c - b * s, b * c + a * s], -1)
+
+    x = w["embed"][tokens]
+    for i in range(lm.L):
+        q, k, v = (norm(x, w["norm%d" % i]) @ w["qkv%d" % i].t()).split([2 * D * H, 2 * D * K, 2 * D * K], 1)
+        q, k, v = turn(norm(q.view(-1, H, 2, D), w["qn%d" % i])), turn(norm(k.view(-1, K, 2, D), w["kn%d" % i])), v.view(-1, K, 2 * D)
+        rows = []
+        for a, b in zip(starts, starts[1:]):
+            heads = []
+            for h in range(H):
+                g = h // (H // K)
+                see = torch.ones(b - a, b - a).tril().bool()
+                p = [torch.softmax((q[a:b, h, m] @ k[a:b, g, m].t() / math.sqrt(D)).masked_fill(~see, -math.inf), 1) for m in (0, 1)]
+                heads.append((p[0] - w["lam%d" % i][h] * p[1]) @ v[a:b, g])
+            rows.append(torch.stack(heads, 1))
+        x = x + norm(torch.cat(rows), w["head%d" % i], lm.post).flatten(1) @ w["out%d" % i].t()
+    z = norm(x, w["norm"]) @ w["embed"].t()
+    z.backward(dlogits.double().cpu())
+    return z.detach(), {n: t.grad for n, t in w.items()}
+
+
+@pytest.mark.parametrize("dtype,kv_heads", [(torch.float32, 2), (torch.float32, 1), (torch.bfloat16, 2)])
+def test_gradients_with_normalised_queries(dtype, kv_heads):
+    """fp32: some thirty sums of fp32 products between a weight and the logits, 1e-4; bf16 (one layer, a small lambda): some seven roundings of 2^-9, 2e-2 (as without norms)."""
+    from paper_2010_02838_amd.diff_lm import DiffLM, copying_batch
+    exact = dtype is torch.float32
+    lm = DiffLM(50, layers=2 if exact else 1, heads=4, kv_heads=kv_heads, head_dim=32, lambda_init=0.5 if exact else 0.2, seed=3, dtype=dtype, qk_norm=True)
+    gen = torch.Generator(device=DEV).manual_seed(2)
+    for n in lm.w:
+        if n[:2] in ("qn", "kn"):
+            lm.w[n].copy_(1 + 0.3 * torch.randn(32, generator=gen, device=DEV))
+            lm.p[n].copy_(lm.w[n])
+    tokens, positions, starts, _ = copying_batch(5, 20, 50, seed=1)
+    z = lm.forward(tokens, positions, starts, 40)
+    dz = torch.randn(z.shape, generator=gen, device=DEV).bfloat16().float()
+    lm.backward(dz)
+    want, grads = reference(lm, tokens, starts, positions, dz)
+    tol = 1e-4 if exact else 2e-2
+    assert (z.double().cpu() - want).norm() <= tol * want.norm()
+    for n, g in grads.items():
+        if n[:3] != "lam" or exact:      # (a few lambdas: sums of terms of either sign that may cancel)
+            assert (lm.g[n].double().cpu() - g).norm() <= tol * g.norm(), n
+
+
+def test_gradients_repeat_and_words_that_do_not_occur():
+    from paper_2010_02838_amd.diff_lm import DiffLM, copying_batch
+    lm = DiffLM(300, layers=1, heads=4, kv_heads=2, head_dim=32, seed=3, qk_norm=True)
+    tokens, positions, starts, _ = copying_batch(100, 20, 7, seed=1)
+    first = None
+    for _ in range(4):
+        z = lm.forward(tokens, positions, starts, 40)
+        lm.backward(torch.where(torch.arange(300, device=DEV) < 7, torch.cos(z), 0.0))
+        got = {k: g.clone() for k, g in lm.g.items()}
+        first = first or got
+        assert all(torch.equal(g, first[k]) for k, g in got.items())
+    assert (got["embed"][7:] == 0).all() and (got["embed"][:7] != 0).any(1).all()
+
+
+@pytest.mark.parametrize("qk_norm", [False, True])
+def test_decoding_from_a_cache_in_8_bits(qk_norm):
+    """Against a decoder in fp32 that keeps, in place of its new tokens' keys and values, what the coded cache holds of them: the same numbers, other orders of fp32
+    sums (1e-4).  (It does not quantise its own: an element next to the border between two codes falls on either side by its last bit, and a code is 1 / 127 of
+    the largest element, so that one such token moves the logits by more than 1e-4.)  What is held is the element to half a step.  Prompts first, of different
+    lengths, then token by token; a sequence begins anew on the way."""
+    from paper_2010_02838_amd.diff_lm import Decoder, DiffLM
+
+    class Rounded(Decoder):
+        def _attend(self, i, q, k, v, at):
+            held_k, held_v = torch.empty_like(k[:, None].contiguous()), torch.empty_like(v[:, None].contiguous())
+            cache = coded.caches[i]
+            cache.read(cache.rows(held_k, held_v, first=at.int()), held_k, held_v)
+            for held, x in ((held_k[:, 0], k), (held_v[:, 0], v)):
+                step = x.abs().amax(-1, keepdim=True) * (1 + 2.0 ** -7) / 127
+                assert ((held - x).abs() <= 0.5 * step + 1e-4 * x.abs().amax()).all()
+            super()._attend(i, q, held_k[:, 0], held_v[:, 0], at)
+
+    lm = DiffLM(50, layers=2, heads=4, kv_heads=2, head_dim=32, seed=4, qk_norm=qk_norm)
+    words = torch.randint(0, 50, (3, 200), generator=torch.Generator().manual_seed(5)).to(DEV)
+    coded, plain = lm.decoder(3, 300, cache_bits=8), Rounded(lm, 3, 300)
+    for t in range(150):
+        if t == 100:
+            for d in (coded, plain):
+                d.lens[1] = 0
+        a, b = coded.step(words[:, t]), plain.step(words[:, t])
+        assert (a - b).norm() <= 1e-4 * b.norm(), t
+    # prompts: what they leave in the caches is what they would have left token by token; in fp32 the prompt's own pass is not rounded
+    lens = [70, 1, 129]
+    prompt = torch.cat([words[i, :n] for i, n in enumerate(lens)])
+    starts = torch.tensor([0, 70, 71, 200], dtype=torch.int32, device=DEV)
+    plain = lm.decoder(3, 300)
+    za, zb = coded.prefill(prompt, starts, 129), plain.prefill(prompt, starts, 129)
+    assert torch.equal(za, zb)
+    positions = torch.cat([torch.arange(n) for n in lens]).int()[None].to(DEV)
+    z = lm.forward(prompt, positions, starts, 129)
+    assert (za - z).norm() <= 1e-4 * z.norm()
+    for i in range(lm.L):
+        k, v = (t.clone() for t in (plain.k[i], plain.v[i]))
+        coded.caches[i].read(coded.caches[i].rows(k, v, counts=coded.lens), k, v)
+        for b, n in enumerate(lens):
+            for got, want in ((k[b, :n], plain.k[i][b, :n]), (v[b, :n], plain.v[i][b, :n])):
+                assert ((got - want).abs() <= (0.5 + 2.0 ** -7) * want.abs().amax(-1, keepdim=True) * (1 + 2.0 ** -7) / 127).all()     # half a step of the largest
+        plain.k[i].copy_(torch.where(torch.isfinite(k), k, 0.0))
+        plain.v[i].copy_(torch.where(torch.isfinite(v), v, 0.0))
+    a, b = coded.step(words[:, 199]), plain.step(words[:, 199])
+    new = (a - b).norm()     # (the new token's own key and value are codes in one of them: half a step of one key among many)
+    assert new <= 3e-2 * b.norm()
+
+
+def test_decoder_refuses():
+    from paper_2010_02838_amd.diff_lm import DiffLM
+    lm = DiffLM(20, layers=1, heads=2, kv_heads=1, head_dim=16, seed=2)
+    with pytest.raises(ValueError):
+        lm.decoder(2, 6, cache_bits=4)
+    for bits in (None, 8):
+        decoder = lm.decoder(2, 6, cache_bits=bits)
+        words = torch.randint(0, 20, (12,), generator=torch.Generator().manual_seed(1)).to(DEV)
+        for starts, longest in (([0, 7, 12], 7), ([0, 6], 6), ([0, 6, 11], 6), ([1, 6, 12], 6), ([0, 6, 12], 5), ([0, 14, 12], 6)):
+            with pytest.raises(ValueError):
+                decoder.prefill(words, torch.tensor(starts, dtype=torch.int32, device=DEV), longest)
+        decoder.prefill(words[:9], torch.tensor([0, 3, 9], dtype=torch.int32, device=DEV), 6)
+        with pytest.raises(ValueError):
+            decoder.step(words[:2])       # one of them is full
+        decoder.lens.zero_()
+        first = [decoder.step(words[2 * t:2 * t + 2]) for t in range(6)]
+        with pytest.raises(ValueError):
+            decoder.step(words[:2])
+        decoder.lens.zero_()
+        for t in range(6):
+            assert torch.equal(decoder.step(words[2 * t:2 * t + 2]), first[t])
+
+
+def test_captured_training_operators():
+    """Embedding, norm with rotation, the update of a cache and their gradients in one graph: replays, with eager work between them, equal the eager run bit for bit."""
+    from paper_2010_02838_amd import binding as B
+    gen = torch.Generator(device=DEV).manual_seed(6)
+    for rows in (300, 17000):       # (places counted, and a radix sort)
+        table = torch.randn(500, 256, generator=gen, device=DEV).bfloat16()
+        tokens = torch.randint(-1, 500, (rows,), generator=gen, device=DEV)
+        x, y, dy, dx = (torch.randn(rows, 256, generator=gen, device=DEV).bfloat16() for _ in range(4))
+        dtable, dgain = torch.empty(500, 256, device=DEV), torch.empty(64, device=DEV)
+        gain, pos = torch.ones(64, device=DEV).bfloat16(), torch.arange(rows, dtype=torch.int32, device=DEV)[None]
+        rope = B.rotary_desc(64, (32,), 1e4, torch.bfloat16)
+        heads = lambda t: t.view(rows, 4, 64)   # noqa: E731
+        nws = torch.empty(B.norm_rotary_workspace_bytes(rope, rows, 1), dtype=torch.uint8, device=DEV)
+        ews = torch.empty(B.embedding_workspace_bytes(rows, 500, 256), dtype=torch.uint8, device=DEV)
+
+        def step():
+            B.codistill_embedding(tokens, table, x, 16.0)
+            B.codistill_norm_rotary(rope, pos, [(heads(x), gain, heads(y))])
+            B.codistill_norm_rotary_backward(rope, pos, [(heads(x), gain, heads(dy), heads(dx), dgain)], nws)
+            B.codistill_embedding_backward(tokens, dx, dtable, ews, 16.0)
+            B.codistill_embedding_backward(tokens, dx, dtable, ews, 2.0, accumulate=True)
+
+        results = []
+
+        def snapshot():
+            torch.cuda.synchronize()
+            results.append([t.clone() for t in (x, y, dx, dgain, dtable)])
+            for t in (x, y, dx, dgain, dtable, nws, ews):
+                t.fill_(7)
+
+        side = torch.cuda.Stream()
+        step()
+        snapshot()
+        graph = torch.cuda.CUDAGraph()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            step()
+            snapshot()
+            with torch.cuda.graph(graph, stream=side):
+                step()
+        torch.cuda.current_stream().wait_stream(side)
+        for _ in range(3):
+            graph.replay()
+            snapshot()
+            (torch.randn(1 << 20, device=DEV) ** 2).sum().item()
+        for r in results[1:]:
+            assert all(torch.equal(a, b) for a, b in zip(results[0], r))
