@@ -19,8 +19,8 @@ namespace {
 
 constexpr uint32_t NO_WORD = 0x7fffffffu;   // sorted behind all words
 constexpr int RANK_ROWS = 16384;            // most rows whose places are counted
-constexpr int RANK_EACH = 16;               // rows of a workgroup there
-constexpr int DIGIT_BITS = 10, SORT_CHUNKS = 256, SORT_LEAST = 2048, SORT_WAVES = 8;
+constexpr int RANK_EACH = 16, RANK_AHEAD = 8;   // rows of a workgroup there, loads in flight
+constexpr int DIGIT_BITS = 10, SORT_CHUNKS = 256, SORT_LEAST = 1024, SORT_WAVES = 8;
 constexpr int SUM_WAVES = 8;                // waves of a block of rows
 constexpr int FILL_BLOCKS = 1024;
 
@@ -28,8 +28,8 @@ struct EmbedArgs {
   const void* tokens; const void* table; const void* dy; void* y; float* dtable;
   int32_t *order, *words, *order2, *words2, *counts;   // rows and words in sorted order; the same between passes of the radix sort; counts [digits][chunks]
   float* partial;                                      // [blocks][2][width]: sums of a block's first and last words, where others have parts of them
-  int64_t rows, vocabulary, width, row_stride;
-  int32_t token_bytes, accumulate, each, blocks, slabs, chunk, chunks, shift, digits, from_tokens, sort_blocks;
+  int64_t rows, vocabulary, width, row_stride, sums;   // sums: workgroups that add up; the others write zeros
+  int32_t token_bytes, accumulate, each, blocks, slabs, chunk, chunks, shift, digits, from_tokens;
   float scale;
 };
 
@@ -71,21 +71,9 @@ __global__ void __launch_bounds__(256) embedding_kernel(EmbedArgs a, int lanes) 
 }
 
 // ---- the order of the rows --------------------------------------------------------------------------------------------------
-// zeros for the whole table, by the workgroups behind `first`
-__device__ inline void zero_table(const EmbedArgs& a, int first) {
-  const int64_t n = a.vocabulary * a.width, whole = n / 4, step = (int64_t)(gridDim.x - first) * blockDim.x, at = (int64_t)(blockIdx.x - first) * blockDim.x + threadIdx.x;
-  if ((reinterpret_cast<uintptr_t>(a.dtable) & 15) == 0) {
-    for (int64_t i = at; i < whole; i += step) reinterpret_cast<uint4*>(a.dtable)[i] = make_uint4(0, 0, 0, 0);
-    for (int64_t i = 4 * whole + at; i < n; i += step) a.dtable[i] = 0.f;
-  } else {
-    for (int64_t i = at; i < n; i += step) a.dtable[i] = 0.f;
-  }
-}
-
 // Few rows: place of row i = rows with a smaller word + rows in front of it with the same.  A wave compares 64 rows with one of the
 // workgroup's at a time; what it counts is scalar.
 __global__ void __launch_bounds__(256) embedding_rank_kernel(EmbedArgs a) {
-  if ((int)blockIdx.x >= a.sort_blocks) return zero_table(a, a.sort_blocks);
   __shared__ uint32_t mine[RANK_EACH];
   __shared__ int found[4][RANK_EACH];
   const int i0 = blockIdx.x * RANK_EACH, rows = (int)a.rows, wave = threadIdx.x >> 6;
@@ -98,16 +86,26 @@ __global__ void __launch_bounds__(256) embedding_rank_kernel(EmbedArgs a) {
     w[r] = __builtin_amdgcn_readfirstlane(mine[r]);
     count[r] = 0;
   }
-  for (int j0 = wave * 64; j0 < rows; j0 += 256) {
-    const int j = j0 + (threadIdx.x & 63);
-    const uint32_t other = j < rows ? word_of(a, j) : 0xffffffffu;
-    if (j0 + 64 <= i0 || j0 >= i0 + RANK_EACH) {   // all 64 in front of the workgroup's rows, or all behind
-      const uint32_t same = j0 < i0;
+  for (int k0 = wave * 64; k0 < rows; k0 += 256 * RANK_AHEAD) {
+    uint32_t others[RANK_AHEAD];
 #pragma unroll
-      for (int r = 0; r < RANK_EACH; r++) count[r] += __popcll(__ballot(other < w[r] + same));
-    } else {
+    for (int u = 0; u < RANK_AHEAD; u++) {
+      const int j = k0 + 256 * u + (threadIdx.x & 63);
+      others[u] = j < rows ? word_of(a, j) : 0xffffffffu;
+    }
 #pragma unroll
-      for (int r = 0; r < RANK_EACH; r++) count[r] += __popcll(__ballot(other < w[r] + (j < i0 + r ? 1u : 0u)));
+    for (int u = 0; u < RANK_AHEAD; u++) {
+      const int j0 = k0 + 256 * u;
+      const uint32_t other = others[u];
+      if (j0 + 64 <= i0 || j0 >= i0 + RANK_EACH) {   // all 64 in front of the workgroup's rows, or all behind
+        const uint32_t same = j0 < i0;
+#pragma unroll
+        for (int r = 0; r < RANK_EACH; r++) count[r] += __popcll(__ballot(other < w[r] + same));
+      } else {
+        const int j = j0 + (threadIdx.x & 63);
+#pragma unroll
+        for (int r = 0; r < RANK_EACH; r++) count[r] += __popcll(__ballot(other < w[r] + (j < i0 + r ? 1u : 0u)));
+      }
     }
   }
   if ((threadIdx.x & 63) == 0) {
@@ -128,7 +126,6 @@ __device__ inline uint32_t sort_key(const EmbedArgs& a, int64_t i) {
   return w == NO_WORD ? (uint32_t)a.vocabulary : w;
 }
 __global__ void __launch_bounds__(512) embedding_count_kernel(EmbedArgs a) {
-  if ((int)blockIdx.x >= a.chunks) return zero_table(a, a.chunks);
   __shared__ int count[1 << DIGIT_BITS];
   for (int d = threadIdx.x; d < a.digits; d += 512) count[d] = 0;
   __syncthreads();
@@ -147,12 +144,14 @@ __global__ void __launch_bounds__(512) embedding_scatter_kernel(EmbedArgs a) {
 #pragma unroll
   for (int k = 0; k < 2; k++) {
     const int d = 2 * threadIdx.x + k;
-    if (d < a.digits)
-      for (int c = 0; c < a.chunks; c++) {
-        const int n = a.counts[d * a.chunks + c];
-        before[k] += c < me ? n : 0;
-        all[k] += n;
+    if (d < a.digits) {
+#pragma unroll 8
+      for (int c = 0; c < a.chunks; c += 4) {   // (rows of whole vectors: what lies behind the chunks is zero)
+        const int4 n = *reinterpret_cast<const int4*>(a.counts + d * a.chunks + c);
+        before[k] += (c < me ? n.x : 0) + (c + 1 < me ? n.y : 0) + (c + 2 < me ? n.z : 0) + (c + 3 < me ? n.w : 0);
+        all[k] += (n.x + n.y) + (n.z + n.w);
       }
+    }
   }
   // exclusive sum of `all` over the digits
   int sum = all[0] + all[1];
@@ -223,10 +222,54 @@ template <int V> __device__ inline void add_row(float* to, const float (&sum)[V]
   }
 }
 
+// The first place in from .. to - 1 of the sorted words that is not below w (or `to`): a wave looks at 64 places at a time.
+__device__ inline int64_t lower_bound(const int32_t* words, uint32_t w, int64_t from, int64_t to) {
+  const int lane = threadIdx.x & 63;
+  while (from < to) {
+    const int64_t step = (to - from + 63) / 64, at = from + lane * step;
+    const uint64_t below = __ballot(at < to && (uint32_t)words[at] < w);
+    const int n = __popcll(below);   // places 0 .. n - 1 are below
+    if (n == 0) return from;
+    const int64_t next = from + (n - 1) * step + 1;
+    to = min(to, from + n * step);
+    from = next;
+  }
+  return from;
+}
+// Zeros in the rows of words that do not occur: a workgroup takes 512 words at a time.
+__device__ inline void zero_absent(const EmbedArgs& a, int me, int all) {
+  __shared__ uint8_t there[64 * SUM_WAVES];
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const bool vector = a.width % 4 == 0 && (reinterpret_cast<uintptr_t>(a.dtable) & 15) == 0;
+  for (int64_t w0 = (int64_t)me * 64 * SUM_WAVES; w0 < a.vocabulary; w0 += (int64_t)all * 64 * SUM_WAVES) {
+    const int64_t first = lower_bound(a.words, (uint32_t)w0, 0, a.rows), last = lower_bound(a.words, (uint32_t)w0 + 64 * SUM_WAVES, first, a.rows);
+    const uint32_t mine = (uint32_t)w0 + threadIdx.x;
+    int64_t from = first, to = last;
+    while (from < to) {
+      const int64_t middle = (from + to) / 2;
+      if ((uint32_t)a.words[middle] < mine) from = middle + 1; else to = middle;
+    }
+    __syncthreads();
+    there[threadIdx.x] = from < last && (uint32_t)a.words[from] == mine;
+    __syncthreads();
+    const int n = (int)min((int64_t)64 * SUM_WAVES, a.vocabulary - w0);
+    for (int i = wave; i < n; i += SUM_WAVES) {
+      if (there[i]) continue;
+      float* const row = a.dtable + (w0 + i) * a.width;
+      if (vector) {
+        for (int64_t col = 4 * lane; col < a.width; col += 256) *reinterpret_cast<uint4*>(row + col) = make_uint4(0, 0, 0, 0);
+      } else {
+        for (int64_t col = lane; col < a.width; col += 64) row[col] = 0.f;
+      }
+    }
+  }
+}
+
 // A block of SUM_WAVES * each rows in sorted order, 64 V columns.  A wave adds up `each` of them, writes the words that are its alone and leaves its first and
 // its last word's sum in LDS; the waves' ends are then put together, column by column, in their order.
 template <typename T, int V>
 __global__ void __launch_bounds__(64 * SUM_WAVES) embedding_sum_kernel(EmbedArgs a) {
+  if ((int64_t)blockIdx.x >= a.sums) return zero_absent(a, (int)(blockIdx.x - a.sums), (int)(gridDim.x - a.sums));
   __shared__ float ends[2][SUM_WAVES][64 * V];
   __shared__ uint32_t word[2][SUM_WAVES];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, block = blockIdx.x / a.slabs, slab = blockIdx.x % a.slabs;
@@ -323,34 +366,43 @@ __global__ void __launch_bounds__(64 * SUM_WAVES) embedding_sum_kernel(EmbedArgs
   }
 }
 
-// A word that goes on behind the block where it begins: its parts, first to last.  One workgroup for every block and 64 columns; most have nothing to do.
+// A word that goes on behind the block where it begins: its parts, first to last.  One workgroup for every block and 64 V columns, a quarter of the parts a wave; most have
+// nothing to do.
+template <int V>
 __global__ void __launch_bounds__(256) embedding_join_kernel(EmbedArgs a) {
-  __shared__ float red[4][64];
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, per = (int)((a.width + 63) / 64), block = blockIdx.x / per;
+  __shared__ float red[4][64 * V];
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, per = (int)((a.width + 64 * V - 1) / (64 * V)), block = blockIdx.x / per;
   const int64_t size = (int64_t)SUM_WAVES * a.each, begin = block * size, end = begin + size;
   if (end >= a.rows) return;
-  const uint32_t w = (uint32_t)a.words[end - 1];
-  if (w == NO_WORD || (uint32_t)a.words[end] != w || ((uint32_t)a.words[begin] == w && begin > 0 && (uint32_t)a.words[begin - 1] == w)) return;
+  const uint32_t w = (uint32_t)a.words[end - 1], next = (uint32_t)a.words[end], first = (uint32_t)a.words[begin], in_front = begin > 0 ? (uint32_t)a.words[begin - 1] : NO_WORD;
+  if (w == NO_WORD || next != w || (first == w && in_front == w)) return;
   // the last block that begins with it: the words are sorted
   int last = block + 1, beyond = a.blocks;
   while (beyond - last > 1) {
     const int middle = (last + beyond) / 2;
     if ((uint32_t)a.words[middle * size] == w) last = middle; else beyond = middle;
   }
-  const int64_t col = (int64_t)(blockIdx.x % per) * 64 + lane;
-  float s = 0.f;
+  const int64_t col = (int64_t)(blockIdx.x % per) * 64 * V + lane * V;
+  float s[V];
+#pragma unroll
+  for (int e = 0; e < V; e++) s[e] = 0.f;
   if (col < a.width) {
-    // parts block .. last, a run of them for each wave
     const int n = last - block + 1, run = (n + 3) / 4, lo = min(wave * run, n), hi = min(lo + run, n);
 #pragma unroll 8
-    for (int i = lo; i < hi; i++) s += a.partial[((int64_t)(block + i) * 2 + (i ? 0 : 1)) * a.width + col];
+    for (int i = lo; i < hi; i++) {
+      float x[V];
+      load_run<float, V>(a.partial + ((int64_t)(block + i) * 2 + (i ? 0 : 1)) * a.width + col, x);
+#pragma unroll
+      for (int e = 0; e < V; e++) s[e] += x[e];
+    }
   }
-  red[wave][lane] = s;
+#pragma unroll
+  for (int e = 0; e < V; e++) red[wave][lane * V + e] = s[e];
   __syncthreads();
   if (wave == 0 && col < a.width) {
-    s = ((red[0][lane] + red[1][lane]) + red[2][lane]) + red[3][lane];
-    float* const p = a.dtable + (int64_t)w * a.width + col;
-    *p = a.accumulate ? *p + a.scale * s : a.scale * s;
+#pragma unroll
+    for (int e = 0; e < V; e++) s[e] = ((red[0][lane * V + e] + red[1][lane * V + e]) + red[2][lane * V + e]) + red[3][lane * V + e];
+    add_row<V>(a.dtable + (int64_t)w * a.width + col, s, a.scale, a.accumulate, V >= 4);
   }
 }
 
@@ -376,7 +428,7 @@ static EmbedLayout layout_of(int dtype, int64_t rows, int64_t vocabulary, int64_
   l.blocks = (int32_t)cdiv(rows, (int64_t)SUM_WAVES * l.each);
   const int64_t chunk = cdiv(rows, SORT_CHUNKS);
   l.chunk = (int32_t)(cdiv(chunk > SORT_LEAST ? chunk : SORT_LEAST, 64 * SORT_WAVES) * 64 * SORT_WAVES);
-  l.chunks = (int32_t)cdiv(rows, l.chunk);
+  l.chunks = (int32_t)(cdiv(cdiv(rows, l.chunk), 4) * 4);   // (the last ones may be empty)
   const int bits = bits_of(vocabulary);
   l.passes = (int32_t)cdiv(bits, DIGIT_BITS);
   l.digit_bits = (int32_t)cdiv(bits, l.passes);
@@ -476,13 +528,11 @@ extern "C" int codistill_embedding_backward(const cd_embedding* desc, const void
   a.token_bytes = desc->token_bytes; a.scale = desc->scale; a.accumulate = accumulate != 0;
   a.order = reinterpret_cast<int32_t*>(ws + l.order); a.words = reinterpret_cast<int32_t*>(ws + l.words); a.partial = reinterpret_cast<float*>(ws + l.partial);
   a.each = l.each; a.blocks = l.blocks; a.slabs = l.slabs;
-  const int64_t zeros = accumulate ? 0 : cdiv(desc->vocabulary * desc->width, 4096);
-  const unsigned fill = (unsigned)(zeros < FILL_BLOCKS ? zeros : FILL_BLOCKS);
+  const int64_t zeros = accumulate ? 0 : cdiv(desc->vocabulary, 64 * SUM_WAVES), fill = zeros < FILL_BLOCKS ? zeros : FILL_BLOCKS;
   hipStream_t s = static_cast<hipStream_t>(stream);
   ProfScope prof(CD_K_GLUE, s, (double)a.rows * a.width, (double)a.rows * a.width * re + 4.0 * a.vocabulary * a.width);
   if (desc->rows <= RANK_ROWS) {
-    a.sort_blocks = (int32_t)cdiv(desc->rows, RANK_EACH);
-    hipLaunchKernelGGL(embedding_rank_kernel, dim3(a.sort_blocks + fill), dim3(256), 0, s, a);
+    if (desc->rows) hipLaunchKernelGGL(embedding_rank_kernel, dim3((unsigned)cdiv(desc->rows, RANK_EACH)), dim3(256), 0, s, a);
   } else {
     int32_t *order = a.order, *words = a.words, *order2 = reinterpret_cast<int32_t*>(ws + l.order2), *words2 = reinterpret_cast<int32_t*>(ws + l.words2);
     a.counts = reinterpret_cast<int32_t*>(ws + l.counts);
@@ -492,15 +542,19 @@ extern "C" int codistill_embedding_backward(const cd_embedding* desc, const void
       a.order = here ? order : order2; a.words = here ? words : words2;
       a.order2 = here ? order2 : order; a.words2 = here ? words2 : words;
       a.from_tokens = pass == 0; a.shift = pass * l.digit_bits;
-      hipLaunchKernelGGL(embedding_count_kernel, dim3(a.chunks + (pass == 0 ? fill : 0)), dim3(512), 0, s, a);
+      hipLaunchKernelGGL(embedding_count_kernel, dim3(a.chunks), dim3(512), 0, s, a);
       hipLaunchKernelGGL(embedding_scatter_kernel, dim3(a.chunks), dim3(512), 0, s, a);
     }
   }
-  if (desc->rows == 0) return check_launch("embedding_backward");
-  const dim3 blocks((unsigned)(l.blocks * l.slabs));
+  a.sums = (int64_t)l.blocks * l.slabs;
+  const dim3 blocks((unsigned)(a.sums + fill));
   auto sum = [&](auto kernel) { hipLaunchKernelGGL(kernel, blocks, dim3(64 * SUM_WAVES), 0, s, a); };
   if (re == 2) { if (run == 8) sum(embedding_sum_kernel<bf16_t, 8>); else if (run == 4) sum(embedding_sum_kernel<bf16_t, 4>); else sum(embedding_sum_kernel<bf16_t, 1>); }
   else { if (run == 4) sum(embedding_sum_kernel<float, 4>); else sum(embedding_sum_kernel<float, 1>); }
-  if (l.blocks > 1) hipLaunchKernelGGL(embedding_join_kernel, dim3((unsigned)((l.blocks - 1) * cdiv(desc->width, 64))), dim3(256), 0, s, a);
+  if (l.blocks > 1) {
+    const int64_t joins = l.blocks - 1;
+    if (run > 1) hipLaunchKernelGGL((embedding_join_kernel<4>), dim3((unsigned)(joins * cdiv(desc->width, 256))), dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((embedding_join_kernel<1>), dim3((unsigned)(joins * cdiv(desc->width, 64))), dim3(256), 0, s, a);
+  }
   return check_launch("embedding_backward");
 }

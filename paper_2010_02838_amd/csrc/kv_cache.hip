@@ -18,7 +18,8 @@ namespace {
 constexpr int KV_TILE = 64;           // tokens that are worked on together: pages are whole tiles
 constexpr float KV_LEAST = 0x1p-100f;
 constexpr int KV_WAVES = 4;           // waves of a workgroup of the attention
-constexpr int KV_TARGET = 1024;       // workgroups that fill the chip
+constexpr int KV_TARGET = 512;        // workgroups that fill the chip
+constexpr int KV_MOST_PARTS = 512;
 constexpr float LOG2E = 1.4426950408889634f;
 
 typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
@@ -62,14 +63,39 @@ __device__ inline uint16_t scale_of(uint32_t top) {
   while (127.f * bf16_to_f32((bf16_t)s) < t) s++;
   return (uint16_t)s;
 }
-// rint(x / s), exactly: a first guess and what is left of it, which fp32 holds without rounding
-__device__ inline int code_of(float x, float s, float inverse) {
-  float k = rintf(x * inverse);
-  const float rest = fmaf(-k, s, x), half = 0.5f * s;
-  const bool odd = (int)k & 1;
-  if (rest > half || (rest == half && odd)) k += 1.f;
-  if (rest < -half || (rest == -half && odd)) k -= 1.f;
-  return (int)fminf(fmaxf(k, -127.f), 127.f);
+// rint(x / s) in the lowest byte, exactly.  t is the quotient rounded once (a product and a correction by what it leaves, which fp32 holds exactly), and a quotient that
+// is not halfway between two codes does not round to there: s has 8 bits, so it lies at least half a step of fp32 and 2^-32 of itself away.  Adding 1.5 2^23 rounds
+// to nearest even.
+__device__ inline uint32_t code_of(float x, float s, float inverse) {
+  float t = x * inverse;
+  t = fmaf(fmaf(-t, s, x), inverse, t);
+  return __builtin_bit_cast(uint32_t, t + 0x1.8p23f);
+}
+__device__ inline uint32_t bytes_of(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {   // the lowest bytes of four
+  return __builtin_amdgcn_perm(__builtin_amdgcn_perm(d, c, 0x0c0c0400u), __builtin_amdgcn_perm(b, a, 0x0c0c0400u), 0x05040100u);
+}
+// eight codes and their scale: `lanes` neighbours share it
+__device__ inline uint2 quantise(const float (&x)[8], int lanes, uint16_t* scale) {
+  uint32_t top = 0;
+#pragma unroll
+  for (int e = 0; e < 8; e++) top = max(top, magnitude(x[e]));
+  top = lanes_max(top, lanes);
+  *scale = scale_of(top);
+  if (top >= 0x7f800000u) return make_uint2(0, 0);
+  const float s = bf16_to_f32(*scale), inverse = 1.f / s;
+  uint32_t w[8];
+#pragma unroll
+  for (int e = 0; e < 8; e++) w[e] = code_of(x[e], s, inverse);
+  return make_uint2(bytes_of(w[0], w[1], w[2], w[3]), bytes_of(w[4], w[5], w[6], w[7]));
+}
+// four words of four bytes, rows for columns
+__device__ inline void transpose4(uint32_t (&w)[4]) {
+  const uint32_t lo01 = __builtin_amdgcn_perm(w[1], w[0], 0x05010400u), hi01 = __builtin_amdgcn_perm(w[1], w[0], 0x07030602u);
+  const uint32_t lo23 = __builtin_amdgcn_perm(w[3], w[2], 0x05010400u), hi23 = __builtin_amdgcn_perm(w[3], w[2], 0x07030602u);
+  w[0] = __builtin_amdgcn_perm(lo23, lo01, 0x05040100u);
+  w[1] = __builtin_amdgcn_perm(lo23, lo01, 0x07060302u);
+  w[2] = __builtin_amdgcn_perm(hi23, hi01, 0x05040100u);
+  w[3] = __builtin_amdgcn_perm(hi23, hi01, 0x07060302u);
 }
 template <typename T> __device__ inline void load8(const T* p, float (&x)[8]) {
   if constexpr (sizeof(T) == 2) {
@@ -137,114 +163,123 @@ __device__ inline KvTile tile_of(const KvRowArgs& a) {
   return t;
 }
 
-constexpr int V_ROW = KV_TILE + 4;   // bytes of a channel's row in LDS
+// Two waves of a workgroup take the keys, two the values (as much work), 8 channels a lane.  Values go through LDS as they are quantised, token by token, and
+// leave it channel by channel, 8 tokens of 4 channels a thread; rows of 4 bytes more than the channels keep both sides off each other's banks.
+constexpr int V_PAD = 4, V_WORDS = (256 + V_PAD) / 4;   // words of a token's row, widest heads
 
 template <typename T>
 __global__ void __launch_bounds__(256) kv_write_kernel(KvRowArgs a) {
-  __shared__ __align__(16) int8_t tile[256 * V_ROW];
+  __shared__ uint32_t tile[KV_TILE * V_WORDS];
   const KvTile t = tile_of(a);
   if (t.lo >= t.hi || t.page < 0) return;
   const KvArgs& c = a.c;
   const int64_t head = t.page * c.kv_heads + t.h;
   uint16_t* const scales = c.scales + head * 3 * c.page_tokens + t.slot0;
-  // keys: a lane takes 8 channels
-  {
-    const int sub = threadIdx.x % a.k_lanes, per_wg = 256 / a.k_lanes, ch = sub * 8;
-    for (int g = threadIdx.x / a.k_lanes; g < 2 * (t.hi - t.lo); g += per_wg) {
+  const int lane = threadIdx.x & 127, words = (2 * c.dim + V_PAD) / 4;
+  if (threadIdx.x < 128) {
+    const int sub = lane % a.k_lanes, per_wg = 128 / a.k_lanes, ch = sub * 8;
+    for (int g = lane / a.k_lanes; g < 2 * (t.hi - t.lo); g += per_wg) {
       const int slot = t.lo + (g >> 1), m = g & 1;
       const int64_t from = a.starts ? (t.row0 + slot) * a.k_token : t.b * a.k_batch + (t.i0 + slot) * a.k_token;
       float x[8];
 #pragma unroll
       for (int e = 0; e < 8; e++) x[e] = 0.f;
       if (ch < c.dim) load8<T>(static_cast<const T*>(a.k_in) + from + (int64_t)(2 * t.h + m) * c.dim + ch, x);
-      uint32_t top = 0;
-#pragma unroll
-      for (int e = 0; e < 8; e++) top = max(top, magnitude(x[e]));
-      top = lanes_max(top, a.k_lanes);
-      const uint16_t sb = scale_of(top);
-      const float s = bf16_to_f32(sb), inverse = 1.f / s;
-      if (sub == 0) scales[(int64_t)m * c.page_tokens + slot] = sb;
-      if (ch < c.dim) {
-        uint32_t w[2] = {0, 0};
-        if (top < 0x7f800000u) {
-#pragma unroll
-          for (int e = 0; e < 8; e++) w[e >> 2] |= (uint32_t)(uint8_t)code_of(x[e], s, inverse) << 8 * (e & 3);
-        }
-        *reinterpret_cast<uint2*>(c.k + ((head * c.page_tokens + t.slot0 + slot) * 2 + m) * c.padded + ch) = make_uint2(w[0], w[1]);
-      }
+      uint16_t s;
+      const uint2 w = quantise(x, a.k_lanes, &s);
+      if (sub == 0) scales[(int64_t)m * c.page_tokens + slot] = s;
+      if (ch < c.dim) *reinterpret_cast<uint2*>(c.k + ((head * c.page_tokens + t.slot0 + slot) * 2 + m) * c.padded + ch) = w;
     }
-  }
-  // values: the same, and through LDS, so that the tokens of a channel are written side by side
-  {
-    const int sub = threadIdx.x % a.v_lanes, per_wg = 256 / a.v_lanes, ch = sub * 8;
-    for (int g = threadIdx.x / a.v_lanes; g < t.hi - t.lo; g += per_wg) {
+  } else {
+    const int sub = lane % a.v_lanes, per_wg = 128 / a.v_lanes, ch = sub * 8;
+    for (int g = lane / a.v_lanes; g < t.hi - t.lo; g += per_wg) {
       const int slot = t.lo + g;
       const int64_t from = a.starts ? (t.row0 + slot) * a.v_token : t.b * a.v_batch + (t.i0 + slot) * a.v_token;
       float x[8];
 #pragma unroll
       for (int e = 0; e < 8; e++) x[e] = 0.f;
       if (ch < 2 * c.dim) load8<T>(static_cast<const T*>(a.v_in) + from + (int64_t)t.h * 2 * c.dim + ch, x);
-      uint32_t top = 0;
-#pragma unroll
-      for (int e = 0; e < 8; e++) top = max(top, magnitude(x[e]));
-      top = lanes_max(top, a.v_lanes);
-      const uint16_t sb = scale_of(top);
-      const float s = bf16_to_f32(sb), inverse = 1.f / s;
-      if (sub == 0) scales[(int64_t)2 * c.page_tokens + slot] = sb;
+      uint16_t s;
+      const uint2 w = quantise(x, a.v_lanes, &s);
+      if (sub == 0) scales[(int64_t)2 * c.page_tokens + slot] = s;
       if (ch < 2 * c.dim) {
-#pragma unroll
-        for (int e = 0; e < 8; e++) tile[(ch + e) * V_ROW + slot] = top < 0x7f800000u ? (int8_t)code_of(x[e], s, inverse) : (int8_t)0;
+        tile[slot * words + ch / 4] = w.x;
+        tile[slot * words + ch / 4 + 1] = w.y;
       }
     }
   }
   __syncthreads();
   int8_t* const v = c.v + head * 2 * c.dim * c.page_tokens + t.slot0;
-  const int q0 = t.lo >> 2, quads = ((t.hi + 3) >> 2) - q0;
-  for (int i = threadIdx.x; i < 2 * c.dim * quads; i += 256) {
-    const int ch = i / quads, s0 = 4 * (q0 + i % quads);
-    int8_t* const to = v + (int64_t)ch * c.page_tokens + s0;
-    const int8_t* const from = tile + ch * V_ROW + s0;
-    if (s0 >= t.lo && s0 + 4 <= t.hi) {
-      *reinterpret_cast<uint32_t*>(to) = *reinterpret_cast<const uint32_t*>(from);
-    } else {
-      for (int e = 0; e < 4; e++)
-        if (s0 + e >= t.lo && s0 + e < t.hi) to[e] = from[e];
+  const int o0 = t.lo >> 3, octets = ((t.hi + 7) >> 3) - o0;   // (rows in front of and behind the tokens hold anything: they are not written)
+  for (int i = threadIdx.x; i < c.dim / 2 * octets; i += 256) {
+    const int q = i / octets, s0 = 8 * (o0 + i - q * octets);
+    uint32_t lo[4], hi[4];
+#pragma unroll
+    for (int e = 0; e < 4; e++) {
+      lo[e] = tile[(s0 + e) * words + q];
+      hi[e] = tile[(s0 + 4 + e) * words + q];
+    }
+    transpose4(lo);
+    transpose4(hi);
+#pragma unroll
+    for (int e = 0; e < 4; e++) {
+      int8_t* const to = v + (int64_t)(4 * q + e) * c.page_tokens + s0;
+      if (s0 >= t.lo && s0 + 8 <= t.hi) {
+        *reinterpret_cast<uint2*>(to) = make_uint2(lo[e], hi[e]);
+      } else {
+        for (int j = 0; j < 8; j++)
+          if (s0 + j >= t.lo && s0 + j < t.hi) to[j] = (int8_t)((j < 4 ? lo[e] : hi[e]) >> 8 * (j & 3));
+      }
     }
   }
 }
 
+template <typename T> __device__ inline void store_values(T* to, uint2 w, float s) {
+  float x[8];
+#pragma unroll
+  for (int e = 0; e < 8; e++) x[e] = (float)(int8_t)((e < 4 ? w.x : w.y) >> 8 * (e & 3)) * s;
+  store8<T>(to, x);
+}
 template <typename T>
 __global__ void __launch_bounds__(256) kv_read_kernel(KvRowArgs a) {
-  __shared__ __align__(16) int8_t tile[256 * V_ROW];
+  __shared__ uint32_t tile[KV_TILE * V_WORDS];
   const KvTile t = tile_of(a);
   if (t.lo >= t.hi) return;
   const KvArgs& c = a.c;
   const bool there = t.page >= 0;
   const int64_t head = there ? t.page * c.kv_heads + t.h : 0;
   const uint16_t* const scales = c.scales + head * 3 * c.page_tokens + t.slot0;
+  const int words = (2 * c.dim + V_PAD) / 4;
+  if (there) {
+    const int8_t* const v = c.v + head * 2 * c.dim * c.page_tokens + t.slot0;
+    const int o0 = t.lo >> 3, octets = ((t.hi + 7) >> 3) - o0;
+    for (int i = threadIdx.x; i < c.dim / 2 * octets; i += 256) {
+      const int q = i / octets, s0 = 8 * (o0 + i - q * octets);
+      uint32_t lo[4], hi[4];
+#pragma unroll
+      for (int e = 0; e < 4; e++) {
+        const uint2 w = *reinterpret_cast<const uint2*>(v + (int64_t)(4 * q + e) * c.page_tokens + s0);
+        lo[e] = w.x;
+        hi[e] = w.y;
+      }
+      transpose4(lo);
+      transpose4(hi);
+#pragma unroll
+      for (int e = 0; e < 4; e++) {
+        tile[(s0 + e) * words + q] = lo[e];
+        tile[(s0 + 4 + e) * words + q] = hi[e];
+      }
+    }
+  }
   {
     const int sub = threadIdx.x % a.k_lanes, per_wg = 256 / a.k_lanes, ch = sub * 8;
     for (int g = threadIdx.x / a.k_lanes; g < 2 * (t.hi - t.lo); g += per_wg) {
       const int slot = t.lo + (g >> 1), m = g & 1;
       if (ch >= c.dim) continue;
       const int64_t to = a.starts ? (t.row0 + slot) * a.k_token : t.b * a.k_batch + (t.i0 + slot) * a.k_token;
-      float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-      if (there) {
-        const float s = bf16_to_f32(scales[(int64_t)m * c.page_tokens + slot]);
-        int8_t w[8];
-        load_run<int8_t, 8>(c.k + ((head * c.page_tokens + t.slot0 + slot) * 2 + m) * c.padded + ch, w);
-#pragma unroll
-        for (int e = 0; e < 8; e++) x[e] = (float)w[e] * s;
-      }
-      store8<T>(static_cast<T*>(a.k_out) + to + (int64_t)(2 * t.h + m) * c.dim + ch, x);
-    }
-  }
-  if (there) {
-    const int8_t* const v = c.v + head * 2 * c.dim * c.page_tokens + t.slot0;
-    const int q0 = t.lo >> 2, quads = ((t.hi + 3) >> 2) - q0;
-    for (int i = threadIdx.x; i < 2 * c.dim * quads; i += 256) {
-      const int ch = i / quads, s0 = 4 * (q0 + i % quads);
-      *reinterpret_cast<uint32_t*>(tile + ch * V_ROW + s0) = *reinterpret_cast<const uint32_t*>(v + (int64_t)ch * c.page_tokens + s0);
+      uint2 w = make_uint2(0, 0);
+      if (there) w = *reinterpret_cast<const uint2*>(c.k + ((head * c.page_tokens + t.slot0 + slot) * 2 + m) * c.padded + ch);
+      store_values<T>(static_cast<T*>(a.k_out) + to + (int64_t)(2 * t.h + m) * c.dim + ch, w, there ? bf16_to_f32(scales[(int64_t)m * c.page_tokens + slot]) : 0.f);
     }
   }
   __syncthreads();
@@ -254,13 +289,8 @@ __global__ void __launch_bounds__(256) kv_read_kernel(KvRowArgs a) {
       const int slot = t.lo + g;
       if (ch >= 2 * c.dim) continue;
       const int64_t to = a.starts ? (t.row0 + slot) * a.v_token : t.b * a.v_batch + (t.i0 + slot) * a.v_token;
-      float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-      if (there) {
-        const float s = bf16_to_f32(scales[(int64_t)2 * c.page_tokens + slot]);
-#pragma unroll
-        for (int e = 0; e < 8; e++) x[e] = (float)tile[(ch + e) * V_ROW + slot] * s;
-      }
-      store8<T>(static_cast<T*>(a.v_out) + to + (int64_t)t.h * 2 * c.dim + ch, x);
+      const uint2 w = there ? make_uint2(tile[slot * words + ch / 4], tile[slot * words + ch / 4 + 1]) : make_uint2(0, 0);
+      store_values<T>(static_cast<T*>(a.v_out) + to + (int64_t)t.h * 2 * c.dim + ch, w, there ? bf16_to_f32(scales[(int64_t)2 * c.page_tokens + slot]) : 0.f);
     }
   }
 }
@@ -328,13 +358,13 @@ template <int N> __device__ inline void split8(const float (&x)[8], v8bf (&out)[
     }
 }
 
-struct KvRow { int query, head; int64_t sees; bool real; };   // sees: keys in front of and at the last visible one
+struct KvRow { int query, head, sees; bool real; };   // sees: keys in front of and at the last visible one
 
 // NK: 32-channel steps of a map's key; RT: tiles of 8 rows
 template <typename T, int NK, int RT>
-__global__ void __launch_bounds__(64 * KV_WAVES) kv_attention_kernel(KvAttnArgs a) {
+__global__ void __launch_bounds__(64 * KV_WAVES, NK <= 2 && RT == 1 ? 2 : 1) kv_attention_kernel(KvAttnArgs a) {
   constexpr int NC = 4 * NK, TQ = Terms<T>::Q, TP = Terms<T>::P, COLS = 16 * RT;
-  __shared__ float sums[COLS][64 * NK + 1];
+  __shared__ float sums[KV_WAVES][COLS][64 * NK + 4];
   __shared__ float tops[KV_WAVES][COLS], totals[KV_WAVES][COLS];
   const KvArgs& c = a.c;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, col = lane & 15, grp = lane >> 4, map = col >> 3;
@@ -342,25 +372,25 @@ __global__ void __launch_bounds__(64 * KV_WAVES) kv_attention_kernel(KvAttnArgs 
   const int tile = id % a.tiles; id /= a.tiles;
   const int part = id % a.parts; id /= a.parts;
   const int h = id % c.kv_heads, b = id / c.kv_heads;
-  const int64_t room = (int64_t)c.seq_pages * c.page_tokens;
-  const int64_t nk = min(max((int64_t)a.k_lens[b], (int64_t)0), room), nq = a.q_lens ? min(max(a.q_lens[b], 0), a.tq) : a.tq;
+  const int nk = min(max(a.k_lens[b], 0), c.seq_pages * c.page_tokens), nq = a.q_lens ? min(max(a.q_lens[b], 0), a.tq) : a.tq;
   auto row_of = [&](int r) {
     KvRow w;
     w.query = r / a.group;
-    w.head = h * a.group + r % a.group;
+    w.head = h * a.group + r - w.query * a.group;
     w.real = r < a.rows && w.query < nq;
-    w.sees = !w.real ? 0 : a.causal ? max((int64_t)0, min(nk, w.query + nk - nq + 1)) : nk;
+    w.sees = !w.real ? 0 : a.causal ? max(0, min(nk, w.query - nq + nk + 1)) : nk;
     return w;
   };
   const int row0 = tile * 8 * RT;
   // all rows of the tile see at least `least` keys, none more than `most`
-  int64_t least = nk, most = 0;
-  int64_t sees[RT];
+  int least = nk, most = 0, sees[RT];
   v8bf q[RT][2][NK][TQ];
 #pragma unroll
   for (int rt = 0; rt < RT; rt++) {
     const KvRow w = row_of(row0 + 8 * rt + (col & 7));
     sees[rt] = w.sees;
+    least = min(least, w.sees);
+    most = max(most, w.sees);
     const T* from = static_cast<const T*>(a.q) + b * a.q_batch + w.query * a.q_token + (int64_t)(2 * w.head + map) * c.dim;
 #pragma unroll
     for (int s = 0; s < NK; s++) {
@@ -369,29 +399,23 @@ __global__ void __launch_bounds__(64 * KV_WAVES) kv_attention_kernel(KvAttnArgs 
 #pragma unroll
       for (int e = 0; e < 8; e++) x[e] = 0.f;
       if (w.real && ch < c.dim) load8<T>(from + ch, x);
-      v8bf mine[TQ], none[TQ];
+      v8bf mine[TQ];
       split8<TQ>(x, mine);
-#pragma unroll
-      for (int e = 0; e < 8; e++) x[e] = 0.f;
-      split8<TQ>(x, none);
 #pragma unroll
       for (int n = 0; n < TQ; n++)
 #pragma unroll
-        for (int m = 0; m < 2; m++) q[rt][m][s][n] = map == m ? mine[n] : none[n];
+        for (int m = 0; m < 2; m++)
+#pragma unroll
+          for (int e = 0; e < 8; e++) q[rt][m][s][n][e] = map == m ? mine[n][e] : (__bf16)0.f;
     }
   }
 #pragma unroll
-  for (int rt = 0; rt < RT; rt++) {
-    least = min(least, sees[rt]);
-    most = max(most, sees[rt]);
-  }
-#pragma unroll
   for (int o = 1; o < 8; o *= 2) {
-    least = min(least, (int64_t)__shfl_xor((long long)least, o, 64));
-    most = max(most, (int64_t)__shfl_xor((long long)most, o, 64));
+    least = min(least, __shfl_xor(least, o, 64));
+    most = max(most, __shfl_xor(most, o, 64));
   }
-  const int blocks = __builtin_amdgcn_readfirstlane((int)((most + KV_TILE - 1) / KV_TILE));
-  const int whole = __builtin_amdgcn_readfirstlane((int)(least / KV_TILE));   // blocks that all rows see whole
+  const int blocks = __builtin_amdgcn_readfirstlane((most + KV_TILE - 1) / KV_TILE);
+  const int whole = __builtin_amdgcn_readfirstlane(least / KV_TILE);   // blocks that all rows see whole
   const int from = (int)((int64_t)blocks * part / a.parts), to = (int)((int64_t)blocks * (part + 1) / a.parts);
 
   v4f acc[RT][NC];
@@ -406,6 +430,7 @@ __global__ void __launch_bounds__(64 * KV_WAVES) kv_attention_kernel(KvAttnArgs 
   uint2 kc[4][2][NK];
   uint4 vc[NC];
   uint4 ks[2], vs[2];     // bf16 scales of the lane's 16 keys: its own map's, the values'
+  const int last_ch = 2 * c.dim - 16;
   auto load_keys = [&](int64_t page, int slot) {
     const int64_t head = page * c.kv_heads + h;
     const int8_t* const base = c.k + (head * c.page_tokens + slot) * 2 * c.padded;
@@ -414,7 +439,7 @@ __global__ void __launch_bounds__(64 * KV_WAVES) kv_attention_kernel(KvAttnArgs 
     for (int t = 0; t < 4; t++)
 #pragma unroll
       for (int m = 0; m < 2; m++) {
-        const int8_t* const p = base + ((16 * (col >> 2) + 4 * t + (col & 3)) * 2 + m) * c.padded + grp * 8 * NK;
+        const int8_t* const p = base + ((16 * (col >> 2) + 4 * t + (col & 3)) * 2 + m) * (32 * NK) + grp * 8 * NK;
         if constexpr (NK % 2 == 0) {
 #pragma unroll
           for (int s = 0; s < NK; s += 2) {
@@ -450,11 +475,10 @@ __global__ void __launch_bounds__(64 * KV_WAVES) kv_attention_kernel(KvAttnArgs 
   if (blk < to) load_keys(page, slot);
   while (blk < to) {
     {
-      const int64_t head = page * c.kv_heads + h;
-      const int8_t* const base = c.v + head * 2 * c.dim * c.page_tokens + slot;
+      const int8_t* const base = c.v + (page * c.kv_heads + h) * 2 * c.dim * c.page_tokens + slot;
 #pragma unroll
-      for (int n = 0; n < NC; n++)
-        if (16 * n < 2 * c.dim) vc[n] = *reinterpret_cast<const uint4*>(base + (int64_t)(16 * n + col) * c.page_tokens + 16 * grp);
+      for (int n = 0; n < NC; n++)   // (channels behind the last one: the last ones again, which nobody reads)
+        vc[n] = *reinterpret_cast<const uint4*>(base + (int64_t)(min(16 * n, last_ch) + col) * c.page_tokens + 16 * grp);
     }
     v4f sc[RT][4];
 #pragma unroll
@@ -488,8 +512,8 @@ __global__ void __launch_bounds__(64 * KV_WAVES) kv_attention_kernel(KvAttnArgs 
       float p[16], high = -INFINITY;
 #pragma unroll
       for (int i = 0; i < 16; i++) p[i] = sc[rt][i >> 2][i & 3] * kf[i];
+      const int left = sees[rt] - now * KV_TILE - 16 * grp;   // visible ones of the lane's 16 keys
       if (now >= whole) {
-        const int64_t left = sees[rt] - (int64_t)now * KV_TILE - 16 * grp;   // visible ones of the lane's 16 keys
 #pragma unroll
         for (int i = 0; i < 16; i++) p[i] = i < left ? p[i] : -INFINITY;
       }
@@ -513,144 +537,149 @@ __global__ void __launch_bounds__(64 * KV_WAVES) kv_attention_kernel(KvAttnArgs 
         sum += p[i];
       }
       total[rt] += sum;
-      // (a scale that no key of the row belongs to may be anything: it is not multiplied by a weight of zero)
+      if (now >= whole) {   // (the scale of a key that the row does not see may be anything: it is not multiplied by a weight of zero)
 #pragma unroll
-      for (int i = 0; i < 16; i++) p[i] = now >= whole && i >= sees[rt] - (int64_t)now * KV_TILE - 16 * grp ? 0.f : p[i] * vf[i];
+        for (int i = 0; i < 16; i++) p[i] = i < left ? p[i] * vf[i] : 0.f;
+      } else {
+#pragma unroll
+        for (int i = 0; i < 16; i++) p[i] *= vf[i];
+      }
       split8<TP>(*reinterpret_cast<float(*)[8]>(p), w[rt][0]);
       split8<TP>(*reinterpret_cast<float(*)[8]>(p + 8), w[rt][1]);
     }
 #pragma unroll
-    for (int n = 0; n < NC; n++)
-      if (16 * n < 2 * c.dim) {
-        const v8bf lo = codes_as_bf16(make_uint2(vc[n].x, vc[n].y)), hi = codes_as_bf16(make_uint2(vc[n].z, vc[n].w));
+    for (int n = 0; n < NC; n++) {
+      const v8bf lo = codes_as_bf16(make_uint2(vc[n].x, vc[n].y)), hi = codes_as_bf16(make_uint2(vc[n].z, vc[n].w));
 #pragma unroll
-        for (int rt = 0; rt < RT; rt++)
+      for (int rt = 0; rt < RT; rt++)
 #pragma unroll
-          for (int e = TP - 1; e >= 0; e--) {
-            acc[rt][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(lo, w[rt][0][e], acc[rt][n], 0, 0, 0);
-            acc[rt][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(hi, w[rt][1][e], acc[rt][n], 0, 0, 0);
-          }
-      }
+        for (int e = TP - 1; e >= 0; e--) {
+          acc[rt][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(lo, w[rt][0][e], acc[rt][n], 0, 0, 0);
+          acc[rt][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(hi, w[rt][1][e], acc[rt][n], 0, 0, 0);
+        }
+    }
   }
 
-  // the waves' sums, in their order
+  // the waves' sums, brought to the largest maximum
 #pragma unroll
   for (int rt = 0; rt < RT; rt++) {
     total[rt] += __shfl_xor(total[rt], 16, 64);
     total[rt] += __shfl_xor(total[rt], 32, 64);
-    if (grp == 0) {
-      tops[wave][16 * rt + col] = top[rt];
-      totals[wave][16 * rt + col] = total[rt];
-    }
+    if (grp == 0) tops[wave][16 * rt + col] = top[rt];
   }
   __syncthreads();
-  float f[RT];
 #pragma unroll
   for (int rt = 0; rt < RT; rt++) {
     float high = tops[0][16 * rt + col];
 #pragma unroll
-    for (int q = 1; q < KV_WAVES; q++) high = fmaxf(high, tops[q][16 * rt + col]);
-    f[rt] = top[rt] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(top[rt] - high);   // (a wave without keys has zeros)
+    for (int w = 1; w < KV_WAVES; w++) high = fmaxf(high, tops[w][16 * rt + col]);
+    const float f = top[rt] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(top[rt] - high);   // (a wave without keys has zeros)
+    if (grp == 0) totals[wave][16 * rt + col] = total[rt] * f;
+#pragma unroll
+    for (int n = 0; n < NC; n++)
+      *reinterpret_cast<float4*>(&sums[wave][16 * rt + col][16 * n + 4 * grp]) = make_float4(acc[rt][n][0] * f, acc[rt][n][1] * f, acc[rt][n][2] * f, acc[rt][n][3] * f);
   }
-  for (int q = 0; q < KV_WAVES; q++) {
-    if (wave == q) {
-#pragma unroll
-      for (int rt = 0; rt < RT; rt++)
-#pragma unroll
-        for (int n = 0; n < NC; n++)
-#pragma unroll
-          for (int i = 0; i < 4; i++) {
-            float* const p = &sums[16 * rt + col][16 * n + 4 * grp + i];
-            const float v = acc[rt][n][i] * f[rt];
-            *p = q ? *p + v : v;
-          }
-    }
-    __syncthreads();
-  }
-  // maxima and sums of a column
-  auto column = [&](int at, float* high, float* all) {
-    float m = tops[0][at], t = 0.f;
-#pragma unroll
-    for (int q = 1; q < KV_WAVES; q++) m = fmaxf(m, tops[q][at]);
-#pragma unroll
-    for (int q = 0; q < KV_WAVES; q++) t += totals[q][at] * (tops[q][at] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(tops[q][at] - m));
-    *high = m;
-    *all = t;
-  };
-  const int width = 2 * c.dim;
-  for (int i = threadIdx.x; i < 8 * RT * width; i += 64 * KV_WAVES) {
-    const int r = i / width, ch = i % width, at = 16 * (r >> 3) + (r & 7);
+  __syncthreads();
+  const int width = 2 * c.dim, quads = width / 4;
+  for (int i = threadIdx.x; i < 8 * RT * quads; i += 64 * KV_WAVES) {
+    const int r = i / quads, ch = 4 * (i - r * quads), at = 16 * (r >> 3) + (r & 7);
     if (row0 + r >= a.rows) break;
-    float m[2], t[2];
-    column(at, &m[0], &t[0]);
-    column(at + 8, &m[1], &t[1]);
-    const float o[2] = {sums[at][ch], sums[at + 8][ch]};
+    float o[2][4], t[2];
+#pragma unroll
+    for (int k = 0; k < 2; k++) {
+      t[k] = ((totals[0][at + 8 * k] + totals[1][at + 8 * k]) + totals[2][at + 8 * k]) + totals[3][at + 8 * k];
+#pragma unroll
+      for (int w = 0; w < KV_WAVES; w++) {
+        const float4 v = *reinterpret_cast<const float4*>(&sums[w][at + 8 * k][ch]);
+        const float x[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int e = 0; e < 4; e++) o[k][e] = w ? o[k][e] + x[e] : x[e];
+      }
+    }
     if (a.parts > 1) {
       const int64_t to_part = (((int64_t)b * c.kv_heads + h) * a.rows + row0 + r) * a.parts + part;
 #pragma unroll
       for (int k = 0; k < 2; k++) {
-        a.part[(to_part * 2 + k) * width + ch] = o[k];
+        *reinterpret_cast<float4*>(a.part + (to_part * 2 + k) * width + ch) = make_float4(o[k][0], o[k][1], o[k][2], o[k][3]);
         if (ch == 0) {
-          a.part_ml[(to_part * 2 + k) * 2] = m[k];
+          const int to = at + 8 * k;
+          a.part_ml[(to_part * 2 + k) * 2] = fmaxf(fmaxf(tops[0][to], tops[1][to]), fmaxf(tops[2][to], tops[3][to]));
           a.part_ml[(to_part * 2 + k) * 2 + 1] = t[k];
         }
       }
     } else {
       const KvRow w = row_of(row0 + r);
       const float lam = a.lam[a.lam_token ? ((int64_t)b * a.tq + w.query) * a.heads + w.head : w.head];
-      const float v = (t[0] == 0.f ? 0.f : o[0] / t[0]) - (t[1] == 0.f ? 0.f : lam * (o[1] / t[1]));
-      static_cast<T*>(a.out)[b * a.o_batch + w.query * a.o_token + (int64_t)w.head * width + ch] = Cvt<T>::st(w.real && w.sees > 0 ? v : 0.f);
+      const bool seen = w.real && w.sees > 0;
+      float v[4];
+#pragma unroll
+      for (int e = 0; e < 4; e++) v[e] = seen ? (t[0] == 0.f ? 0.f : o[0][e] / t[0]) - (t[1] == 0.f ? 0.f : lam * (o[1][e] / t[1])) : 0.f;
+      store_run<T, 4>(static_cast<T*>(a.out) + b * a.o_batch + w.query * a.o_token + (int64_t)w.head * width + ch, v);
     }
   }
 }
 
-// The parts of a row, in their order: 32 channels and 8 runs of parts a workgroup.
+// The parts of a row: a workgroup takes 32 channels, 8 of its threads every eighth part of one.
 template <typename T>
 __global__ void __launch_bounds__(256) kv_join_kernel(KvAttnArgs a) {
-  __shared__ float red[8][2][32], red_total[8][2];
+  __shared__ float factor[2][KV_MOST_PARTS], red[8][2][32], most[4][2], totals[4][2];
   const KvArgs& c = a.c;
-  const int width = 2 * c.dim, chunks = (width + 31) / 32;
+  const int width = 2 * c.dim, chunks = (width + 31) / 32, wave = threadIdx.x >> 6;
   const int64_t row = blockIdx.x / chunks;
   const int ch = (int)(blockIdx.x % chunks) * 32 + (threadIdx.x & 31), run = threadIdx.x >> 5;
   const int unit = (int)(row / a.rows), r = (int)(row % a.rows), b = unit / c.kv_heads, h = unit % c.kv_heads;
-  const float* const ml = a.part_ml + row * a.parts * 4;
-  const float* const sums = a.part + row * a.parts * 2 * width;
-  float high[2] = {-INFINITY, -INFINITY};
-  for (int p = threadIdx.x & 31; p < a.parts; p += 32) {
-    high[0] = fmaxf(high[0], ml[4 * p]);
-    high[1] = fmaxf(high[1], ml[4 * p + 2]);
+  const float* const sums = a.part + row * a.parts * 2 * width + min(ch, width - 1);
+  const float4* const ml = reinterpret_cast<const float4*>(a.part_ml) + row * a.parts;   // maximum and sum of the first map, of the second
+  constexpr int EACH = KV_MOST_PARTS / 256;
+  float4 mine[EACH];
+  float high[2] = {-INFINITY, -INFINITY}, total[2] = {0.f, 0.f};
+#pragma unroll
+  for (int e = 0; e < EACH; e++) {
+    const int p = threadIdx.x + 256 * e;
+    mine[e] = p < a.parts ? ml[p] : make_float4(-INFINITY, 0.f, -INFINITY, 0.f);
+    high[0] = fmaxf(high[0], mine[e].x);
+    high[1] = fmaxf(high[1], mine[e].z);
   }
 #pragma unroll
-  for (int o = 1; o < 32; o *= 2) {
-    high[0] = fmaxf(high[0], __shfl_xor(high[0], o, 64));
-    high[1] = fmaxf(high[1], __shfl_xor(high[1], o, 64));
+  for (int k = 0; k < 2; k++) {
+    high[k] = wave_max(high[k]);
+    if ((threadIdx.x & 63) == 0) most[wave][k] = high[k];
   }
-  const int each = (a.parts + 7) / 8, from = min(run * each, a.parts), to = min(from + each, a.parts);
-  float sum[2] = {0.f, 0.f}, total[2] = {0.f, 0.f};
-  for (int p = from; p < to; p++) {
+  __syncthreads();
 #pragma unroll
-    for (int k = 0; k < 2; k++) {
-      const float m = ml[4 * p + 2 * k], t = ml[4 * p + 2 * k + 1];
-      const float f = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - high[k]);   // (a part without keys has zeros)
-      total[k] += t * f;
-      if (ch < width) sum[k] += sums[((int64_t)p * 2 + k) * width + ch] * f;
+  for (int k = 0; k < 2; k++) high[k] = fmaxf(fmaxf(most[0][k], most[1][k]), fmaxf(most[2][k], most[3][k]));
+#pragma unroll
+  for (int e = 0; e < EACH; e++) {
+    const int p = threadIdx.x + 256 * e;
+    if (p < a.parts) {   // (a part without keys has zeros)
+      factor[0][p] = mine[e].x == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(mine[e].x - high[0]);
+      factor[1][p] = mine[e].z == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(mine[e].z - high[1]);
+      total[0] += mine[e].y * factor[0][p];
+      total[1] += mine[e].w * factor[1][p];
     }
   }
 #pragma unroll
   for (int k = 0; k < 2; k++) {
-    red[run][k][threadIdx.x & 31] = sum[k];
-    if ((threadIdx.x & 31) == 0) red_total[run][k] = total[k];
+    total[k] = wave_sum(total[k]);
+    if ((threadIdx.x & 63) == 0) totals[wave][k] = total[k];
   }
+  __syncthreads();
+  float sum[2] = {0.f, 0.f};
+#pragma unroll 8
+  for (int p = run; p < a.parts; p += 8) {
+    sum[0] += sums[(int64_t)p * 2 * width] * factor[0][p];
+    sum[1] += sums[((int64_t)p * 2 + 1) * width] * factor[1][p];
+  }
+  red[run][0][threadIdx.x & 31] = sum[0];
+  red[run][1][threadIdx.x & 31] = sum[1];
   __syncthreads();
   if (threadIdx.x >= 32 || ch >= width) return;
 #pragma unroll
   for (int k = 0; k < 2; k++) {
-    sum[k] = total[k] = 0.f;
+    total[k] = ((totals[0][k] + totals[1][k]) + totals[2][k]) + totals[3][k];
+    sum[k] = 0.f;
 #pragma unroll
-    for (int q = 0; q < 8; q++) {
-      sum[k] += red[q][k][threadIdx.x];
-      total[k] += red_total[q][k];
-    }
+    for (int q = 0; q < 8; q++) sum[k] += red[q][k][threadIdx.x];
   }
   const int query = r / a.group, head = h * a.group + r % a.group;
   const float lam = a.lam[a.lam_token ? ((int64_t)b * a.tq + query) * a.heads + head : head];
@@ -747,12 +776,12 @@ static int check_attention(const char* what, const cd_kv_cache* c, const cd_kv_a
   return CD_OK;
 }
 static int rows_of(const cd_kv_cache* c, const cd_kv_attn* d) { return d->tq * (d->heads / c->kv_heads); }
-// (fp32 queries take three times the registers)
-static int row_tiles(const cd_kv_cache* c, const cd_kv_attn* d) { return rows_of(c, d) > 8 && c->dtype == CD_BF16 ? 2 : 1; }
-// Workgroups of a sequence and key head: enough to fill the chip, each with at least two blocks for every wave.
+// Two tiles of rows share what is read, where there are registers for their sums (fp32 queries take three times a tile's registers).
+static int row_tiles(const cd_kv_cache* c, const cd_kv_attn* d) { return rows_of(c, d) > 8 && c->dtype == CD_BF16 && c->head_dim <= 64 ? 2 : 1; }
+// Workgroups of a sequence and key head: enough to fill the chip, each with at least a block for every wave.
 static int parts_of(const cd_kv_cache* c, const cd_kv_attn* d) {
   const int64_t groups = (int64_t)c->sequences * c->kv_heads * cdiv(rows_of(c, d), 8 * row_tiles(c, d));
-  const int64_t blocks = (int64_t)c->seq_pages * c->page_tokens / KV_TILE, most = blocks / (2 * KV_WAVES), want = cdiv(KV_TARGET, groups > 0 ? groups : 1);
+  const int64_t blocks = (int64_t)c->seq_pages * c->page_tokens / KV_TILE, most = blocks / KV_WAVES < KV_MOST_PARTS ? blocks / KV_WAVES : KV_MOST_PARTS, want = cdiv(KV_TARGET, groups > 0 ? groups : 1);
   const int64_t parts = want < most ? want : most;
   return parts < 1 ? 1 : (int)parts;
 }
@@ -839,13 +868,14 @@ extern "C" int codistill_kv_diff_attention(const cd_kv_cache* cache, const cd_kv
   auto with = [&](auto type) {
     typedef decltype(type) T;
     auto run = [&](auto nk) {
-      if constexpr (sizeof(T) == 2) {
+      constexpr int NK = decltype(nk)::value;
+      if constexpr (sizeof(T) == 2 && NK <= 2) {
         if (rt == 2) {
-          hipLaunchKernelGGL((kv_attention_kernel<T, decltype(nk)::value, 2>), grid, dim3(64 * KV_WAVES), 0, s, a);
+          hipLaunchKernelGGL((kv_attention_kernel<T, NK, 2>), grid, dim3(64 * KV_WAVES), 0, s, a);
           return;
         }
       }
-      hipLaunchKernelGGL((kv_attention_kernel<T, decltype(nk)::value, 1>), grid, dim3(64 * KV_WAVES), 0, s, a);
+      hipLaunchKernelGGL((kv_attention_kernel<T, NK, 1>), grid, dim3(64 * KV_WAVES), 0, s, a);
     };
     switch (a.c.padded / 32) {
       case 1: run(std::integral_constant<int, 1>()); break;
