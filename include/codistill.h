@@ -530,8 +530,8 @@ int codistill_norm_rotary_backward(const cd_rotary* rope, const int32_t* positio
  *   dtable   device fp32 [vocabulary][width], contiguous.  accumulate 0: written whole, zeros for words that do not occur; otherwise the sums are added to
  *            it, and rows of words that do not occur are not touched
  * The rows of a word are added up in fp32 in an order that depends on the tokens alone: the same inputs give the same bits.
- *   workspace  codistill_embedding_workspace_bytes (the same for every content of tokens)
- * rows == 0 is allowed (tokens, y, dy and workspace may then be NULL).
+ *   workspace  codistill_embedding_workspace_bytes (the same for every content of tokens; may be 0: then NULL is fine)
+ * rows == 0 is allowed (tokens, y and dy may then be NULL).
  * Errors (nothing launched): CD_ERR_INVALID_ARG: NULL pointers, pointers not aligned to their elements (workspace: 16 bytes), rows outside 0 .. 2^30, vocabulary
  * outside 1 .. 2^31 - 2, width outside 1 .. 65536, a row longer than its stride, a scale that is not finite, token_bytes other than 4 and 8;
  * CD_ERR_UNSUPPORTED: rows * width above 2^40; CD_ERR_WORKSPACE_TOO_SMALL.

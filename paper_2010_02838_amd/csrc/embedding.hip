@@ -18,6 +18,7 @@ namespace cd {
 namespace {
 
 constexpr uint32_t NO_WORD = 0x7fffffffu;   // sorted behind all words
+constexpr int SMALL_ROWS = 512;              // most rows that one workgroup puts in order for itself
 constexpr int RANK_ROWS = 16384;            // most rows whose places are counted
 constexpr int RANK_EACH = 16, RANK_AHEAD = 8;   // rows of a workgroup there, loads in flight
 constexpr int DIGIT_BITS = 10, SORT_CHUNKS = 256, SORT_LEAST = 1024, SORT_WAVES = 8;
@@ -33,10 +34,9 @@ struct EmbedArgs {
   float scale;
 };
 
-__device__ inline uint32_t word_of(const EmbedArgs& a, int64_t i) {
-  const int64_t w = a.token_bytes == 8 ? static_cast<const int64_t*>(a.tokens)[i] : static_cast<const int32_t*>(a.tokens)[i];
-  return w >= 0 && w < a.vocabulary ? (uint32_t)w : NO_WORD;
-}
+__device__ inline uint32_t word_from(const EmbedArgs& a, int64_t token) { return token >= 0 && token < a.vocabulary ? (uint32_t)token : NO_WORD; }
+template <typename TOK> __device__ inline uint32_t word_of(const EmbedArgs& a, int64_t i) { return word_from(a, static_cast<const TOK*>(a.tokens)[i]); }
+__device__ inline uint32_t word_of(const EmbedArgs& a, int64_t i) { return a.token_bytes == 8 ? word_of<int64_t>(a, i) : word_of<int32_t>(a, i); }
 
 // ---- lookup ---------------------------------------------------------------------------------------------------------------
 // TT: the table's type, RT: the rows'; V: elements of a run
@@ -71,13 +71,33 @@ __global__ void __launch_bounds__(256) embedding_kernel(EmbedArgs a, int lanes) 
 }
 
 // ---- the order of the rows --------------------------------------------------------------------------------------------------
-// Few rows: place of row i = rows with a smaller word + rows in front of it with the same.  A wave compares 64 rows with one of the
-// workgroup's at a time; what it counts is scalar.
+// 1 where a < b (a up to 2^31 - 1, b up to 2^31): the sign of their difference, which is faster than a comparison, whose result travels through a mask
+__device__ inline uint32_t below(uint32_t a, uint32_t b) { return (a - b) >> 31; }
+// Few rows: place of row i = rows with a smaller word + rows in front of it with the same.  A lane compares its row with each of the workgroup's; the lanes'
+// counts are added up at the end.  (Comparisons and the addition of their carries, or counts of their masks in scalar registers: 15 us for 8192 rows.)
+// the sum over a wave, in lane 63
+__device__ inline int sum_of_wave(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);   // one, two, four and eight lanes up inside rows of 16
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);   // a row's last lane to the next row
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);   // the first half's last lane to the second half
+  return x;
+}
+template <typename TOK>
 __global__ void __launch_bounds__(256) embedding_rank_kernel(EmbedArgs a) {
   __shared__ uint32_t mine[RANK_EACH];
   __shared__ int found[4][RANK_EACH];
-  const int i0 = blockIdx.x * RANK_EACH, rows = (int)a.rows, wave = threadIdx.x >> 6;
-  if (threadIdx.x < RANK_EACH) mine[threadIdx.x] = i0 + (int)threadIdx.x < rows ? word_of(a, i0 + threadIdx.x) : 0;
+  const int i0 = blockIdx.x * RANK_EACH, rows = (int)a.rows, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  if (threadIdx.x < RANK_EACH) mine[threadIdx.x] = i0 + (int)threadIdx.x < rows ? word_of<TOK>(a, i0 + threadIdx.x) : 0;
+  TOK others[RANK_AHEAD];
+  auto fetch = [&](int k0) {   // rows k0 .. + 63 and every 256 from there
+#pragma unroll
+    for (int u = 0; u < RANK_AHEAD; u++)
+      if (k0 + 256 * u < rows) others[u] = static_cast<const TOK*>(a.tokens)[min(k0 + 256 * u + lane, rows - 1)];
+  };
+  fetch(wave * 64);
   __syncthreads();
   uint32_t w[RANK_EACH];
   int count[RANK_EACH];
@@ -87,30 +107,28 @@ __global__ void __launch_bounds__(256) embedding_rank_kernel(EmbedArgs a) {
     count[r] = 0;
   }
   for (int k0 = wave * 64; k0 < rows; k0 += 256 * RANK_AHEAD) {
-    uint32_t others[RANK_AHEAD];
+    uint32_t now[RANK_AHEAD];
 #pragma unroll
-    for (int u = 0; u < RANK_AHEAD; u++) {
-      const int j = k0 + 256 * u + (threadIdx.x & 63);
-      others[u] = j < rows ? word_of(a, j) : 0xffffffffu;
-    }
+    for (int u = 0; u < RANK_AHEAD; u++) now[u] = k0 + 256 * u + lane < rows ? word_from(a, others[u]) : NO_WORD;
+    if (k0 + 256 * RANK_AHEAD < rows) fetch(k0 + 256 * RANK_AHEAD);
 #pragma unroll
     for (int u = 0; u < RANK_AHEAD; u++) {
       const int j0 = k0 + 256 * u;
-      const uint32_t other = others[u];
+      if (j0 >= rows) break;
       if (j0 + 64 <= i0 || j0 >= i0 + RANK_EACH) {   // all 64 in front of the workgroup's rows, or all behind
         const uint32_t same = j0 < i0;
 #pragma unroll
-        for (int r = 0; r < RANK_EACH; r++) count[r] += __popcll(__ballot(other < w[r] + same));
+        for (int r = 0; r < RANK_EACH; r++) count[r] += below(now[u], w[r] + same);
       } else {
-        const int j = j0 + (threadIdx.x & 63);
 #pragma unroll
-        for (int r = 0; r < RANK_EACH; r++) count[r] += __popcll(__ballot(other < w[r] + (j < i0 + r ? 1u : 0u)));
+        for (int r = 0; r < RANK_EACH; r++) count[r] += below(now[u], w[r] + below(j0 + lane, i0 + r));
       }
     }
   }
-  if ((threadIdx.x & 63) == 0) {
 #pragma unroll
-    for (int r = 0; r < RANK_EACH; r++) found[wave][r] = count[r];
+  for (int r = 0; r < RANK_EACH; r++) {
+    const int all = sum_of_wave(count[r]);
+    if (lane == 63) found[wave][r] = all;
   }
   __syncthreads();
   if (threadIdx.x < RANK_EACH && i0 + (int)threadIdx.x < rows) {
@@ -205,20 +223,27 @@ __global__ void __launch_bounds__(512) embedding_scatter_kernel(EmbedArgs a) {
 }
 
 // ---- sums -------------------------------------------------------------------------------------------------------------------
-template <int V> __device__ inline void add_row(float* to, const float (&sum)[V], float scale, bool accumulate, bool vector) {
-  if (V >= 4 && vector) {
+template <int V> __device__ inline void load_floats(const float* p, float (&x)[V]) {
+  if constexpr (V >= 4) {
 #pragma unroll
     for (int e = 0; e < V; e += 4) {
-      float4 t = make_float4(scale * sum[e], scale * sum[e + 1], scale * sum[e + 2], scale * sum[e + 3]);
-      if (accumulate) {
-        const float4 old = *reinterpret_cast<const float4*>(to + e);
-        t = make_float4(old.x + t.x, old.y + t.y, old.z + t.z, old.w + t.w);
-      }
-      *reinterpret_cast<float4*>(to + e) = t;
+      const float4 t = *reinterpret_cast<const float4*>(p + e);
+      x[e] = t.x; x[e + 1] = t.y; x[e + 2] = t.z; x[e + 3] = t.w;
     }
   } else {
 #pragma unroll
-    for (int e = 0; e < V; e++) to[e] = accumulate ? to[e] + scale * sum[e] : scale * sum[e];
+    for (int e = 0; e < V; e++) x[e] = p[e];
+  }
+}
+// to = old + scale sum, old being zero or what is there
+template <int V> __device__ inline void put_row(float* to, const float (&old)[V], const float (&sum)[V], float scale) {
+  if constexpr (V >= 4) {
+#pragma unroll
+    for (int e = 0; e < V; e += 4)
+      *reinterpret_cast<float4*>(to + e) = make_float4(old[e] + scale * sum[e], old[e + 1] + scale * sum[e + 1], old[e + 2] + scale * sum[e + 2], old[e + 3] + scale * sum[e + 3]);
+  } else {
+#pragma unroll
+    for (int e = 0; e < V; e++) to[e] = old[e] + scale * sum[e];
   }
 }
 
@@ -237,20 +262,27 @@ __device__ inline int64_t lower_bound(const int32_t* words, uint32_t w, int64_t 
   return from;
 }
 // Zeros in the rows of words that do not occur: a workgroup takes 512 words at a time.
-__device__ inline void zero_absent(const EmbedArgs& a, int me, int all) {
+template <bool SMALL> __device__ inline void zero_absent(const EmbedArgs& a, int me, int all) {
   __shared__ uint8_t there[64 * SUM_WAVES];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const bool vector = a.width % 4 == 0 && (reinterpret_cast<uintptr_t>(a.dtable) & 15) == 0;
   for (int64_t w0 = (int64_t)me * 64 * SUM_WAVES; w0 < a.vocabulary; w0 += (int64_t)all * 64 * SUM_WAVES) {
-    const int64_t first = lower_bound(a.words, (uint32_t)w0, 0, a.rows), last = lower_bound(a.words, (uint32_t)w0 + 64 * SUM_WAVES, first, a.rows);
-    const uint32_t mine = (uint32_t)w0 + threadIdx.x;
-    int64_t from = first, to = last;
-    while (from < to) {
-      const int64_t middle = (from + to) / 2;
-      if ((uint32_t)a.words[middle] < mine) from = middle + 1; else to = middle;
-    }
     __syncthreads();
-    there[threadIdx.x] = from < last && (uint32_t)a.words[from] == mine;
+    if constexpr (SMALL) {   // (the rows are not in order yet)
+      there[threadIdx.x] = 0;
+      __syncthreads();
+      const int64_t at = (int64_t)threadIdx.x < a.rows ? (int64_t)word_of(a, threadIdx.x) - w0 : -1;
+      if (at >= 0 && at < 64 * SUM_WAVES) there[at] = 1;
+    } else {
+      const int64_t first = lower_bound(a.words, (uint32_t)w0, 0, a.rows), last = lower_bound(a.words, (uint32_t)w0 + 64 * SUM_WAVES, first, a.rows);
+      const uint32_t mine = (uint32_t)w0 + threadIdx.x;
+      int64_t from = first, to = last;
+      while (from < to) {
+        const int64_t middle = (from + to) / 2;
+        if ((uint32_t)a.words[middle] < mine) from = middle + 1; else to = middle;
+      }
+      there[threadIdx.x] = from < last && (uint32_t)a.words[from] == mine;
+    }
     __syncthreads();
     const int n = (int)min((int64_t)64 * SUM_WAVES, a.vocabulary - w0);
     for (int i = wave; i < n; i += SUM_WAVES) {
@@ -267,9 +299,11 @@ __device__ inline void zero_absent(const EmbedArgs& a, int me, int all) {
 
 // A block of SUM_WAVES * each rows in sorted order, 64 V columns.  A wave adds up `each` of them, writes the words that are its alone and leaves its first and
 // its last word's sum in LDS; the waves' ends are then put together, column by column, in their order.
-template <typename T, int V>
+// SMALL: up to SMALL_ROWS rows, which are one block; every workgroup puts them in order itself, in LDS, and nothing is left to join.
+template <typename T, int V, bool SMALL>
 __global__ void __launch_bounds__(64 * SUM_WAVES) embedding_sum_kernel(EmbedArgs a) {
-  if ((int64_t)blockIdx.x >= a.sums) return zero_absent(a, (int)(blockIdx.x - a.sums), (int)(gridDim.x - a.sums));
+  static_assert(SMALL_ROWS == 64 * SUM_WAVES, "a row for each thread");
+  if ((int64_t)blockIdx.x >= a.sums) return zero_absent<SMALL>(a, (int)(blockIdx.x - a.sums), (int)(gridDim.x - a.sums));
   __shared__ float ends[2][SUM_WAVES][64 * V];
   __shared__ uint32_t word[2][SUM_WAVES];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, block = blockIdx.x / a.slabs, slab = blockIdx.x % a.slabs;
@@ -278,72 +312,108 @@ __global__ void __launch_bounds__(64 * SUM_WAVES) embedding_sum_kernel(EmbedArgs
   const int64_t from = (int64_t)block * SUM_WAVES * a.each + (int64_t)wave * a.each;
   const int n = (int)max((int64_t)0, min((int64_t)a.each, a.rows - from));
   // this wave's rows and words: one a lane
-  const int row_here = lane < n ? a.order[from + lane] : 0;
-  const uint32_t word_here = lane < n ? (uint32_t)a.words[from + lane] : NO_WORD;
+  int row_here = 0;
+  uint32_t word_here = NO_WORD;
+  if constexpr (SMALL) {
+    __shared__ __align__(16) uint32_t unsorted[SMALL_ROWS];
+    __shared__ uint32_t in_order[2][SMALL_ROWS];
+    const uint32_t me = (int64_t)threadIdx.x < a.rows ? word_of(a, threadIdx.x) : NO_WORD;
+    unsorted[threadIdx.x] = me;
+    __syncthreads();
+    // rows in front of the wave's, among them, and behind them (behind the last one: no word, which is below none)
+    int place = 0;
+    const int from_wave = 64 * wave, rows = (int)a.rows;
+    auto count = [&](int j, uint32_t limit) {
+      const uint4 other = *reinterpret_cast<const uint4*>(unsorted + j);
+      place += below(other.x, limit) + below(other.y, limit);
+      place += below(other.z, limit) + below(other.w, limit);
+    };
+#pragma unroll 4
+    for (int j = 0; j < min(from_wave, rows); j += 4) count(j, me + 1);
+#pragma unroll 4
+    for (int j = from_wave; j < min(from_wave + 64, rows); j++) place += below(unsorted[j], me + below(j, threadIdx.x));
+#pragma unroll 4
+    for (int j = from_wave + 64; j < rows; j += 4) count(j, me);
+    if ((int64_t)threadIdx.x < a.rows) {
+      in_order[0][place] = threadIdx.x;
+      in_order[1][place] = me;
+    }
+    __syncthreads();
+    if (lane < n) {
+      row_here = in_order[0][from + lane];
+      word_here = in_order[1][from + lane];
+    }
+  } else if (lane < n) {
+    row_here = a.order[from + lane];
+    word_here = (uint32_t)a.words[from + lane];
+  }
   float sum[V];
 #pragma unroll
   for (int e = 0; e < V; e++) sum[e] = 0.f;
-  uint32_t first = __builtin_amdgcn_readlane(word_here, 0), open = first;
-  bool one = true;     // no word has ended yet
-  auto close = [&]() {   // `open` has ended inside this wave's rows
-    if (one) {
-#pragma unroll
-      for (int e = 0; e < V; e++) ends[0][wave][lane * V + e] = sum[e];
-    } else if (mine) {
-      add_row<V>(a.dtable + (int64_t)open * a.width + col, sum, a.scale, a.accumulate, V >= 4);
-    }
-    one = false;
-#pragma unroll
-    for (int e = 0; e < V; e++) sum[e] = 0.f;
-  };
-  constexpr int AHEAD = 4;
+  const uint32_t first = __builtin_amdgcn_readlane(word_here, 0), final = __builtin_amdgcn_readlane(word_here, n > 0 ? n - 1 : 0);
+  constexpr int AHEAD = SMALL ? 16 : 4;
   for (int i0 = 0; i0 < n; i0 += AHEAD) {
     T t[AHEAD][V];
+    float old[AHEAD][V];
+    // rows, and what the table's gradient holds for words that end here and are this wave's alone, on their way together
 #pragma unroll
     for (int k = 0; k < AHEAD; k++) {
       const int i = i0 + k;
 #pragma unroll
-      for (int e = 0; e < V; e++) t[k][e] = T(0);
-      if (i < n && __builtin_amdgcn_readlane(word_here, i) != NO_WORD && mine)
-        load_run<T, V>(static_cast<const T*>(a.dy) + (int64_t)__builtin_amdgcn_readlane(row_here, i) * a.row_stride + col, t[k]);
+      for (int e = 0; e < V; e++) {
+        t[k][e] = T(0);
+        old[k][e] = 0.f;
+      }
+      if (i >= n || !mine) continue;
+      const uint32_t w = __builtin_amdgcn_readlane(word_here, i);
+      if (w != NO_WORD) load_run<T, V>(static_cast<const T*>(a.dy) + (int64_t)__builtin_amdgcn_readlane(row_here, i) * a.row_stride + col, t[k]);
+      if (a.accumulate && w != first && w != final && __builtin_amdgcn_readlane(word_here, i + 1) != w) load_floats<V>(a.dtable + (int64_t)w * a.width + col, old[k]);
     }
 #pragma unroll
     for (int k = 0; k < AHEAD; k++) {
       const int i = i0 + k;
       if (i >= n) break;
       const uint32_t w = __builtin_amdgcn_readlane(word_here, i);
-      if (w != open) {
-        close();
-        open = w;
-      }
 #pragma unroll
       for (int e = 0; e < V; e++) sum[e] += Cvt<T>::ld(t[k][e]);
+      if (w == final || __builtin_amdgcn_readlane(word_here, i + 1) == w) continue;
+      // the word ends, and is not the last one (i + 1 < n)
+      if (w == first) {
+#pragma unroll
+        for (int e = 0; e < V; e++) ends[0][wave][lane * V + e] = sum[e];
+      } else if (mine) {
+        put_row<V>(a.dtable + (int64_t)w * a.width + col, old[k], sum, a.scale);
+      }
+#pragma unroll
+      for (int e = 0; e < V; e++) sum[e] = 0.f;
     }
   }
 #pragma unroll
-  for (int e = 0; e < V; e++) ends[one ? 0 : 1][wave][lane * V + e] = sum[e];
+  for (int e = 0; e < V; e++) ends[first == final ? 0 : 1][wave][lane * V + e] = sum[e];
   if (lane == 0) {
     word[0][wave] = first;
-    word[1][wave] = one ? first : open;     // (the same word: one sum)
+    word[1][wave] = final;     // (the same word: one sum)
   }
-  __syncthreads();
   const int64_t begin = (int64_t)block * SUM_WAVES * a.each, end = min(begin + (int64_t)SUM_WAVES * a.each, a.rows);
   const uint32_t in_front = begin > 0 ? (uint32_t)a.words[begin - 1] : NO_WORD, behind = end < a.rows ? (uint32_t)a.words[end] : NO_WORD;
+  __syncthreads();
   for (int c = threadIdx.x; c < 64 * V; c += 64 * SUM_WAVES) {
     const int64_t to = (int64_t)slab * 64 * V + c;
     if (to >= a.width) break;
+    float old[2][SUM_WAVES];
+#pragma unroll
+    for (int q = 0; q < SUM_WAVES; q++)
+#pragma unroll
+      for (int k = 0; k < 2; k++) old[k][q] = a.accumulate && word[k][q] != NO_WORD ? a.dtable[(int64_t)word[k][q] * a.width + to] : 0.f;
     uint32_t w = word[0][0];
-    float s = ends[0][0][c];
+    float s = ends[0][0][c], was = old[0][0];
     bool started = w != in_front;     // here, not in an earlier block
     auto put = [&](bool goes_on) {
       if (w == NO_WORD) return;
-      if (started && !goes_on) {
-        float* const p = a.dtable + (int64_t)w * a.width + to;
-        *p = a.accumulate ? *p + a.scale * s : a.scale * s;
-      } else {
-        a.partial[((int64_t)block * 2 + (started ? 1 : 0)) * a.width + to] = s;
-      }
+      if (started && !goes_on) a.dtable[(int64_t)w * a.width + to] = was + a.scale * s;
+      else a.partial[((int64_t)block * 2 + (started ? 1 : 0)) * a.width + to] = s;
     };
+#pragma unroll
     for (int q = 0; q < SUM_WAVES; q++) {
       if (q > 0) {
         if (word[0][q] == w) {
@@ -352,6 +422,7 @@ __global__ void __launch_bounds__(64 * SUM_WAVES) embedding_sum_kernel(EmbedArgs
           put(false);
           w = word[0][q];
           s = ends[0][q][c];
+          was = old[0][q];
           started = true;
         }
       }
@@ -359,6 +430,7 @@ __global__ void __launch_bounds__(64 * SUM_WAVES) embedding_sum_kernel(EmbedArgs
         put(false);
         w = word[1][q];
         s = ends[1][q][c];
+        was = old[1][q];
         started = true;
       }
     }
@@ -391,7 +463,7 @@ __global__ void __launch_bounds__(256) embedding_join_kernel(EmbedArgs a) {
 #pragma unroll 8
     for (int i = lo; i < hi; i++) {
       float x[V];
-      load_run<float, V>(a.partial + ((int64_t)(block + i) * 2 + (i ? 0 : 1)) * a.width + col, x);
+      load_floats<V>(a.partial + ((int64_t)(block + i) * 2 + (i ? 0 : 1)) * a.width + col, x);
 #pragma unroll
       for (int e = 0; e < V; e++) s[e] += x[e];
     }
@@ -402,7 +474,10 @@ __global__ void __launch_bounds__(256) embedding_join_kernel(EmbedArgs a) {
   if (wave == 0 && col < a.width) {
 #pragma unroll
     for (int e = 0; e < V; e++) s[e] = ((red[0][lane * V + e] + red[1][lane * V + e]) + red[2][lane * V + e]) + red[3][lane * V + e];
-    add_row<V>(a.dtable + (int64_t)w * a.width + col, s, a.scale, a.accumulate, V >= 4);
+    float* const to = a.dtable + (int64_t)w * a.width + col;
+    float old[V] = {};
+    if (a.accumulate) load_floats<V>(to, old);
+    put_row<V>(to, old, s, a.scale);
   }
 }
 
@@ -423,6 +498,11 @@ static EmbedLayout layout_of(int dtype, int64_t rows, int64_t vocabulary, int64_
   EmbedLayout l = {};
   l.run = run;
   l.slabs = (int32_t)cdiv(width, 64 * run);
+  if (rows <= SMALL_ROWS) {   // one block
+    l.each = (int32_t)cdiv(rows, SUM_WAVES);
+    l.blocks = 1;
+    return l;
+  }
   l.each = 4;
   while (l.each < 64 && rows * l.slabs > (int64_t)l.each * SUM_WAVES * 1024) l.each *= 2;
   l.blocks = (int32_t)cdiv(rows, (int64_t)SUM_WAVES * l.each);
@@ -512,13 +592,16 @@ extern "C" int codistill_embedding_workspace_bytes(const cd_embedding* desc, siz
 extern "C" int codistill_embedding_backward(const cd_embedding* desc, const void* tokens, const void* dy, float* dtable, int accumulate, void* workspace,
                                             size_t workspace_bytes, void* stream) {
   if (const int rc = check("embedding_backward", desc)) return rc;
-  CD_REQUIRE(dtable && ((tokens && dy && workspace) || desc->rows == 0), "embedding_backward: NULL pointer argument");
+  CD_REQUIRE(dtable && ((tokens && dy) || desc->rows == 0), "embedding_backward: NULL pointer argument");
   const int re = size_of(desc->row_dtype);
   CD_REQUIRE(whole(tokens, desc->token_bytes) && whole(dy, re) && whole(dtable, 4) && whole(workspace, 16), "embedding_backward: misaligned pointer");
+  const bool small = desc->rows <= SMALL_ROWS;
   int run = run_of(desc->row_dtype, desc->width);
-  if (run > 1 && !(whole(dtable, 16) && whole(dy, run * re) && (desc->rows <= 1 || desc->row_stride % run == 0))) run = 1;
+  if (small) run = desc->row_dtype == CD_BF16 && desc->width % 2 == 0 ? 2 : 1;   // (the columns are what workgroups are there for)
+  if (run > 1 && !(whole(dtable, run < 4 ? 4 * run : 16) && whole(dy, run * re) && (desc->rows <= 1 || desc->row_stride % run == 0))) run = 1;
   size_t need = 0;
   codistill_embedding_workspace_bytes(desc, &need);
+  CD_REQUIRE(workspace || need == 0, "embedding_backward: NULL pointer argument");
   if (workspace_bytes < need) return set_error(CD_ERR_WORKSPACE_TOO_SMALL, "embedding_backward: workspace of %zu bytes, %zu needed", workspace_bytes, need);
   if (desc->rows == 0 && accumulate) return CD_OK;
   const EmbedLayout l = layout_of(desc->row_dtype, desc->rows, desc->vocabulary, desc->width, run);
@@ -531,9 +614,11 @@ extern "C" int codistill_embedding_backward(const cd_embedding* desc, const void
   const int64_t zeros = accumulate ? 0 : cdiv(desc->vocabulary, 64 * SUM_WAVES), fill = zeros < FILL_BLOCKS ? zeros : FILL_BLOCKS;
   hipStream_t s = static_cast<hipStream_t>(stream);
   ProfScope prof(CD_K_GLUE, s, (double)a.rows * a.width, (double)a.rows * a.width * re + 4.0 * a.vocabulary * a.width);
-  if (desc->rows <= RANK_ROWS) {
-    if (desc->rows) hipLaunchKernelGGL(embedding_rank_kernel, dim3((unsigned)cdiv(desc->rows, RANK_EACH)), dim3(256), 0, s, a);
-  } else {
+  if (!small && desc->rows <= RANK_ROWS) {
+    const dim3 ranks((unsigned)cdiv(desc->rows, RANK_EACH));
+    if (desc->token_bytes == 8) hipLaunchKernelGGL((embedding_rank_kernel<int64_t>), ranks, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((embedding_rank_kernel<int32_t>), ranks, dim3(256), 0, s, a);
+  } else if (!small) {
     int32_t *order = a.order, *words = a.words, *order2 = reinterpret_cast<int32_t*>(ws + l.order2), *words2 = reinterpret_cast<int32_t*>(ws + l.words2);
     a.counts = reinterpret_cast<int32_t*>(ws + l.counts);
     a.chunk = l.chunk; a.chunks = l.chunks; a.digits = 1 << l.digit_bits;
@@ -547,10 +632,17 @@ extern "C" int codistill_embedding_backward(const cd_embedding* desc, const void
     }
   }
   a.sums = (int64_t)l.blocks * l.slabs;
+  if (desc->rows == 0) a.sums = 0;
   const dim3 blocks((unsigned)(a.sums + fill));
   auto sum = [&](auto kernel) { hipLaunchKernelGGL(kernel, blocks, dim3(64 * SUM_WAVES), 0, s, a); };
-  if (re == 2) { if (run == 8) sum(embedding_sum_kernel<bf16_t, 8>); else if (run == 4) sum(embedding_sum_kernel<bf16_t, 4>); else sum(embedding_sum_kernel<bf16_t, 1>); }
-  else { if (run == 4) sum(embedding_sum_kernel<float, 4>); else sum(embedding_sum_kernel<float, 1>); }
+  if (small) {
+    if (re == 2) { if (run == 2) sum(embedding_sum_kernel<bf16_t, 2, true>); else sum(embedding_sum_kernel<bf16_t, 1, true>); }
+    else sum(embedding_sum_kernel<float, 1, true>);
+  } else if (re == 2) {
+    if (run == 8) sum(embedding_sum_kernel<bf16_t, 8, false>); else if (run == 4) sum(embedding_sum_kernel<bf16_t, 4, false>); else sum(embedding_sum_kernel<bf16_t, 1, false>);
+  } else {
+    if (run == 4) sum(embedding_sum_kernel<float, 4, false>); else sum(embedding_sum_kernel<float, 1, false>);
+  }
   if (l.blocks > 1) {
     const int64_t joins = l.blocks - 1;
     if (run > 1) hipLaunchKernelGGL((embedding_join_kernel<4>), dim3((unsigned)(joins * cdiv(desc->width, 256))), dim3(256), 0, s, a);

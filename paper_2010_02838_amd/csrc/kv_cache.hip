@@ -18,7 +18,7 @@ namespace {
 constexpr int KV_TILE = 64;           // tokens that are worked on together: pages are whole tiles
 constexpr float KV_LEAST = 0x1p-100f;
 constexpr int KV_WAVES = 4;           // waves of a workgroup of the attention
-constexpr int KV_TARGET = 512;        // workgroups that fill the chip
+constexpr int KV_CUS = 256;
 constexpr int KV_MOST_PARTS = 512;
 constexpr float LOG2E = 1.4426950408889634f;
 
@@ -48,20 +48,24 @@ __device__ inline int64_t page_of(const KvArgs& c, int b, int64_t pos, int* slot
 // ---- codes --------------------------------------------------------------------------------------------------------------
 // magnitudes as integers: larger numbers are larger, infinities and NaN largest
 __device__ inline uint32_t magnitude(float x) { return __builtin_bit_cast(uint32_t, x) & 0x7fffffffu; }
+// the largest of `lanes` neighbours (a power of two up to 32), each of which receives it: exchanges inside rows of 16 lanes, which need no LDS
 __device__ inline uint32_t lanes_max(uint32_t v, int lanes) {
-  for (int o = lanes >> 1; o > 0; o >>= 1) {
-    const uint32_t u = __shfl_xor(v, o, 64);
-    v = v > u ? v : u;
-  }
+  auto with = [&](uint32_t u) { v = v > u ? v : u; };
+  if (lanes > 1) with(__builtin_amdgcn_mov_dpp(v, 0xb1, 0xf, 0xf, true));    // lane ^ 1
+  if (lanes > 2) with(__builtin_amdgcn_mov_dpp(v, 0x4e, 0xf, 0xf, true));    // lane ^ 2
+  if (lanes > 4) with(__builtin_amdgcn_mov_dpp(v, 0x141, 0xf, 0xf, true));   // the other four of eight
+  if (lanes > 8) with(__builtin_amdgcn_mov_dpp(v, 0x140, 0xf, 0xf, true));   // the other eight of sixteen
+  if (lanes > 16) with(__shfl_xor(v, 16, 64));
   return v;
 }
-// the smallest bf16 number that is at least top / 127 (127 times a bf16 number is exact in fp32); NaN where an element is not finite
+// the smallest bf16 number that is at least top / 127 (127 times a bf16 number is exact in fp32); NaN where an element is not finite.  The product with
+// 1 / 127, cut to bf16, is at most two below.
 __device__ inline uint16_t scale_of(uint32_t top) {
-  if (top >= 0x7f800000u) return 0x7fc0;
   const float t = __builtin_bit_cast(float, top);
-  uint32_t s = __builtin_bit_cast(uint32_t, fmaxf(t / 127.f, KV_LEAST)) >> 16;
-  while (127.f * bf16_to_f32((bf16_t)s) < t) s++;
-  return (uint16_t)s;
+  uint32_t s = __builtin_bit_cast(uint32_t, fmaxf(t * (1.f / 127.f), KV_LEAST)) >> 16;
+  s += 127.f * bf16_to_f32((bf16_t)s) < t;
+  s += 127.f * bf16_to_f32((bf16_t)s) < t;
+  return top >= 0x7f800000u ? 0x7fc0 : (uint16_t)s;
 }
 // rint(x / s) in the lowest byte, exactly.  t is the quotient rounded once (a product and a correction by what it leaves, which fp32 holds exactly), and a quotient that
 // is not halfway between two codes does not round to there: s has 8 bits, so it lies at least half a step of fp32 and 2^-32 of itself away.  Adding 1.5 2^23 rounds
@@ -82,7 +86,7 @@ __device__ inline uint2 quantise(const float (&x)[8], int lanes, uint16_t* scale
   top = lanes_max(top, lanes);
   *scale = scale_of(top);
   if (top >= 0x7f800000u) return make_uint2(0, 0);
-  const float s = bf16_to_f32(*scale), inverse = 1.f / s;
+  const float s = bf16_to_f32(*scale), inverse = __builtin_amdgcn_rcpf(s);   // (off by 2^-23: the correction's error is 2^-45)
   uint32_t w[8];
 #pragma unroll
   for (int e = 0; e < 8; e++) w[e] = code_of(x[e], s, inverse);
@@ -165,6 +169,7 @@ __device__ inline KvTile tile_of(const KvRowArgs& a) {
 
 // Two waves of a workgroup take the keys, two the values (as much work), 8 channels a lane.  Values go through LDS as they are quantised, token by token, and
 // leave it channel by channel, 8 tokens of 4 channels a thread; rows of 4 bytes more than the channels keep both sides off each other's banks.
+constexpr int KV_AHEAD = 4;   // tokens of a lane whose loads are in flight together
 constexpr int V_PAD = 4, V_WORDS = (256 + V_PAD) / 4;   // words of a token's row, widest heads
 
 template <typename T>
@@ -177,34 +182,52 @@ __global__ void __launch_bounds__(256) kv_write_kernel(KvRowArgs a) {
   uint16_t* const scales = c.scales + head * 3 * c.page_tokens + t.slot0;
   const int lane = threadIdx.x & 127, words = (2 * c.dim + V_PAD) / 4;
   if (threadIdx.x < 128) {
-    const int sub = lane % a.k_lanes, per_wg = 128 / a.k_lanes, ch = sub * 8;
-    for (int g = lane / a.k_lanes; g < 2 * (t.hi - t.lo); g += per_wg) {
-      const int slot = t.lo + (g >> 1), m = g & 1;
-      const int64_t from = a.starts ? (t.row0 + slot) * a.k_token : t.b * a.k_batch + (t.i0 + slot) * a.k_token;
-      float x[8];
+    const int sub = lane % a.k_lanes, per_wg = 128 / a.k_lanes, ch = sub * 8, all = 2 * (t.hi - t.lo);
+    const T* const in = static_cast<const T*>(a.k_in) + (a.starts ? 0 : t.b * a.k_batch) + (int64_t)2 * t.h * c.dim + ch;
+    const int64_t row = a.starts ? t.row0 : t.i0;
+    for (int g0 = lane / a.k_lanes; g0 < all; g0 += KV_AHEAD * per_wg) {
+      float x[KV_AHEAD][8];
 #pragma unroll
-      for (int e = 0; e < 8; e++) x[e] = 0.f;
-      if (ch < c.dim) load8<T>(static_cast<const T*>(a.k_in) + from + (int64_t)(2 * t.h + m) * c.dim + ch, x);
-      uint16_t s;
-      const uint2 w = quantise(x, a.k_lanes, &s);
-      if (sub == 0) scales[(int64_t)m * c.page_tokens + slot] = s;
-      if (ch < c.dim) *reinterpret_cast<uint2*>(c.k + ((head * c.page_tokens + t.slot0 + slot) * 2 + m) * c.padded + ch) = w;
+      for (int u = 0; u < KV_AHEAD; u++) {
+        const int g = g0 + u * per_wg;
+#pragma unroll
+        for (int e = 0; e < 8; e++) x[u][e] = 0.f;
+        if (ch < c.dim && g < all) load8<T>(in + (row + t.lo + (g >> 1)) * a.k_token + (g & 1) * c.dim, x[u]);
+      }
+#pragma unroll
+      for (int u = 0; u < KV_AHEAD; u++) {
+        const int g = g0 + u * per_wg, slot = t.lo + (g >> 1), m = g & 1;
+        if (g >= all) break;   // (for all lanes that share a scale)
+        uint16_t s;
+        const uint2 w = quantise(x[u], a.k_lanes, &s);
+        if (sub == 0) scales[(int64_t)m * c.page_tokens + slot] = s;
+        if (ch < c.dim) *reinterpret_cast<uint2*>(c.k + ((head * c.page_tokens + t.slot0 + slot) * 2 + m) * c.padded + ch) = w;
+      }
     }
   } else {
-    const int sub = lane % a.v_lanes, per_wg = 128 / a.v_lanes, ch = sub * 8;
-    for (int g = lane / a.v_lanes; g < t.hi - t.lo; g += per_wg) {
-      const int slot = t.lo + g;
-      const int64_t from = a.starts ? (t.row0 + slot) * a.v_token : t.b * a.v_batch + (t.i0 + slot) * a.v_token;
-      float x[8];
+    const int sub = lane % a.v_lanes, per_wg = 128 / a.v_lanes, ch = sub * 8, all = t.hi - t.lo;
+    const T* const in = static_cast<const T*>(a.v_in) + (a.starts ? 0 : t.b * a.v_batch) + (int64_t)2 * t.h * c.dim + ch;
+    const int64_t row = a.starts ? t.row0 : t.i0;
+    for (int g0 = lane / a.v_lanes; g0 < all; g0 += KV_AHEAD * per_wg) {
+      float x[KV_AHEAD][8];
 #pragma unroll
-      for (int e = 0; e < 8; e++) x[e] = 0.f;
-      if (ch < 2 * c.dim) load8<T>(static_cast<const T*>(a.v_in) + from + (int64_t)t.h * 2 * c.dim + ch, x);
-      uint16_t s;
-      const uint2 w = quantise(x, a.v_lanes, &s);
-      if (sub == 0) scales[(int64_t)2 * c.page_tokens + slot] = s;
-      if (ch < 2 * c.dim) {
-        tile[slot * words + ch / 4] = w.x;
-        tile[slot * words + ch / 4 + 1] = w.y;
+      for (int u = 0; u < KV_AHEAD; u++) {
+        const int g = g0 + u * per_wg;
+#pragma unroll
+        for (int e = 0; e < 8; e++) x[u][e] = 0.f;
+        if (ch < 2 * c.dim && g < all) load8<T>(in + (row + t.lo + g) * a.v_token, x[u]);
+      }
+#pragma unroll
+      for (int u = 0; u < KV_AHEAD; u++) {
+        const int g = g0 + u * per_wg, slot = t.lo + g;
+        if (g >= all) break;   // (for all lanes that share a scale)
+        uint16_t s;
+        const uint2 w = quantise(x[u], a.v_lanes, &s);
+        if (sub == 0) scales[(int64_t)2 * c.page_tokens + slot] = s;
+        if (ch < 2 * c.dim) {
+          tile[slot * words + ch / 4] = w.x;
+          tile[slot * words + ch / 4 + 1] = w.y;
+        }
       }
     }
   }
@@ -781,7 +804,8 @@ static int row_tiles(const cd_kv_cache* c, const cd_kv_attn* d) { return rows_of
 // Workgroups of a sequence and key head: enough to fill the chip, each with at least a block for every wave.
 static int parts_of(const cd_kv_cache* c, const cd_kv_attn* d) {
   const int64_t groups = (int64_t)c->sequences * c->kv_heads * cdiv(rows_of(c, d), 8 * row_tiles(c, d));
-  const int64_t blocks = (int64_t)c->seq_pages * c->page_tokens / KV_TILE, most = blocks / KV_WAVES < KV_MOST_PARTS ? blocks / KV_WAVES : KV_MOST_PARTS, want = cdiv(KV_TARGET, groups > 0 ? groups : 1);
+  const int64_t blocks = (int64_t)c->seq_pages * c->page_tokens / KV_TILE, most = blocks / KV_WAVES < KV_MOST_PARTS ? blocks / KV_WAVES : KV_MOST_PARTS;
+  const int64_t want = KV_CUS * (c->head_dim <= 64 && row_tiles(c, d) == 1 ? 2 : 1) / (groups > 0 ? groups : 1);
   const int64_t parts = want < most ? want : most;
   return parts < 1 ? 1 : (int)parts;
 }

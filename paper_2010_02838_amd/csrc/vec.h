@@ -1,4 +1,4 @@
-// Runs of N elements as one load or store where they fill 8 or 16 bytes, element by element otherwise.
+// Runs of N elements as one load (of 4, 8 or 16 bytes) or store (of 8 or 16) where they fill it, element by element otherwise.
 #pragma once
 #include "common.h"
 
@@ -11,6 +11,9 @@ template <typename T, int N> __device__ static inline void load_run(const T* p, 
   } else if constexpr (N * sizeof(T) == 8) {
     const uint2 u = *reinterpret_cast<const uint2*>(p);
     __builtin_memcpy(out, &u, 8);
+  } else if constexpr (N * sizeof(T) == 4) {
+    const uint32_t u = *reinterpret_cast<const uint32_t*>(p);
+    __builtin_memcpy(out, &u, 4);
   } else {
 #pragma unroll
     for (int i = 0; i < N; i++) out[i] = p[i];

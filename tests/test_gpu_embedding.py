@@ -62,7 +62,7 @@ def check(tokens, dy, words, scale=1.0, accumulate=False, seed=0):
 
 @pytest.mark.parametrize("kind", ["uniform", "one", "runs", "none", "text"])
 @pytest.mark.parametrize("rows,words,width,dtype", [
-    (1, 1, 1, F32), (2, 3, 8, BF), (31, 5, 64, F32), (33, 40, 333, BF), (300, 64, 256, F32), (300, 1000, 513, F32), (2000, 7, 100, BF), (5000, 3000, 512, BF), (16384, 1024, 40, BF),
+    (1, 1, 1, F32), (2, 3, 8, BF), (100, 1000, 7, BF), (511, 70000, 64, F32), (512, 300, 66, BF), (512, 20, 130, F32), (513, 300, 66, BF), (31, 5, 64, F32), (33, 40, 333, BF), (300, 64, 256, F32), (300, 1000, 513, F32), (2000, 7, 100, BF), (5000, 3000, 512, BF), (16384, 1024, 40, BF),
     (16385, 1023, 40, F32), (16385, 1024, 40, BF), (40000, 70000, 16, F32), (70000, 2 ** 21, 8, BF), (20000, 1, 24, F32)])
 def test_gradients(rows, words, width, dtype, kind):
     gen = torch.Generator(device=DEV).manual_seed(rows)

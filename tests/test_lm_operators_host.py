@@ -68,7 +68,7 @@ def test_norm_rotary_binding():
 
 
 def emb(**kw):
-    d = dict(table_dtype=B.CD_BF16, row_dtype=B.CD_F32, token_bytes=8, scale=1.0, rows=10, vocabulary=100, width=64, row_stride=64)
+    d = dict(table_dtype=B.CD_BF16, row_dtype=B.CD_F32, token_bytes=8, scale=1.0, rows=1000, vocabulary=100, width=64, row_stride=64)
     d.update(kw)
     return B.Embedding(**d)
 
