@@ -18,7 +18,7 @@ namespace cd {
 namespace {
 
 constexpr uint32_t NO_WORD = 0x7fffffffu;   // sorted behind all words
-constexpr int SMALL_ROWS = 512;              // most rows that one workgroup puts in order for itself
+constexpr int SMALL_ROWS = 512, SMALL_BLOCK = 32;   // most rows that a workgroup puts in order for itself, places it takes of them
 constexpr int RANK_ROWS = 16384;            // most rows whose places are counted
 constexpr int RANK_EACH = 16, RANK_AHEAD = 8;   // rows of a workgroup there, loads in flight
 constexpr int DIGIT_BITS = 10, SORT_CHUNKS = 256, SORT_LEAST = 1024, SORT_WAVES = 8;
@@ -34,7 +34,12 @@ struct EmbedArgs {
   float scale;
 };
 
-__device__ inline uint32_t word_from(const EmbedArgs& a, int64_t token) { return token >= 0 && token < a.vocabulary ? (uint32_t)token : NO_WORD; }
+// (halves of 32 bits: a token whose upper half is not zero, or whose lower half is no word, is none)
+__device__ inline uint32_t word_from(const EmbedArgs& a, int64_t token) {
+  const uint32_t low = (uint32_t)token < (uint32_t)a.vocabulary ? (uint32_t)token : NO_WORD;
+  return (uint32_t)(token >> 32) == 0 ? low : NO_WORD;
+}
+__device__ inline uint32_t word_from(const EmbedArgs& a, int32_t token) { return (uint32_t)token < (uint32_t)a.vocabulary ? (uint32_t)token : NO_WORD; }
 template <typename TOK> __device__ inline uint32_t word_of(const EmbedArgs& a, int64_t i) { return word_from(a, static_cast<const TOK*>(a.tokens)[i]); }
 __device__ inline uint32_t word_of(const EmbedArgs& a, int64_t i) { return a.token_bytes == 8 ? word_of<int64_t>(a, i) : word_of<int32_t>(a, i); }
 
@@ -71,7 +76,7 @@ __global__ void __launch_bounds__(256) embedding_kernel(EmbedArgs a, int lanes) 
 }
 
 // ---- the order of the rows --------------------------------------------------------------------------------------------------
-// 1 where a < b (a up to 2^31 - 1, b up to 2^31): the sign of their difference, which is faster than a comparison, whose result travels through a mask
+// 1 where a < b (-1 <= a < 2^31, 0 <= b <= 2^31): the sign of their difference, which is faster than a comparison, whose result travels through a mask
 __device__ inline uint32_t below(uint32_t a, uint32_t b) { return (a - b) >> 31; }
 // Few rows: place of row i = rows with a smaller word + rows in front of it with the same.  A lane compares its row with each of the workgroup's; the lanes'
 // counts are added up at the end.  (Comparisons and the addition of their carries, or counts of their masks in scalar registers: 15 us for 8192 rows.)
@@ -112,16 +117,17 @@ __global__ void __launch_bounds__(256) embedding_rank_kernel(EmbedArgs a) {
     for (int u = 0; u < RANK_AHEAD; u++) now[u] = k0 + 256 * u + lane < rows ? word_from(a, others[u]) : NO_WORD;
     if (k0 + 256 * RANK_AHEAD < rows) fetch(k0 + 256 * RANK_AHEAD);
 #pragma unroll
-    for (int u = 0; u < RANK_AHEAD; u++) {
-      const int j0 = k0 + 256 * u;
+    for (int u = 0; u < RANK_AHEAD; u += 2) {
+      const int j0 = k0 + 256 * u, j1 = j0 + 256;
       if (j0 >= rows) break;
-      if (j0 + 64 <= i0 || j0 >= i0 + RANK_EACH) {   // all 64 in front of the workgroup's rows, or all behind
-        const uint32_t same = j0 < i0;
+      const bool among = (j0 < i0 + RANK_EACH && j0 + 64 > i0) || (j1 < i0 + RANK_EACH && j1 + 64 > i0);
+      if (!among) {   // all 64 rows in front of the workgroup's rows, or all behind
+        const uint32_t x = now[u] - (j0 < i0), y = now[u + 1] - (j1 < i0);
 #pragma unroll
-        for (int r = 0; r < RANK_EACH; r++) count[r] += below(now[u], w[r] + same);
+        for (int r = 0; r < RANK_EACH; r++) count[r] += below(x, w[r]) + below(y, w[r]);
       } else {
 #pragma unroll
-        for (int r = 0; r < RANK_EACH; r++) count[r] += below(now[u], w[r] + below(j0 + lane, i0 + r));
+        for (int r = 0; r < RANK_EACH; r++) count[r] += below(now[u], w[r] + below(j0 + lane, i0 + r)) + below(now[u + 1], w[r] + below(j1 + lane, i0 + r));
       }
     }
   }
@@ -299,18 +305,19 @@ template <bool SMALL> __device__ inline void zero_absent(const EmbedArgs& a, int
 
 // A block of SUM_WAVES * each rows in sorted order, 64 V columns.  A wave adds up `each` of them, writes the words that are its alone and leaves its first and
 // its last word's sum in LDS; the waves' ends are then put together, column by column, in their order.
-// SMALL: up to SMALL_ROWS rows, which are one block; every workgroup puts them in order itself, in LDS, and nothing is left to join.
+// SMALL: up to SMALL_ROWS rows.  Every workgroup puts all of them in order itself, in LDS, and takes the words that begin among its SMALL_BLOCK places, whole:
+// nothing is left to join, and the gradient is one launch.
 template <typename T, int V, bool SMALL>
 __global__ void __launch_bounds__(64 * SUM_WAVES) embedding_sum_kernel(EmbedArgs a) {
   static_assert(SMALL_ROWS == 64 * SUM_WAVES, "a row for each thread");
   if ((int64_t)blockIdx.x >= a.sums) return zero_absent<SMALL>(a, (int)(blockIdx.x - a.sums), (int)(gridDim.x - a.sums));
   __shared__ float ends[2][SUM_WAVES][64 * V];
   __shared__ uint32_t word[2][SUM_WAVES];
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, block = blockIdx.x / a.slabs, slab = blockIdx.x % a.slabs;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, block = blockIdx.x / a.slabs, slab = blockIdx.x % a.slabs;
   const int64_t col = (int64_t)slab * 64 * V + lane * V;
   const bool mine = col < a.width;     // (a width of whole runs)
-  const int64_t from = (int64_t)block * SUM_WAVES * a.each + (int64_t)wave * a.each;
-  const int n = (int)max((int64_t)0, min((int64_t)a.each, a.rows - from));
+  int64_t from = (int64_t)block * SUM_WAVES * a.each + (int64_t)wave * a.each;
+  int n = (int)max((int64_t)0, min((int64_t)a.each, a.rows - from));
   // this wave's rows and words: one a lane
   int row_here = 0;
   uint32_t word_here = NO_WORD;
@@ -328,17 +335,34 @@ __global__ void __launch_bounds__(64 * SUM_WAVES) embedding_sum_kernel(EmbedArgs
       place += below(other.x, limit) + below(other.y, limit);
       place += below(other.z, limit) + below(other.w, limit);
     };
+    if (from_wave < rows) {
 #pragma unroll 4
-    for (int j = 0; j < min(from_wave, rows); j += 4) count(j, me + 1);
+      for (int j = 0; j < from_wave; j += 4) count(j, me + 1);
 #pragma unroll 4
-    for (int j = from_wave; j < min(from_wave + 64, rows); j++) place += below(unsorted[j], me + below(j, threadIdx.x));
+      for (int j = from_wave; j < from_wave + 64; j++) place += below(unsorted[j], me + below(j, threadIdx.x));
 #pragma unroll 4
-    for (int j = from_wave + 64; j < rows; j += 4) count(j, me);
+      for (int j = from_wave + 64; j < rows; j += 4) count(j, me);
+    }
+    __shared__ int limits[2];    // where the block's words begin and end
+    in_order[1][threadIdx.x] = NO_WORD;
+    if (threadIdx.x < 2) limits[threadIdx.x] = SMALL_ROWS;
+    __syncthreads();
     if ((int64_t)threadIdx.x < a.rows) {
       in_order[0][place] = threadIdx.x;
       in_order[1][place] = me;
     }
     __syncthreads();
+    const uint32_t here = in_order[1][threadIdx.x], in_front = threadIdx.x ? in_order[1][threadIdx.x - 1] : 0xffffffffu;
+    const bool begins = here != in_front;    // a word, or the rows without one
+#pragma unroll
+    for (int k = 0; k < 2; k++) {
+      const uint64_t set = __ballot(begins && (int)threadIdx.x >= SMALL_BLOCK * (block + k));
+      if (set && lane == 0) atomicMin(&limits[k], 64 * wave + __ffsll((unsigned long long)set) - 1);
+    }
+    __syncthreads();
+    const int begin = limits[0], end = limits[1], each = (end - begin + SUM_WAVES - 1) / SUM_WAVES;
+    from = begin + wave * each;
+    n = max(0, min(each, end - (int)from));
     if (lane < n) {
       row_here = in_order[0][from + lane];
       word_here = in_order[1][from + lane];
@@ -347,66 +371,88 @@ __global__ void __launch_bounds__(64 * SUM_WAVES) embedding_sum_kernel(EmbedArgs
     row_here = a.order[from + lane];
     word_here = (uint32_t)a.words[from + lane];
   }
+  // Real rows come first.  What the loop needs of a row is one bit (whether its word ends with it, and is not the wave's last) and an offset.
+  const int real = __popcll(__ballot(word_here != NO_WORD));
+  const uint32_t after = __shfl_down(word_here, 1, 64);
+  const uint64_t last_of_word = __ballot(lane + 1 < real && word_here != after);
+  const uint32_t first = __builtin_amdgcn_readfirstlane(word_here), final = __builtin_amdgcn_readlane(word_here, max(real - 1, 0));
+  const int64_t offset = (int64_t)row_here * a.row_stride;
+  const uint32_t offset_low = (uint32_t)offset, offset_high = (uint32_t)(offset >> 32);
+  const T* const rows_here = static_cast<const T*>(a.dy) + (mine ? col : 0);   // (lanes behind the width read the first columns, and write nothing)
+  float* const table_here = a.dtable + (mine ? col : 0);
   float sum[V];
 #pragma unroll
   for (int e = 0; e < V; e++) sum[e] = 0.f;
-  const uint32_t first = __builtin_amdgcn_readlane(word_here, 0), final = __builtin_amdgcn_readlane(word_here, n > 0 ? n - 1 : 0);
-  constexpr int AHEAD = SMALL ? 16 : 4;
-  for (int i0 = 0; i0 < n; i0 += AHEAD) {
+  bool one = true;     // the wave's first word has not ended
+  constexpr int AHEAD = SMALL ? 8 : 4;
+  for (int i0 = 0; i0 < real; i0 += AHEAD) {
     T t[AHEAD][V];
     float old[AHEAD][V];
-    // rows, and what the table's gradient holds for words that end here and are this wave's alone, on their way together
+    // rows, and what the table's gradient holds for words that end with them, on their way together
 #pragma unroll
     for (int k = 0; k < AHEAD; k++) {
-      const int i = i0 + k;
+      const int i = min(i0 + k, real - 1);
+      const int64_t from = (int64_t)(((uint64_t)__builtin_amdgcn_readlane(offset_high, i) << 32) | __builtin_amdgcn_readlane(offset_low, i));
+      load_run<T, V>(rows_here + from, t[k]);
+    }
+    if (a.accumulate) {
 #pragma unroll
-      for (int e = 0; e < V; e++) {
-        t[k][e] = T(0);
-        old[k][e] = 0.f;
-      }
-      if (i >= n || !mine) continue;
-      const uint32_t w = __builtin_amdgcn_readlane(word_here, i);
-      if (w != NO_WORD) load_run<T, V>(static_cast<const T*>(a.dy) + (int64_t)__builtin_amdgcn_readlane(row_here, i) * a.row_stride + col, t[k]);
-      if (a.accumulate && w != first && w != final && __builtin_amdgcn_readlane(word_here, i + 1) != w) load_floats<V>(a.dtable + (int64_t)w * a.width + col, old[k]);
+      for (int k = 0; k < AHEAD; k++)
+        if (last_of_word >> (i0 + k) & 1) load_floats<V>(table_here + (int64_t)__builtin_amdgcn_readlane(word_here, i0 + k) * a.width, old[k]);
     }
 #pragma unroll
     for (int k = 0; k < AHEAD; k++) {
       const int i = i0 + k;
-      if (i >= n) break;
-      const uint32_t w = __builtin_amdgcn_readlane(word_here, i);
+      if (i >= real) break;
 #pragma unroll
       for (int e = 0; e < V; e++) sum[e] += Cvt<T>::ld(t[k][e]);
-      if (w == final || __builtin_amdgcn_readlane(word_here, i + 1) == w) continue;
-      // the word ends, and is not the last one (i + 1 < n)
-      if (w == first) {
+      if (!(last_of_word >> i & 1)) continue;
+      if (one) {
+        one = false;
 #pragma unroll
         for (int e = 0; e < V; e++) ends[0][wave][lane * V + e] = sum[e];
       } else if (mine) {
-        put_row<V>(a.dtable + (int64_t)w * a.width + col, old[k], sum, a.scale);
+        if (!a.accumulate) {
+#pragma unroll
+          for (int e = 0; e < V; e++) old[k][e] = 0.f;
+        }
+        put_row<V>(table_here + (int64_t)__builtin_amdgcn_readlane(word_here, i) * a.width, old[k], sum, a.scale);
       }
 #pragma unroll
       for (int e = 0; e < V; e++) sum[e] = 0.f;
     }
   }
 #pragma unroll
-  for (int e = 0; e < V; e++) ends[first == final ? 0 : 1][wave][lane * V + e] = sum[e];
+  for (int e = 0; e < V; e++) ends[one ? 0 : 1][wave][lane * V + e] = sum[e];
   if (lane == 0) {
     word[0][wave] = first;
     word[1][wave] = final;     // (the same word: one sum)
   }
   const int64_t begin = (int64_t)block * SUM_WAVES * a.each, end = min(begin + (int64_t)SUM_WAVES * a.each, a.rows);
-  const uint32_t in_front = begin > 0 ? (uint32_t)a.words[begin - 1] : NO_WORD, behind = end < a.rows ? (uint32_t)a.words[end] : NO_WORD;
+  const uint32_t in_front = !SMALL && begin > 0 ? (uint32_t)a.words[begin - 1] : NO_WORD, behind = !SMALL && end < a.rows ? (uint32_t)a.words[end] : NO_WORD;
   __syncthreads();
+  uint32_t words[2][SUM_WAVES];
+#pragma unroll
+  for (int q = 0; q < SUM_WAVES; q++)
+#pragma unroll
+    for (int k = 0; k < 2; k++) words[k][q] = word[k][q];
+#pragma unroll
+  for (int q = 0; q < SUM_WAVES; q++)
+#pragma unroll
+    for (int k = 0; k < 2; k++) words[k][q] = __builtin_amdgcn_readfirstlane(words[k][q]);
   for (int c = threadIdx.x; c < 64 * V; c += 64 * SUM_WAVES) {
     const int64_t to = (int64_t)slab * 64 * V + c;
     if (to >= a.width) break;
-    float old[2][SUM_WAVES];
+    float old[2][SUM_WAVES], part[2][SUM_WAVES];
 #pragma unroll
     for (int q = 0; q < SUM_WAVES; q++)
 #pragma unroll
-      for (int k = 0; k < 2; k++) old[k][q] = a.accumulate && word[k][q] != NO_WORD ? a.dtable[(int64_t)word[k][q] * a.width + to] : 0.f;
-    uint32_t w = word[0][0];
-    float s = ends[0][0][c], was = old[0][0];
+      for (int k = 0; k < 2; k++) {
+        part[k][q] = ends[k][q][c];
+        old[k][q] = a.accumulate && words[k][q] != NO_WORD ? a.dtable[(int64_t)words[k][q] * a.width + to] : 0.f;
+      }
+    uint32_t w = words[0][0];
+    float s = part[0][0], was = old[0][0];
     bool started = w != in_front;     // here, not in an earlier block
     auto put = [&](bool goes_on) {
       if (w == NO_WORD) return;
@@ -416,20 +462,20 @@ __global__ void __launch_bounds__(64 * SUM_WAVES) embedding_sum_kernel(EmbedArgs
 #pragma unroll
     for (int q = 0; q < SUM_WAVES; q++) {
       if (q > 0) {
-        if (word[0][q] == w) {
-          s += ends[0][q][c];
+        if (words[0][q] == w) {
+          s += part[0][q];
         } else {
           put(false);
-          w = word[0][q];
-          s = ends[0][q][c];
+          w = words[0][q];
+          s = part[0][q];
           was = old[0][q];
           started = true;
         }
       }
-      if (word[1][q] != word[0][q]) {
+      if (words[1][q] != words[0][q]) {
         put(false);
-        w = word[1][q];
-        s = ends[1][q][c];
+        w = words[1][q];
+        s = part[1][q];
         was = old[1][q];
         started = true;
       }
@@ -498,9 +544,8 @@ static EmbedLayout layout_of(int dtype, int64_t rows, int64_t vocabulary, int64_
   EmbedLayout l = {};
   l.run = run;
   l.slabs = (int32_t)cdiv(width, 64 * run);
-  if (rows <= SMALL_ROWS) {   // one block
-    l.each = (int32_t)cdiv(rows, SUM_WAVES);
-    l.blocks = 1;
+  if (rows <= SMALL_ROWS) {   // (no workspace)
+    l.blocks = (int32_t)cdiv(rows, SMALL_BLOCK);
     return l;
   }
   l.each = 4;
@@ -632,7 +677,6 @@ extern "C" int codistill_embedding_backward(const cd_embedding* desc, const void
     }
   }
   a.sums = (int64_t)l.blocks * l.slabs;
-  if (desc->rows == 0) a.sums = 0;
   const dim3 blocks((unsigned)(a.sums + fill));
   auto sum = [&](auto kernel) { hipLaunchKernelGGL(kernel, blocks, dim3(64 * SUM_WAVES), 0, s, a); };
   if (small) {
@@ -643,7 +687,7 @@ extern "C" int codistill_embedding_backward(const cd_embedding* desc, const void
   } else {
     if (run == 4) sum(embedding_sum_kernel<float, 4, false>); else sum(embedding_sum_kernel<float, 1, false>);
   }
-  if (l.blocks > 1) {
+  if (l.blocks > 1 && !small) {
     const int64_t joins = l.blocks - 1;
     if (run > 1) hipLaunchKernelGGL((embedding_join_kernel<4>), dim3((unsigned)(joins * cdiv(desc->width, 256))), dim3(256), 0, s, a);
     else hipLaunchKernelGGL((embedding_join_kernel<1>), dim3((unsigned)(joins * cdiv(desc->width, 64))), dim3(256), 0, s, a);
