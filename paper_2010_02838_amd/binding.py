@@ -516,39 +516,46 @@ def codistill_head_norm_backward(x, gain, dy, dx, dgain, workspace, eps=1e-5, po
 _NORM_ROTARY_ARRAYS = {n: NormRotaryTensor * n for n in range(1, CD_ROPE_MAX_TENSORS + 1)}
 
 
+def _rope_rows(t, shape, dt, dim):
+    """A token's stride of a tensor that is turned."""
+    s = t.stride()
+    if t.shape != shape or t.dtype is not dt:
+        raise ValueError("norm_rotary: tensors are [tokens, heads, dim] of the descriptor's type")
+    if s[2] != 1 or s[1] != dim:
+        _inner(t, 2, "norm_rotary")
+    return s[0]
+
+
 def _norm_rotary_tensors(desc, positions, tensors, backward):
     """The descriptors of (x, gain, y) or (x, gain, dy, dx, dgain), checked against the rotation's."""
-    n, tokens, dim, dt = len(tensors), positions.shape[1], desc.dim, torch.bfloat16 if desc.dtype == CD_BF16 else torch.float32
-    if positions.dtype is not torch.int32 or not positions.is_contiguous() or positions.shape[0] < desc.axes:
+    n, dim, dt = len(tensors), desc.dim, torch.bfloat16 if desc.dtype == CD_BF16 else torch.float32
+    axes, tokens = positions.shape
+    if positions.dtype is not torch.int32 or axes < desc.axes or not positions.is_contiguous():
         raise ValueError("norm_rotary: positions are contiguous int32 [axes, tokens]")
     if n not in _NORM_ROTARY_ARRAYS:
         raise ValueError("norm_rotary: %d tensors, up to %d in a call" % (n, CD_ROPE_MAX_TENSORS))
-    arr = _NORM_ROTARY_ARRAYS[n]()
-    for a, t in zip(arr, tensors):
-        x, gain, dgain = t[0], t[1], t[4] if backward else None
+    rows = []
+    for t in tensors:
+        x, gain = t[0], t[1]
         shape = x.shape
         if len(shape) != 3 or shape[0] != tokens or shape[2] != dim:
             raise ValueError("norm_rotary: tensors are [tokens, heads, dim] of the descriptor's type")
-        moved = (x, t[2], t[3]) if backward else (x, t[2])
-        for m in moved:
-            if m.shape != shape or m.dtype is not dt:
-                raise ValueError("norm_rotary: tensors are [tokens, heads, dim] of the descriptor's type")
-            if m.stride()[1:] != (dim, 1):
-                _inner(m, 2, "norm_rotary")
-        if gain is not None and (gain.shape != (dim,) or gain.dtype is not dt or not gain.is_contiguous()):
-            raise ValueError("norm_rotary: a gain is contiguous [dim] of the descriptor's type")
-        if dgain is not None and (dgain.shape != (dim,) or dgain.dtype is not torch.float32 or not dgain.is_contiguous()):
-            raise ValueError("norm_rotary: a gain's gradient is contiguous fp32 [dim]")
-        a.x, a.heads, a.x_token = x.data_ptr(), shape[1], x.stride(0)
         if gain is not None:
-            a.gain = gain.data_ptr()
+            if gain.dtype is not dt or gain.shape != (dim,) or not gain.is_contiguous():
+                raise ValueError("norm_rotary: a gain is contiguous [dim] of the descriptor's type")
+            gain = gain.data_ptr()
+        xs = _rope_rows(x, shape, dt, dim)
         if backward:
-            a.dy, a.dx, a.dy_token, a.dx_token = t[2].data_ptr(), t[3].data_ptr(), t[2].stride(0), t[3].stride(0)
+            _, _, dy, dx, dgain = t
             if dgain is not None:
-                a.dgain = dgain.data_ptr()
+                if dgain.dtype is not torch.float32 or dgain.shape != (dim,) or not dgain.is_contiguous():
+                    raise ValueError("norm_rotary: a gain's gradient is contiguous fp32 [dim]")
+                dgain = dgain.data_ptr()
+            rows.append((x.data_ptr(), gain, None, dy.data_ptr(), dx.data_ptr(), dgain, shape[1], xs, 0, _rope_rows(dy, shape, dt, dim), _rope_rows(dx, shape, dt, dim)))
         else:
-            a.y, a.y_token = t[2].data_ptr(), t[2].stride(0)
-    return arr, n, tokens
+            y = t[2]
+            rows.append((x.data_ptr(), gain, y.data_ptr(), None, None, None, shape[1], xs, _rope_rows(y, shape, dt, dim), 0, 0))
+    return _NORM_ROTARY_ARRAYS[n](*rows), n, tokens
 
 
 def codistill_norm_rotary(desc, positions, tensors, eps=1e-5):
@@ -571,11 +578,15 @@ def codistill_norm_rotary_backward(desc, positions, tensors, workspace, eps=1e-5
 
 
 def _embedding_desc(tokens, vocabulary, rows, table_dtype, scale):
-    if tokens.dtype not in (torch.int32, torch.int64) or tokens.dim() != 1 or not tokens.is_contiguous():
+    size = 8 if tokens.dtype is torch.int64 else 4 if tokens.dtype is torch.int32 else 0
+    if not size or tokens.dim() != 1 or not tokens.is_contiguous():
         raise ValueError("embedding: tokens are contiguous int32 or int64 [rows]")
-    if rows.dim() != 2 or rows.shape[0] != tokens.shape[0] or (rows.shape[1] > 1 and rows.stride(1) != 1):
+    if rows.dim() != 2:
         raise ValueError("embedding: rows are [rows, width], the channels of a row contiguous")
-    return Embedding(table_dtype, _dtype(rows), tokens.element_size(), scale, rows.shape[0], vocabulary, rows.shape[1], rows.stride(0))
+    (n, width), (stride, inner) = rows.shape, rows.stride()
+    if n != tokens.shape[0] or (width > 1 and inner != 1):
+        raise ValueError("embedding: rows are [rows, width], the channels of a row contiguous")
+    return Embedding(table_dtype, _dtype(rows), size, scale, n, vocabulary, width, stride)
 
 
 def codistill_embedding(tokens, table, y, scale=1.0):

@@ -9,6 +9,8 @@
 // instructions: of the keys a lane takes a run of one token's channels, of the values 16 tokens of one channel, which is why values are
 // stored with the tokens side by side.  No copy in LDS, no exchange between lanes.
 #include "common.h"
+#include "conv_rules.h"
+#include "kernels.h"
 #include "vec.h"
 #include <math.h>
 
@@ -32,15 +34,18 @@ struct KvArgs {
   const int32_t* table;
   int64_t pages;
   int32_t sequences, kv_heads, dim, padded, page_tokens, seq_pages;
+  FastDiv by_page, by_heads;   // by page_tokens, kv_heads
 };
+// n / d for n below 2^31
+__device__ inline int quotient(int n, FastDiv d) { return (int)div_by((unsigned)n, d); }
 
 // The page of a sequence's tokens from `pos` on, and the place in it; or -1 where the sequence has none (the table may hold anything).
 __device__ inline int64_t page_of(const KvArgs& c, int b, int64_t pos, int* slot) {
   *slot = 0;
   if (pos < 0 || pos > INT32_MAX) return -1;
-  const uint32_t p = (uint32_t)pos / (uint32_t)c.page_tokens;
-  if (p >= (uint32_t)c.seq_pages) return -1;
-  *slot = (int)((uint32_t)pos - p * (uint32_t)c.page_tokens);
+  const int p = quotient((int)pos, c.by_page);
+  if (p >= c.seq_pages) return -1;
+  *slot = (int)pos - p * c.page_tokens;
   const int64_t at = (int64_t)b * c.seq_pages + p, page = c.table ? c.table[at] : at;
   return page >= 0 && page < c.pages ? page : -1;
 }
@@ -131,6 +136,7 @@ struct KvRowArgs {
   const int32_t* first; const int32_t* counts; const int32_t* starts;
   int64_t rows, k_token, k_batch, v_token, v_batch;
   int32_t max_new, tiles, k_lanes, v_lanes;   // lanes of a key, of a value (powers of two)
+  FastDiv by_tiles;
 };
 
 // What a workgroup of the writing or reading kernel works on: the tokens of one sequence that lie in one tile of the cache.
@@ -143,9 +149,9 @@ struct KvTile {
 };
 __device__ inline KvTile tile_of(const KvRowArgs& a) {
   KvTile t;
-  const int unit = blockIdx.x / a.tiles, n_tile = blockIdx.x % a.tiles;
-  t.b = unit / a.c.kv_heads;
-  t.h = unit % a.c.kv_heads;
+  const int unit = quotient(blockIdx.x, a.by_tiles), n_tile = blockIdx.x - unit * a.tiles;
+  t.b = quotient(unit, a.c.by_heads);
+  t.h = unit - t.b * a.c.kv_heads;
   const int64_t first = a.first ? a.first[t.b] : 0;
   int64_t from = 0, n = a.max_new;
   if (a.starts) {      // rows of the tensors only, whatever the table says
@@ -341,6 +347,7 @@ struct KvAttnArgs {
   float* part; float* part_ml;            // sums of a part [unit][row][part][2][2 dim], maxima and sums [unit][row][part][2][2]
   int64_t q_token, q_batch, o_token, o_batch;
   int32_t tq, heads, group, rows, causal, lam_token, parts, tiles;
+  FastDiv by_tiles, by_parts, by_group, by_quads;   // by tiles, parts, group, dim / 2
   float factor;                           // scale log2(e)
 };
 
@@ -381,7 +388,7 @@ template <int N> __device__ inline void split8(const float (&x)[8], v8bf (&out)[
     }
 }
 
-struct KvRow { int query, head, sees; bool real; };   // sees: keys in front of and at the last visible one
+struct KvRow { int query, head; bool real; };
 
 // NK: 32-channel steps of a map's key; RT: tiles of 8 rows
 template <typename T, int NK, int RT>
@@ -391,29 +398,29 @@ __global__ void __launch_bounds__(64 * KV_WAVES, NK <= 2 && RT == 1 ? 2 : 1) kv_
   __shared__ float tops[KV_WAVES][COLS], totals[KV_WAVES][COLS];
   const KvArgs& c = a.c;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, col = lane & 15, grp = lane >> 4, map = col >> 3;
-  int id = blockIdx.x;
-  const int tile = id % a.tiles; id /= a.tiles;
-  const int part = id % a.parts; id /= a.parts;
-  const int h = id % c.kv_heads, b = id / c.kv_heads;
+  int id = blockIdx.x, next = quotient(id, a.by_tiles);
+  const int tile = id - next * a.tiles;
+  id = next;
+  next = quotient(id, a.by_parts);
+  const int part = id - next * a.parts, b = quotient(next, c.by_heads), h = next - b * c.kv_heads;
   const int nk = min(max(a.k_lens[b], 0), c.seq_pages * c.page_tokens), nq = a.q_lens ? min(max(a.q_lens[b], 0), a.tq) : a.tq;
+  auto seen_by = [&](int query) { return a.causal ? max(0, min(nk, query - nq + nk + 1)) : nk; };
   auto row_of = [&](int r) {
     KvRow w;
-    w.query = r / a.group;
+    w.query = quotient(r, a.by_group);
     w.head = h * a.group + r - w.query * a.group;
     w.real = r < a.rows && w.query < nq;
-    w.sees = !w.real ? 0 : a.causal ? max(0, min(nk, w.query - nq + nk + 1)) : nk;
     return w;
   };
-  const int row0 = tile * 8 * RT;
-  // all rows of the tile see at least `least` keys, none more than `most`
-  int least = nk, most = 0, sees[RT];
+  // all real rows of the tile see at least `least` keys, none more than `most`; the others are computed like the last one and not written
+  const int row0 = tile * 8 * RT, first_query = quotient(row0, a.by_group), last_query = min(quotient(row0 + 8 * RT - 1, a.by_group), nq - 1);
+  const int least = first_query < nq ? seen_by(first_query) : 0, most = first_query < nq ? seen_by(last_query) : 0;
+  int sees[RT];
   v8bf q[RT][2][NK][TQ];
 #pragma unroll
   for (int rt = 0; rt < RT; rt++) {
     const KvRow w = row_of(row0 + 8 * rt + (col & 7));
-    sees[rt] = w.sees;
-    least = min(least, w.sees);
-    most = max(most, w.sees);
+    sees[rt] = w.real ? seen_by(w.query) : most;
     const T* from = static_cast<const T*>(a.q) + b * a.q_batch + w.query * a.q_token + (int64_t)(2 * w.head + map) * c.dim;
 #pragma unroll
     for (int s = 0; s < NK; s++) {
@@ -432,14 +439,10 @@ __global__ void __launch_bounds__(64 * KV_WAVES, NK <= 2 && RT == 1 ? 2 : 1) kv_
           for (int e = 0; e < 8; e++) q[rt][m][s][n][e] = map == m ? mine[n][e] : (__bf16)0.f;
     }
   }
-#pragma unroll
-  for (int o = 1; o < 8; o *= 2) {
-    least = min(least, __shfl_xor(least, o, 64));
-    most = max(most, __shfl_xor(most, o, 64));
-  }
-  const int blocks = __builtin_amdgcn_readfirstlane((most + KV_TILE - 1) / KV_TILE);
-  const int whole = __builtin_amdgcn_readfirstlane(least / KV_TILE);   // blocks that all rows see whole
-  const int from = (int)((int64_t)blocks * part / a.parts), to = (int)((int64_t)blocks * (part + 1) / a.parts);
+  const int blocks = (most + KV_TILE - 1) / KV_TILE, whole = least / KV_TILE;   // whole: blocks that all rows see to their ends
+  // a run of blocks for each part, the first `more` of them one longer
+  const int each = quotient(blocks, a.by_parts), more = blocks - each * a.parts;
+  const int from = part * each + min(part, more), to = from + each + (part < more);
 
   v4f acc[RT][NC];
   float top[RT], total[RT];
@@ -605,7 +608,7 @@ __global__ void __launch_bounds__(64 * KV_WAVES, NK <= 2 && RT == 1 ? 2 : 1) kv_
   __syncthreads();
   const int width = 2 * c.dim, quads = width / 4;
   for (int i = threadIdx.x; i < 8 * RT * quads; i += 64 * KV_WAVES) {
-    const int r = i / quads, ch = 4 * (i - r * quads), at = 16 * (r >> 3) + (r & 7);
+    const int r = quotient(i, a.by_quads), ch = 4 * (i - r * quads), at = 16 * (r >> 3) + (r & 7);
     if (row0 + r >= a.rows) break;
     float o[2][4], t[2];
 #pragma unroll
@@ -633,7 +636,7 @@ __global__ void __launch_bounds__(64 * KV_WAVES, NK <= 2 && RT == 1 ? 2 : 1) kv_
     } else {
       const KvRow w = row_of(row0 + r);
       const float lam = a.lam[a.lam_token ? ((int64_t)b * a.tq + w.query) * a.heads + w.head : w.head];
-      const bool seen = w.real && w.sees > 0;
+      const bool seen = w.real && seen_by(w.query) > 0;
       float v[4];
 #pragma unroll
       for (int e = 0; e < 4; e++) v[e] = seen ? (t[0] == 0.f ? 0.f : o[0][e] / t[0]) - (t[1] == 0.f ? 0.f : lam * (o[1][e] / t[1])) : 0.f;
@@ -734,7 +737,8 @@ static int check_cache(const char* what, const cd_kv_cache* c, bool pointers) {
   return CD_OK;
 }
 static KvArgs cache_args(const cd_kv_cache* c) {
-  return {c->k, c->v, c->scales, c->table, c->pages, c->sequences, c->kv_heads, c->head_dim, padded_dim(c->head_dim), c->page_tokens, c->seq_pages};
+  return {c->k, c->v, c->scales, c->table, c->pages, c->sequences, c->kv_heads, c->head_dim, padded_dim(c->head_dim), c->page_tokens, c->seq_pages,
+          fast_div(c->page_tokens), fast_div(c->kv_heads)};
 }
 static int lanes_for(int runs) {
   int lanes = 1;
@@ -775,6 +779,7 @@ static KvRowArgs row_args(const cd_kv_cache* c, const cd_kv_rows* r) {
   a.k_token = r->k_token; a.k_batch = r->k_batch; a.v_token = r->v_token; a.v_batch = r->v_batch;
   a.max_new = r->max_new;
   a.tiles = (int32_t)((r->max_new + 126ll) / KV_TILE);   // (the first token may be the last of its tile)
+  a.by_tiles = fast_div(a.tiles);
   a.k_lanes = lanes_for(c->head_dim / 8);
   a.v_lanes = lanes_for(c->head_dim / 4);
   return a;
@@ -882,6 +887,7 @@ extern "C" int codistill_kv_diff_attention(const cd_kv_cache* cache, const cd_kv
   a.parts = parts_of(cache, desc);
   const int rt = row_tiles(cache, desc);
   a.tiles = (int)cdiv(a.rows, 8 * rt);
+  a.by_tiles = fast_div(a.tiles); a.by_parts = fast_div(a.parts); a.by_group = fast_div(a.group); a.by_quads = fast_div(cache->head_dim / 2);
   a.factor = (desc->scale > 0.f ? desc->scale : 1.f / sqrtf((float)cache->head_dim)) * LOG2E;
   a.part_ml = static_cast<float*>(workspace);
   a.part = a.part_ml + (size_t)a.parts * cache->sequences * cache->kv_heads * a.rows * 4;
