@@ -24,13 +24,17 @@ constexpr int RANK_EACH = 16, RANK_AHEAD = 8;   // rows of a workgroup there, lo
 constexpr int DIGIT_BITS = 10, SORT_CHUNKS = 256, SORT_LEAST = 1024, SORT_WAVES = 8;
 constexpr int SUM_WAVES = 8;                // waves of a block of rows
 constexpr int FILL_BLOCKS = 1024;
+// From here on what is read once (rows of dy) or written and not read again here (rows of y, zeros) bypasses the caches, which the table's rows are left to: 65536 rows of
+// 1024 bf16 channels on as many words (134 MB of rows, 268 MB of gradients): lookup 51 -> 30 us, sums 92 -> 73.  Rows of 8.4 MB, which the operator in front
+// has left in the caches: sums 8.8 -> 9.4.
+constexpr int64_t STREAM_BYTES = 64 << 20;
 
 struct EmbedArgs {
   const void* tokens; const void* table; const void* dy; void* y; float* dtable;
   int32_t *order, *words, *order2, *words2, *counts;   // rows and words in sorted order; the same between passes of the radix sort; counts [digits][chunks]
   float* partial;                                      // [blocks][2][width]: sums of a block's first and last words, where others have parts of them
   int64_t rows, vocabulary, width, row_stride, sums;   // sums: workgroups that add up; the others write zeros
-  int32_t token_bytes, accumulate, each, blocks, slabs, chunk, chunks, shift, digits, from_tokens;
+  int32_t token_bytes, accumulate, zero_stream, each, blocks, slabs, chunk, chunks, shift, digits, from_tokens;
   float scale;
 };
 
@@ -44,8 +48,11 @@ template <typename TOK> __device__ inline uint32_t word_of(const EmbedArgs& a, i
 __device__ inline uint32_t word_of(const EmbedArgs& a, int64_t i) { return a.token_bytes == 8 ? word_of<int64_t>(a, i) : word_of<int32_t>(a, i); }
 
 // ---- lookup ---------------------------------------------------------------------------------------------------------------
-// TT: the table's type, RT: the rows'; V: elements of a run
-template <typename TT, typename RT, int V>
+// TT: the table's type, RT: the rows'; V: elements of a run; STREAM: rows bypass the caches
+template <typename RT, int V, bool STREAM> __device__ inline void put_run(RT* p, const float (&x)[V]) {
+  if constexpr (STREAM) store_run_stream<RT, V>(p, x); else store_run<RT, V>(p, x);
+}
+template <typename TT, typename RT, int V, bool STREAM>
 __global__ void __launch_bounds__(256) embedding_kernel(EmbedArgs a, int lanes) {
   const int64_t per_wg = 256 / lanes;
   for (int64_t i = blockIdx.x * per_wg + threadIdx.x / lanes; i < a.rows; i += gridDim.x * per_wg) {
@@ -66,10 +73,10 @@ __global__ void __launch_bounds__(256) embedding_kernel(EmbedArgs a, int lanes) 
       // (runs of 8 floats are two stores)
       if constexpr (sizeof(RT) * V == 32) {
         float lo[4] = {out[0], out[1], out[2], out[3]}, hi[4] = {out[4], out[5], out[6], out[7]};
-        store_run<RT, 4>(to + c, lo);
-        store_run<RT, 4>(to + c + 4, hi);
+        put_run<RT, 4, STREAM>(to + c, lo);
+        put_run<RT, 4, STREAM>(to + c + 4, hi);
       } else {
-        store_run<RT, V>(to + c, out);
+        put_run<RT, V, STREAM>(to + c, out);
       }
     }
   }
@@ -160,16 +167,16 @@ __global__ void __launch_bounds__(512) embedding_count_kernel(EmbedArgs a) {
 }
 __global__ void __launch_bounds__(512) embedding_scatter_kernel(EmbedArgs a) {
   __shared__ int at[SORT_WAVES][1 << DIGIT_BITS];
-  __shared__ int sums[8];
+  __shared__ int sums[2][8];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, me = blockIdx.x;
   for (int d = lane; d < a.digits; d += 64) at[wave][d] = 0;
-  // a thread's two digits: rows of them in chunks in front, and in all
+  // a thread's digits (one, and one 512 behind it): rows of them in chunks in front, and in all
   int before[2] = {0, 0}, all[2] = {0, 0};
 #pragma unroll
   for (int k = 0; k < 2; k++) {
-    const int d = 2 * threadIdx.x + k;
+    const int d = threadIdx.x + 512 * k;
     if (d < a.digits) {
-#pragma unroll 8
+#pragma unroll 16
       for (int c = 0; c < a.chunks; c += 4) {   // (rows of whole vectors: what lies behind the chunks is zero)
         const int4 n = *reinterpret_cast<const int4*>(a.counts + d * a.chunks + c);
         before[k] += (c < me ? n.x : 0) + (c + 1 < me ? n.y : 0) + (c + 2 < me ? n.z : 0) + (c + 3 < me ? n.w : 0);
@@ -177,17 +184,25 @@ __global__ void __launch_bounds__(512) embedding_scatter_kernel(EmbedArgs a) {
       }
     }
   }
-  // exclusive sum of `all` over the digits
-  int sum = all[0] + all[1];
+  // rows of smaller digits
+  int base[2] = {0, 0};
 #pragma unroll
-  for (int o = 1; o < 64; o *= 2) {
-    const int up = __shfl_up(sum, o, 64);
-    if (lane >= o) sum += up;
+  for (int k = 0; k < 2; k++) {
+    int sum = all[k];
+#pragma unroll
+    for (int o = 1; o < 64; o *= 2) {
+      const int up = __shfl_up(sum, o, 64);
+      if (lane >= o) sum += up;
+    }
+    if (lane == 63) sums[k][wave] = sum;
+    base[k] = sum - all[k];
   }
-  if (lane == 63) sums[wave] = sum;
   __syncthreads();
-  int base = sum - all[0] - all[1];
-  for (int q = 0; q < wave; q++) base += sums[q];
+#pragma unroll
+  for (int q = 0; q < 8; q++) {
+    base[0] += q < wave ? sums[0][q] : 0;
+    base[1] += sums[0][q] + (q < wave ? sums[1][q] : 0);
+  }
   // each wave counts its own run of the chunk
   const int64_t from = (int64_t)me * a.chunk, to = min(from + a.chunk, a.rows);
   const int64_t run = a.chunk / SORT_WAVES, mine = min(from + wave * run, to), end = min(mine + run, to);
@@ -195,9 +210,9 @@ __global__ void __launch_bounds__(512) embedding_scatter_kernel(EmbedArgs a) {
   __syncthreads();
 #pragma unroll
   for (int k = 0; k < 2; k++) {
-    const int d = 2 * threadIdx.x + k;
+    const int d = threadIdx.x + 512 * k;
     if (d < a.digits) {
-      int place = base + (k ? all[0] : 0) + before[k];
+      int place = base[k] + before[k];
       for (int q = 0; q < SORT_WAVES; q++) {
         const int n = at[q][d];
         at[q][d] = place;
@@ -294,7 +309,9 @@ template <bool SMALL> __device__ inline void zero_absent(const EmbedArgs& a, int
     for (int i = wave; i < n; i += SUM_WAVES) {
       if (there[i]) continue;
       float* const row = a.dtable + (w0 + i) * a.width;
-      if (vector) {
+      if (vector && a.zero_stream) {
+        for (int64_t col = 4 * lane; col < a.width; col += 256) __builtin_nontemporal_store(run4_t{0, 0, 0, 0}, reinterpret_cast<run4_t*>(row + col));
+      } else if (vector) {
         for (int64_t col = 4 * lane; col < a.width; col += 256) *reinterpret_cast<uint4*>(row + col) = make_uint4(0, 0, 0, 0);
       } else {
         for (int64_t col = lane; col < a.width; col += 64) row[col] = 0.f;
@@ -307,7 +324,7 @@ template <bool SMALL> __device__ inline void zero_absent(const EmbedArgs& a, int
 // its last word's sum in LDS; the waves' ends are then put together, column by column, in their order.
 // SMALL: up to SMALL_ROWS rows.  Every workgroup puts all of them in order itself, in LDS, and takes the words that begin among its SMALL_BLOCK places, whole:
 // nothing is left to join, and the gradient is one launch.
-template <typename T, int V, bool SMALL>
+template <typename T, int V, bool SMALL, bool STREAM>
 __global__ void __launch_bounds__(64 * SUM_WAVES) embedding_sum_kernel(EmbedArgs a) {
   static_assert(SMALL_ROWS == 64 * SUM_WAVES, "a row for each thread");
   if ((int64_t)blockIdx.x >= a.sums) return zero_absent<SMALL>(a, (int)(blockIdx.x - a.sums), (int)(gridDim.x - a.sums));
@@ -393,7 +410,7 @@ __global__ void __launch_bounds__(64 * SUM_WAVES) embedding_sum_kernel(EmbedArgs
     for (int k = 0; k < AHEAD; k++) {
       const int i = min(i0 + k, real - 1);
       const int64_t from = (int64_t)(((uint64_t)__builtin_amdgcn_readlane(offset_high, i) << 32) | __builtin_amdgcn_readlane(offset_low, i));
-      load_run<T, V>(rows_here + from, t[k]);
+      if constexpr (STREAM) load_run_stream<T, V>(rows_here + from, t[k]); else load_run<T, V>(rows_here + from, t[k]);
     }
     if (a.accumulate) {
 #pragma unroll
@@ -613,11 +630,19 @@ extern "C" int codistill_embedding(const cd_embedding* desc, const void* tokens,
   const dim3 grid((unsigned)(groups < 16384 ? groups : 16384));
   hipStream_t s = static_cast<hipStream_t>(stream);
   ProfScope prof(CD_K_GLUE, s, (double)a.rows * a.width, (double)a.rows * a.width * (te + re));
-  auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, a, lanes); };
-  if (te == 2 && re == 2) { if (v == 8) run(embedding_kernel<bf16_t, bf16_t, 8>); else if (v == 4) run(embedding_kernel<bf16_t, bf16_t, 4>); else run(embedding_kernel<bf16_t, bf16_t, 1>); }
-  else if (te == 2) { if (v == 8) run(embedding_kernel<bf16_t, float, 8>); else if (v == 4) run(embedding_kernel<bf16_t, float, 4>); else run(embedding_kernel<bf16_t, float, 1>); }
-  else if (re == 2) { if (v == 4) run(embedding_kernel<float, bf16_t, 4>); else run(embedding_kernel<float, bf16_t, 1>); }
-  else { if (v == 4) run(embedding_kernel<float, float, 4>); else run(embedding_kernel<float, float, 1>); }
+  auto with = [&](auto table_type, auto row_type, auto run) {
+    typedef decltype(table_type) TT;
+    typedef decltype(row_type) RT;
+    constexpr int V = decltype(run)::value;
+    if (V > 1 && desc->rows * desc->width * re >= STREAM_BYTES) hipLaunchKernelGGL((embedding_kernel<TT, RT, V, (V > 1)>), grid, dim3(256), 0, s, a, lanes);
+    else hipLaunchKernelGGL((embedding_kernel<TT, RT, V, false>), grid, dim3(256), 0, s, a, lanes);
+  };
+  auto rows = [&](auto table_type, auto run) { if (re == 2) with(table_type, bf16_t(), run); else with(table_type, float(), run); };
+  if (te == 2 && v == 8) rows(bf16_t(), std::integral_constant<int, 8>());
+  else if (te == 2 && v == 4) rows(bf16_t(), std::integral_constant<int, 4>());
+  else if (te == 2) rows(bf16_t(), std::integral_constant<int, 1>());
+  else if (v == 4) rows(float(), std::integral_constant<int, 4>());
+  else rows(float(), std::integral_constant<int, 1>());
   return check_launch("embedding");
 }
 
@@ -654,6 +679,8 @@ extern "C" int codistill_embedding_backward(const cd_embedding* desc, const void
   EmbedArgs a = {};
   a.tokens = tokens; a.dy = dy; a.dtable = dtable; a.rows = desc->rows; a.vocabulary = desc->vocabulary; a.width = desc->width; a.row_stride = desc->row_stride;
   a.token_bytes = desc->token_bytes; a.scale = desc->scale; a.accumulate = accumulate != 0;
+  const bool past = desc->rows * desc->width * re >= STREAM_BYTES;
+  a.zero_stream = desc->vocabulary * desc->width * 4 >= STREAM_BYTES;
   a.order = reinterpret_cast<int32_t*>(ws + l.order); a.words = reinterpret_cast<int32_t*>(ws + l.words); a.partial = reinterpret_cast<float*>(ws + l.partial);
   a.each = l.each; a.blocks = l.blocks; a.slabs = l.slabs;
   const int64_t zeros = accumulate ? 0 : cdiv(desc->vocabulary, 64 * SUM_WAVES), fill = zeros < FILL_BLOCKS ? zeros : FILL_BLOCKS;
@@ -680,12 +707,15 @@ extern "C" int codistill_embedding_backward(const cd_embedding* desc, const void
   const dim3 blocks((unsigned)(a.sums + fill));
   auto sum = [&](auto kernel) { hipLaunchKernelGGL(kernel, blocks, dim3(64 * SUM_WAVES), 0, s, a); };
   if (small) {
-    if (re == 2) { if (run == 2) sum(embedding_sum_kernel<bf16_t, 2, true>); else sum(embedding_sum_kernel<bf16_t, 1, true>); }
-    else sum(embedding_sum_kernel<float, 1, true>);
+    if (re == 2) { if (run == 2) sum(embedding_sum_kernel<bf16_t, 2, true, false>); else sum(embedding_sum_kernel<bf16_t, 1, true, false>); }
+    else sum(embedding_sum_kernel<float, 1, true, false>);
   } else if (re == 2) {
-    if (run == 8) sum(embedding_sum_kernel<bf16_t, 8, false>); else if (run == 4) sum(embedding_sum_kernel<bf16_t, 4, false>); else sum(embedding_sum_kernel<bf16_t, 1, false>);
+    if (run == 8) { if (past) sum(embedding_sum_kernel<bf16_t, 8, false, true>); else sum(embedding_sum_kernel<bf16_t, 8, false, false>); }
+    else if (run == 4) sum(embedding_sum_kernel<bf16_t, 4, false, false>);
+    else sum(embedding_sum_kernel<bf16_t, 1, false, false>);
   } else {
-    if (run == 4) sum(embedding_sum_kernel<float, 4, false>); else sum(embedding_sum_kernel<float, 1, false>);
+    if (run == 4) { if (past) sum(embedding_sum_kernel<float, 4, false, true>); else sum(embedding_sum_kernel<float, 4, false, false>); }
+    else sum(embedding_sum_kernel<float, 1, false, false>);
   }
   if (l.blocks > 1 && !small) {
     const int64_t joins = l.blocks - 1;

@@ -19,6 +19,29 @@ template <typename T, int N> __device__ static inline void load_run(const T* p, 
     for (int i = 0; i < N; i++) out[i] = p[i];
   }
 }
+typedef uint32_t run4_t __attribute__((ext_vector_type(4)));
+// the same past the caches, where 16 bytes are read once
+template <typename T, int N> __device__ static inline void load_run_stream(const T* p, T (&out)[N]) {
+  if constexpr (N * sizeof(T) == 16) {
+    const run4_t u = __builtin_nontemporal_load(reinterpret_cast<const run4_t*>(p));
+    __builtin_memcpy(out, &u, 16);
+  } else {
+    load_run<T, N>(p, out);
+  }
+}
+template <typename T, int N> __device__ static inline void store_run_stream(T* p, const float (&in)[N]) {
+  if constexpr (N * sizeof(T) == 16) {
+    T t[N];
+#pragma unroll
+    for (int i = 0; i < N; i++) t[i] = Cvt<T>::st(in[i]);
+    run4_t u;
+    __builtin_memcpy(&u, t, 16);
+    __builtin_nontemporal_store(u, reinterpret_cast<run4_t*>(p));
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; i++) p[i] = Cvt<T>::st(in[i]);
+  }
+}
 template <typename T, int N> __device__ static inline void store_run(T* p, const float (&in)[N]) {
   T t[N];
 #pragma unroll
