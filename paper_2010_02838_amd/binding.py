@@ -346,6 +346,17 @@ def _stream_ptr():
     return _raw_stream(torch.cuda.current_device()) if _raw_stream else torch.cuda.current_stream().cuda_stream
 
 
+def _stream_of(*tensors):
+    """The current stream's handle, for tensors that all lie on the current device (a kernel would read another one's, or the host's, addresses)."""
+    where = tensors[0].get_device()
+    for t in tensors:
+        if t.get_device() != where:
+            raise ValueError("tensors on different devices")
+    if where < 0 or where != torch.cuda.current_device():
+        raise ValueError("tensors on %s, which is not the current GPU" % (tensors[0].device,))
+    return _raw_stream(where) if _raw_stream else torch.cuda.current_stream().cuda_stream
+
+
 def _dtype(t):
     if t.dtype is torch.bfloat16:
         return CD_BF16
@@ -562,7 +573,8 @@ def codistill_norm_rotary(desc, positions, tensors, eps=1e-5):
     """Head norm with a rotary position behind it.  desc: rotary_desc(); positions: int32 [axes, tokens]; tensors: up to four (x, gain, y) of [tokens, heads, dim]
     (y may be x), gain [dim] or None."""
     arr, n, tokens = _norm_rotary_tensors(desc, positions, tensors, False)
-    _check(lib.codistill_norm_rotary(desc, positions.data_ptr(), tokens, arr, n, eps, _stream_ptr()))
+    on = _stream_of(positions, *[x for t in tensors for x in t if x is not None])
+    _check(lib.codistill_norm_rotary(desc, positions.data_ptr(), tokens, arr, n, eps, on))
 
 
 def norm_rotary_workspace_bytes(desc, tokens, n_tensors):
@@ -574,7 +586,8 @@ def norm_rotary_workspace_bytes(desc, tokens, n_tensors):
 def codistill_norm_rotary_backward(desc, positions, tensors, workspace, eps=1e-5):
     """Gradients of codistill_norm_rotary: tensors are (x, gain, dy, dx, dgain), dx may be dy, dgain fp32 [dim] or None where there is no gain."""
     arr, n, tokens = _norm_rotary_tensors(desc, positions, tensors, True)
-    _check(lib.codistill_norm_rotary_backward(desc, positions.data_ptr(), tokens, arr, n, eps, workspace.data_ptr(), _room(workspace), _stream_ptr()))
+    on = _stream_of(positions, workspace, *[x for t in tensors for x in t if x is not None])
+    _check(lib.codistill_norm_rotary_backward(desc, positions.data_ptr(), tokens, arr, n, eps, workspace.data_ptr(), _room(workspace), on))
 
 
 def _embedding_desc(tokens, vocabulary, rows, table_dtype, scale):
@@ -594,7 +607,7 @@ def codistill_embedding(tokens, table, y, scale=1.0):
     if table.dim() != 2 or not table.is_contiguous() or table.shape[1] != y.shape[-1]:
         raise ValueError("embedding: the table is contiguous [vocabulary, width]")
     d = _embedding_desc(tokens, table.shape[0], y, _dtype(table), scale)
-    _check(lib.codistill_embedding(d, tokens.data_ptr(), table.data_ptr(), y.data_ptr(), _stream_ptr()))
+    _check(lib.codistill_embedding(d, tokens.data_ptr(), table.data_ptr(), y.data_ptr(), _stream_of(table, tokens, y)))
 
 
 def embedding_workspace_bytes(rows, vocabulary, width):
@@ -611,7 +624,8 @@ def codistill_embedding_backward(tokens, dy, dtable, workspace, scale=1.0, accum
     if dtable.dim() != 2 or not dtable.is_contiguous() or dtable.dtype is not torch.float32 or dtable.shape[1] != dy.shape[-1]:
         raise ValueError("embedding_backward: the table's gradient is contiguous fp32 [vocabulary, width]")
     d = _embedding_desc(tokens, dtable.shape[0], dy, CD_F32, scale)
-    _check(lib.codistill_embedding_backward(d, tokens.data_ptr(), dy.data_ptr(), dtable.data_ptr(), accumulate, _ptr(workspace), _room(workspace), _stream_ptr()))
+    on = _stream_of(dtable, tokens, dy) if workspace is None else _stream_of(dtable, tokens, dy, workspace)
+    _check(lib.codistill_embedding_backward(d, tokens.data_ptr(), dy.data_ptr(), dtable.data_ptr(), accumulate, _ptr(workspace), _room(workspace), on))
 
 
 def adamw_table(tensors, state_bits, grad_dtype):

@@ -19,7 +19,9 @@ namespace {
 
 constexpr uint32_t NO_WORD = 0x7fffffffu;   // sorted behind all words
 constexpr int SMALL_ROWS = 512, SMALL_BLOCK = 32;   // most rows that a workgroup puts in order for itself, places it takes of them
-constexpr int RANK_ROWS = 16384;            // most rows whose places are counted
+// Most rows whose places are counted, for each launch of two that the radix sort would take and one more.  Gradients of 64 channels, counted and sorted, us: vocabularies
+// below 1024 (one digit) 4096 rows 15.7 and 19.1, 8192 20.7 and 19.7; up to 2^20 (two) 8192 21.6 and 27.7, 10240 27.9 and 29.4, 12288 30.4 and 29.1, 16384 40 and 30.
+constexpr int RANK_ROWS = 3840;
 constexpr int RANK_EACH = 16, RANK_AHEAD = 8;   // rows of a workgroup there, loads in flight
 constexpr int DIGIT_BITS = 10, SORT_CHUNKS = 256, SORT_LEAST = 1024, SORT_WAVES = 8;
 constexpr int SUM_WAVES = 8;                // waves of a block of rows
@@ -557,6 +559,8 @@ struct EmbedLayout {
   int32_t slabs, each, blocks, chunk, chunks, passes, digit_bits;
   size_t order, words, order2, words2, counts, partial, bytes;
 };
+static int passes_of(int64_t vocabulary) { return (int)cdiv(bits_of(vocabulary), DIGIT_BITS); }
+static bool counted(int64_t rows, int64_t vocabulary) { return rows <= RANK_ROWS * (passes_of(vocabulary) + 1); }
 static EmbedLayout layout_of(int dtype, int64_t rows, int64_t vocabulary, int64_t width, int run) {
   EmbedLayout l = {};
   l.run = run;
@@ -571,14 +575,13 @@ static EmbedLayout layout_of(int dtype, int64_t rows, int64_t vocabulary, int64_
   const int64_t chunk = cdiv(rows, SORT_CHUNKS);
   l.chunk = (int32_t)(cdiv(chunk > SORT_LEAST ? chunk : SORT_LEAST, 64 * SORT_WAVES) * 64 * SORT_WAVES);
   l.chunks = (int32_t)(cdiv(cdiv(rows, l.chunk), 4) * 4);   // (the last ones may be empty)
-  const int bits = bits_of(vocabulary);
-  l.passes = (int32_t)cdiv(bits, DIGIT_BITS);
-  l.digit_bits = (int32_t)cdiv(bits, l.passes);
+  l.passes = passes_of(vocabulary);
+  l.digit_bits = (int32_t)cdiv(bits_of(vocabulary), l.passes);
   size_t at = 0;
   auto room = [&](size_t n) { const size_t was = at; at += align_up(n, 256); return was; };
   l.order = room(rows * 4);
   l.words = room(rows * 4);
-  if (rows > RANK_ROWS) {
+  if (!counted(rows, vocabulary)) {
     l.order2 = room(rows * 4);
     l.words2 = room(rows * 4);
     l.counts = room(((size_t)l.chunks << l.digit_bits) * 4);
@@ -686,7 +689,7 @@ extern "C" int codistill_embedding_backward(const cd_embedding* desc, const void
   const int64_t zeros = accumulate ? 0 : cdiv(desc->vocabulary, 64 * SUM_WAVES), fill = zeros < FILL_BLOCKS ? zeros : FILL_BLOCKS;
   hipStream_t s = static_cast<hipStream_t>(stream);
   ProfScope prof(CD_K_GLUE, s, (double)a.rows * a.width, (double)a.rows * a.width * re + 4.0 * a.vocabulary * a.width);
-  if (!small && desc->rows <= RANK_ROWS) {
+  if (!small && counted(desc->rows, desc->vocabulary)) {
     const dim3 ranks((unsigned)cdiv(desc->rows, RANK_EACH));
     if (desc->token_bytes == 8) hipLaunchKernelGGL((embedding_rank_kernel<int64_t>), ranks, dim3(256), 0, s, a);
     else hipLaunchKernelGGL((embedding_rank_kernel<int32_t>), ranks, dim3(256), 0, s, a);

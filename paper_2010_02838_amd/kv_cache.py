@@ -77,12 +77,17 @@ class KVCache:
         for name, t, m in (("first", first, self.sequences), ("counts", counts, self.sequences), ("starts", starts, self.sequences + 1)):
             setattr(r, name, self._table(name, t, m))
         r.keep = (first, counts, starts)
-        r.layout = tuple((t.shape, t.stride(), t.dtype) for t in (k, v))
+        r.layout, r.cache = tuple((t.shape, t.stride(), t.dtype) for t in (k, v)), self._sizes()
         return r
 
-    @staticmethod
-    def _laid_out(layout, tensors):
-        for t, want in zip(tensors, layout):
+    def _sizes(self):
+        """What a descriptor has in common with the caches that it may be used with."""
+        return self.sequences, self.kv_heads, self.head_dim, self.dtype, self.k.device
+
+    def _laid_out(self, desc, tensors):
+        if desc.cache != self._sizes():
+            raise ValueError("KVCache: a descriptor of a cache of other sizes")
+        for t, want in zip(tensors, desc.layout):
             if (t.shape, t.stride(), t.dtype) != want and ((t.shape, t.dtype) != (want[0], want[2]) or any(
                     n > 1 and x != y for n, x, y in zip(t.shape, t.stride(), want[1]))):
                 raise ValueError("KVCache: a tensor of shape %s, strides %s, %s where the descriptor has %s, %s, %s" % (
@@ -90,13 +95,13 @@ class KVCache:
 
     def write(self, rows, k, v):
         """Rows of new tokens into the cache."""
-        self._laid_out(rows.layout, (k, v))
-        B._check(B.lib.codistill_kv_write(self.desc, rows, k.data_ptr(), v.data_ptr(), B._stream_ptr()))
+        self._laid_out(rows, (k, v))
+        B._check(B.lib.codistill_kv_write(self.desc, rows, k.data_ptr(), v.data_ptr(), B._stream_of(self.k, k, v)))
 
     def read(self, rows, k, v):
         """What the cache holds for these rows, as values; zeros where it has no place for them."""
-        self._laid_out(rows.layout, (k, v))
-        B._check(B.lib.codistill_kv_read(self.desc, rows, k.data_ptr(), v.data_ptr(), B._stream_ptr()))
+        self._laid_out(rows, (k, v))
+        B._check(B.lib.codistill_kv_read(self.desc, rows, k.data_ptr(), v.data_ptr(), B._stream_of(self.k, k, v)))
 
     def attention(self, q, out, lam, k_lens, causal=False, scale=0.0, q_lens=None):
         """What attend() of tensors laid out like these needs to know; kept by the caller, with workspace_bytes.
@@ -119,7 +124,7 @@ class KVCache:
             raise ValueError("KVCache: k_lens says how many tokens the cache holds")
         d.k_lens, d.q_lens = self._table("k_lens", k_lens, self.sequences), self._table("q_lens", q_lens, self.sequences)
         d.keep = (k_lens, q_lens)
-        d.layout = tuple((t.shape, t.stride(), t.dtype) for t in (q, out, lam))
+        d.layout, d.cache = tuple((t.shape, t.stride(), t.dtype) for t in (q, out, lam)), self._sizes()
         b = ctypes.c_size_t()
         B._check(B.lib.codistill_kv_diff_attention_workspace_bytes(self.desc, d, ctypes.byref(b)))
         d.workspace_bytes = b.value
@@ -127,5 +132,6 @@ class KVCache:
 
     def attend(self, desc, q, lam, out, workspace=None):
         """out = (softmax(q_1 k_1) - lam softmax(q_2 k_2)) v against the first k_lens tokens of every sequence."""
-        self._laid_out(desc.layout, (q, out, lam))
-        B._check(B.lib.codistill_kv_diff_attention(self.desc, desc, q.data_ptr(), lam.data_ptr(), out.data_ptr(), B._ptr(workspace), B._room(workspace), B._stream_ptr()))
+        self._laid_out(desc, (q, out, lam))
+        on = B._stream_of(self.k, q, lam, out) if workspace is None else B._stream_of(self.k, q, lam, out, workspace)
+        B._check(B.lib.codistill_kv_diff_attention(self.desc, desc, q.data_ptr(), lam.data_ptr(), out.data_ptr(), B._ptr(workspace), B._room(workspace), on))

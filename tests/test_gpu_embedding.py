@@ -62,7 +62,7 @@ def check(tokens, dy, words, scale=1.0, accumulate=False, seed=0):
 
 @pytest.mark.parametrize("kind", ["uniform", "one", "runs", "none", "text"])
 @pytest.mark.parametrize("rows,words,width,dtype", [
-    (1, 1, 1, F32), (2, 3, 8, BF), (100, 1000, 7, BF), (511, 70000, 64, F32), (512, 300, 66, BF), (512, 20, 130, F32), (513, 300, 66, BF), (31, 5, 64, F32), (33, 40, 333, BF), (300, 64, 256, F32), (300, 1000, 513, F32), (2000, 7, 100, BF), (5000, 3000, 512, BF), (16384, 1024, 40, BF),
+    (1, 1, 1, F32), (2, 3, 8, BF), (100, 1000, 7, BF), (511, 70000, 64, F32), (512, 300, 66, BF), (512, 20, 130, F32), (513, 300, 66, BF), (31, 5, 64, F32), (33, 40, 333, BF), (300, 64, 256, F32), (300, 1000, 513, F32), (2000, 7, 100, BF), (5000, 3000, 512, BF), (7680, 1000, 40, BF), (7681, 1000, 40, BF), (11520, 1024, 24, F32), (11521, 1024, 24, F32), (15360, 2 ** 20, 8, F32), (16384, 1024, 40, BF),
     (16385, 1023, 40, F32), (16385, 1024, 40, BF), (40000, 70000, 16, F32), (70000, 2 ** 21, 8, BF), (20000, 1, 24, F32)])
 def test_gradients(rows, words, width, dtype, kind):
     gen = torch.Generator(device=DEV).manual_seed(rows)
@@ -148,3 +148,22 @@ def test_against_differences():
     d = torch.randn(40, 64, generator=gen, device=DEV)
     got, want = (value(table + d) - value(table - d)) / 2, float((g.double() * d.double()).sum())
     assert abs(got - want) <= 1e-5 * float((dy.double() * y.double()).norm())
+
+
+def test_tables_beyond_32_bits():
+    """A table of 2.3e9 elements: words, rows and zeros behind 2^31 elements."""
+    from paper_2010_02838_amd import binding as B
+    words, width = 2 ** 21 + 2 ** 17, 1024
+    table = torch.zeros(words, width, dtype=BF, device=DEV)
+    tokens = torch.tensor([words - 1, 0, words - 2, 2 ** 21, words - 1], device=DEV).repeat(200)
+    table[tokens] = torch.randn(5, width, generator=torch.Generator(device=DEV).manual_seed(1), device=DEV).bfloat16().repeat(200, 1)
+    y = torch.empty(1000, width, dtype=BF, device=DEV)
+    B.codistill_embedding(tokens, table, y)
+    assert torch.equal(y, table[tokens])
+    g = torch.full((words, width), math.nan, device=DEV)
+    gradient(tokens, y, g)
+    for w, n in ((words - 1, 400), (0, 200), (words - 2, 200), (2 ** 21, 200)):
+        assert torch.equal(g[w], y[tokens == w].double().sum(0).float()) or ((g[w] - y[tokens == w].double().sum(0)).abs() <= n * 2.0 ** -24 * y[tokens == w].double().abs().sum(0)).all()
+    g[torch.tensor([words - 1, 0, words - 2, 2 ** 21], device=DEV)] = 0
+    for part in g.split(1 << 17):
+        assert (part == 0).all()

@@ -395,3 +395,66 @@ def test_captured_with_a_cache_that_grows():
             c.attend(c.attention(q, eager, lam, at, causal=True), q, lam, eager, torch.empty_like(ws))
             assert torch.equal(eager, out) and at.tolist() == [102 + i, 1902 + i]
             other.k.zero_()
+
+
+def test_offsets_beyond_32_bits():
+    """Ten million tokens of 512 bytes: the last ones lie beyond 2^31 bytes of the keys and of the values.  All others are zeros: a score of zero each."""
+    from paper_2010_02838_amd.kv_cache import KVCache
+    page, D = 1 << 21, 128
+    c = KVCache(1, 5 * page, 1, D, F32, page, device=DEV)
+    assert c.k.numel() > 2 ** 31 and c.v.numel() > 2 ** 31
+    c.k.zero_()
+    c.v.zero_()
+    c.scales.fill_(1.0)
+    k, v = new_rows(F32, (1, 70), 1, D, spread=0.0)
+    at = torch.tensor([5 * page - 70], dtype=torch.int32, device=DEV)
+    rows = c.rows(k, v, first=at)
+    c.write(rows, k, v)
+    hk, hv = torch.empty_like(k.contiguous()), torch.empty_like(v.contiguous())
+    c.read(c.rows(hk, hv, first=at), hk, hv)
+    (ck, sk), (cv, sv) = quantised(k[0].cpu().double().numpy()), quantised(v[0].cpu().double().numpy())
+    assert np.array_equal(hk[0].cpu().double().numpy(), ck * sk[..., None]) and np.array_equal(hv[0].cpu().double().numpy(), cv * sv[..., None])
+    q = 3 * torch.randn(1, 2, 2, 2, D, generator=torch.Generator(device=DEV).manual_seed(3), device=DEV)
+    out, lam, lens = torch.empty(1, 2, 2, 2 * D, device=DEV), torch.tensor([0.5, 0.8], device=DEV), torch.tensor([5 * page], dtype=torch.int32, device=DEV)
+    attend(c, q, out, lam, lens, causal=True)
+    for i in range(2):
+        n = 70 - 1 + i          # the first query does not see the last token
+        for h in range(2):
+            want, size = 0.0, 0.0
+            for m, f in ((0, 1.0), (1, -float(lam[h]))):
+                s = D ** -0.5 * hk[0, :n, 0, m].cpu().double().numpy() @ q[0, i, h, m].cpu().double().numpy()
+                e = np.exp(s - max(s.max(), 0.0))
+                p = e / (e.sum() + (5 * page - 70) * math.exp(-max(s.max(), 0.0)))
+                want, size = want + f * p @ hv[0, :n, 0].cpu().double().numpy(), size + abs(f) * p @ np.abs(hv[0, :n, 0].cpu().double().numpy())
+            # (a sum of ten million equal weights in chains of 1300 additions a lane: 2^-24 * 1300 more than 2^-15)
+            assert (np.abs(out[0, i, h].cpu().double().numpy() - want) <= 2.0 ** -12 * size).all()
+
+
+def test_on_another_stream_beside_others():
+    """Two caches written and attended from on two streams at once: the same bits as one after the other."""
+    sets = []
+    for seed, dtype in ((1, BF), (2, F32)):
+        c, q, _, out, lam, at = problem(dtype, [900, 2000], 1, 8, 2, 64, room=2048, page=256, seed=seed)
+        k, v = new_rows(dtype, (2, 1), 2, 64, seed=seed)
+        d = c.attention(q, out, lam, at, causal=True)
+        sets.append((c, c.rows(k, v, first=at - 1), k, v, d, q, lam, out, torch.empty(d.workspace_bytes, dtype=torch.uint8, device=DEV)))
+
+    def run(c, rows, k, v, d, q, lam, out, ws):
+        for _ in range(20):
+            c.write(rows, k, v)
+            c.attend(d, q, lam, out, ws)
+
+    for s in sets:
+        run(*s)
+    torch.cuda.synchronize()
+    want = [s[7].clone() for s in sets]
+    for s in sets:
+        s[7].fill_(7.0)
+    streams = [torch.cuda.Stream() for _ in sets]
+    for st in streams:
+        st.wait_stream(torch.cuda.current_stream())
+    for s, st in zip(sets, streams):
+        with torch.cuda.stream(st):
+            run(*s)
+    torch.cuda.synchronize()
+    assert all(torch.equal(s[7], w) for s, w in zip(sets, want))

@@ -213,3 +213,29 @@ def test_cache_class():
             c.attention(*args)
     with pytest.raises(ValueError):
         c.attend(d, q, lam, out[:, :2])
+
+
+def test_tensors_on_the_host_are_refused():
+    """The kernels would read host memory by its address."""
+    d, pos, x, g = rope(), torch.zeros(1, 4, dtype=torch.int32), torch.zeros(4, 2, 64), torch.zeros(64)
+    ws, t, table = torch.zeros(1 << 20, dtype=torch.uint8), torch.zeros(4, dtype=torch.int64), torch.zeros(9, 8)
+    c = KVCache(2, 100, 2, 16, torch.float32, 64, device="cpu")
+    k, v, q, out = torch.zeros(2, 3, 2, 2, 16), torch.zeros(2, 3, 2, 32), torch.zeros(2, 3, 4, 2, 16), torch.zeros(2, 3, 4, 32)
+    rows, lam = c.rows(k, v), torch.zeros(4)
+    attn_ = c.attention(q, out, lam, torch.zeros(2, dtype=torch.int32))
+    for call in (lambda: B.codistill_norm_rotary(d, pos, [(x, g, x)]), lambda: B.codistill_norm_rotary_backward(d, pos, [(x, g, x, x, g)], ws),
+                 lambda: B.codistill_embedding(t, table, torch.zeros(4, 8)), lambda: B.codistill_embedding_backward(t, torch.zeros(4, 8), table, ws),
+                 lambda: c.write(rows, k, v), lambda: c.read(rows, k, v), lambda: c.attend(attn_, q, lam, out)):
+        with pytest.raises(ValueError, match="GPU"):
+            call()
+
+
+def test_descriptors_of_other_caches():
+    c, other = KVCache(2, 100, 2, 16, torch.float32, 64, device="cpu"), KVCache(2, 100, 1, 32, torch.float32, 64, device="cpu")
+    k, v, q, out, lam = torch.zeros(2, 3, 2, 2, 16), torch.zeros(2, 3, 2, 32), torch.zeros(2, 3, 4, 2, 16), torch.zeros(2, 3, 4, 32), torch.zeros(4)
+    with pytest.raises(ValueError, match="other sizes"):
+        other.write(c.rows(k, v), k, v)
+    with pytest.raises(ValueError, match="other sizes"):
+        other.read(c.rows(k, v), k, v)
+    with pytest.raises(ValueError, match="other sizes"):
+        other.attend(c.attention(q, out, lam, torch.zeros(2, dtype=torch.int32)), q, lam, out)
