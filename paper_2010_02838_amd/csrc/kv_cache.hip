@@ -330,9 +330,9 @@ __global__ void __launch_bounds__(256) kv_read_kernel(KvRowArgs a) {
 //
 // Memory-bound: a key and its value are read once, 4 dim + 6 bytes, for all queries of all heads that share them.
 //
-// Rows.  Row r of a sequence is query r / group of head r % group.  A 16x16x32 product has 16 columns: 8 rows, each once for either map.  A token's
-// two keys, one behind the other, are ONE key of 2 dim channels, and a column's query is zero in the other map's channels: the product is the score of
-// the column's own map, both maps share the running maximum's and the accumulators' code, and both are weights of one read of the values.
+// Rows.  Row r of a sequence is query r / group of head r % group.  A 16x16x32 product has 16 columns: 8 rows, each once for either map.  Both keys of a token are
+// multiplied with all columns and a column keeps its own map's score; from there on a map is a row like any other, with its own running maximum, and both maps
+// are weights of one read of the values.
 //
 // Tiles.  64 keys are four products, and row 4 g + i of product t is key 16 g + 4 t + i, so that lane l (g = l / 16), which holds the scores of
 // column l % 16 for those rows, has the keys 16 g .. 16 g + 15: their values of one channel are the 16 bytes that it loads, and its weights
@@ -416,7 +416,7 @@ __global__ void __launch_bounds__(64 * KV_WAVES, NK <= 2 && RT == 1 ? 2 : 1) kv_
   const int row0 = tile * 8 * RT, first_query = quotient(row0, a.by_group), last_query = min(quotient(row0 + 8 * RT - 1, a.by_group), nq - 1);
   const int least = first_query < nq ? seen_by(first_query) : 0, most = first_query < nq ? seen_by(last_query) : 0;
   int sees[RT];
-  v8bf q[RT][2][NK][TQ];
+  v8bf q[RT][NK][TQ];      // the lane's row and map
 #pragma unroll
   for (int rt = 0; rt < RT; rt++) {
     const KvRow w = row_of(row0 + 8 * rt + (col & 7));
@@ -429,14 +429,7 @@ __global__ void __launch_bounds__(64 * KV_WAVES, NK <= 2 && RT == 1 ? 2 : 1) kv_
 #pragma unroll
       for (int e = 0; e < 8; e++) x[e] = 0.f;
       if (w.real && ch < c.dim) load8<T>(from + ch, x);
-      v8bf mine[TQ];
-      split8<TQ>(x, mine);
-#pragma unroll
-      for (int n = 0; n < TQ; n++)
-#pragma unroll
-        for (int m = 0; m < 2; m++)
-#pragma unroll
-          for (int e = 0; e < 8; e++) q[rt][m][s][n][e] = map == m ? mine[n][e] : (__bf16)0.f;
+      split8<TQ>(x, q[rt][s]);
     }
   }
   const int blocks = (most + KV_TILE - 1) / KV_TILE, whole = least / KV_TILE;   // whole: blocks that all rows see to their ends
@@ -509,18 +502,24 @@ __global__ void __launch_bounds__(64 * KV_WAVES, NK <= 2 && RT == 1 ? 2 : 1) kv_
     v4f sc[RT][4];
 #pragma unroll
     for (int t = 0; t < 4; t++) {
+      v4f both[RT][2];
 #pragma unroll
-      for (int rt = 0; rt < RT; rt++) sc[rt][t] = v4f{0.f, 0.f, 0.f, 0.f};
+      for (int m = 0; m < 2; m++) {
 #pragma unroll
-      for (int m = 0; m < 2; m++)
+        for (int rt = 0; rt < RT; rt++) both[rt][m] = v4f{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int s = 0; s < NK; s++) {
           const v8bf key = codes_as_bf16(kc[t][m][s]);
 #pragma unroll
           for (int rt = 0; rt < RT; rt++)
 #pragma unroll
-            for (int n = TQ - 1; n >= 0; n--) sc[rt][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(key, q[rt][m][s][n], sc[rt][t], 0, 0, 0);
+            for (int n = TQ - 1; n >= 0; n--) both[rt][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(key, q[rt][s][n], both[rt][m], 0, 0, 0);
         }
+      }
+#pragma unroll
+      for (int rt = 0; rt < RT; rt++)
+#pragma unroll
+        for (int i = 0; i < 4; i++) sc[rt][t][i] = map ? both[rt][1][i] : both[rt][0][i];
     }
     float kf[16], vf[16];
 #pragma unroll
