@@ -578,8 +578,8 @@ int codistill_embedding_backward(const cd_embedding* desc, const void* tokens, c
  * numbers, with fp32 accumulators and softmax statistics.
  * head_dim: multiples of 8 up to 128 (CD_ERR_UNSUPPORTED otherwise).  page_tokens: a multiple of 64, up to 2^21.
  * Errors (nothing launched): CD_ERR_INVALID_ARG: NULL or misaligned pointers (16 bytes; tables and lambda 4), sizes out of range (sequences * kv_heads and all rows of
- * queries up to 2^24, a sequence's room below 2^31 - 64), pages < sequences * seq_pages without a table, heads no multiple of kv_heads, strides that are no multiple of 16 bytes or
- * shorter than a token, rows to be written (out, and those of codistill_kv_read) that share memory, starts together with counts, packed sequences without their longest one, scale < 0 or not finite;
+ * queries up to 2^24, a sequence's room below 2^31 - 64), pages < sequences * seq_pages without a table, heads no multiple of kv_heads, strides that are no multiple of 16 bytes, shorter
+ * than a token or above 2^31 elements a token or 2^38 a sequence, rows to be written (out, and those of codistill_kv_read) that share memory, starts together with counts, packed sequences without their longest one, scale < 0 or not finite;
  * CD_ERR_WORKSPACE_TOO_SMALL.
  */
 typedef struct {

@@ -346,15 +346,24 @@ def _stream_ptr():
     return _raw_stream(torch.cuda.current_device()) if _raw_stream else torch.cuda.current_stream().cuda_stream
 
 
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
+def _stream_on(where):
+    """The current stream's handle, for tensors on device number `where`, which has to be the current one (a kernel would read another one's, or the host's,
+    addresses)."""
+    if where < 0 or where != _current_device():
+        raise ValueError("tensors on %s, which is not the current GPU" % ("the host" if where < 0 else "device %d" % where))
+    return _raw_stream(where) if _raw_stream else torch.cuda.current_stream().cuda_stream
+
+
 def _stream_of(*tensors):
-    """The current stream's handle, for tensors that all lie on the current device (a kernel would read another one's, or the host's, addresses)."""
+    """The same for tensors that all lie on one device."""
     where = tensors[0].get_device()
     for t in tensors:
         if t.get_device() != where:
             raise ValueError("tensors on different devices")
-    if where < 0 or where != torch.cuda.current_device():
-        raise ValueError("tensors on %s, which is not the current GPU" % (tensors[0].device,))
-    return _raw_stream(where) if _raw_stream else torch.cuda.current_stream().cuda_stream
+    return _stream_on(where)
 
 
 def _dtype(t):
@@ -527,11 +536,11 @@ def codistill_head_norm_backward(x, gain, dy, dx, dgain, workspace, eps=1e-5, po
 _NORM_ROTARY_ARRAYS = {n: NormRotaryTensor * n for n in range(1, CD_ROPE_MAX_TENSORS + 1)}
 
 
-def _rope_rows(t, shape, dt, dim):
+def _rope_rows(t, shape, dt, dim, where):
     """A token's stride of a tensor that is turned."""
     s = t.stride()
-    if t.shape != shape or t.dtype is not dt:
-        raise ValueError("norm_rotary: tensors are [tokens, heads, dim] of the descriptor's type")
+    if t.shape != shape or t.dtype is not dt or t.get_device() != where:
+        raise ValueError("norm_rotary: tensors are [tokens, heads, dim] of the descriptor's type, on the positions' device")
     if s[2] != 1 or s[1] != dim:
         _inner(t, 2, "norm_rotary")
     return s[0]
@@ -540,7 +549,7 @@ def _rope_rows(t, shape, dt, dim):
 def _norm_rotary_tensors(desc, positions, tensors, backward):
     """The descriptors of (x, gain, y) or (x, gain, dy, dx, dgain), checked against the rotation's."""
     n, dim, dt = len(tensors), desc.dim, torch.bfloat16 if desc.dtype == CD_BF16 else torch.float32
-    axes, tokens = positions.shape
+    (axes, tokens), where = positions.shape, positions.get_device()
     if positions.dtype is not torch.int32 or axes < desc.axes or not positions.is_contiguous():
         raise ValueError("norm_rotary: positions are contiguous int32 [axes, tokens]")
     if n not in _NORM_ROTARY_ARRAYS:
@@ -552,29 +561,28 @@ def _norm_rotary_tensors(desc, positions, tensors, backward):
         if len(shape) != 3 or shape[0] != tokens or shape[2] != dim:
             raise ValueError("norm_rotary: tensors are [tokens, heads, dim] of the descriptor's type")
         if gain is not None:
-            if gain.dtype is not dt or gain.shape != (dim,) or not gain.is_contiguous():
-                raise ValueError("norm_rotary: a gain is contiguous [dim] of the descriptor's type")
+            if gain.dtype is not dt or gain.shape != (dim,) or not gain.is_contiguous() or gain.get_device() != where:
+                raise ValueError("norm_rotary: a gain is contiguous [dim] of the descriptor's type, on the positions' device")
             gain = gain.data_ptr()
-        xs = _rope_rows(x, shape, dt, dim)
+        xs = _rope_rows(x, shape, dt, dim, where)
         if backward:
             _, _, dy, dx, dgain = t
             if dgain is not None:
-                if dgain.dtype is not torch.float32 or dgain.shape != (dim,) or not dgain.is_contiguous():
-                    raise ValueError("norm_rotary: a gain's gradient is contiguous fp32 [dim]")
+                if dgain.dtype is not torch.float32 or dgain.shape != (dim,) or not dgain.is_contiguous() or dgain.get_device() != where:
+                    raise ValueError("norm_rotary: a gain's gradient is contiguous fp32 [dim], on the positions' device")
                 dgain = dgain.data_ptr()
-            rows.append((x.data_ptr(), gain, None, dy.data_ptr(), dx.data_ptr(), dgain, shape[1], xs, 0, _rope_rows(dy, shape, dt, dim), _rope_rows(dx, shape, dt, dim)))
+            rows.append((x.data_ptr(), gain, None, dy.data_ptr(), dx.data_ptr(), dgain, shape[1], xs, 0, _rope_rows(dy, shape, dt, dim, where), _rope_rows(dx, shape, dt, dim, where)))
         else:
             y = t[2]
-            rows.append((x.data_ptr(), gain, y.data_ptr(), None, None, None, shape[1], xs, _rope_rows(y, shape, dt, dim), 0, 0))
-    return _NORM_ROTARY_ARRAYS[n](*rows), n, tokens
+            rows.append((x.data_ptr(), gain, y.data_ptr(), None, None, None, shape[1], xs, _rope_rows(y, shape, dt, dim, where), 0, 0))
+    return _NORM_ROTARY_ARRAYS[n](*rows), n, tokens, where
 
 
 def codistill_norm_rotary(desc, positions, tensors, eps=1e-5):
     """Head norm with a rotary position behind it.  desc: rotary_desc(); positions: int32 [axes, tokens]; tensors: up to four (x, gain, y) of [tokens, heads, dim]
     (y may be x), gain [dim] or None."""
-    arr, n, tokens = _norm_rotary_tensors(desc, positions, tensors, False)
-    on = _stream_of(positions, *[x for t in tensors for x in t if x is not None])
-    _check(lib.codistill_norm_rotary(desc, positions.data_ptr(), tokens, arr, n, eps, on))
+    arr, n, tokens, where = _norm_rotary_tensors(desc, positions, tensors, False)
+    _check(lib.codistill_norm_rotary(desc, positions.data_ptr(), tokens, arr, n, eps, _stream_on(where)))
 
 
 def norm_rotary_workspace_bytes(desc, tokens, n_tensors):
@@ -585,9 +593,10 @@ def norm_rotary_workspace_bytes(desc, tokens, n_tensors):
 
 def codistill_norm_rotary_backward(desc, positions, tensors, workspace, eps=1e-5):
     """Gradients of codistill_norm_rotary: tensors are (x, gain, dy, dx, dgain), dx may be dy, dgain fp32 [dim] or None where there is no gain."""
-    arr, n, tokens = _norm_rotary_tensors(desc, positions, tensors, True)
-    on = _stream_of(positions, workspace, *[x for t in tensors for x in t if x is not None])
-    _check(lib.codistill_norm_rotary_backward(desc, positions.data_ptr(), tokens, arr, n, eps, workspace.data_ptr(), _room(workspace), on))
+    arr, n, tokens, where = _norm_rotary_tensors(desc, positions, tensors, True)
+    if workspace.get_device() != where:
+        raise ValueError("norm_rotary: the workspace is on another device than the positions")
+    _check(lib.codistill_norm_rotary_backward(desc, positions.data_ptr(), tokens, arr, n, eps, workspace.data_ptr(), _room(workspace), _stream_on(where)))
 
 
 def _embedding_desc(tokens, vocabulary, rows, table_dtype, scale):

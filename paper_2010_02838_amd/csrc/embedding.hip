@@ -8,9 +8,12 @@
 // added into memory by two workgroups: the same inputs give the same bits.  Words that do not occur are zeroed by workgroups beside the
 // first launch of the sort.
 //
-// The order.  Few rows: a row's place is the number of rows in front of it, counted by comparing it with all of them (64 comparisons are one
-// vector instruction and two scalar ones: 8192 rows are 2^20 of those, a few microseconds of the chip, and one launch).  Many rows: a radix sort, two
-// launches for each digit of up to 10 bits: digits of a chunk are counted, then every chunk knows where its own begin.
+// The order.  Up to 512 rows: in LDS, by every workgroup for itself.  Few rows: a row's place is the number of rows in front of it, counted by comparing it with all of
+// them in one launch (8192 rows: 12.4 us, of which the comparisons, two and a half instructions for 64 of them, are 7).  Many rows: a radix sort, two launches for each digit
+// of up to 10 bits (65536 rows 4.8 + 9.4 us a digit): digits of a chunk are counted, then every chunk knows where its own begin.
+//
+// 8192 rows of 512 bf16 channels among 32768 words, beside what the table's gradient holds: lookup 4.8 us, order 12.4, sums 8.8, parts 4.5: latency, 26 MB are 5.  65536 rows of 1024
+// among as many words, all written: lookup 29.7 (180 MB), order 28.4, sums and zeros 72.6 (402 MB, 5.5 TB/s), parts 5.4.  300 rows of 256 fp32 channels: 2.7 and 10.2.
 #include "common.h"
 #include "vec.h"
 
@@ -18,7 +21,9 @@ namespace cd {
 namespace {
 
 constexpr uint32_t NO_WORD = 0x7fffffffu;   // sorted behind all words
-constexpr int SMALL_ROWS = 512, SMALL_BLOCK = 32;   // most rows that a workgroup puts in order for itself, places it takes of them
+// Most rows that a workgroup puts in order for itself, and places it takes of them.  One launch and three, us: 64 rows of 512 bf16 channels 7.2 and 11.9, 300 10.0 and 12.4,
+// 512 of 1024 12.0 and 12.1, 500 of two words 13.1 and 12.3.
+constexpr int SMALL_ROWS = 512, SMALL_BLOCK = 32;
 // Most rows whose places are counted, for each launch of two that the radix sort would take and one more.  Gradients of 64 channels, counted and sorted, us: vocabularies
 // below 1024 (one digit) 4096 rows 15.7 and 19.1, 8192 20.7 and 19.7; up to 2^20 (two) 8192 21.6 and 27.7, 10240 27.9 and 29.4, 12288 30.4 and 29.1, 16384 40 and 30.
 constexpr int RANK_ROWS = 3840;

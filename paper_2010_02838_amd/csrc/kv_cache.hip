@@ -8,6 +8,9 @@
 // key head, whatever the page, are what a wave takes at a time, and both products read them from memory straight into the registers of the matrix
 // instructions: of the keys a lane takes a run of one token's channels, of the values 16 tokens of one channel, which is why values are
 // stored with the tokens side by side.  No copy in LDS, no exchange between lanes.
+//
+// Writing and reading move bytes: 14510 tokens of 24 packed prompts, 4 key heads of 64 in bf16 (45 MB each way), 15.0 and 12.7 us, where the copy rate is 9.4; a workgroup's
+// rows are all asked for at once, so that the chip loads, computes and stores in turns.  One token of each of 16 sequences: 4.9 and 3.6, a launch and its latencies.
 #include "common.h"
 #include "conv_rules.h"
 #include "kernels.h"
@@ -175,7 +178,7 @@ __device__ inline KvTile tile_of(const KvRowArgs& a) {
 
 // Two waves of a workgroup take the keys, two the values (as much work), 8 channels a lane.  Values go through LDS as they are quantised, token by token, and
 // leave it channel by channel, 8 tokens of 4 channels a thread; rows of 4 bytes more than the channels keep both sides off each other's banks.
-constexpr int KV_AHEAD = 4;   // tokens of a lane whose loads are in flight together
+constexpr int KV_AHEAD = 4;   // tokens of a lane whose loads are in flight together (2, 4, 8: 16.6, 15.0 and 15.2 us for the prompts below)
 constexpr int V_PAD = 4, V_WORDS = (256 + V_PAD) / 4;   // words of a token's row, widest heads
 
 template <typename T>
@@ -339,7 +342,11 @@ __global__ void __launch_bounds__(256) kv_read_kernel(KvRowArgs a) {
 // are the second product's operand as they lie.
 //
 // Roundings.  Codes are exact in bf16.  fp32 queries, and the weights times the values' scales, are sums of three bf16 numbers (all 24 bits), bf16 models'
-// weights of two (16 bits): memory bounds the kernel, and the second product costs nothing that shows.
+// weights of two (16 bits): results are then off by their own rounding alone, 1.7e-3 as a 2-norm, and the second product costs 5 to 9 %.
+//
+// 16 sequences of 2000 to 8000 tokens, one query each, 16 heads of 64 on 4 (80 MB): 21.6 us (3.7 TB/s; 17 are the copy rate), and 4.7 for the join; the same on bf16 keys and
+// values takes 41 and 6.  One of 131072 on 2 key heads (40 MB): 14.9 and 5.2.  Five of up to 4096, four queries, heads of 128: 14.4 and 4.6, of which the bytes are 2.4: a launch, the chain
+// from the lengths to the first keys, and one or two blocks a wave, one wave a SIMD.
 struct KvAttnArgs {
   KvArgs c;
   const void* q; const float* lam; void* out;
@@ -715,6 +722,7 @@ __global__ void __launch_bounds__(256) kv_join_kernel(KvAttnArgs a) {
 
 // ---- host -------------------------------------------------------------------------------------------------------------------
 static int elem_of(const cd_kv_cache* c) { return c->dtype == CD_BF16 ? 2 : 4; }
+constexpr int64_t KV_FAR = 1ll << 31;   // largest stride of a token (of a sequence: 128 times that), so that no offset passes 63 bits
 static int padded_dim(int dim) { return (dim + 31) / 32 * 32; }
 
 static int check_cache(const char* what, const cd_kv_cache* c, bool pointers) {
@@ -755,6 +763,7 @@ static int check_rows(const char* what, const cd_kv_cache* c, const cd_kv_rows* 
   CD_REQUIRE(((reinterpret_cast<uintptr_t>(r->first) | reinterpret_cast<uintptr_t>(r->counts) | reinterpret_cast<uintptr_t>(r->starts)) & 3) == 0, "%s: misaligned table", what);
   if (r->max_new == 0) return CD_OK;
   CD_REQUIRE((k && v) || (r->starts && r->rows == 0), "%s: NULL pointer argument", what);
+  CD_REQUIRE(r->k_token <= KV_FAR && r->v_token <= KV_FAR && r->k_batch <= 128 * KV_FAR && r->v_batch <= 128 * KV_FAR, "%s: strides out of range", what);
   const int vec = 16 / elem_of(c);
   const int64_t least = (int64_t)c->kv_heads * 2 * c->head_dim;
   CD_REQUIRE(aligned16(k) && aligned16(v), "%s: pointers must be 16-byte aligned", what);
@@ -790,6 +799,7 @@ static int check_attention(const char* what, const cd_kv_cache* c, const cd_kv_a
   CD_REQUIRE(d->tq >= 0 && d->heads >= 1 && d->heads <= 65536 && d->heads % c->kv_heads == 0, "%s: tq=%d, heads=%d for %d key heads", what, d->tq, d->heads, c->kv_heads);
   CD_REQUIRE(d->lambda_kind == CD_LAMBDA_HEAD || d->lambda_kind == CD_LAMBDA_TOKEN, "%s: unknown lambda kind %d", what, d->lambda_kind);
   CD_REQUIRE(d->scale >= 0.f && d->scale < __builtin_inff(), "%s: scale must be finite and not negative", what);
+  CD_REQUIRE(d->q_token <= KV_FAR && d->o_token <= KV_FAR && d->q_batch <= 128 * KV_FAR && d->o_batch <= 128 * KV_FAR, "%s: strides out of range", what);
   const int vec = 16 / elem_of(c);
   const int64_t least = (int64_t)d->heads * 2 * c->head_dim;
   CD_REQUIRE(d->tq <= 1 || (d->q_token >= least && d->o_token >= least && d->q_token % vec == 0 && d->o_token % vec == 0),
@@ -803,9 +813,17 @@ static int check_attention(const char* what, const cd_kv_cache* c, const cd_kv_a
   return CD_OK;
 }
 static int rows_of(const cd_kv_cache* c, const cd_kv_attn* d) { return d->tq * (d->heads / c->kv_heads); }
-// Two tiles of rows share what is read, where there are registers for their sums (fp32 queries take three times a tile's registers).
-static int row_tiles(const cd_kv_cache* c, const cd_kv_attn* d) { return rows_of(c, d) > 8 && c->dtype == CD_BF16 && c->head_dim <= 64 ? 2 : 1; }
-// Workgroups of a sequence and key head: enough to fill the chip, each with at least a block for every wave.
+// Two tiles of rows share what is read, where there are registers for their sums (fp32 queries take three times a tile's registers) and enough blocks to read
+// (of at most so many tokens: the lengths are on the device).  Two tiles and one, us: 16 queries of a key head on 16 x 4 caches of 8192 tokens, heads of 64, 39.9 and
+// 46.7; on 2 caches of 131072 34.0 and 45.2; but on 16 of 8192 16.7 and 16.4, on 4 of 600 12.3 and 9.6.
+constexpr int KV_SHARED_BLOCKS = 3072;
+static int row_tiles(const cd_kv_cache* c, const cd_kv_attn* d) {
+  const int64_t blocks = (int64_t)c->sequences * c->kv_heads * ((int64_t)c->seq_pages * c->page_tokens / KV_TILE);
+  return rows_of(c, d) > 8 && c->dtype == CD_BF16 && c->head_dim <= 64 && blocks >= KV_SHARED_BLOCKS ? 2 : 1;
+}
+// Workgroups of a sequence and key head: as many as run at once (two a compute unit, wide heads and double tiles one), each with at least a block for every wave.
+// Half as many, as many and twice as many, with the join, us: 16 x 4 caches of up to 8192 tokens, heads of 64, 28.9, 26.4 and 27.9; 2 of 131072 18.3, 19.8 and 24.4; 10 of up to
+// 4096, heads of 128, 22.4, 20.1 and 23.0.
 static int parts_of(const cd_kv_cache* c, const cd_kv_attn* d) {
   const int64_t groups = (int64_t)c->sequences * c->kv_heads * cdiv(rows_of(c, d), 8 * row_tiles(c, d));
   const int64_t blocks = (int64_t)c->seq_pages * c->page_tokens / KV_TILE, most = blocks / KV_WAVES < KV_MOST_PARTS ? blocks / KV_WAVES : KV_MOST_PARTS;

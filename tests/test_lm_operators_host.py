@@ -152,7 +152,7 @@ def test_cache_sizes():
 @pytest.mark.parametrize("call", ["codistill_kv_write", "codistill_kv_read"])
 def test_cache_rows(call):
     f = lambda r, k=5 * M, v=6 * M, c=None: getattr(B.lib, call)(c if c is not None else cache(), r, k, v, None)   # noqa: E731
-    for kw in (dict(max_new=-1), dict(k_token=255), dict(k_token=260), dict(v_token=8), dict(v_batch=-8), dict(k_batch=257), dict(first=4 * M + 2), dict(counts=4 * M + 1),
+    for kw in (dict(max_new=-1), dict(k_token=255), dict(k_token=260), dict(v_token=8), dict(v_batch=-8), dict(k_batch=257), dict(k_token=(1 << 31) + 8), dict(v_token=1 << 62), dict(k_batch=1 << 39), dict(first=4 * M + 2), dict(counts=4 * M + 1),
                dict(starts=4 * M + 2, rows=9), dict(starts=4 * M, rows=-1), dict(starts=4 * M, rows=9, counts=4 * M), dict(starts=4 * M, rows=9, max_new=0)):
         assert f(rows(**kw)) == BAD, kw
     assert f(rows(), k=None) == BAD and f(rows(), v=None) == BAD and f(rows(), k=5 * M + 8) == BAD and f(None) == BAD
@@ -164,7 +164,7 @@ def test_cache_rows(call):
 
 def test_cache_attention():
     for kw in (dict(tq=-1), dict(heads=3), dict(heads=0), dict(heads=1 << 17), dict(lambda_kind=2), dict(scale=-1.0), dict(scale=float("nan")), dict(scale=float("inf")),
-               dict(q_token=511), dict(q_token=516), dict(o_token=8), dict(o_batch=512), dict(q_batch=-8), dict(q_batch=1537), dict(o_batch=0), dict(q_lens=M + 2), dict(k_lens=M + 1),
+               dict(q_token=511), dict(q_token=516), dict(o_token=8), dict(o_batch=512), dict(q_batch=-8), dict(q_batch=1537), dict(o_batch=0), dict(q_token=1 << 62), dict(o_token=1 << 32), dict(o_batch=1 << 62), dict(q_batch=1 << 39), dict(q_lens=M + 2), dict(k_lens=M + 1),
                dict(k_lens=None), dict(tq=1 << 23, o_batch=1 << 40)):
         assert attend(d=attn(**kw)) == BAD and B.lib.codistill_last_error(), kw
     for kw in (dict(q=None), dict(lam=None), dict(out=None), dict(q=M + 8), dict(out=M + 8), dict(lam=M + 2), dict(ws=M + 8)):
