@@ -216,13 +216,14 @@ def held(c, b, n):
     """Values of the first n tokens of a sequence, float64, and which of them have a page."""
     K, D = c.kv_heads, c.head_dim
     k, v, there = np.zeros((n, K, 2, D)), np.zeros((n, K, 2 * D)), np.zeros(n, dtype=bool)
-    ck, cv, cs = c.k.cpu().double().numpy(), c.v.cpu().double().numpy(), c.scales.cpu().double().numpy()
-    for j in range(n):
-        p = place(c, b, j)
+    P = c.desc.page_tokens
+    for j in range(0, n, P):
+        p, m = place(c, b, j), min(P, n - j)
         if p is not None:
-            k[j] = ck[p[0], :, p[1], :, :D] * cs[p[0], :, :2, p[1], None]
-            v[j] = cv[p[0], :, :, p[1]] * cs[p[0], :, 2, p[1], None]
-            there[j] = True
+            ck, cv, cs = (t[p[0]].cpu().double().numpy() for t in (c.k, c.v, c.scales))
+            k[j:j + m] = (ck[..., :D] * cs[:, :2].transpose(0, 2, 1)[..., None]).swapaxes(0, 1)[:m]
+            v[j:j + m] = (cv * cs[:, 2:]).transpose(2, 0, 1)[:m]
+            there[j:j + m] = True
     return k, v, there
 
 
@@ -296,6 +297,20 @@ def test_attention_in_parts(dtype, lens, heads, kv_heads, dim, tq, page):
     first = out.clone()
     attend(c, q, out, lam, at, causal=True)
     assert torch.equal(first, out)
+
+
+@pytest.mark.parametrize("heads,kv_heads,dim,tq", [(16, 2, 64, 2), (9, 1, 32, 1), (12, 4, 8, 7), (8, 1, 40, 5), (32, 2, 24, 1)])
+@pytest.mark.parametrize("many", [False, True])
+def test_two_tiles_of_rows(heads, kv_heads, dim, tq, many):
+    """Nine rows and more of bf16 heads up to 64 on caches with room for 3072 blocks: a few sequences in parts, and many without."""
+    lens = [tq, 700, 65] if not many else [(37 * i) % 400 for i in range(3072 // (12 * kv_heads))]
+    room = 64 * (-(-3072 // (len(lens) * kv_heads)))
+    c, q, wide, out, lam, at = problem(BF, lens, tq, heads, kv_heads, dim, room=room, page=64 if many else 1024, lam_token=many)
+    qn = torch.tensor([tq if i % 3 else tq - 1 for i in range(len(lens))], dtype=torch.int32, device=DEV)
+    d = attend(c, q, out, lam, at, causal=True, q_lens=qn)
+    assert (d.workspace_bytes > 0) != many
+    check_attention(c, q, lam, at, out, True, q_lens=qn)
+    assert (wide[..., :8] == 7).all() and (wide[..., -8:] == 7).all()
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
