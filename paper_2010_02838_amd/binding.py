@@ -536,46 +536,45 @@ def codistill_head_norm_backward(x, gain, dy, dx, dgain, workspace, eps=1e-5, po
 _NORM_ROTARY_ARRAYS = {n: NormRotaryTensor * n for n in range(1, CD_ROPE_MAX_TENSORS + 1)}
 
 
-def _rope_rows(t, shape, dt, dim, where):
-    """A token's stride of a tensor that is turned."""
-    s = t.stride()
-    if t.shape != shape or t.dtype is not dt or t.get_device() != where:
-        raise ValueError("norm_rotary: tensors are [tokens, heads, dim] of the descriptor's type, on the positions' device")
-    if s[2] != 1 or s[1] != dim:
-        _inner(t, 2, "norm_rotary")
-    return s[0]
-
-
 def _norm_rotary_tensors(desc, positions, tensors, backward):
-    """The descriptors of (x, gain, y) or (x, gain, dy, dx, dgain), checked against the rotation's."""
+    """The descriptors of (x, gain, y) or (x, gain, dy, dx, dgain), checked against the rotation's.  (Written out: the checks are most of a small call's time.)"""
     n, dim, dt = len(tensors), desc.dim, torch.bfloat16 if desc.dtype == CD_BF16 else torch.float32
-    (axes, tokens), where = positions.shape, positions.get_device()
+    (axes, tokens), where, one = positions.shape, positions.get_device(), (dim,)
     if positions.dtype is not torch.int32 or axes < desc.axes or not positions.is_contiguous():
         raise ValueError("norm_rotary: positions are contiguous int32 [axes, tokens]")
     if n not in _NORM_ROTARY_ARRAYS:
         raise ValueError("norm_rotary: %d tensors, up to %d in a call" % (n, CD_ROPE_MAX_TENSORS))
-    rows = []
-    for t in tensors:
-        x, gain = t[0], t[1]
-        shape = x.shape
-        if len(shape) != 3 or shape[0] != tokens or shape[2] != dim:
-            raise ValueError("norm_rotary: tensors are [tokens, heads, dim] of the descriptor's type")
-        if gain is not None:
-            if gain.dtype is not dt or gain.shape != (dim,) or not gain.is_contiguous() or gain.get_device() != where:
-                raise ValueError("norm_rotary: a gain is contiguous [dim] of the descriptor's type, on the positions' device")
-            gain = gain.data_ptr()
-        xs = _rope_rows(x, shape, dt, dim, where)
+    arr = _NORM_ROTARY_ARRAYS[n]()
+    for a, t in zip(arr, tensors):
         if backward:
-            _, _, dy, dx, dgain = t
-            if dgain is not None:
-                if dgain.dtype is not torch.float32 or dgain.shape != (dim,) or not dgain.is_contiguous() or dgain.get_device() != where:
-                    raise ValueError("norm_rotary: a gain's gradient is contiguous fp32 [dim], on the positions' device")
-                dgain = dgain.data_ptr()
-            rows.append((x.data_ptr(), gain, None, dy.data_ptr(), dx.data_ptr(), dgain, shape[1], xs, 0, _rope_rows(dy, shape, dt, dim, where), _rope_rows(dx, shape, dt, dim, where)))
+            x, gain, dy, out, dgain = t
         else:
-            y = t[2]
-            rows.append((x.data_ptr(), gain, y.data_ptr(), None, None, None, shape[1], xs, _rope_rows(y, shape, dt, dim, where), 0, 0))
-    return _NORM_ROTARY_ARRAYS[n](*rows), n, tokens, where
+            x, gain, out = t
+        shape, xs, os = x.shape, x.stride(), out.stride()
+        if (len(shape) != 3 or shape[0] != tokens or shape[2] != dim or out.shape != shape or x.dtype is not dt or out.dtype is not dt or x.get_device() != where
+                or out.get_device() != where):
+            raise ValueError("norm_rotary: tensors are [tokens, heads, dim] of the descriptor's type, on the positions' device")
+        if xs[2] != 1 or os[2] != 1 or xs[1] != dim or os[1] != dim:
+            _inner(x, 2, "norm_rotary"), _inner(out, 2, "norm_rotary")
+        a.x, a.heads, a.x_token = x.data_ptr(), shape[1], xs[0]
+        if gain is not None:
+            if gain.dtype is not dt or gain.shape != one or not gain.is_contiguous() or gain.get_device() != where:
+                raise ValueError("norm_rotary: a gain is contiguous [dim] of the descriptor's type, on the positions' device")
+            a.gain = gain.data_ptr()
+        if not backward:
+            a.y, a.y_token = out.data_ptr(), os[0]
+            continue
+        ds = dy.stride()
+        if dy.shape != shape or dy.dtype is not dt or dy.get_device() != where:
+            raise ValueError("norm_rotary: tensors are [tokens, heads, dim] of the descriptor's type, on the positions' device")
+        if ds[2] != 1 or ds[1] != dim:
+            _inner(dy, 2, "norm_rotary")
+        a.dy, a.dx, a.dy_token, a.dx_token = dy.data_ptr(), out.data_ptr(), ds[0], os[0]
+        if dgain is not None:
+            if dgain.dtype is not torch.float32 or dgain.shape != one or not dgain.is_contiguous() or dgain.get_device() != where:
+                raise ValueError("norm_rotary: a gain's gradient is contiguous fp32 [dim], on the positions' device")
+            a.dgain = dgain.data_ptr()
+    return arr, n, tokens, where
 
 
 def codistill_norm_rotary(desc, positions, tensors, eps=1e-5):
