@@ -12,6 +12,8 @@
 // 8192 tokens of 16 + 16 heads of 64 in bf16 (33.6 MB a tensor): forward 16.5 us (4.1 TB/s), backward 23.3 (4.3), the sum over its workgroups 3.9; norms and rotation apart
 // take 30.9 and 43.2.  16 tokens of 32 + 8 heads: 4.8, a launch and its latencies.
 #include "common.h"
+#include "conv_rules.h"
+#include "kernels.h"
 #include "rotary.h"
 #include "vec.h"
 
@@ -36,11 +38,15 @@ struct NormRopeArgs {
   int64_t tokens;
   const int32_t* pos;
   float* partial;                            // backward: [workgroups][dim]
+  FastDiv by_heads[CD_ROPE_MAX_TENSORS];
   float eps;
   uint64_t freq[CD_ROPE_MAX_PAIRS];          // turns a position, as a fraction of 2^64
   uint8_t axis[CD_ROPE_MAX_PAIRS];
 };
 static_assert(sizeof(NormRopeArgs) <= 4096, "kernel arguments");
+
+// n / d for n below 2^31
+__device__ inline int quotient(int n, FastDiv d) { return (int)div_by((unsigned)n, d); }
 
 struct Angles { float c[NR_TOKENS * CD_ROPE_MAX_PAIRS], s[NR_TOKENS * CD_ROPE_MAX_PAIRS]; };
 
@@ -112,49 +118,72 @@ template <typename T, int V> __device__ inline void load_gain(const void* gain, 
   }
 }
 
+// A workgroup works on one tensor (blockIdx.y), whose gains its lanes hold in registers.
 // NV: runs a lane holds of each half (single channels of wide heads: two)
 template <typename T, int V, bool PAIRS, int NV>
 __global__ void __launch_bounds__(256) norm_rotary_kernel(NormRopeArgs a) {
   __shared__ Angles angles;
   const int64_t t0 = (int64_t)blockIdx.x * a.block_tokens;
   const int nt = (int)min((int64_t)a.block_tokens, a.tokens - t0);
-  fill_angles<T>(a, angles, t0, nt);
-  __syncthreads();
-  const int sub = threadIdx.x % a.lanes, per_wg = 256 / a.lanes, half = a.dim >> 1, every = a.heads_end[a.n_tensors - 1];
-  for (int i = threadIdx.x / a.lanes; i < nt * every; i += per_wg) {
-    const int t = i / every;
-    int h = i - t * every, n = 0;
-    while (h >= a.heads_end[n]) n++;
-    if (n) h -= a.heads_end[n - 1];
-    const T* x = static_cast<const T*>(a.t[n].x) + (t0 + t) * a.t[n].x_token + (int64_t)h * a.dim;
-    T* y = static_cast<T*>(a.t[n].out) + (t0 + t) * a.t[n].out_token + (int64_t)h * a.dim;
-    float u[NV][V], w[NV][V], sq = 0.f;
+  const int sub = threadIdx.x % a.lanes, per_wg = 256 / a.lanes, half = a.dim >> 1, n = blockIdx.y;
+  const int heads = a.heads_end[n] - (n ? a.heads_end[n - 1] : 0), all = nt * heads;
+  const NormRopeTensor me = a.t[n];
+  T x[NV][2][V];
+  int t = 0, h = 0;
+  // a head is on its way while the one before it is turned, the first one while the angles are computed
+  auto fetch = [&](int i) {
+    t = quotient(i, a.by_heads[n]);
+    h = i - t * heads;
+    const T* from = static_cast<const T*>(me.x) + (t0 + t) * me.x_token + (int64_t)h * a.dim;
 #pragma unroll
     for (int k = 0; k < NV; k++) {
       const Place<V, PAIRS> at(sub, k, a.lanes, half);
-#pragma unroll
-      for (int e = 0; e < V; e++) u[k][e] = w[k][e] = 0.f;
       if (at.live) {
-        load_floats<T, V>(x + at.first, u[k]);
-        load_floats<T, V>(x + at.second, w[k]);
+        load_run<T, V>(from + at.first, x[k][0]);
+        load_run<T, V>(from + at.second, x[k][1]);
       }
-#pragma unroll
-      for (int e = 0; e < V; e++) sq += u[k][e] * u[k][e] + w[k][e] * w[k][e];
     }
+  };
+  int i = threadIdx.x / a.lanes;
+  if (i < all) fetch(i);
+  float gu[NV][V], gw[NV][V];
+#pragma unroll
+  for (int k = 0; k < NV; k++) {
+    const Place<V, PAIRS> at(sub, k, a.lanes, half);
+    if (at.live) {
+      load_gain<T, V>(me.gain, at.first, gu[k]);
+      load_gain<T, V>(me.gain, at.second, gw[k]);
+    }
+  }
+  fill_angles<T>(a, angles, t0, nt);
+  __syncthreads();
+  while (i < all) {
+    float u[NV][V], w[NV][V], sq = 0.f;
+#pragma unroll
+    for (int k = 0; k < NV; k++) {
+      const bool live = Place<V, PAIRS>(sub, k, a.lanes, half).live;
+#pragma unroll
+      for (int e = 0; e < V; e++) {
+        u[k][e] = live ? Cvt<T>::ld(x[k][0][e]) : 0.f;
+        w[k][e] = live ? Cvt<T>::ld(x[k][1][e]) : 0.f;
+        sq += u[k][e] * u[k][e] + w[k][e] * w[k][e];
+      }
+    }
+    T* const y = static_cast<T*>(me.out) + (t0 + t) * me.out_token + (int64_t)h * a.dim;
+    const float *c = angles.c + t * CD_ROPE_MAX_PAIRS, *s = angles.s + t * CD_ROPE_MAX_PAIRS;
+    i += per_wg;
+    if (i < all) fetch(i);
     const float r = 1.f / sqrtf(lanes_sum(sq, a.lanes) / a.dim + a.eps);
 #pragma unroll
     for (int k = 0; k < NV; k++) {
       const Place<V, PAIRS> at(sub, k, a.lanes, half);
       if (!at.live) continue;
-      float gu[V], gw[V];
-      load_gain<T, V>(a.t[n].gain, at.first, gu);
-      load_gain<T, V>(a.t[n].gain, at.second, gw);
 #pragma unroll
       for (int e = 0; e < V; e++) {
-        u[k][e] *= r * gu[e];
-        w[k][e] *= r * gw[e];
+        u[k][e] *= r * gu[k][e];
+        w[k][e] *= r * gw[k][e];
       }
-      turn<V, PAIRS>(u[k], w[k], angles.c + t * CD_ROPE_MAX_PAIRS, angles.s + t * CD_ROPE_MAX_PAIRS, at, a.n_pairs, 1.f);
+      turn<V, PAIRS>(u[k], w[k], c, s, at, a.n_pairs, 1.f);
       store_run<T, V>(y + at.first, u[k]);
       store_run<T, V>(y + at.second, w[k]);
     }
@@ -360,10 +389,11 @@ extern "C" int codistill_norm_rotary(const cd_rotary* rope, const int32_t* posit
   if (tokens == 0) return CD_OK;
   // enough workgroups for two rounds of the chip before a workgroup takes several tokens
   a.block_tokens = (int32_t)(tokens >= 512 * NR_TOKENS ? NR_TOKENS : tokens <= 512 ? 1 : tokens / 512);
+  for (int64_t i = 0; i < n_tensors; i++) a.by_heads[i] = fast_div((unsigned)tensors[i].heads);
   const double n = (double)tokens * a.heads_end[n_tensors - 1] * a.dim, elem = rope->dtype == CD_BF16 ? 2 : 4;
   hipStream_t s = static_cast<hipStream_t>(stream);
   ProfScope prof(CD_K_NORM, s, 8 * n, 2 * elem * n);
-  const dim3 grid((unsigned)cdiv(tokens, a.block_tokens));
+  const dim3 grid((unsigned)cdiv(tokens, a.block_tokens), (unsigned)n_tensors);
   dispatch(rope, bytes, [&](auto type, auto v, auto pairs, auto nv) {
     hipLaunchKernelGGL((norm_rotary_kernel<decltype(type), decltype(v)::value, decltype(pairs)::value, decltype(nv)::value>), grid, dim3(256), 0, s, a);
   });
