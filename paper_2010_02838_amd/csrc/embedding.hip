@@ -9,11 +9,12 @@
 // first launch of the sort.
 //
 // The order.  Up to 512 rows: in LDS, by every workgroup for itself.  Few rows: a row's place is the number of rows in front of it, counted by comparing it with all of
-// them in one launch (8192 rows: 12.4 us, of which the comparisons, two and a half instructions for 64 of them, are 7).  Many rows: a radix sort, two launches for each digit
+// them in one launch (8192 rows: 11.7 us, of which the comparisons, two and a half instructions for 64 of them, are 7).  Many rows: a radix sort, two launches for each digit
 // of up to 10 bits (65536 rows 4.8 + 9.4 us a digit): digits of a chunk are counted, then every chunk knows where its own begin.
 //
-// 8192 rows of 512 bf16 channels among 32768 words, beside what the table's gradient holds: lookup 4.8 us, order 12.4, sums 8.8, parts 4.5: latency, 26 MB are 5.  65536 rows of 1024
-// among as many words, all written: lookup 29.7 (180 MB), order 28.4, sums and zeros 72.6 (402 MB, 5.5 TB/s), parts 5.4.  300 rows of 256 fp32 channels: 2.7 and 10.2.
+// 8192 rows of 512 bf16 channels among 32768 words, beside what the table's gradient holds: lookup 5.6 us, order 11.7, sums 9.9, parts 4.5: latency, 26 MB are 5.  65536 rows of 1024
+// among as many words, all written: lookup 45 (169 MB, 3.7 TB/s; 30 where the caches still hold much of the table), order 28.5, sums and zeros 73 (402 MB, 5.5 TB/s), parts 5.4.
+// 300 rows of 256 fp32 channels: 2.6 and 9.9.
 #include "common.h"
 #include "vec.h"
 
@@ -32,7 +33,7 @@ constexpr int DIGIT_BITS = 10, SORT_CHUNKS = 256, SORT_LEAST = 1024, SORT_WAVES 
 constexpr int SUM_WAVES = 8;                // waves of a block of rows
 constexpr int FILL_BLOCKS = 1024;
 // From here on what is read once (rows of dy) or written and not read again here (rows of y, zeros) bypasses the caches, which the table's rows are left to: 65536 rows of
-// 1024 bf16 channels on as many words (134 MB of rows, 268 MB of gradients): lookup 51 -> 30 us, sums 92 -> 73.  Rows of 8.4 MB, which the operator in front
+// 1024 bf16 channels on as many words (134 MB of rows, 268 MB of gradients): lookup 51 -> 30 us where the table is looked up again and again, 50 -> 45 where it comes from memory, sums 93 -> 73.  Rows of 8.4 MB, which the operator in front
 // has left in the caches: sums 8.8 -> 9.4.
 constexpr int64_t STREAM_BYTES = 64 << 20;
 

@@ -9,7 +9,7 @@
 // instructions: of the keys a lane takes a run of one token's channels, of the values 16 tokens of one channel, which is why values are
 // stored with the tokens side by side.  No copy in LDS, no exchange between lanes.
 //
-// Writing and reading move bytes: 14510 tokens of 24 packed prompts, 4 key heads of 64 in bf16 (45 MB each way), 15.0 and 12.7 us, where the copy rate is 9.4; a workgroup's
+// Writing and reading move bytes: 14510 tokens of 24 packed prompts, 4 key heads of 64 in bf16 (45 MB each way), 16.0 and 13.5 us (prompts that the caches hold 15.0 and 12.7), where the copy rate is 9.4; a workgroup's
 // rows are all asked for at once, so that the chip loads, computes and stores in turns.  One token of each of 16 sequences: 4.9 and 3.6, a launch and its latencies.
 #include "common.h"
 #include "conv_rules.h"
@@ -344,8 +344,8 @@ __global__ void __launch_bounds__(256) kv_read_kernel(KvRowArgs a) {
 // Roundings.  Codes are exact in bf16.  fp32 queries, and the weights times the values' scales, are sums of three bf16 numbers (all 24 bits), bf16 models'
 // weights of two (16 bits): results are then off by their own rounding alone, 1.7e-3 as a 2-norm, and the second product costs 5 to 9 %.
 //
-// 16 sequences of 2000 to 8000 tokens, one query each, 16 heads of 64 on 4 (80 MB): 21.6 us (3.7 TB/s; 17 are the copy rate), and 4.7 for the join; the same on bf16 keys and
-// values takes 41 and 6.  One of 131072 on 2 key heads (40 MB): 14.9 and 5.2.  Five of up to 4096, four queries, heads of 128: 14.4 and 4.6, of which the bytes are 2.4: a launch, the chain
+// 16 sequences of 2000 to 8000 tokens, one query each, 16 heads of 64 on 4 (80 MB): 22.2 us (3.6 TB/s; 17 are the copy rate), and 4.6 for the join; the same on bf16 keys and
+// values takes 41 and 6.  One of 124000 on 2 key heads (47 MB): 15.0 and 5.2.  Five of up to 4096, four queries, heads of 128: 14.6 and 4.6, of which the bytes are 2.4: a launch, the chain
 // from the lengths to the first keys, and one or two blocks a wave, one wave a SIMD.
 struct KvAttnArgs {
   KvArgs c;

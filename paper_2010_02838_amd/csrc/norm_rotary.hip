@@ -9,8 +9,11 @@
 // workgroup computes the cosines and sines of its tokens once, into LDS, for all heads.  dg is summed in registers (a lane meets the same
 // channels in every head that it walks), over the workgroup's lanes, and over the workgroups by a second launch, always in the same order.
 //
-// 8192 tokens of 16 + 16 heads of 64 in bf16 (33.6 MB a tensor): forward 16.5 us (4.1 TB/s), backward 23.3 (4.3), the sum over its workgroups 3.9; norms and rotation apart
-// take 30.9 and 43.2.  16 tokens of 32 + 8 heads: 4.8, a launch and its latencies.
+// A workgroup works on one tensor, so that its lanes hold their channels' gains in registers: read again for every head they are as many loads as the heads
+// themselves (21.0 us where 17.2 are taken now), from LDS 19.5.
+//
+// 8192 tokens of 16 + 16 heads of 64 in bf16 (33.6 MB a tensor), tensors that come from memory: forward 17.2 us (3.9 TB/s), backward 25.4 (4.0), the sum over its
+// workgroups 4.0; tensors that the caches hold 15 and 23.  Norms and rotation apart take 30.9 and 43.2.  16 tokens of 32 + 8 heads: 4.6, a launch and its latencies.
 #include "common.h"
 #include "conv_rules.h"
 #include "kernels.h"
@@ -118,7 +121,7 @@ template <typename T, int V> __device__ inline void load_gain(const void* gain, 
   }
 }
 
-// A workgroup works on one tensor (blockIdx.y), whose gains its lanes hold in registers.
+// blockIdx.y: the tensor
 // NV: runs a lane holds of each half (single channels of wide heads: two)
 template <typename T, int V, bool PAIRS, int NV>
 __global__ void __launch_bounds__(256) norm_rotary_kernel(NormRopeArgs a) {
