@@ -534,7 +534,7 @@ int codistill_norm_rotary_backward(const cd_rotary* rope, const int32_t* positio
  * rows == 0 is allowed (tokens, y and dy may then be NULL).
  * Errors (nothing launched): CD_ERR_INVALID_ARG: NULL pointers, pointers not aligned to their elements (workspace: 16 bytes), rows outside 0 .. 2^30, vocabulary
  * outside 1 .. 2^31 - 2, width outside 1 .. 65536, a row longer than its stride, a scale that is not finite, token_bytes other than 4 and 8;
- * CD_ERR_UNSUPPORTED: rows * width above 2^40; CD_ERR_WORKSPACE_TOO_SMALL.
+ * CD_ERR_UNSUPPORTED: rows times the width in units of 64, rounded up, at 2^32 or above; CD_ERR_WORKSPACE_TOO_SMALL.
  */
 typedef struct {
   int32_t table_dtype, row_dtype;    /* CD_F32 or CD_BF16 */
@@ -577,8 +577,8 @@ int codistill_embedding_backward(const cd_embedding* desc, const void* tokens, c
  * Products are exact in the codes; queries in fp32 and all weights go through the bf16 matrix instructions as sums of two (CD_BF16: weights) or three bf16
  * numbers, with fp32 accumulators and softmax statistics.
  * head_dim: multiples of 8 up to 128 (CD_ERR_UNSUPPORTED otherwise).  page_tokens: a multiple of 64, up to 2^21.
- * Errors (nothing launched): CD_ERR_INVALID_ARG: NULL or misaligned pointers (16 bytes; tables and lambda 4), sizes out of range (sequences * kv_heads and all rows of
- * queries up to 2^24, a sequence's room below 2^31 - 64), pages < sequences * seq_pages without a table, heads no multiple of kv_heads, strides that are no multiple of 16 bytes, shorter
+ * Errors (nothing launched): CD_ERR_INVALID_ARG: NULL or misaligned pointers (16 bytes; tables and lambda 4), sizes out of range (sequences * kv_heads up to 2^24, tq * heads * sequences
+ * below it, sequences * kv_heads * (max_new / 64 + 2) below 2^31, a sequence's room below 2^31 - 64), pages < sequences * seq_pages without a table, heads no multiple of kv_heads, strides that are no multiple of 16 bytes, shorter
  * than a token or above 2^31 elements a token or 2^38 a sequence, rows to be written (out, and those of codistill_kv_read) that share memory, starts together with counts, packed sequences without their longest one, scale < 0 or not finite;
  * CD_ERR_WORKSPACE_TOO_SMALL.
  */

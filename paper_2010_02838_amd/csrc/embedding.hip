@@ -607,7 +607,7 @@ static int check(const char* what, const cd_embedding* d) {
   CD_REQUIRE(d->row_stride >= d->width || d->rows <= 1, "%s: a row is longer than its stride", what);
   CD_REQUIRE(d->row_stride <= (1ll << 32), "%s: row_stride=%lld out of range", what, (long long)d->row_stride);
   CD_REQUIRE(d->scale - d->scale == 0.f, "%s: scale must be finite", what);
-  if (d->rows * d->width > (1ll << 40)) return set_error(CD_ERR_UNSUPPORTED, "%s: %lld rows of %lld", what, (long long)d->rows, (long long)d->width);
+  if (d->rows * cdiv(d->width, 64) >= (1ll << 32)) return set_error(CD_ERR_UNSUPPORTED, "%s: %lld rows of %lld", what, (long long)d->rows, (long long)d->width);
   return CD_OK;
 }
 static bool whole(const void* p, int64_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }

@@ -139,6 +139,7 @@ struct KvRowArgs {
   const int32_t* first; const int32_t* counts; const int32_t* starts;
   int64_t rows, k_token, k_batch, v_token, v_batch;
   int32_t max_new, tiles, k_lanes, v_lanes;   // lanes of a key, of a value (powers of two)
+  uint32_t all;                               // tiles of all sequences and key heads, below 2^31
   FastDiv by_tiles;
 };
 
@@ -152,7 +153,12 @@ struct KvTile {
 };
 __device__ inline KvTile tile_of(const KvRowArgs& a) {
   KvTile t;
-  const int unit = quotient(blockIdx.x, a.by_tiles), n_tile = blockIdx.x - unit * a.tiles;
+  const uint32_t id = blockIdx.y * gridDim.x + blockIdx.x;   // (a launch holds fewer than 2^32 threads along x)
+  if (id >= a.all) {
+    t.lo = t.hi = 0;
+    return t;
+  }
+  const int unit = quotient((int)id, a.by_tiles), n_tile = (int)id - unit * a.tiles;
   t.b = quotient(unit, a.c.by_heads);
   t.h = unit - t.b * a.c.kv_heads;
   const int64_t first = a.first ? a.first[t.b] : 0;
@@ -780,6 +786,10 @@ static int check_rows(const char* what, const cd_kv_cache* c, const cd_kv_rows* 
   CD_REQUIRE((int64_t)c->sequences * c->kv_heads * ((r->max_new + 126ll) / KV_TILE) <= INT32_MAX, "%s: too many tiles", what);
   return CD_OK;
 }
+static dim3 row_grid(const KvRowArgs& a) {
+  const unsigned across = a.all < (1u << 22) ? a.all : 1u << 22;
+  return dim3(across, (unsigned)cdiv((int64_t)a.all, (int64_t)across));
+}
 static KvRowArgs row_args(const cd_kv_cache* c, const cd_kv_rows* r) {
   KvRowArgs a = {};
   a.c = cache_args(c);
@@ -787,6 +797,7 @@ static KvRowArgs row_args(const cd_kv_cache* c, const cd_kv_rows* r) {
   a.k_token = r->k_token; a.k_batch = r->k_batch; a.v_token = r->v_token; a.v_batch = r->v_batch;
   a.max_new = r->max_new;
   a.tiles = (int32_t)((r->max_new + 126ll) / KV_TILE);   // (the first token may be the last of its tile)
+  a.all = (uint32_t)((int64_t)a.tiles * c->sequences * c->kv_heads);
   a.by_tiles = fast_div(a.tiles);
   a.k_lanes = lanes_for(c->head_dim / 8);
   a.v_lanes = lanes_for(c->head_dim / 4);
@@ -808,7 +819,7 @@ static int check_attention(const char* what, const cd_kv_cache* c, const cd_kv_a
   CD_REQUIRE(c->sequences == 1 || d->tq == 0 ||
                  (d->o_batch >= least && (d->o_batch >= (int64_t)(d->tq - 1) * d->o_token + least || d->tq == 1 || d->o_token >= (int64_t)(c->sequences - 1) * d->o_batch + least)),
              "%s: sequences of out share memory", what);
-  CD_REQUIRE((int64_t)d->tq * (d->heads / c->kv_heads) * c->sequences * c->kv_heads <= (1 << 24), "%s: %d queries of %d heads in %d sequences", what, d->tq, d->heads, c->sequences);
+  CD_REQUIRE((int64_t)d->tq * (d->heads / c->kv_heads) * c->sequences * c->kv_heads < (1 << 24), "%s: %d queries of %d heads in %d sequences", what, d->tq, d->heads, c->sequences);
   CD_REQUIRE((reinterpret_cast<uintptr_t>(d->q_lens) & 3) == 0 && (reinterpret_cast<uintptr_t>(d->k_lens) & 3) == 0, "%s: misaligned table", what);
   return CD_OK;
 }
@@ -855,7 +866,7 @@ extern "C" int codistill_kv_write(const cd_kv_cache* cache, const cd_kv_rows* ro
   const double n = (rows->starts ? (double)rows->rows : (double)cache->sequences * rows->max_new) * cache->kv_heads * 4 * cache->head_dim;
   hipStream_t s = static_cast<hipStream_t>(stream);
   ProfScope prof(CD_K_GLUE, s, 6 * n, n * (elem_of(cache) + 1));
-  const dim3 grid((unsigned)(a.tiles * cache->sequences * cache->kv_heads));
+  const dim3 grid = row_grid(a);
   if (cache->dtype == CD_BF16) hipLaunchKernelGGL((kv_write_kernel<bf16_t>), grid, dim3(256), 0, s, a);
   else hipLaunchKernelGGL((kv_write_kernel<float>), grid, dim3(256), 0, s, a);
   return check_launch("kv_write");
@@ -869,7 +880,7 @@ extern "C" int codistill_kv_read(const cd_kv_cache* cache, const cd_kv_rows* row
   const double n = (rows->starts ? (double)rows->rows : (double)cache->sequences * rows->max_new) * cache->kv_heads * 4 * cache->head_dim;
   hipStream_t s = static_cast<hipStream_t>(stream);
   ProfScope prof(CD_K_GLUE, s, n, n * (elem_of(cache) + 1));
-  const dim3 grid((unsigned)(a.tiles * cache->sequences * cache->kv_heads));
+  const dim3 grid = row_grid(a);
   if (cache->dtype == CD_BF16) hipLaunchKernelGGL((kv_read_kernel<bf16_t>), grid, dim3(256), 0, s, a);
   else hipLaunchKernelGGL((kv_read_kernel<float>), grid, dim3(256), 0, s, a);
   return check_launch("kv_read");

@@ -121,12 +121,13 @@ template <typename T, int V> __device__ inline void load_gain(const void* gain, 
   }
 }
 
-// blockIdx.y: the tensor
+// blockIdx.y: the tensor; x and z: tokens (a launch holds fewer than 2^32 threads along x)
 // NV: runs a lane holds of each half (single channels of wide heads: two)
 template <typename T, int V, bool PAIRS, int NV>
 __global__ void __launch_bounds__(256) norm_rotary_kernel(NormRopeArgs a) {
   __shared__ Angles angles;
-  const int64_t t0 = (int64_t)blockIdx.x * a.block_tokens;
+  const int64_t t0 = ((int64_t)blockIdx.z * gridDim.x + blockIdx.x) * a.block_tokens;
+  if (t0 >= a.tokens) return;
   const int nt = (int)min((int64_t)a.block_tokens, a.tokens - t0);
   const int sub = threadIdx.x % a.lanes, per_wg = 256 / a.lanes, half = a.dim >> 1, n = blockIdx.y;
   const int heads = a.heads_end[n] - (n ? a.heads_end[n - 1] : 0), all = nt * heads;
@@ -396,7 +397,8 @@ extern "C" int codistill_norm_rotary(const cd_rotary* rope, const int32_t* posit
   const double n = (double)tokens * a.heads_end[n_tensors - 1] * a.dim, elem = rope->dtype == CD_BF16 ? 2 : 4;
   hipStream_t s = static_cast<hipStream_t>(stream);
   ProfScope prof(CD_K_NORM, s, 8 * n, 2 * elem * n);
-  const dim3 grid((unsigned)cdiv(tokens, a.block_tokens), (unsigned)n_tensors);
+  const int64_t blocks = cdiv(tokens, a.block_tokens), across = blocks < (1 << 22) ? blocks : 1 << 22;
+  const dim3 grid((unsigned)across, (unsigned)n_tensors, (unsigned)cdiv(blocks, across));
   dispatch(rope, bytes, [&](auto type, auto v, auto pairs, auto nv) {
     hipLaunchKernelGGL((norm_rotary_kernel<decltype(type), decltype(v)::value, decltype(pairs)::value, decltype(nv)::value>), grid, dim3(256), 0, s, a);
   });

@@ -473,3 +473,21 @@ def test_on_another_stream_beside_others():
             run(*s)
     torch.cuda.synchronize()
     assert all(torch.equal(s[7], w) for s, w in zip(sets, want))
+
+
+def test_more_tiles_than_a_launch_has_workgroups_across():
+    """4096 packed sequences of up to two tokens whose longest one may be 33000: 17 million tiles, nearly all without a row."""
+    S, H, D = 4096, 8, 8
+    counts = torch.arange(S, device=DEV) % 3
+    starts = torch.cat([counts.new_zeros(1), counts.cumsum(0)]).int()
+    k, v = new_rows(BF, (int(starts[-1]),), H, D)
+    caches = [make(BF, S, 64, H, D) for _ in range(2)]
+    back = []
+    for c, longest in zip(caches, (2, 33000)):
+        rows = c.rows(k, v, starts=starts, max_new=longest)
+        c.write(rows, k, v)
+        hk, hv = torch.full_like(k, 7.0), torch.full_like(v, 7.0)
+        c.read(c.rows(hk, hv, starts=starts, max_new=longest), hk, hv)
+        back += [(hk, hv)]
+    assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip((caches[0].k, caches[0].v, caches[0].scales), (caches[1].k, caches[1].v, caches[1].scales)))
+    assert torch.equal(back[0][0], back[1][0]) and torch.equal(back[0][1], back[1][1])

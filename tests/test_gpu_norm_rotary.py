@@ -199,3 +199,18 @@ def test_it_is_the_norm_and_the_rotation():
     size = pair_size(n.cpu().double(), True, 32)
     B.codistill_rotary(p.desc, p.pos, [(n, n)])
     assert ((n.cpu().double() - p.y[0].cpu().double()).abs() <= 4e-6 * size).all()
+
+
+def test_more_tokens_than_a_launch_has_workgroups_across():
+    """Heads of two channels, 33 million tokens that repeat themselves: the bits of the first ones."""
+    from paper_2010_02838_amd import binding as B
+    tokens, period = (1 << 25) + 5, 1009
+    desc = B.rotary_desc(2, (1,), 1e4, BF)
+    gen = torch.Generator(device=DEV).manual_seed(0)
+    x, g = torch.randn(period, 1, 2, generator=gen, device=DEV).to(BF), torch.ones(2, dtype=BF, device=DEV)
+    pos = torch.randint(0, 1000, (1, period), generator=gen, device=DEV, dtype=torch.int32)
+    at = torch.arange(tokens, device=DEV) % period
+    few, many, y = torch.empty_like(x), x[at], torch.full((tokens, 1, 2), 7.0, dtype=BF, device=DEV)
+    B.codistill_norm_rotary(desc, pos, [(x, g, few)], EPS)
+    B.codistill_norm_rotary(desc, pos[:, at].contiguous(), [(many, g, y)], EPS)
+    assert torch.equal(y, few[at])

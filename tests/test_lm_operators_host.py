@@ -239,3 +239,16 @@ def test_descriptors_of_other_caches():
         other.read(c.rows(k, v), k, v)
     with pytest.raises(ValueError, match="other sizes"):
         other.attend(c.attention(q, out, lam, torch.zeros(2, dtype=torch.int32)), q, lam, out)
+
+
+def test_sizes_beyond_a_launch():
+    """Grids of 2^32 threads and more are errors in the checks, not of the launch."""
+    many = cache(sequences=1 << 12, kv_heads=1 << 12, seq_pages=1, pages=1 << 12)
+    assert attend(many, attn(tq=1, heads=1 << 12, q_token=1 << 19, o_token=1 << 19, q_batch=1 << 19, o_batch=1 << 19)) == BAD
+    for call in (B.lib.codistill_kv_write, B.lib.codistill_kv_read):
+        assert call(many, rows(starts=4 * M, rows=9, max_new=8192, k_token=1 << 19, v_token=1 << 19), 5 * M, 6 * M, None) == BAD
+        assert b"too many tiles" in B.lib.codistill_last_error()
+    for kw in (dict(rows=1 << 30, width=256, row_stride=256), dict(rows=1 << 23, width=32768, row_stride=32768), dict(rows=1 << 29, width=449, row_stride=449)):
+        n = ctypes.c_size_t()
+        assert B.lib.codistill_embedding_workspace_bytes(emb(**kw), ctypes.byref(n)) == UNSUPPORTED
+        assert B.lib.codistill_embedding(emb(**kw), M, 2 * M, 3 * M, None) == UNSUPPORTED
