@@ -79,9 +79,9 @@ class DiffLM:
         return to_q, to_k, v, fused
 
     def _embed(self, tokens):
-        """The residual stream's beginning, fp32."""
+        """The residual stream's beginning, fp32: zero where a token is no word."""
         x = torch.empty(tokens.numel(), self.d, device=self.dev)
-        B.codistill_embedding(tokens.contiguous(), self.p["embed"], x)
+        B.codistill_embedding(tokens.to(self.dev).contiguous(), self.p["embed"], x)
         return x
 
     def forward(self, tokens, positions, starts, longest):
@@ -137,7 +137,7 @@ class DiffLM:
             self.g["qkv%d" % i].copy_(fused.t() @ y)
             dx = dx + self._norm_backward(x, "norm%d" % i, fused @ self.p["qkv%d" % i])
         ws = torch.empty(B.embedding_workspace_bytes(tokens.numel(), self.V, self.d), dtype=torch.uint8, device=self.dev)
-        B.codistill_embedding_backward(tokens.contiguous(), dx, self.g["embed"], ws, accumulate=True)   # (beside the projection's gradient)
+        B.codistill_embedding_backward(tokens.to(self.dev).contiguous(), dx, self.g["embed"], ws, accumulate=True)   # (beside the projection's gradient)
 
     def update(self, lr):
         self.updates += 1
