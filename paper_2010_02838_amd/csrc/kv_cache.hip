@@ -9,7 +9,7 @@
 // instructions: of the keys a lane takes a run of one token's channels, of the values 16 tokens of one channel, which is why values are
 // stored with the tokens side by side.  No copy in LDS, no exchange between lanes.
 //
-// Writing and reading move bytes: 14510 tokens of 24 packed prompts, 4 key heads of 64 in bf16 (45 MB each way), 16.0 and 13.5 us (prompts that the caches hold 15.0 and 12.7), where the copy rate is 9.4; a workgroup's
+// Writing and reading move bytes: 14510 tokens of 24 packed prompts, 4 key heads of 64 in bf16 (45 MB each way), 16.0 and 13.1 us (prompts that the caches hold 15.0 and 12.7; without the arithmetic of the codes 2 less), where the copy rate is 9.4; a workgroup's
 // rows are all asked for at once, so that the chip loads, computes and stores in turns.  One token of each of 16 sequences: 4.9 and 3.6, a launch and its latencies.
 #include "common.h"
 #include "conv_rules.h"
@@ -827,7 +827,7 @@ static int rows_of(const cd_kv_cache* c, const cd_kv_attn* d) { return d->tq * (
 // Two tiles of rows share what is read, where there are registers for their sums (fp32 queries take three times a tile's registers) and enough blocks to read
 // (of at most so many tokens: the lengths are on the device).  Two tiles and one, us: 16 queries of a key head on 16 x 4 caches of 8192 tokens, heads of 64, 39.9 and
 // 46.7; on 2 caches of 131072 34.0 and 45.2; but on 16 of 8192 16.7 and 16.4, on 4 of 600 12.3 and 9.6.
-constexpr int KV_SHARED_BLOCKS = 3072;
+constexpr int KV_SHARED_BLOCKS = 2560;
 static int row_tiles(const cd_kv_cache* c, const cd_kv_attn* d) {
   const int64_t blocks = (int64_t)c->sequences * c->kv_heads * ((int64_t)c->seq_pages * c->page_tokens / KV_TILE);
   return rows_of(c, d) > 8 && c->dtype == CD_BF16 && c->head_dim <= 64 && blocks >= KV_SHARED_BLOCKS ? 2 : 1;

@@ -302,9 +302,9 @@ def test_attention_in_parts(dtype, lens, heads, kv_heads, dim, tq, page):
 @pytest.mark.parametrize("heads,kv_heads,dim,tq", [(16, 2, 64, 2), (9, 1, 32, 1), (12, 4, 8, 7), (8, 1, 40, 5), (32, 2, 24, 1)])
 @pytest.mark.parametrize("many", [False, True])
 def test_two_tiles_of_rows(heads, kv_heads, dim, tq, many):
-    """Nine rows and more of bf16 heads up to 64 on caches with room for 3072 blocks: a few sequences in parts, and many without."""
-    lens = [tq, 700, 65] if not many else [(37 * i) % 400 for i in range(3072 // (12 * kv_heads))]
-    room = 64 * (-(-3072 // (len(lens) * kv_heads)))
+    """Nine rows and more of bf16 heads up to 64 on caches with room for 2560 blocks: a few sequences in parts, and many without."""
+    lens = [tq, 700, 65] if not many else [(37 * i) % 400 for i in range(2560 // (10 * kv_heads))]
+    room = 64 * (-(-2560 // (len(lens) * kv_heads)))
     c, q, wide, out, lam, at = problem(BF, lens, tq, heads, kv_heads, dim, room=room, page=64 if many else 1024, lam_token=many)
     qn = torch.tensor([tq if i % 3 else tq - 1 for i in range(len(lens))], dtype=torch.int32, device=DEV)
     d = attend(c, q, out, lam, at, causal=True, q_lens=qn)
