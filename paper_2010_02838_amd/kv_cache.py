@@ -12,7 +12,7 @@ class KVCache:
 
     room: tokens of a sequence, rounded up to whole pages of page_tokens (a multiple of 64).  Without a table every sequence has pages of its own; table: int32 [sequences,
     pages of a sequence] on the device, into a pool of `pages` pages, which the caller fills and changes as sequences come and go (an entry outside the pool is no
-    page).  buffers: (k, v, scales) of an earlier cache of the same sizes; new ones are not cleared, since only what was written is seen."""
+    page).  buffers: (k, v, scales) of an earlier cache of the same sizes, on one device with the table; new ones are not cleared, since only what was written is seen."""
 
     def __init__(self, sequences, room, kv_heads, head_dim, dtype, page_tokens=256, table=None, pages=None, buffers=None, device="cuda:0"):
         if dtype not in (torch.bfloat16, torch.float32):
@@ -39,6 +39,8 @@ class KVCache:
         for b, s, t in zip(buffers, shapes, kinds):
             if b.dtype is not t or tuple(b.shape) != s or not b.is_contiguous():
                 raise ValueError("KVCache: buffers are contiguous %s" % (shapes,))
+            if b.device != buffers[0].device:
+                raise ValueError("KVCache: buffers on different devices, %s and %s" % (buffers[0].device, b.device))
         self.k, self.v, self.scales = buffers
         if table is not None and table.device != self.k.device:
             raise ValueError("KVCache: the table is on another device than the cache")

@@ -252,3 +252,17 @@ def test_sizes_beyond_a_launch():
         n = ctypes.c_size_t()
         assert B.lib.codistill_embedding_workspace_bytes(emb(**kw), ctypes.byref(n)) == UNSUPPORTED
         assert B.lib.codistill_embedding(emb(**kw), M, 2 * M, 3 * M, None) == UNSUPPORTED
+
+
+def test_buffers_of_a_cache_on_different_devices():
+    """Only the keys' device is looked at in a call: the others would be handed to the kernels as addresses of another device's memory, or of the host's."""
+    c = KVCache(2, 100, 2, 16, torch.float32, 64, device="cpu")
+    for i in range(3):
+        buffers = [c.k, c.v, c.scales]
+        buffers[i] = buffers[i].to("meta")
+        with pytest.raises(ValueError, match="device"):
+            KVCache(2, 100, 2, 16, torch.float32, 64, buffers=buffers)
+    table = torch.zeros(2, 2, dtype=torch.int32)
+    with pytest.raises(ValueError, match="device"):
+        KVCache(2, 100, 2, 16, torch.float32, 64, table=table.to("meta"), buffers=(c.k, c.v, c.scales))
+    assert KVCache(2, 100, 2, 16, torch.float32, 64, table=table, buffers=(c.k, c.v, c.scales)).pages == 4
