@@ -501,12 +501,13 @@ int codistill_adamw_unpack(const cd_adamw_plan* plan, const void* device_table, 
  *              heads dim elements apart, tokens x_token / y_token apart; y may be x.  gain: device [dim] in rope->dtype, shared by the tensor's heads, or NULL (1)
  *   rope, positions   as for codistill_rotary
  * Backward: dx, and dgain (fp32 [dim], the sum over all tokens and heads in a fixed order: the same inputs give the same bits).  x is read again and its
- * statistics are taken again: nothing is kept.  dx may be dy.  dgain is NULL exactly where gain is; y is not looked at (nor are dy, dx and
+ * statistics are taken again: nothing is kept.  dx may be dy.  dgain is NULL exactly where gain is, and every tensor has its own (a gain that several tensors share has
+ * the sum of theirs as its gradient); y is not looked at (nor are dy, dx and
  * dgain in the forward pass).
  *   workspace  codistill_norm_rotary_workspace_bytes
  * tokens == 0 is allowed (dgain is then zero; x, y, dy, dx and positions may be NULL).  Any even dim up to 2 * CD_ROPE_MAX_PAIRS; heads whose halves, pointers and
  * strides are multiples of 16 or 8 bytes move in vectors, others element by element.
- * Errors (nothing launched): CD_ERR_INVALID_ARG as for codistill_rotary, and eps negative or not finite; CD_ERR_WORKSPACE_TOO_SMALL.
+ * Errors (nothing launched): CD_ERR_INVALID_ARG as for codistill_rotary, and eps negative or not finite, dgains that share memory; CD_ERR_WORKSPACE_TOO_SMALL.
  */
 typedef struct {
   const void *x, *gain;

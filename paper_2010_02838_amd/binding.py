@@ -591,7 +591,8 @@ def norm_rotary_workspace_bytes(desc, tokens, n_tensors):
 
 
 def codistill_norm_rotary_backward(desc, positions, tensors, workspace, eps=1e-5):
-    """Gradients of codistill_norm_rotary: tensors are (x, gain, dy, dx, dgain), dx may be dy, dgain fp32 [dim] or None where there is no gain."""
+    """Gradients of codistill_norm_rotary: tensors are (x, gain, dy, dx, dgain), dx may be dy, dgain fp32 [dim], each tensor's own (a gain
+    that tensors share has their sum as its gradient), or None where there is no gain."""
     arr, n, tokens, where = _norm_rotary_tensors(desc, positions, tensors, True)
     if workspace.get_device() != where:
         raise ValueError("norm_rotary: the workspace is on another device than the positions")

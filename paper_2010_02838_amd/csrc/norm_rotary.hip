@@ -352,6 +352,11 @@ static int fill(const char* what, NormRopeArgs& a, const cd_rotary* rope, const 
     CD_REQUIRE((t.x_token >= least && out_token >= least && dy_token >= least) || tokens <= 1, "%s: a token of tensor %lld is longer than its stride", what, (long long)i);
     CD_REQUIRE(whole(t.x, elem) && whole(out, elem) && whole(t.gain, elem) && (!backward || (whole(t.dy, elem) && whole(t.dgain, 4))),
                "%s: misaligned pointer in tensor %lld", what, (long long)i);
+    // a gain may be several tensors', the sums of its gradient are one tensor's each
+    for (int64_t j = 0; backward && t.dgain && j < i; j++) {
+      const uintptr_t here = reinterpret_cast<uintptr_t>(t.dgain), other = reinterpret_cast<uintptr_t>(tensors[j].dgain), bytes = (uintptr_t)rope->dim * 4;
+      CD_REQUIRE(!other || (here < other ? other - here : here - other) >= bytes, "%s: the gains' gradients of tensors %lld and %lld share memory", what, (long long)j, (long long)i);
+    }
     // (the stride of a single token is not gone by)
     runs.add(t.x, tokens > 1 ? t.x_token : 0, elem);
     runs.add(out, tokens > 1 ? out_token : 0, elem);

@@ -266,3 +266,16 @@ def test_buffers_of_a_cache_on_different_devices():
     with pytest.raises(ValueError, match="device"):
         KVCache(2, 100, 2, 16, torch.float32, 64, table=table.to("meta"), buffers=(c.k, c.v, c.scales))
     assert KVCache(2, 100, 2, 16, torch.float32, 64, table=table, buffers=(c.k, c.v, c.scales)).pages == 4
+
+
+def test_gradients_of_gains_that_share_memory():
+    """A gain may be shared by queries and keys, its gradient's sums may not: each tensor writes its own, and one would be lost."""
+    two = lambda *at: (B.NormRotaryTensor * 2)(*[B.NormRotaryTensor(x=M, gain=2 * M, dy=4 * M, dx=5 * M, dgain=a, heads=2, x_token=128, dy_token=128, dx_token=128) for a in at])   # noqa: E731
+    for tokens in (4, 0):
+        for at in ((6 * M, 6 * M), (6 * M, 6 * M + 63 * 4), (6 * M + 63 * 4, 6 * M), (6 * M, 6 * M + 4)):
+            assert backward(tensors=two(*at), n=2, tokens=tokens) == BAD and b"share" in B.lib.codistill_last_error(), at
+    # (64 channels apart is far enough, and without gains nothing is written: stopped by the checks behind this one)
+    for at in ((6 * M, 6 * M + 64 * 4), (6 * M + 64 * 4, 6 * M)):
+        assert backward(tensors=two(*at), n=2, room=0) == SMALL
+    none = (B.NormRotaryTensor * 2)(*[B.NormRotaryTensor(x=M, dy=4 * M, dx=5 * M, heads=2, x_token=128, dy_token=128, dx_token=128) for _ in range(2)])
+    assert backward(tensors=none, n=2, room=0) == SMALL
