@@ -530,7 +530,7 @@ int codistill_norm_rotary_backward(const cd_rotary* rope, const int32_t* positio
  *   table    device [vocabulary][width] in table_dtype, contiguous;  y, dy  device [rows][width] in row_dtype, row_stride elements apart
  *   dtable   device fp32 [vocabulary][width], contiguous.  accumulate 0: written whole, zeros for words that do not occur; otherwise the sums are added to
  *            it, and rows of words that do not occur are not touched
- * The rows of a word are added up in fp32 in an order that depends on the tokens alone: the same inputs give the same bits.
+ * The rows of a word are added up in fp32 in an order that depends on the tokens, the sizes and row_dtype alone: the same inputs give the same bits, wherever they lie.
  *   workspace  codistill_embedding_workspace_bytes (the same for every content of tokens; may be 0: then NULL is fine)
  * rows == 0 is allowed (tokens, y and dy may then be NULL).
  * Errors (nothing launched): CD_ERR_INVALID_ARG: NULL pointers, pointers not aligned to their elements (workspace: 16 bytes), rows outside 0 .. 2^30, vocabulary

@@ -575,8 +575,11 @@ static EmbedLayout layout_of(int dtype, int64_t rows, int64_t vocabulary, int64_
     l.blocks = (int32_t)cdiv(rows, SMALL_BLOCK);
     return l;
   }
+  // Rows of a wave follow from the sizes and the type alone, not from the runs that this call's pointers allow: the order of a word's sum, and so its bits, are the same
+  // wherever the tensors lie.
+  const int64_t widest = cdiv(width, 64 * run_of(dtype, width));
   l.each = 4;
-  while (l.each < 64 && rows * l.slabs > (int64_t)l.each * SUM_WAVES * 1024) l.each *= 2;
+  while (l.each < 64 && rows * widest > (int64_t)l.each * SUM_WAVES * 1024) l.each *= 2;
   l.blocks = (int32_t)cdiv(rows, (int64_t)SUM_WAVES * l.each);
   const int64_t chunk = cdiv(rows, SORT_CHUNKS);
   l.chunk = (int32_t)(cdiv(chunk > SORT_LEAST ? chunk : SORT_LEAST, 64 * SORT_WAVES) * 64 * SORT_WAVES);
@@ -658,13 +661,7 @@ extern "C" int codistill_embedding(const cd_embedding* desc, const void* tokens,
 extern "C" int codistill_embedding_workspace_bytes(const cd_embedding* desc, size_t* bytes) {
   if (const int rc = check("embedding_workspace_bytes", desc)) return rc;
   CD_REQUIRE(bytes != nullptr, "embedding_workspace_bytes: output pointer is NULL");
-  // (which runs a call takes depends on its pointers: room for any of them)
-  size_t most = 0;
-  for (int run : {8, 4, 1}) {
-    const EmbedLayout l = layout_of(desc->row_dtype, desc->rows, desc->vocabulary, desc->width, run);
-    most = l.bytes > most ? l.bytes : most;
-  }
-  *bytes = most;
+  *bytes = layout_of(desc->row_dtype, desc->rows, desc->vocabulary, desc->width, 1).bytes;   // (the same for all runs)
   return CD_OK;
 }
 

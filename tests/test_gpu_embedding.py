@@ -167,3 +167,23 @@ def test_tables_beyond_32_bits():
     g[torch.tensor([words - 1, 0, words - 2, 2 ** 21], device=DEV)] = 0
     for part in g.split(1 << 17):
         assert (part == 0).all()
+
+
+@pytest.mark.parametrize("rows,words,width,dtype", [(300, 40, 66, BF), (8192, 300, 1024, BF), (6000, 500, 516, BF), (5000, 9, 1024, F32), (20000, 300, 520, BF)])
+def test_the_same_bits_wherever_tensors_lie(rows, words, width, dtype):
+    """Rows or a gradient that begin inside a vector, or rows whose stride is none, are added up element by element, in the same order: that follows from the tokens, the width and
+    the type."""
+    gen = torch.Generator(device=DEV).manual_seed(rows)
+    dy, tokens = torch.randn(rows, width, generator=gen, device=DEV).to(dtype), tokens_of("text", rows, words)
+    want = torch.empty(words, width, device=DEV)
+    gradient(tokens, dy, want, 0.7)
+    flat, flat_g = torch.zeros(rows * width + 8, dtype=dtype, device=DEV), torch.empty(words * width + 8, device=DEV)
+    apart = torch.zeros(rows, width + 1, dtype=dtype, device=DEV)[:, :width]
+    apart.copy_(dy)
+    for off, off_g in ((1, 0), (0, 1), (3, 2), (4, 4)):
+        moved, got = flat[off:off + rows * width].view(rows, width), flat_g[off_g:off_g + words * width].view(words, width)
+        moved.copy_(dy)
+        gradient(tokens, moved, got, 0.7)
+        assert torch.equal(got, want), (off, off_g)
+    gradient(tokens, apart, flat_g[:words * width].view(words, width), 0.7)
+    assert torch.equal(flat_g[:words * width].view(words, width), want)
