@@ -526,7 +526,8 @@ int codistill_norm_rotary_backward(const cd_rotary* rope, const int32_t* positio
 /*
  * Embedding lookup with a factor, and the gradient of its table by sorted tokens:
  *     y[i] = scale table[tokens[i]],       dtable[w] (+)= scale * (sum of dy[i] over the rows i with tokens[i] == w)
- *   tokens   device int32 or int64 [rows] (token_bytes 4 or 8); a token outside [0, vocabulary) is none: its row of y is zero, its row of dy is not read
+ *   tokens   device int32 or int64 [rows] (token_bytes 4 or 8); a token outside [0, vocabulary) is none: its row of y is zero, its row of dy is not read.
+ *            token_bytes | CD_TOKENS_AS_INDEX: -vocabulary .. -1 are words too, counted from the end, and a token that is none is a mistake that shows: its row of y is NaN
  *   table    device [vocabulary][width] in table_dtype, contiguous;  y, dy  device [rows][width] in row_dtype, row_stride elements apart
  *   dtable   device fp32 [vocabulary][width], contiguous.  accumulate 0: written whole, zeros for words that do not occur; otherwise the sums are added to
  *            it, and rows of words that do not occur are not touched
@@ -534,9 +535,10 @@ int codistill_norm_rotary_backward(const cd_rotary* rope, const int32_t* positio
  *   workspace  codistill_embedding_workspace_bytes (the same for every content of tokens; may be 0: then NULL is fine)
  * rows == 0 is allowed (tokens, y and dy may then be NULL).
  * Errors (nothing launched): CD_ERR_INVALID_ARG: NULL pointers, pointers not aligned to their elements (workspace: 16 bytes), rows outside 0 .. 2^30, vocabulary
- * outside 1 .. 2^31 - 2, width outside 1 .. 65536, a row longer than its stride, a scale that is not finite, token_bytes other than 4 and 8;
+ * outside 1 .. 2^31 - 2, width outside 1 .. 65536, a row longer than its stride, a scale that is not finite, token_bytes other than 4 and 8, with or without CD_TOKENS_AS_INDEX;
  * CD_ERR_UNSUPPORTED: rows times the width in units of 64, rounded up, at 2^32 or above; CD_ERR_WORKSPACE_TOO_SMALL.
  */
+enum { CD_TOKENS_AS_INDEX = 16 };
 typedef struct {
   int32_t table_dtype, row_dtype;    /* CD_F32 or CD_BF16 */
   int32_t token_bytes;

@@ -28,6 +28,7 @@ CD_MAX_STAGES, CD_NAME_LEN, CD_LOSS_MAX_PEERS = 4, 48, 8
 CD_ROPE_HALVES, CD_ROPE_PAIRS = 0, 1
 CD_ROPE_MAX_PAIRS, CD_ROPE_MAX_TENSORS = 128, 4
 CD_LAMBDA_HEAD, CD_LAMBDA_TOKEN = 0, 1
+CD_TOKENS_AS_INDEX = 16
 HEAD_NORM_MAX_WIDTH = 1024
 ADAMW_BLOCK = 256   # elements that share an exponent in 8-bit moments
 KERNEL_CLASSES = ["conv_fprop", "conv_dgrad", "conv_wgrad", "norm", "glue", "linear", "loss", "sgd", "conv_fprop_narrow",
@@ -599,7 +600,7 @@ def codistill_norm_rotary_backward(desc, positions, tensors, workspace, eps=1e-5
     _check(lib.codistill_norm_rotary_backward(desc, positions.data_ptr(), tokens, arr, n, eps, workspace.data_ptr(), _room(workspace), _stream_on(where)))
 
 
-def _embedding_desc(tokens, vocabulary, rows, table_dtype, scale):
+def _embedding_desc(tokens, vocabulary, rows, table_dtype, scale, index):
     size = 8 if tokens.dtype is torch.int64 else 4 if tokens.dtype is torch.int32 else 0
     if not size or tokens.dim() != 1 or not tokens.is_contiguous():
         raise ValueError("embedding: tokens are contiguous int32 or int64 [rows]")
@@ -608,14 +609,15 @@ def _embedding_desc(tokens, vocabulary, rows, table_dtype, scale):
     (n, width), (stride, inner) = rows.shape, rows.stride()
     if n != tokens.shape[0] or (width > 1 and inner != 1):
         raise ValueError("embedding: rows are [rows, width], the channels of a row contiguous")
-    return Embedding(table_dtype, _dtype(rows), size, scale, n, vocabulary, width, stride)
+    return Embedding(table_dtype, _dtype(rows), size | CD_TOKENS_AS_INDEX if index else size, scale, n, vocabulary, width, stride)
 
 
-def codistill_embedding(tokens, table, y, scale=1.0):
-    """y[i] = scale table[tokens[i]], zero where a token lies outside the table.  tokens int32 or int64 [rows], table [vocabulary, width], y [rows, width]; both bf16 or fp32."""
+def codistill_embedding(tokens, table, y, scale=1.0, index=False):
+    """y[i] = scale table[tokens[i]], zero where a token lies outside the table.  tokens int32 or int64 [rows], table [vocabulary, width], y [rows, width]; both bf16 or fp32.
+    index: tokens below zero count from the table's end, and rows of tokens that are no index are NaN."""
     if table.dim() != 2 or not table.is_contiguous() or table.shape[1] != y.shape[-1]:
         raise ValueError("embedding: the table is contiguous [vocabulary, width]")
-    d = _embedding_desc(tokens, table.shape[0], y, _dtype(table), scale)
+    d = _embedding_desc(tokens, table.shape[0], y, _dtype(table), scale, index)
     _check(lib.codistill_embedding(d, tokens.data_ptr(), table.data_ptr(), y.data_ptr(), _stream_of(table, tokens, y)))
 
 
@@ -628,11 +630,11 @@ def embedding_workspace_bytes(rows, vocabulary, width):
     return most
 
 
-def codistill_embedding_backward(tokens, dy, dtable, workspace, scale=1.0, accumulate=False):
-    """dtable[w] = (or +=) scale times the sum of dy's rows whose token is w.  dy [rows, width] bf16 or fp32, dtable fp32 [vocabulary, width]."""
+def codistill_embedding_backward(tokens, dy, dtable, workspace, scale=1.0, accumulate=False, index=False):
+    """dtable[w] = (or +=) scale times the sum of dy's rows whose token is w (index: as in the lookup).  dy [rows, width] bf16 or fp32, dtable fp32 [vocabulary, width]."""
     if dtable.dim() != 2 or not dtable.is_contiguous() or dtable.dtype is not torch.float32 or dtable.shape[1] != dy.shape[-1]:
         raise ValueError("embedding_backward: the table's gradient is contiguous fp32 [vocabulary, width]")
-    d = _embedding_desc(tokens, dtable.shape[0], dy, CD_F32, scale)
+    d = _embedding_desc(tokens, dtable.shape[0], dy, CD_F32, scale, index)
     on = _stream_of(dtable, tokens, dy) if workspace is None else _stream_of(dtable, tokens, dy, workspace)
     _check(lib.codistill_embedding_backward(d, tokens.data_ptr(), dy.data_ptr(), dtable.data_ptr(), accumulate, _ptr(workspace), _room(workspace), on))
 

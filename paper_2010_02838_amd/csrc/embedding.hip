@@ -43,15 +43,20 @@ struct EmbedArgs {
   float* partial;                                      // [blocks][2][width]: sums of a block's first and last words, where others have parts of them
   int64_t rows, vocabulary, width, row_stride, sums;   // sums: workgroups that add up; the others write zeros
   int32_t token_bytes, accumulate, zero_stream, each, blocks, slabs, chunk, chunks, shift, digits, from_tokens;
-  float scale;
+  int32_t from_end;            // what is added to a token below zero: the vocabulary where tokens are an index, or nothing
+  float scale, absent;         // absent: elements of a row without a word
 };
 
 // (halves of 32 bits: a token whose upper half is not zero, or whose lower half is no word, is none)
 __device__ inline uint32_t word_from(const EmbedArgs& a, int64_t token) {
+  token += token < 0 ? a.from_end : 0;
   const uint32_t low = (uint32_t)token < (uint32_t)a.vocabulary ? (uint32_t)token : NO_WORD;
   return (uint32_t)(token >> 32) == 0 ? low : NO_WORD;
 }
-__device__ inline uint32_t word_from(const EmbedArgs& a, int32_t token) { return (uint32_t)token < (uint32_t)a.vocabulary ? (uint32_t)token : NO_WORD; }
+__device__ inline uint32_t word_from(const EmbedArgs& a, int32_t token) {
+  token += token < 0 ? a.from_end : 0;
+  return (uint32_t)token < (uint32_t)a.vocabulary ? (uint32_t)token : NO_WORD;
+}
 template <typename TOK> __device__ inline uint32_t word_of(const EmbedArgs& a, int64_t i) { return word_from(a, static_cast<const TOK*>(a.tokens)[i]); }
 __device__ inline uint32_t word_of(const EmbedArgs& a, int64_t i) { return a.token_bytes == 8 ? word_of<int64_t>(a, i) : word_of<int32_t>(a, i); }
 
@@ -71,7 +76,7 @@ __global__ void __launch_bounds__(256) embedding_kernel(EmbedArgs a, int lanes) 
       float out[V];
       if (w == NO_WORD) {
 #pragma unroll
-        for (int e = 0; e < V; e++) out[e] = 0.f;
+        for (int e = 0; e < V; e++) out[e] = a.absent;
       } else {
         TT t[V];
         load_run<TT, V>(from + c, t);
@@ -600,10 +605,12 @@ static EmbedLayout layout_of(int dtype, int64_t rows, int64_t vocabulary, int64_
   return l;
 }
 
+static int32_t token_size(const cd_embedding* d) { return d->token_bytes & ~CD_TOKENS_AS_INDEX; }
 static int check(const char* what, const cd_embedding* d) {
   CD_REQUIRE(d != nullptr, "%s: NULL pointer argument", what);
   CD_REQUIRE((d->table_dtype == CD_F32 || d->table_dtype == CD_BF16) && (d->row_dtype == CD_F32 || d->row_dtype == CD_BF16), "%s: unknown dtype", what);
-  CD_REQUIRE(d->token_bytes == 4 || d->token_bytes == 8, "%s: token_bytes=%d must be 4 or 8", what, d->token_bytes);
+  const int32_t size = token_size(d);
+  CD_REQUIRE(size == 4 || size == 8, "%s: token_bytes=%d must be 4 or 8, or with CD_TOKENS_AS_INDEX", what, d->token_bytes);
   CD_REQUIRE(d->rows >= 0 && d->rows <= (1ll << 30), "%s: rows=%lld out of range", what, (long long)d->rows);
   CD_REQUIRE(d->vocabulary >= 1 && d->vocabulary < (int64_t)NO_WORD, "%s: vocabulary=%lld out of range", what, (long long)d->vocabulary);
   CD_REQUIRE(d->width >= 1 && d->width <= 65536, "%s: width=%lld outside 1..65536", what, (long long)d->width);
@@ -612,6 +619,12 @@ static int check(const char* what, const cd_embedding* d) {
   CD_REQUIRE(d->scale - d->scale == 0.f, "%s: scale must be finite", what);
   if (d->rows * cdiv(d->width, 64) >= (1ll << 32)) return set_error(CD_ERR_UNSUPPORTED, "%s: %lld rows of %lld", what, (long long)d->rows, (long long)d->width);
   return CD_OK;
+}
+static void set_tokens(EmbedArgs& a, const cd_embedding* d) {
+  const bool index = d->token_bytes & CD_TOKENS_AS_INDEX;
+  a.token_bytes = token_size(d);
+  a.from_end = index ? (int32_t)d->vocabulary : 0;
+  a.absent = index ? __builtin_nanf("") : 0.f;
 }
 static bool whole(const void* p, int64_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
 static int size_of(int dtype) { return dtype == CD_BF16 ? 2 : 4; }
@@ -625,11 +638,12 @@ extern "C" int codistill_embedding(const cd_embedding* desc, const void* tokens,
   if (const int rc = check("embedding", desc)) return rc;
   CD_REQUIRE(table && ((tokens && y) || desc->rows == 0), "embedding: NULL pointer argument");
   const int te = size_of(desc->table_dtype), re = size_of(desc->row_dtype);
-  CD_REQUIRE(whole(tokens, desc->token_bytes) && whole(table, te) && whole(y, re), "embedding: misaligned pointer");
+  CD_REQUIRE(whole(tokens, token_size(desc)) && whole(table, te) && whole(y, re), "embedding: misaligned pointer");
   if (desc->rows == 0) return CD_OK;
   EmbedArgs a = {};
   a.tokens = tokens; a.table = table; a.y = y; a.rows = desc->rows; a.vocabulary = desc->vocabulary; a.width = desc->width;
-  a.row_stride = desc->row_stride; a.token_bytes = desc->token_bytes; a.scale = desc->scale;
+  a.row_stride = desc->row_stride; a.scale = desc->scale;
+  set_tokens(a, desc);
   // runs of 8 where both sides move 16 bytes or more a lane, of 4 where 8 or more, single elements otherwise
   auto fits = [&](int v) {
     const int64_t tb = (int64_t)v * te < 16 ? v * te : 16, rb = (int64_t)v * re < 16 ? v * re : 16;
@@ -670,7 +684,7 @@ extern "C" int codistill_embedding_backward(const cd_embedding* desc, const void
   if (const int rc = check("embedding_backward", desc)) return rc;
   CD_REQUIRE(dtable && ((tokens && dy) || desc->rows == 0), "embedding_backward: NULL pointer argument");
   const int re = size_of(desc->row_dtype);
-  CD_REQUIRE(whole(tokens, desc->token_bytes) && whole(dy, re) && whole(dtable, 4) && whole(workspace, 16), "embedding_backward: misaligned pointer");
+  CD_REQUIRE(whole(tokens, token_size(desc)) && whole(dy, re) && whole(dtable, 4) && whole(workspace, 16), "embedding_backward: misaligned pointer");
   const bool small = desc->rows <= SMALL_ROWS;
   int run = run_of(desc->row_dtype, desc->width);
   if (small) run = desc->row_dtype == CD_BF16 && desc->width % 2 == 0 ? 2 : 1;   // (the columns are what workgroups are there for)
@@ -684,7 +698,8 @@ extern "C" int codistill_embedding_backward(const cd_embedding* desc, const void
   char* const ws = static_cast<char*>(workspace);
   EmbedArgs a = {};
   a.tokens = tokens; a.dy = dy; a.dtable = dtable; a.rows = desc->rows; a.vocabulary = desc->vocabulary; a.width = desc->width; a.row_stride = desc->row_stride;
-  a.token_bytes = desc->token_bytes; a.scale = desc->scale; a.accumulate = accumulate != 0;
+  a.scale = desc->scale; a.accumulate = accumulate != 0;
+  set_tokens(a, desc);
   const bool past = desc->rows * desc->width * re >= STREAM_BYTES;
   a.zero_stream = desc->vocabulary * desc->width * 4 >= STREAM_BYTES;
   a.order = reinterpret_cast<int32_t*>(ws + l.order); a.words = reinterpret_cast<int32_t*>(ws + l.words); a.partial = reinterpret_cast<float*>(ws + l.partial);
@@ -694,7 +709,7 @@ extern "C" int codistill_embedding_backward(const cd_embedding* desc, const void
   ProfScope prof(CD_K_GLUE, s, (double)a.rows * a.width, (double)a.rows * a.width * re + 4.0 * a.vocabulary * a.width);
   if (!small && counted(desc->rows, desc->vocabulary)) {
     const dim3 ranks((unsigned)cdiv(desc->rows, RANK_EACH));
-    if (desc->token_bytes == 8) hipLaunchKernelGGL((embedding_rank_kernel<int64_t>), ranks, dim3(256), 0, s, a);
+    if (a.token_bytes == 8) hipLaunchKernelGGL((embedding_rank_kernel<int64_t>), ranks, dim3(256), 0, s, a);
     else hipLaunchKernelGGL((embedding_rank_kernel<int32_t>), ranks, dim3(256), 0, s, a);
   } else if (!small) {
     int32_t *order = a.order, *words = a.words, *order2 = reinterpret_cast<int32_t*>(ws + l.order2), *words2 = reinterpret_cast<int32_t*>(ws + l.words2);

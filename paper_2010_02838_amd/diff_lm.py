@@ -78,15 +78,25 @@ class DiffLM:
         B.codistill_norm_rotary(self.rope, positions, [(a.flatten(1, 2), self.p[n % i], b.flatten(1, 2)) for a, n, b in ((q, "qn%d", to_q), (k, "kn%d", to_k))], EPS)
         return to_q, to_k, v, fused
 
+    def _tokens(self, tokens):
+        """Tokens as the embedding takes them.  They are an index: -1 is the last word.  Tokens that are none are refused on the host; on the device nobody waits for them, and
+        the residual stream begins with NaN there."""
+        if tokens.get_device() < 0 and tokens.numel():
+            least, most = int(tokens.min()), int(tokens.max())
+            if least < -self.V or most >= self.V:
+                raise ValueError("diff_lm: tokens %d .. %d outside a vocabulary of %d" % (least, most, self.V))
+        return tokens.to(self.dev).contiguous()
+
     def _embed(self, tokens):
-        """The residual stream's beginning, fp32: zero where a token is no word."""
+        """The residual stream's beginning, fp32."""
         x = torch.empty(tokens.numel(), self.d, device=self.dev)
-        B.codistill_embedding(tokens.to(self.dev).contiguous(), self.p["embed"], x)
+        B.codistill_embedding(tokens, self.p["embed"], x, index=True)
         return x
 
     def forward(self, tokens, positions, starts, longest):
-        """Logits fp32 [rows, V]; keeps what backward() needs.  tokens int64 [rows], positions int32 [1, rows], starts int32 [sequences + 1]."""
-        rows, dev, dt = tokens.numel(), self.dev, self.dt
+        """Logits fp32 [rows, V]; keeps what backward() needs.  tokens int64 [rows] (below zero: counted from the vocabulary's end; logits that see one outside it are NaN,
+        on the host it is an error), positions int32 [1, rows], starts int32 [sequences + 1]."""
+        tokens, rows, dev, dt = self._tokens(tokens), tokens.numel(), self.dev, self.dt
         x = self._embed(tokens)
         layers = []
         for i in range(self.L):
@@ -137,7 +147,7 @@ class DiffLM:
             self.g["qkv%d" % i].copy_(fused.t() @ y)
             dx = dx + self._norm_backward(x, "norm%d" % i, fused @ self.p["qkv%d" % i])
         ws = torch.empty(B.embedding_workspace_bytes(tokens.numel(), self.V, self.d), dtype=torch.uint8, device=self.dev)
-        B.codistill_embedding_backward(tokens.to(self.dev).contiguous(), dx, self.g["embed"], ws, accumulate=True)   # (beside the projection's gradient)
+        B.codistill_embedding_backward(tokens, dx, self.g["embed"], ws, accumulate=True, index=True)   # (beside the projection's gradient)
 
     def update(self, lr):
         self.updates += 1
@@ -187,8 +197,9 @@ class Decoder:
         B.codistill_diff_attention(self.desc, self.q, self.k[i], self.v[i], lam, self.out, workspace=self.ws)
 
     def step(self, tokens):
-        """tokens int64 [sequences]: logits fp32 [sequences, V] of what follows."""
+        """tokens int64 [sequences], as in DiffLM.forward: logits fp32 [sequences, V] of what follows."""
         lm = self.lm
+        tokens = lm._tokens(tokens)
         if self.oldest >= self.room:   # (one past the caches' end; the device is asked only here, whether the old ones have begun anew)
             self.oldest = int(self.lens.max())
             if self.oldest >= self.room:
@@ -213,6 +224,7 @@ class Decoder:
         """All sequences begin anew with a prompt each, packed: tokens int64 [rows], starts int32 [sequences + 1], the longest one's tokens.  Logits fp32
         [rows, V].  A prompt's tokens see each other as they are; what follows sees what the caches hold of them."""
         lm, rows, ends = self.lm, tokens.numel(), starts.tolist()
+        tokens = lm._tokens(tokens)
         lens = [b - a for a, b in zip(ends, ends[1:])]
         if len(lens) != self.S or ends[0] != 0 or ends[-1] != rows or min(lens) < 0 or max(lens) > longest or not 0 < longest <= self.room:
             raise ValueError("decoder: %d packed prompts of up to %d tokens (the longest one given), got starts %s" % (self.S, self.room, ends))

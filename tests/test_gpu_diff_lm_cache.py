@@ -215,3 +215,57 @@ def test_captured_training_operators():
             (torch.randn(1 << 20, device=DEV) ** 2).sum().item()
         for r in results[1:]:
             assert all(torch.equal(a, b) for a, b in zip(results[0], r))
+
+
+def network(**kw):
+    from paper_2010_02838_amd.diff_lm import DiffLM
+    return DiffLM(30, **dict(dict(layers=2, heads=2, kv_heads=1, head_dim=16, lambda_init=0.5, seed=3), **kw))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_tokens_that_count_from_the_end(dtype):
+    """As in any index: the last word is -1, in the network, its gradient, a prompt and a decoder's step."""
+    from paper_2010_02838_amd.diff_lm import copying_batch
+    lm = network(dtype=dtype)
+    tokens, positions, starts, _ = copying_batch(4, 9, 30, seed=1)
+    got = []
+    for t in (tokens, torch.where(torch.arange(len(tokens), device=DEV) % 3 == 0, tokens - 30, tokens), (tokens - 30).cpu()):
+        z = lm.forward(t, positions, starts, 18)
+        lm.backward(torch.cos(z))
+        decoder = lm.decoder(4, 20)
+        got.append((z, lm.g["embed"].clone(), decoder.prefill(t, starts, 18), decoder.step(t[:4])))
+    assert torch.isfinite(got[0][0]).all() and all(torch.equal(a, b) for other in got[1:] for a, b in zip(got[0], other))
+
+
+@pytest.mark.parametrize("bad", [30, -31, 2 ** 32, 2 ** 40, -2 ** 63])
+def test_tokens_that_are_no_words(bad):
+    """On the host they are refused.  On the device nothing waits for them to be looked at: the logits from there on are NaN, those of other sequences are as without it."""
+    from paper_2010_02838_amd.diff_lm import copying_batch
+    lm = network()
+    tokens, positions, starts, _ = copying_batch(4, 9, 30, seed=1)
+    _, begin, end, *_ = starts.tolist()   # the second sequence, in whose middle it lies
+    middle = (begin + end) // 2
+    wrong = tokens.clone()
+    wrong[middle] = bad
+    z, want = lm.forward(wrong, positions, starts, 18), lm.forward(tokens, positions, starts, 18)
+    others = torch.ones(len(tokens), dtype=torch.bool, device=DEV)
+    others[begin:end] = False
+    assert torch.equal(z[others], want[others]) and torch.isnan(z[middle:end]).all()
+    for bits in (None, 8):
+        decoder, right = lm.decoder(4, 20, cache_bits=bits), lm.decoder(4, 20, cache_bits=bits)
+        decoder.prefill(wrong, starts, 18), right.prefill(tokens, starts, 18)
+        a, b = decoder.step(tokens[:4]), right.step(tokens[:4])
+        assert torch.isnan(a[1]).all() and torch.equal(a[[0, 2, 3]], b[[0, 2, 3]]) and torch.isfinite(b).all()
+        for d in (decoder, right):       # the sequence begins anew
+            d.lens[1] = 0
+        now = tokens[:4].clone()
+        assert torch.equal(decoder.step(now), right.step(now))
+        now[2] = bad
+        a, b = decoder.step(now), right.step(tokens[:4])
+        assert torch.isnan(a[2]).all() and torch.equal(a[[0, 1, 3]], b[[0, 1, 3]])
+        with pytest.raises(ValueError, match="vocabulary"):
+            decoder.step(now.cpu())
+        with pytest.raises(ValueError, match="vocabulary"):
+            decoder.prefill(wrong.cpu(), starts, 18)
+    with pytest.raises(ValueError, match="vocabulary"):
+        lm.forward(wrong.cpu(), positions, starts, 18)

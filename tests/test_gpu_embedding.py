@@ -187,3 +187,30 @@ def test_the_same_bits_wherever_tensors_lie(rows, words, width, dtype):
         assert torch.equal(got, want), (off, off_g)
     gradient(tokens, apart, flat_g[:words * width].view(words, width), 0.7)
     assert torch.equal(flat_g[:words * width].view(words, width), want)
+
+
+@pytest.mark.parametrize("token_type", [torch.int64, torch.int32])
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("rows,words,width", [(1, 1, 1), (300, 40, 66), (2000, 7, 100), (5000, 3000, 512), (20000, 70000, 24)])
+def test_tokens_as_an_index(rows, words, width, dtype, token_type):
+    """Tokens below zero count from the table's end; one that is no index gives a row of NaN, and its row of dy is not read."""
+    from paper_2010_02838_amd import binding as B
+    gen = torch.Generator().manual_seed(rows)
+    words_of_rows = torch.randint(0, words, (rows,), generator=gen)
+    tokens = torch.where(torch.rand(rows, generator=gen) < 0.5, words_of_rows - words, words_of_rows)
+    lost = torch.rand(rows, generator=gen) < (0.1 if rows > 1 else 0.0)
+    odd = torch.tensor([-words - 1, words, -2 ** 31, 2 ** 31 - 1] + ([2 ** 32, 2 ** 32 + 1, -2 ** 32 - 1, -2 ** 63, 2 ** 63 - 1] if token_type is torch.int64 else []))
+    tokens = torch.where(lost, odd[torch.randint(0, len(odd), (rows,), generator=gen)], tokens).to(token_type).to(DEV)
+    plain, lost = words_of_rows.to(DEV), lost.to(DEV)
+    table = torch.randn(words, width, device=DEV).to(dtype)
+    y, want = (torch.full((rows, width), 7.0, dtype=dtype, device=DEV) for _ in range(2))
+    B.codistill_embedding(tokens, table, y, 1.7, index=True)
+    B.codistill_embedding(plain, table, want, 1.7)
+    assert torch.equal(y[~lost], want[~lost]) and torch.isnan(y[lost]).all()
+    dy = torch.randn(rows, width, device=DEV).to(dtype)
+    want, got = torch.empty(words, width, device=DEV), torch.full((words, width), math.nan, device=DEV)
+    gradient(torch.where(lost, -1, plain), dy, want, 0.7)
+    dy[lost] = math.nan
+    ws = torch.full((B.embedding_workspace_bytes(rows, words, width),), 255, dtype=torch.uint8, device=DEV)
+    B.codistill_embedding_backward(tokens, dy, got, ws, 0.7, index=True)
+    assert torch.equal(got, want)

@@ -279,3 +279,15 @@ def test_gradients_of_gains_that_share_memory():
         assert backward(tensors=two(*at), n=2, room=0) == SMALL
     none = (B.NormRotaryTensor * 2)(*[B.NormRotaryTensor(x=M, dy=4 * M, dx=5 * M, heads=2, x_token=128, dy_token=128, dx_token=128) for _ in range(2)])
     assert backward(tensors=none, n=2, room=0) == SMALL
+
+
+def test_tokens_as_an_index():
+    """A flag beside the tokens' size: sizes are refused with it as they are without."""
+    for size in (4, 8):
+        d = emb(token_bytes=size | B.CD_TOKENS_AS_INDEX, rows=0)
+        assert B.lib.codistill_embedding(d, None, M, None, None) == OK and B.lib.codistill_embedding_backward(d, None, None, M, 1, None, 0, None) == OK
+    for size in (0, 2, 12, 1 << 16 | 8):
+        d = emb(token_bytes=size | B.CD_TOKENS_AS_INDEX)
+        assert B.lib.codistill_embedding(d, M, 2 * M, 3 * M, None) == BAD and B.lib.codistill_embedding_backward(d, M, 2 * M, 3 * M, 0, 4 * M, 1 << 40, None) == BAD
+    assert B.lib.codistill_embedding(emb(token_bytes=8 | B.CD_TOKENS_AS_INDEX), M + 4, 2 * M, 3 * M, None) == BAD      # not aligned to its elements
+    assert B.lib.codistill_embedding_backward(emb(token_bytes=8 | B.CD_TOKENS_AS_INDEX), M + 4, 2 * M, 3 * M, 0, 4 * M, 1 << 40, None) == BAD
