@@ -214,3 +214,82 @@ def test_tokens_as_an_index(rows, words, width, dtype, token_type):
     ws = torch.full((B.embedding_workspace_bytes(rows, words, width),), 255, dtype=torch.uint8, device=DEV)
     B.codistill_embedding_backward(tokens, dy, got, ws, 0.7, index=True)
     assert torch.equal(got, want)
+
+
+# ---- whole numbers, whose sums are exact in any order: a row lost or met twice shows, however many a word has ---------------------------
+
+def whole_numbers(rows, width, dtype, seed=0):
+    gen = torch.Generator(device=DEV).manual_seed(seed)
+    return torch.randint(-8, 9, (rows, width), generator=gen, device=DEV, dtype=torch.int8).to(dtype)
+
+
+def check_exactly(tokens, dy, words, accumulate=False, off=0):
+    """rows times 8 stay below 2^24; the factor is a power of two.  off: the gradient begins so many elements inside a vector."""
+    width = dy.shape[1]
+    assert len(tokens) * 8 + 100 < 2 ** 24
+    flat = torch.full((words * width + 4,), 7.0 if accumulate else math.nan, device=DEV)
+    got = flat[off:off + words * width].view(words, width)
+    gradient(tokens, dy, got, 0.5, accumulate)
+    real = (tokens >= 0) & (tokens < words)
+    want = torch.full((words, width), 14.0 if accumulate else 0.0, device=DEV)
+    want.index_add_(0, tokens[real].long(), dy[real].float())
+    assert torch.equal(got, want * 0.5)
+
+
+STREAM = 64 << 20     # bytes of rows, or of the gradient, from which on they bypass the caches
+
+
+@pytest.mark.parametrize("kind", ["uniform", "one", "runs", "text"])
+@pytest.mark.parametrize("rows,words,width,dtype", [
+    (32767, 3000, 1024, BF), (32768, 3000, 1024, BF), (33001, 9, 1032, BF), (40000, 300, 1028, BF), (16383, 3000, 1024, F32), (16384, 3000, 1024, F32), (20001, 70, 1028, F32), (17000, 300, 1031, F32)])
+def test_gradients_of_large_rows(rows, words, width, dtype, kind):
+    """Around 64 MiB of rows, in runs of 8, of 4 and single."""
+    check_exactly(tokens_of(kind, rows, words), whole_numbers(rows, width, dtype), words)
+
+
+@pytest.mark.parametrize("accumulate", [False, True])
+@pytest.mark.parametrize("kind", ["uniform", "one", "runs", "text"])
+@pytest.mark.parametrize("rows,words,width,dtype", [(130000, 500, 64, BF), (200000, 70000, 40, BF), (262144, 9, 24, F32), (262145, 1024, 7, BF), (300000, 2000, 64, F32), (600000, 5000, 16, BF), (600001, 2 ** 20, 8, F32)])
+def test_gradients_of_many_rows(rows, words, width, dtype, kind, accumulate):
+    """16, 32 and 64 rows a wave; chunks of the sort of 1024 rows, 1536 and 2560."""
+    check_exactly(tokens_of(kind, rows, words), whole_numbers(rows, width, dtype), words, accumulate)
+
+
+@pytest.mark.parametrize("rows", [5, 500, 900, 20000])
+@pytest.mark.parametrize("off", [0, 1])
+def test_zeros_of_large_gradients(rows, off):
+    """Gradients just below 64 MiB, at it and above it, few of whose words occur: whole vectors, and single elements where they begin inside one."""
+    for words, width in ((65535, 256), (65536, 256), (70001, 256), (66000, 255)):
+        check_exactly(tokens_of("text", rows, words, seed=width), whole_numbers(rows, width, BF), words, off=off)
+
+
+@pytest.mark.parametrize("table_dtype", [BF, F32])
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("width,pad", [(1024, 0), (1024, 8), (1028, 0), (1028, 4), (1027, 0)])
+def test_lookups_of_large_rows(table_dtype, dtype, width, pad):
+    """Just below 64 MiB, at it and above; rows apart, in runs of 8, of 4 and single."""
+    from paper_2010_02838_amd import binding as B
+    size = torch.finfo(dtype).bits // 8
+    table = torch.randn(5000, width, generator=torch.Generator(device=DEV).manual_seed(width), device=DEV).to(table_dtype)
+    least = -(-STREAM // (width * size))
+    for rows in (least - 1, least, least + 1001):
+        tokens = tokens_of("text", rows, 5000)
+        wide = torch.full((rows, width + pad), 7.0, dtype=dtype, device=DEV)
+        B.codistill_embedding(tokens, table, wide[:, :width], 1.7)
+        real = (tokens >= 0) & (tokens < 5000)
+        want = torch.where(real[:, None], table[torch.where(real, tokens, 0)].float() * 1.7, torch.zeros((), device=DEV)).to(dtype)
+        assert torch.equal(wide[:, :width], want) and (wide[:, width:] == 7).all()
+
+
+def test_a_vocabulary_of_four_digits():
+    """2^30 words of one channel: four passes of the sort."""
+    words, rows = 2 ** 30, 20000
+    tokens, dy = tokens_of("text", rows, words), whole_numbers(rows, 1, F32)
+    got = torch.full((words, 1), math.nan, device=DEV)
+    gradient(tokens, dy, got)
+    real = (tokens >= 0) & (tokens < words)
+    which, at = torch.unique(tokens[real], return_inverse=True)
+    assert torch.equal(got[which, 0], torch.zeros(len(which), device=DEV).index_add_(0, at, dy[real, 0]))
+    got[which] = 0
+    for part in got.split(1 << 28):
+        assert (part == 0).all()
