@@ -269,3 +269,99 @@ def test_tokens_that_are_no_words(bad):
             decoder.prefill(wrong.cpu(), starts, 18)
     with pytest.raises(ValueError, match="vocabulary"):
         lm.forward(wrong.cpu(), positions, starts, 18)
+
+
+@pytest.mark.parametrize("qk_norm", [False, True])
+def test_decoding_in_bf16_from_a_cache_in_8_bits(qk_norm):
+    """Layer by layer, on what the decoder has there: the codes of its new tokens and of its prompts are exact, its attention is within the bound that the cache's attention is held
+    to (tests of the cache).  Prompts' logits are those of a decoder with bf16 caches, bit for bit, and the network's to some seven roundings, 2e-2."""
+    from test_gpu_kv_cache import check_attention, image, put, same
+    from paper_2010_02838_amd.diff_lm import Decoder, DiffLM
+
+    def token(t, row):
+        return t[row].detach().cpu().double().numpy()
+
+    class Checked(Decoder):
+        def _attend(self, i, q, k, v, at):
+            cache, img = self.caches[i], image(self.caches[i])
+            super()._attend(i, q, k, v, at)
+            lens = self.lens.tolist()
+            for b in range(self.S):
+                put(cache, img, b, lens[b] - 1, token(k, b), token(v, b))
+            same(cache, img)
+            check_attention(cache, q[:, None], self.lm.w["lam%d" % i], self.lens, self.out, True)
+
+    lm = DiffLM(50, layers=1, heads=4, kv_heads=2, head_dim=32, lambda_init=0.2, seed=4, qk_norm=qk_norm, dtype=torch.bfloat16)
+    words = torch.randint(0, 50, (3, 200), generator=torch.Generator().manual_seed(5)).to(DEV)
+    coded, plain, lens = Checked(lm, 3, 300, 8), lm.decoder(3, 300), [70, 1, 129]
+    for t in range(6):
+        coded.step(words[:, t])
+    written, write = [], coded.caches[0].write
+    coded.caches[0].write = lambda rows, k, v: (written.append((k.clone(), v.clone())), write(rows, k, v))
+    prompt, starts = torch.cat([words[i, :n] for i, n in enumerate(lens)]), torch.tensor([0, 70, 71, 200], dtype=torch.int32, device=DEV)
+    img = image(coded.caches[0])
+    za, zb = coded.prefill(prompt, starts, 129), plain.prefill(prompt, starts, 129)
+    coded.caches[0].write = write
+    for b, n in enumerate(lens):
+        for j in range(n):
+            put(coded.caches[0], img, b, j, token(written[0][0], sum(lens[:b]) + j), token(written[0][1], sum(lens[:b]) + j))
+    same(coded.caches[0], img)
+    positions = torch.cat([torch.arange(n) for n in lens]).int()[None].to(DEV)
+    z = lm.forward(prompt, positions, starts, 129)
+    assert torch.equal(za, zb) and (za - z).norm() <= 2e-2 * z.norm()
+    for t in range(6):
+        if t == 3:
+            coded.lens[1] = 0        # a sequence begins anew
+        coded.step(words[:, 190 + t])
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_captured_decoding_operators(dtype):
+    """The kernels of a decoder's step in one graph, lookup, norm with rotation, the update of a cache and the attention against it: every replay equals the eager run of the
+    same tokens bit for bit, with eager work between the replays."""
+    from paper_2010_02838_amd import binding as B
+    from paper_2010_02838_amd.kv_cache import KVCache
+    S, H, K, D = 3, 4, 2, 32
+    gen = torch.Generator(device=DEV).manual_seed(8)
+    table, gain = torch.randn(60, 2 * D * (H + 2 * K), generator=gen, device=DEV).to(dtype), torch.ones(D, device=DEV).to(dtype)
+    rope, lam = B.rotary_desc(D, (D // 2,), 1e4, dtype), torch.full((H,), 0.5, device=DEV)
+
+    def make():
+        s = dict(tokens=torch.zeros(S, dtype=torch.int64, device=DEV), first=torch.tensor([0, 60, 1000], dtype=torch.int32, device=DEV), x=torch.empty(S, table.shape[1], dtype=dtype, device=DEV),
+                 y=torch.empty(S, 2 * D * (H + K), dtype=dtype, device=DEV), out=torch.empty(S, 1, H, 2 * D, dtype=dtype, device=DEV), cache=KVCache(S, 2048, K, D, dtype, 128, device=DEV))
+        s["lens"], s["pos"] = s["first"] + 1, s["first"][None].clone()
+        for t in (s["cache"].k, s["cache"].v):
+            t.fill_(3)
+        s["cache"].scales.fill_(0.02)
+        cut = [2 * D * H, 2 * D * K]
+        s["in"], s["turned"] = s["x"][:, :sum(cut)].split(cut, 1), s["y"].split(cut, 1)
+        s["q"], s["k"] = s["turned"][0].unflatten(1, (H, 2, D))[:, None], s["turned"][1].unflatten(1, (K, 2, D))[:, None]
+        s["v"] = s["x"][:, sum(cut):].unflatten(1, (K, 2 * D))[:, None]
+        s["rows"], s["desc"] = s["cache"].rows(s["k"], s["v"], first=s["first"]), s["cache"].attention(s["q"], s["out"], lam, s["lens"], causal=True)
+        s["ws"] = torch.empty(s["desc"].workspace_bytes, dtype=torch.uint8, device=DEV)
+        return s
+
+    def step(s):
+        B.codistill_embedding(s["tokens"], table, s["x"], 0.5, index=True)
+        B.codistill_norm_rotary(rope, s["pos"], [(a.unflatten(1, (-1, D)), gain, b.unflatten(1, (-1, D))) for a, b in zip(s["in"], s["turned"])])
+        s["cache"].write(s["rows"], s["k"], s["v"])
+        s["cache"].attend(s["desc"], s["q"], lam, s["out"], s["ws"])
+        for t in (s["first"], s["lens"], s["pos"]):
+            t.add_(1)
+
+    eager, captured, side, graph = make(), make(), torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    for s in (eager, captured):
+        step(s)
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=side):
+        step(captured)
+    for i in range(5):
+        for s in (eager, captured):
+            s["tokens"].copy_(torch.tensor([7 * i, 59 - i, i - 5]))
+        captured["ws"].fill_(255)
+        graph.replay()
+        torch.cuda.synchronize()
+        step(eager)
+        (torch.randn(1 << 20, device=DEV) ** 2).sum().item()
+        assert torch.isfinite(eager["out"]).all() and all(torch.equal(eager[n], captured[n]) for n in ("x", "y", "out", "first", "lens", "pos"))
+        assert all(torch.equal(getattr(eager["cache"], n), getattr(captured["cache"], n)) for n in ("k", "v", "scales"))
