@@ -43,22 +43,26 @@ struct EmbedArgs {
   float* partial;                                      // [blocks][2][width]: sums of a block's first and last words, where others have parts of them
   int64_t rows, vocabulary, width, row_stride, sums;   // sums: workgroups that add up; the others write zeros
   int32_t token_bytes, accumulate, zero_stream, each, blocks, slabs, chunk, chunks, shift, digits, from_tokens;
-  int32_t from_end;            // what is added to a token below zero: the vocabulary where tokens are an index, or nothing
+  int32_t from_end;            // tokens are an index: those below zero count from the vocabulary's end
   float scale, absent;         // absent: elements of a row without a word
 };
 
 // (halves of 32 bits: a token whose upper half is not zero, or whose lower half is no word, is none)
 __device__ inline uint32_t word_from(const EmbedArgs& a, int64_t token) {
-  token += token < 0 ? a.from_end : 0;
   const uint32_t low = (uint32_t)token < (uint32_t)a.vocabulary ? (uint32_t)token : NO_WORD;
   return (uint32_t)(token >> 32) == 0 ? low : NO_WORD;
 }
-__device__ inline uint32_t word_from(const EmbedArgs& a, int32_t token) {
-  token += token < 0 ? a.from_end : 0;
-  return (uint32_t)token < (uint32_t)a.vocabulary ? (uint32_t)token : NO_WORD;
+__device__ inline uint32_t word_from(const EmbedArgs& a, int32_t token) { return (uint32_t)token < (uint32_t)a.vocabulary ? (uint32_t)token : NO_WORD; }
+// INDEX: tokens are an index
+template <bool INDEX, typename TOK> __device__ inline uint32_t word_from(const EmbedArgs& a, TOK token) {
+  return word_from(a, INDEX && token < 0 ? (TOK)(token + (TOK)a.vocabulary) : token);
 }
-template <typename TOK> __device__ inline uint32_t word_of(const EmbedArgs& a, int64_t i) { return word_from(a, static_cast<const TOK*>(a.tokens)[i]); }
-__device__ inline uint32_t word_of(const EmbedArgs& a, int64_t i) { return a.token_bytes == 8 ? word_of<int64_t>(a, i) : word_of<int32_t>(a, i); }
+template <bool INDEX, typename TOK> __device__ inline uint32_t word_of(const EmbedArgs& a, int64_t i) { return word_from<INDEX>(a, static_cast<const TOK*>(a.tokens)[i]); }
+__device__ inline uint32_t word_of(const EmbedArgs& a, int64_t i) {
+  uint32_t w = a.token_bytes == 8 ? word_of<false, int64_t>(a, i) : word_of<false, int32_t>(a, i);
+  if (a.from_end && w == NO_WORD) w = a.token_bytes == 8 ? word_of<true, int64_t>(a, i) : word_of<true, int32_t>(a, i);   // (looked at again, so that others do not wait for it)
+  return w;
+}
 
 // ---- lookup ---------------------------------------------------------------------------------------------------------------
 // TT: the table's type, RT: the rows'; V: elements of a run; STREAM: rows bypass the caches
@@ -110,12 +114,12 @@ __device__ inline int sum_of_wave(int x) {
   x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);   // the first half's last lane to the second half
   return x;
 }
-template <typename TOK>
+template <typename TOK, bool INDEX>
 __global__ void __launch_bounds__(256) embedding_rank_kernel(EmbedArgs a) {
   __shared__ uint32_t mine[RANK_EACH];
   __shared__ int found[4][RANK_EACH];
   const int i0 = blockIdx.x * RANK_EACH, rows = (int)a.rows, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-  if (threadIdx.x < RANK_EACH) mine[threadIdx.x] = i0 + (int)threadIdx.x < rows ? word_of<TOK>(a, i0 + threadIdx.x) : 0;
+  if (threadIdx.x < RANK_EACH) mine[threadIdx.x] = i0 + (int)threadIdx.x < rows ? word_of<INDEX, TOK>(a, i0 + threadIdx.x) : 0;
   TOK others[RANK_AHEAD];
   auto fetch = [&](int k0) {   // rows k0 .. + 63 and every 256 from there
 #pragma unroll
@@ -134,7 +138,7 @@ __global__ void __launch_bounds__(256) embedding_rank_kernel(EmbedArgs a) {
   for (int k0 = wave * 64; k0 < rows; k0 += 256 * RANK_AHEAD) {
     uint32_t now[RANK_AHEAD];
 #pragma unroll
-    for (int u = 0; u < RANK_AHEAD; u++) now[u] = k0 + 256 * u + lane < rows ? word_from(a, others[u]) : NO_WORD;
+    for (int u = 0; u < RANK_AHEAD; u++) now[u] = k0 + 256 * u + lane < rows ? word_from<INDEX>(a, others[u]) : NO_WORD;
     if (k0 + 256 * RANK_AHEAD < rows) fetch(k0 + 256 * RANK_AHEAD);
 #pragma unroll
     for (int u = 0; u < RANK_AHEAD; u += 2) {
@@ -257,11 +261,12 @@ __global__ void __launch_bounds__(512) embedding_scatter_kernel(EmbedArgs a) {
 }
 
 // ---- sums -------------------------------------------------------------------------------------------------------------------
+typedef float float4_anywhere_t __attribute__((ext_vector_type(4), aligned(4)));   // (the gradient may begin inside a vector)
 template <int V> __device__ inline void load_floats(const float* p, float (&x)[V]) {
   if constexpr (V >= 4) {
 #pragma unroll
     for (int e = 0; e < V; e += 4) {
-      const float4 t = *reinterpret_cast<const float4*>(p + e);
+      const float4_anywhere_t t = *reinterpret_cast<const float4_anywhere_t*>(p + e);
       x[e] = t.x; x[e + 1] = t.y; x[e + 2] = t.z; x[e + 3] = t.w;
     }
   } else {
@@ -274,7 +279,8 @@ template <int V> __device__ inline void put_row(float* to, const float (&old)[V]
   if constexpr (V >= 4) {
 #pragma unroll
     for (int e = 0; e < V; e += 4)
-      *reinterpret_cast<float4*>(to + e) = make_float4(old[e] + scale * sum[e], old[e + 1] + scale * sum[e + 1], old[e + 2] + scale * sum[e + 2], old[e + 3] + scale * sum[e + 3]);
+      *reinterpret_cast<float4_anywhere_t*>(to + e) =
+          float4_anywhere_t{old[e] + scale * sum[e], old[e + 1] + scale * sum[e + 1], old[e + 2] + scale * sum[e + 2], old[e + 3] + scale * sum[e + 3]};
   } else {
 #pragma unroll
     for (int e = 0; e < V; e++) to[e] = old[e] + scale * sum[e];
@@ -423,7 +429,7 @@ __global__ void __launch_bounds__(64 * SUM_WAVES) embedding_sum_kernel(EmbedArgs
     for (int k = 0; k < AHEAD; k++) {
       const int i = min(i0 + k, real - 1);
       const int64_t from = (int64_t)(((uint64_t)__builtin_amdgcn_readlane(offset_high, i) << 32) | __builtin_amdgcn_readlane(offset_low, i));
-      if constexpr (STREAM) load_run_stream<T, V>(rows_here + from, t[k]); else load_run<T, V>(rows_here + from, t[k]);
+      if constexpr (STREAM) load_run_stream<T, V>(rows_here + from, t[k]); else load_run_anywhere<T, V>(rows_here + from, t[k]);
     }
     if (a.accumulate) {
 #pragma unroll
@@ -563,7 +569,13 @@ static int bits_of(int64_t n) {
   while (b < 62 && (int64_t(1) << b) <= n) b++;
   return b;
 }
-static int run_of(int dtype, int64_t width) { return dtype == CD_BF16 && width % 8 == 0 ? 8 : width % 4 == 0 ? 4 : 1; }
+// Elements that a lane adds up.  They follow from the sizes and the type, not from where the tensors lie, and so do the rows of a wave, the order of a word's sum and its bits.  Rows
+// and gradients that begin inside a vector are moved by the same instructions (8192 rows of 1024 bf16 channels, the whole gradient: 24.1 us, from odd addresses 24.5; by single elements,
+// 4 rows a wave as well, 34).
+static int run_of(int dtype, int64_t rows, int64_t width) {
+  if (rows <= SMALL_ROWS) return dtype == CD_BF16 && width % 2 == 0 ? 2 : 1;   // (the columns are what workgroups are there for)
+  return dtype == CD_BF16 && width % 8 == 0 ? 8 : width % 4 == 0 ? 4 : 1;
+}
 
 struct EmbedLayout {
   int run;                       // elements a lane adds up
@@ -572,19 +584,17 @@ struct EmbedLayout {
 };
 static int passes_of(int64_t vocabulary) { return (int)cdiv(bits_of(vocabulary), DIGIT_BITS); }
 static bool counted(int64_t rows, int64_t vocabulary) { return rows <= RANK_ROWS * (passes_of(vocabulary) + 1); }
-static EmbedLayout layout_of(int dtype, int64_t rows, int64_t vocabulary, int64_t width, int run) {
+static EmbedLayout layout_of(const cd_embedding* d) {
+  const int64_t rows = d->rows, vocabulary = d->vocabulary, width = d->width;
   EmbedLayout l = {};
-  l.run = run;
-  l.slabs = (int32_t)cdiv(width, 64 * run);
+  l.run = run_of(d->row_dtype, rows, width);
+  l.slabs = (int32_t)cdiv(width, 64 * l.run);
   if (rows <= SMALL_ROWS) {   // (no workspace)
     l.blocks = (int32_t)cdiv(rows, SMALL_BLOCK);
     return l;
   }
-  // Rows of a wave follow from the sizes and the type alone, not from the runs that this call's pointers allow: the order of a word's sum, and so its bits, are the same
-  // wherever the tensors lie.
-  const int64_t widest = cdiv(width, 64 * run_of(dtype, width));
   l.each = 4;
-  while (l.each < 64 && rows * widest > (int64_t)l.each * SUM_WAVES * 1024) l.each *= 2;
+  while (l.each < 64 && rows * l.slabs > (int64_t)l.each * SUM_WAVES * 1024) l.each *= 2;
   l.blocks = (int32_t)cdiv(rows, (int64_t)SUM_WAVES * l.each);
   const int64_t chunk = cdiv(rows, SORT_CHUNKS);
   l.chunk = (int32_t)(cdiv(chunk > SORT_LEAST ? chunk : SORT_LEAST, 64 * SORT_WAVES) * 64 * SORT_WAVES);
@@ -623,7 +633,7 @@ static int check(const char* what, const cd_embedding* d) {
 static void set_tokens(EmbedArgs& a, const cd_embedding* d) {
   const bool index = d->token_bytes & CD_TOKENS_AS_INDEX;
   a.token_bytes = token_size(d);
-  a.from_end = index ? (int32_t)d->vocabulary : 0;
+  a.from_end = index;
   a.absent = index ? __builtin_nanf("") : 0.f;
 }
 static bool whole(const void* p, int64_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
@@ -675,7 +685,7 @@ extern "C" int codistill_embedding(const cd_embedding* desc, const void* tokens,
 extern "C" int codistill_embedding_workspace_bytes(const cd_embedding* desc, size_t* bytes) {
   if (const int rc = check("embedding_workspace_bytes", desc)) return rc;
   CD_REQUIRE(bytes != nullptr, "embedding_workspace_bytes: output pointer is NULL");
-  *bytes = layout_of(desc->row_dtype, desc->rows, desc->vocabulary, desc->width, 1).bytes;   // (the same for all runs)
+  *bytes = layout_of(desc).bytes;
   return CD_OK;
 }
 
@@ -686,15 +696,12 @@ extern "C" int codistill_embedding_backward(const cd_embedding* desc, const void
   const int re = size_of(desc->row_dtype);
   CD_REQUIRE(whole(tokens, token_size(desc)) && whole(dy, re) && whole(dtable, 4) && whole(workspace, 16), "embedding_backward: misaligned pointer");
   const bool small = desc->rows <= SMALL_ROWS;
-  int run = run_of(desc->row_dtype, desc->width);
-  if (small) run = desc->row_dtype == CD_BF16 && desc->width % 2 == 0 ? 2 : 1;   // (the columns are what workgroups are there for)
-  if (run > 1 && !(whole(dtable, run < 4 ? 4 * run : 16) && whole(dy, run * re) && (desc->rows <= 1 || desc->row_stride % run == 0))) run = 1;
-  size_t need = 0;
-  codistill_embedding_workspace_bytes(desc, &need);
+  const EmbedLayout l = layout_of(desc);
+  const size_t need = l.bytes;
+  const int run = l.run;
   CD_REQUIRE(workspace || need == 0, "embedding_backward: NULL pointer argument");
   if (workspace_bytes < need) return set_error(CD_ERR_WORKSPACE_TOO_SMALL, "embedding_backward: workspace of %zu bytes, %zu needed", workspace_bytes, need);
   if (desc->rows == 0 && accumulate) return CD_OK;
-  const EmbedLayout l = layout_of(desc->row_dtype, desc->rows, desc->vocabulary, desc->width, run);
   char* const ws = static_cast<char*>(workspace);
   EmbedArgs a = {};
   a.tokens = tokens; a.dy = dy; a.dtable = dtable; a.rows = desc->rows; a.vocabulary = desc->vocabulary; a.width = desc->width; a.row_stride = desc->row_stride;
@@ -709,8 +716,10 @@ extern "C" int codistill_embedding_backward(const cd_embedding* desc, const void
   ProfScope prof(CD_K_GLUE, s, (double)a.rows * a.width, (double)a.rows * a.width * re + 4.0 * a.vocabulary * a.width);
   if (!small && counted(desc->rows, desc->vocabulary)) {
     const dim3 ranks((unsigned)cdiv(desc->rows, RANK_EACH));
-    if (a.token_bytes == 8) hipLaunchKernelGGL((embedding_rank_kernel<int64_t>), ranks, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((embedding_rank_kernel<int32_t>), ranks, dim3(256), 0, s, a);
+    auto rank = [&](auto kernel) { hipLaunchKernelGGL(kernel, ranks, dim3(256), 0, s, a); };
+    if (a.token_bytes == 8) { if (a.from_end) rank(embedding_rank_kernel<int64_t, true>); else rank(embedding_rank_kernel<int64_t, false>); }
+    else if (a.from_end) rank(embedding_rank_kernel<int32_t, true>);
+    else rank(embedding_rank_kernel<int32_t, false>);
   } else if (!small) {
     int32_t *order = a.order, *words = a.words, *order2 = reinterpret_cast<int32_t*>(ws + l.order2), *words2 = reinterpret_cast<int32_t*>(ws + l.words2);
     a.counts = reinterpret_cast<int32_t*>(ws + l.counts);
