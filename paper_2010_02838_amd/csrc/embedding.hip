@@ -9,12 +9,13 @@
 // first launch of the sort.
 //
 // The order.  Up to 512 rows: in LDS, by every workgroup for itself.  Few rows: a row's place is the number of rows in front of it, counted by comparing it with all of
-// them in one launch (8192 rows: 11.7 us, of which the comparisons, two and a half instructions for 64 of them, are 7).  Many rows: a radix sort, two launches for each digit
-// of up to 10 bits (65536 rows 4.8 + 9.4 us a digit): digits of a chunk are counted, then every chunk knows where its own begin.
+// them in one launch (8192 rows: 12.1 us, of which the comparisons, two and a half instructions for 64 of them, are 7).  Many rows: a radix sort, two launches for each digit
+// of up to 10 bits (65536 rows 4.8 + 9.6 us a digit): digits of a chunk are counted, then every chunk knows where its own begin.
 //
-// 8192 rows of 512 bf16 channels among 32768 words, beside what the table's gradient holds: lookup 5.6 us, order 11.7, sums 9.9, parts 4.5: latency, 26 MB are 5.  65536 rows of 1024
-// among as many words, all written: lookup 45 (169 MB, 3.7 TB/s; 30 where the caches still hold much of the table), order 28.5, sums and zeros 73 (402 MB, 5.5 TB/s), parts 5.4.
-// 300 rows of 256 fp32 channels: 2.6 and 9.9.
+// 8192 rows of 512 bf16 channels among 32768 words, beside what the table's gradient holds: lookup 5.1 us, order 12.1, sums 9.6, parts 4.6: latency, 26 MB are 5.  65536 rows of 1024
+// among as many words, all written: lookup 45 (169 MB, 3.7 TB/s; 30 where the caches still hold much of the table), order 28.8, sums and zeros 74 (402 MB, 5.4 TB/s), parts 5.5.
+// 300 rows of 256 fp32 channels: 2.6 and 10.1.  fp32 rows, three sets in turn, lookup and whole gradient added to another: 8192 rows of 512 from a bf16 table 6.8 and 25.4, from an fp32 one 6.6 and 25.1
+// (bf16 rows 5.3 and 24.8); 65536 of 1024 100 and 106, 60 and 106 (bf16 rows 30 and 93).  The 100 are a lane's two stores of 16 bytes, 32 apart, past the caches.
 #include "common.h"
 #include "vec.h"
 
@@ -34,7 +35,9 @@ constexpr int SUM_WAVES = 8;                // waves of a block of rows
 constexpr int FILL_BLOCKS = 1024;
 // From here on what is read once (rows of dy) or written and not read again here (rows of y, zeros) bypasses the caches, which the table's rows are left to: 65536 rows of
 // 1024 bf16 channels on as many words (134 MB of rows, 268 MB of gradients): lookup 51 -> 30 us where the table is looked up again and again, 50 -> 45 where it comes from memory, sums 93 -> 73.  Rows of 8.4 MB, which the operator in front
-// has left in the caches: sums 8.8 -> 9.4.
+// has left in the caches: sums 8.8 -> 9.4.  Between them, rows of 1024 bf16 channels on 32768 words, three sets in turn, through the caches and past them: lookup 16 MiB 7.0 and 6.2 us, 32 MiB 10.9 and 10.0, 64 MiB 21.6 and 17.2, 96 MiB
+// 36 and 23 (fp32 rows of 512 from bf16: 7.0 and 5.8, 10.4 and 10.0, 64 MiB 16.9 and 18.8); gradient with its zeros 48.6 and 45.7, 66 and 57, 78 and 64, 87 and 73: what the operator in front has left decides below 64 MiB.  2000 rows on a gradient of
+// 16, 64 and 256 MiB: 29.6 and 27.2, 30.9 and 28.7, 58.5 and 55.8.
 constexpr int64_t STREAM_BYTES = 64 << 20;
 
 struct EmbedArgs {

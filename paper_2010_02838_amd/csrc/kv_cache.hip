@@ -9,8 +9,9 @@
 // instructions: of the keys a lane takes a run of one token's channels, of the values 16 tokens of one channel, which is why values are
 // stored with the tokens side by side.  No copy in LDS, no exchange between lanes.
 //
-// Writing and reading move bytes: 14510 tokens of 24 packed prompts, 4 key heads of 64 in bf16 (45 MB each way), 16.0 and 13.1 us (prompts that the caches hold 15.0 and 12.7; without the arithmetic of the codes 2 less), where the copy rate is 9.4; a workgroup's
-// rows are all asked for at once, so that the chip loads, computes and stores in turns.  One token of each of 16 sequences: 4.9 and 3.6, a launch and its latencies.
+// Writing and reading move bytes: 14510 tokens of 24 packed prompts, 4 key heads of 64 in bf16 (45 MB each way, 9.4 us at the copy rate), 16.0 and 13.1 us (prompts that the caches hold 15.0 and 12.7;
+// without the arithmetic of the codes 2 less); a workgroup's rows are all asked for at once, so that the chip loads, computes and stores in turns.  14496 tokens in fp32 (75 MB each way, 15.6): 15.7 and 19.6, from the caches in
+// part.  One token of each of 16 sequences: 4.8 and 2.9, a launch and its latencies.
 #include "common.h"
 #include "conv_rules.h"
 #include "kernels.h"
@@ -337,7 +338,9 @@ __global__ void __launch_bounds__(256) kv_read_kernel(KvRowArgs a) {
 //
 //     P_m = softmax over the visible keys of scale q_m . k_m  (m = 1, 2),   out = (P_1 - lambda P_2) v
 //
-// Memory-bound: a key and its value are read once, 4 dim + 6 bytes, for all queries of all heads that share them.
+// Memory-bound where few queries share a key head: a key and its value, 4 dim + 6 bytes, are read once for a tile of 8 rows (two tiles where `row_tiles` says so).  Every further tile is a
+// workgroup that reads and converts them again, through the caches: 16 sequences of 8092 tokens, 4 key heads of 64, take 30.5 us for 4 rows a key head and 73 for 32 (fp32, tiles of
+// 8: 31.2 and 101); 4 of 3996, 2 key heads of 128, 36.7 for 64 rows, where the bytes alone are 3.5.
 //
 // Rows.  Row r of a sequence is query r / group of head r % group.  A 16x16x32 product has 16 columns: 8 rows, each once for either map.  Both keys of a token are
 // multiplied with all columns and a column keeps its own map's score; from there on a map is a row like any other, with its own running maximum, and both maps
@@ -350,8 +353,8 @@ __global__ void __launch_bounds__(256) kv_read_kernel(KvRowArgs a) {
 // Roundings.  Codes are exact in bf16.  fp32 queries, and the weights times the values' scales, are sums of three bf16 numbers (all 24 bits), bf16 models'
 // weights of two (16 bits): results are then off by their own rounding alone, 1.7e-3 as a 2-norm, and the second product costs 5 to 9 %.
 //
-// 16 sequences of 2000 to 8000 tokens, one query each, 16 heads of 64 on 4 (80 MB): 22.2 us (3.6 TB/s; 17 are the copy rate), and 4.6 for the join; the same on bf16 keys and
-// values takes 41 and 6.  One of 124000 on 2 key heads (47 MB): 15.0 and 5.2.  Five of up to 4096, four queries, heads of 128: 14.6 and 4.6, of which the bytes are 2.4: a launch, the chain
+// 16 sequences of 2000 to 8000 tokens, one query each, 16 heads of 64 on 4 (80 MB): 22.3 us (3.6 TB/s; 17 are the copy rate), and 4.1 for the join; the same on bf16 keys and
+// values takes 41 and 6.  One of 124000 on 2 key heads (47 MB): 15.2 and 5.1.  Five of up to 4096, four queries, heads of 128: 14.9 and 4.6, of which the bytes are 2.5: a launch, the chain
 // from the lengths to the first keys, and one or two blocks a wave, one wave a SIMD.
 struct KvAttnArgs {
   KvArgs c;
